@@ -40,8 +40,11 @@ typedef enum {
     PERQ_FMT_MXFP4 = 1,     /* E2M1 elements, one E8M0 scale per 32 elements */
     PERQ_FMT_F32_DEBUG = 2, /* no quantisation: the rotated row as fp32 (test hook) */
     PERQ_FMT_FP4 = 3,       /* E2M1 elements, one fp32 scale per token (Appendix B, FP4 activations) */
-    PERQ_FMT_INT4_ASYM = 4  /* asymmetric INT4, (scale, zero point) per token (Appendix B, INT4 activations) */
+    PERQ_FMT_INT4_ASYM = 4, /* asymmetric INT4, (scale, zero point) per token (Appendix B, INT4 activations) */
+    PERQ_FMT_INT8 = 5       /* symmetric INT8, one fp32 scale per row: the products' operands only */
 } perq_fmt_t;
+
+typedef enum { PERQ_OUT_BF16 = 0, PERQ_OUT_F16 = 1, PERQ_OUT_F32 = 2 } perq_out_t;   /* results of the products */
 
 typedef enum {
     PERQ_OK = 0,
@@ -60,6 +63,8 @@ typedef enum {
 } perq_status_t;
 
 #define PERQ_MAX_D 32768
+#define PERQ_MAX_N 1048576      /* channels of a product (of one expert) */
+#define PERQ_MAX_EXPERTS 1024
 
 /*
  * perq_rotate_quantize -- the online hot path, one fused pass.
@@ -317,12 +322,65 @@ int perq_massdiff_perm_device(const float *chan_abs_sum, int32_t d, int32_t b, i
                               void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * perq_matmul_i8 -- the linear layer that reads the path's codes: the product of codes in 8-bit integers with a scale for
+ * each token and each weight channel.
+ *
+ * Defined by: Sec. 4.3 and the figure on permutation equivariance (the rotated, quantised activations enter the down
+ * projection, whose rows carry the same rotation: (X R~)(W R~)^T = X W^T) and the quantisers of Sec. 3 and Appendix B, whose
+ * values are s * code and, asymmetric, s * (code + z).  For token t and weight channel n
+ *
+ *     y[t][n] = s_t * s_n * ( sum_k a[t][k] w[n][k]  +  z_t * c_n ),      c_n = sum_k w[n][k]
+ *
+ * with z_t = 0 unless a_fmt is PERQ_FMT_INT4_ASYM.  The first sum is exact (32-bit integers; |sum| < 2^31 for every d
+ * allowed); it, the corrected sum, the two products and the result are each rounded once to fp32, the result then to
+ * out_type, to nearest even.  Results are the same from run to run and do not depend on which kernel serves the call.
+ *
+ *   a_codes, a_scales   device: codes and scales of T rows as perq_rotate_quantize writes them for INT4 per token (uint8
+ *                       [T, d/2], float [T]) and INT4_ASYM (uint8 [T, d/2], float [T, 2]: step, zero point), or INT8 codes
+ *                       (int8 [T, d], float [T])
+ *   a_fmt               PERQ_FMT_INT8, PERQ_FMT_INT4 or PERQ_FMT_INT4_ASYM
+ *   w_codes, w_scales   device: the same of N weight channels (rows [N, d]); w_fmt PERQ_FMT_INT8 or PERQ_FMT_INT4
+ *   w_sums              device int32 [N]: c_n; read for INT4_ASYM only (else it may be NULL)
+ *   T, N, d             T == 0 is a no-op; T <= 2^30; 1 <= N <= PERQ_MAX_N; d % 32 == 0, d <= PERQ_MAX_D
+ *   out                 device [T, N] of out_type (perq_out_t), row stride N, written in full
+ *   workspace           device, at least perq_matmul_i8_workspace_bytes(...) bytes (NULL where that is 0).  Its contents
+ *                       need not be kept; calls that may overlap need one each.
+ *
+ * Scales that are infinite or NaN give what fp32 arithmetic makes of the formula.  All device pointers 16-byte aligned.
+ * Errors: NULL, SHAPE, FMT (formats and out_type), ALIGN, WORKSPACE, CUDA.
+ */
+int perq_matmul_i8(const void *a_codes, const float *a_scales, int32_t a_fmt, const void *w_codes, const float *w_scales,
+                   int32_t w_fmt, const int32_t *w_sums, int64_t T, int32_t N, int32_t d, void *out, int32_t out_type,
+                   void *workspace, size_t workspace_bytes, void *stream);
+int perq_matmul_i8_workspace_bytes(int64_t T, int32_t N, int32_t d, int32_t a_fmt, int32_t w_fmt, size_t *bytes);
+
+/*
+ * perq_grouped_matmul_i8 -- the same product grouped by expert, with ragged sizes (no counterpart in the paper, whose
+ * models are dense: a feedforward block of several experts has one down projection each).
+ *
+ * Rows offsets[e] .. offsets[e + 1] of the tokens are expert e's, whose weights are w_codes[e]; an expert may have none.
+ *
+ *   w_codes             codes of [E, N, d]; w_scales float [E, N]; w_sums int32 [E, N]
+ *   offsets             device int32 [E + 1], not decreasing, in 0 .. T.  The host does not look at it, so the call can be
+ *                       captured and replayed with other offsets.  Entries outside 0 .. T are taken into it, and where they
+ *                       decrease the expert has no rows: wrong numbers, never a fault.
+ *   T                   rows of a_codes and out.  Rows before offsets[0] and from offsets[E] on are neither computed nor written.
+ *   E                   1 .. PERQ_MAX_EXPERTS, E * N <= 2^30
+ * Everything else as for perq_matmul_i8.
+ */
+int perq_grouped_matmul_i8(const void *a_codes, const float *a_scales, int32_t a_fmt, const void *w_codes, const float *w_scales,
+                           int32_t w_fmt, const int32_t *w_sums, const int32_t *offsets, int64_t T, int32_t E, int32_t N,
+                           int32_t d, void *out, int32_t out_type, void *workspace, size_t workspace_bytes, void *stream);
+int perq_grouped_matmul_i8_workspace_bytes(int64_t T, int32_t E, int32_t N, int32_t d, int32_t a_fmt, int32_t w_fmt,
+                                           size_t *bytes);
+
+/*
  * perq_device_error -- reads (synchronously, cudaMemcpyFromSymbol) the library's device-side
  * error word on the current device into *flags_host.  0 = no error.  Bit 0 is set when a
  * bounded wait inside a kernel ran out (an asynchronous copy that never completed); the
  * kernel then stops early and its outputs are incomplete.  Bits 1 and 2: such a wait inside the
  * permuted and grouped kernels, for an exact maximum (1) or a free buffer (2); bit 3: in the
- * statistic.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
+ * statistic; bits 4 and 5: in the kernels of the products.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
  *
  * perq_device_error_clear -- writes 0 to that word on the current device (synchronously,
  * cudaMemcpyToSymbol), so that a later read reports only what happened since.  Call it with no

@@ -22,8 +22,10 @@ PERQ_FMT_MXFP4 = 1
 PERQ_FMT_F32_DEBUG = 2
 PERQ_FMT_FP4 = 3
 PERQ_FMT_INT4_ASYM = 4
+PERQ_FMT_INT8 = 5
 FMT_BY_NAME = {"int4": PERQ_FMT_INT4, "mxfp4": PERQ_FMT_MXFP4, "f32": PERQ_FMT_F32_DEBUG, "fp4": PERQ_FMT_FP4,
-               "int4_asym": PERQ_FMT_INT4_ASYM}
+               "int4_asym": PERQ_FMT_INT4_ASYM, "int8": PERQ_FMT_INT8}
+OUT_BY_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}        # perq_out_t
 
 PERQ_OK = 0
 
@@ -64,6 +66,12 @@ def load() -> C.CDLL:
         lib.perq_absmax_perm.argtypes = [vp, i32, vp]
         lib.perq_zigzag_perm.argtypes = [vp, i32, i32, vp]
         for name in ("perq_chan_abs_max", "perq_absmax_perm", "perq_zigzag_perm"):
+            getattr(lib, name).restype = C.c_int
+        lib.perq_matmul_i8.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i32, i32, vp, i32, vp, sz, vp]
+        lib.perq_matmul_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, C.POINTER(sz)]
+        lib.perq_grouped_matmul_i8.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, i64, i32, i32, i32, vp, i32, vp, sz, vp]
+        lib.perq_grouped_matmul_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, C.POINTER(sz)]
+        for name in ("perq_matmul_i8", "perq_matmul_i8_workspace_bytes", "perq_grouped_matmul_i8", "perq_grouped_matmul_i8_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
         lib.perq_device_error.argtypes = [C.POINTER(C.c_uint32)]
         lib.perq_device_error.restype = C.c_int
@@ -318,3 +326,64 @@ def perq_massdiff_perm(chan_abs_sum_host: np.ndarray, b: int) -> np.ndarray:
     rc = load().perq_massdiff_perm(a.ctypes.data_as(C.c_void_p), a.shape[0], b, perm.ctypes.data_as(C.c_void_p))
     _check(rc, "perq_massdiff_perm")
     return perm
+
+
+def perq_matmul_i8_workspace_bytes(T: int, N: int, d: int, a_fmt: int, w_fmt: int) -> int:
+    n = C.c_size_t(0)
+    _check(load().perq_matmul_i8_workspace_bytes(T, N, d, a_fmt, w_fmt, C.byref(n)), "perq_matmul_i8_workspace_bytes")
+    return int(n.value)
+
+
+def perq_grouped_matmul_i8_workspace_bytes(T: int, E: int, N: int, d: int, a_fmt: int, w_fmt: int) -> int:
+    n = C.c_size_t(0)
+    _check(load().perq_grouped_matmul_i8_workspace_bytes(T, E, N, d, a_fmt, w_fmt, C.byref(n)), "perq_grouped_matmul_i8_workspace_bytes")
+    return int(n.value)
+
+
+def _check_codes(codes: torch.Tensor, scales: torch.Tensor, fmt: int, sums: Optional[torch.Tensor] = None):
+    assert codes.is_cuda and codes.is_contiguous() and codes.dtype == (torch.int8 if fmt == PERQ_FMT_INT8 else torch.uint8)
+    rows = codes.numel() // max(1, codes.shape[-1])
+    assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.float32
+    assert scales.numel() == rows * (2 if fmt == PERQ_FMT_INT4_ASYM else 1)
+    assert sums is None or (sums.is_cuda and sums.is_contiguous() and sums.dtype == torch.int32 and sums.numel() == rows)
+
+
+def _product(name, a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream):
+    _check_codes(a_codes, a_scales, a_fmt)
+    _check_codes(w_codes, w_scales, w_fmt, w_sums)
+    T, N = a_codes.shape[0], w_codes.shape[-2]
+    d = a_codes.shape[1] * (1 if a_fmt == PERQ_FMT_INT8 else 2)
+    assert a_codes.dim() == 2 and w_codes.shape[-1] * (1 if w_fmt == PERQ_FMT_INT8 else 2) == d
+    if out is None:
+        out = torch.empty((T, N), dtype=out_dtype, device=a_codes.device)
+    assert out.is_cuda and out.is_contiguous() and out.shape == (T, N)
+    lib = load()
+    if workspace is None:
+        n = (perq_matmul_i8_workspace_bytes(T, N, d, a_fmt, w_fmt) if offsets is None else
+             perq_grouped_matmul_i8_workspace_bytes(T, w_codes.shape[0], N, d, a_fmt, w_fmt))
+        workspace = torch.empty(n, dtype=torch.uint8, device=a_codes.device) if n else None
+    head = (_ptr(a_codes), _ptr(a_scales), a_fmt, _ptr(w_codes), _ptr(w_scales), w_fmt, _ptr(w_sums))
+    tail = (_ptr(out), OUT_BY_DTYPE[out.dtype], _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
+    if offsets is None:
+        rc = lib.perq_matmul_i8(*head, T, N, d, *tail)
+    else:
+        rc = lib.perq_grouped_matmul_i8(*head, _ptr(offsets), T, w_codes.shape[0], N, d, *tail)
+    _check(rc, name)
+    return out
+
+
+def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
+                   w_sums: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """a: codes [T, d] of tokens, w: codes [N, d] of weight channels (int8, or uint8 [.., d / 2] for INT4); returns out [T, N]."""
+    assert w_codes.dim() == 2
+    return _product("perq_matmul_i8", a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, None, out, out_dtype, workspace, stream)
+
+
+def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
+                           offsets: torch.Tensor, w_sums: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                           out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """As perq_matmul_i8 with w [E, N, d] and rows offsets[e] .. offsets[e + 1] (int32 CUDA tensor [E + 1]) of the tokens for expert e."""
+    assert w_codes.dim() == 3
+    assert offsets.is_cuda and offsets.is_contiguous() and offsets.dtype == torch.int32 and offsets.numel() == w_codes.shape[0] + 1
+    return _product("perq_grouped_matmul_i8", a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream)

@@ -1,10 +1,12 @@
 """Builds the CUDA library in-tree: paper_2601_22347_b200/libperq.so (sm_100a only)."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -55,23 +57,31 @@ def build_call(force: bool = False) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into one shared library for sm_100a, and the interpreter's entry to it."""
+    """Compile every .cu under csrc/ (side by side) into one shared library for sm_100a, and the interpreter's entry to it."""
     build_call(force)
     if not force and not needs_build():
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+             "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-I", _CSRC]
+    if verbose:
+        flags.insert(0, "-Xptxas=-v")
+
+    def run(cmd):
+        out = subprocess.run([nvcc] + cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if out.returncode != 0:
+            sys.stderr.write(out.stdout)
+            raise RuntimeError("nvcc failed building libperq.so")
+        if verbose:
+            print(out.stdout)
+
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-I", _CSRC,
-           "-o", tmp] + _sources()
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    out = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if out.returncode != 0:
-        sys.stderr.write(out.stdout)
-        raise RuntimeError("nvcc failed building libperq.so")
-    if verbose:
-        print(out.stdout)
+    with tempfile.TemporaryDirectory() as d:
+        sources = _sources()
+        objects = [os.path.join(d, os.path.basename(p) + ".o") for p in sources]
+        with concurrent.futures.ThreadPoolExecutor(len(sources)) as pool:
+            list(pool.map(lambda p, o: run(flags + ["-c", "-o", o, p]), sources, objects))
+        run(flags + ["-shared", "-o", tmp] + objects)
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 

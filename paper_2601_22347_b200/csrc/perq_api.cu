@@ -16,6 +16,7 @@
 #include <cuda_runtime.h>
 #include <cstring>
 
+#include "perq_host.cuh"
 #include "perq_generic.cuh"
 #include "perq_fast.cuh"
 #include "perq_tok.cuh"
@@ -32,12 +33,6 @@
 namespace {
 
 constexpr int kVersion = 100;   // 0.1.0
-constexpr size_t kMaxSmem = 227 * 1024;
-
-inline bool is_pow2(long long v) { return v > 0 && (v & (v - 1)) == 0; }
-inline int ilog2(int v) { int l = 0; while ((1 << l) < v) ++l; return l; }
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // Order of the base matrix of a b-dimensional Hadamard rotation (Appendix A.1: b = 2^k' * 4t, t the odd part
 // of b): 0 for a power of two (Sylvester all the way), 4t when this library has a base matrix of that order
 // (Paley's second construction: 4t = 2 (q + 1) with q = 5, 13, 17, 29 or 37), -1 otherwise.
@@ -106,43 +101,6 @@ int check_shape(int64_t T, int32_t d, int32_t b, int32_t fmt, int32_t group, int
         if (group != 0) return PERQ_ERR_GROUP;      // one scale per token
     }
     if (g_out) *g_out = g;
-    return PERQ_OK;
-}
-
-int sm_count()
-{
-    static std::atomic<int> cached[64];          // per device ordinal; 0 = not asked yet
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    const bool slot = dev >= 0 && dev < 64;
-    if (slot && cached[dev].load() > 0) return cached[dev].load();
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    if (slot) cached[dev].store(n);
-    return n;
-}
-
-// Opt-in to more than 48 KB of dynamic shared memory.  The attribute belongs to (kernel, device): it is set
-// the first time and whenever a launch needs more than was set before (the call costs a microsecond or two,
-// which matters for the small launches).
-std::mutex g_smem_attr_mutex;
-std::map<std::pair<const void *, int>, size_t> g_smem_attr_set;
-
-template <typename K>
-int allow_smem(K kernel, size_t bytes)
-{
-    if (bytes <= 48 * 1024) return PERQ_OK;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return PERQ_ERR_CUDA;
-    const void *func = reinterpret_cast<const void *>(kernel);
-    std::lock_guard<std::mutex> lock(g_smem_attr_mutex);
-    size_t &have = g_smem_attr_set[std::make_pair(func, dev)];
-    if (have >= bytes) return PERQ_OK;
-    if (cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return PERQ_ERR_CUDA;
-    }
-    have = bytes;
     return PERQ_OK;
 }
 
@@ -1020,16 +978,16 @@ int perq_validate_perm(const int32_t *perm, int32_t d, int32_t *status_dev, void
 int perq_device_error(uint32_t *flags_host)
 {
     if (!flags_host) return PERQ_ERR_NULL;
-    unsigned int v = 0;
-    if (cudaMemcpyFromSymbol(&v, perq::g_perq_device_error, sizeof v) != cudaSuccess) return PERQ_ERR_CUDA;
-    *flags_host = v;
+    unsigned int v = 0, products = 0;
+    if (cudaMemcpyFromSymbol(&v, perq::g_perq_device_error, sizeof v) != cudaSuccess || perq_mm_read_error(&products) != cudaSuccess) return PERQ_ERR_CUDA;
+    *flags_host = v | products;
     return PERQ_OK;
 }
 
 int perq_device_error_clear(void)
 {
     const unsigned int zero = 0;
-    return cudaMemcpyToSymbol(perq::g_perq_device_error, &zero, sizeof zero) == cudaSuccess ? PERQ_OK : PERQ_ERR_CUDA;
+    return cudaMemcpyToSymbol(perq::g_perq_device_error, &zero, sizeof zero) == cudaSuccess && perq_mm_clear_error() == cudaSuccess ? PERQ_OK : PERQ_ERR_CUDA;
 }
 
 int perq_massdiff_perm_device(const float *chan_abs_sum, int32_t d, int32_t b, int32_t *perm, void *workspace,

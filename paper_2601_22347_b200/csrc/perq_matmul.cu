@@ -1,0 +1,195 @@
+// C ABI of the products of codes: argument checks, choice of kernel, tensor maps, launches.
+// Nothing here allocates device memory or synchronises, except where perq.h says so.
+#include "perq.h"
+
+#include <algorithm>
+#include <cstring>
+
+#include "perq_host.cuh"
+#include "perq_mm_few.cuh"
+
+namespace {
+
+// Whether a format's codes lie two to a byte.
+inline bool is_packed(int32_t fmt) { return fmt != PERQ_FMT_INT8; }
+
+// Codes [rows, d] in boxes of `box` rows by 128 bytes; 8-bit codes as operands (128-byte swizzle), packed ones as they lie.
+bool codes_map(CUtensorMap *map, const void *codes, bool packed, uint64_t rows, int d, int box)
+{
+    TensorMapEncode encode = tensor_map_encode();
+    if (encode == nullptr) return false;
+    const uint64_t bytes = packed ? (uint64_t)d / 2 : (uint64_t)d;
+    const cuuint64_t dims[2] = {bytes, rows}, strides[1] = {bytes};
+    const cuuint32_t size[2] = {128, (cuuint32_t)box}, step[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, size, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  packed ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Programmatic stream serialization as everywhere in the library, and clusters.
+template <typename P>
+int launch_product(void (*kernel)(CUtensorMap, CUtensorMap, P), unsigned grid, int threads, size_t smem, int cluster, cudaStream_t st, const CUtensorMap &w,
+                   const CUtensorMap &a, const P &p)
+{
+    if (int rc = allow_smem(kernel, smem)) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, w, a, p) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return PERQ_ERR_CUDA;
+    }
+    return PERQ_OK;
+}
+
+// A product: dense ones are grouped ones of one expert that has all rows.
+struct Product {
+    const void *a, *w;
+    const float *a_scales, *w_scales;
+    const int32_t *w_sums, *offsets;
+    void *out;
+    int64_t T;
+    int32_t N, d, E, a_fmt, w_fmt, out_type;
+};
+
+template <bool W4, bool A4>
+int launch_few(const Product &m, cudaStream_t st)
+{
+    using K = perq_mm::Few<W4, A4>;
+    const int sms = sm_count();
+    if (sms <= 0) return PERQ_ERR_CUDA;
+    perq_mm::FewParams p;
+    std::memset(&p, 0, sizeof(p));
+    // columns for the tokens of a call, or for a little more than an expert has on average
+    const int64_t want = m.offsets ? std::min<int64_t>(m.T, (m.T * 3 / 2 + m.E - 1) / m.E) : m.T;
+    p.nt = want <= 16 ? 16 : want <= 32 ? 32 : want <= 64 ? 64 : 128;
+    p.n_tiles = (m.N + perq_mm::FEW_ROWS - 1) / perq_mm::FEW_ROWS;
+    p.steps = (m.d + K::step_codes - 1) / K::step_codes;
+    // at most as many tiles of tokens as there are experts with rows, and full ones
+    const int64_t token_tiles = m.offsets ? std::min<int64_t>(m.E, m.T) + m.T / p.nt : (m.T + p.nt - 1) / p.nt;
+    const int64_t items = token_tiles * p.n_tiles;
+    if (items >= (1ll << 31)) return PERQ_ERR_SHAPE;
+    p.split = 1;
+    while (p.split < 8 && items * p.split * 2 <= sms && p.split * 2 <= p.steps) p.split *= 2;
+    p.w_bytes = (W4 ? 1 : K::tiles) * perq_mm::FEW_TILE;
+    p.a_bytes = (A4 ? 1 : K::tiles) * (uint32_t)p.nt * 128u;
+    p.a_spread = A4 ? 2u * (uint32_t)p.nt * 128u : 0u;
+    const uint32_t load = p.w_bytes + p.a_bytes, spread = (W4 ? 2u * perq_mm::FEW_TILE : 0u) + p.a_spread;
+    const uint32_t tail = 16 + 8 * 2 * (16 + 4) + 32 + 4 * (m.offsets ? (uint32_t)m.E + 1 : 1);
+    const uint32_t room = (uint32_t)kMaxSmem - 1024 - tail;
+    p.spreads = K::packed ? 2 : 0;
+    p.loads = std::min<uint32_t>(12, (room - p.spreads * spread) / load);
+    p.off_spread = K::packed ? p.loads * load : 0;
+    p.off_bars = p.loads * load + p.spreads * spread;
+    p.off_first = p.off_bars + 16 + 16 * (p.loads + p.spreads) + 32;
+    const size_t smem = 1024 + p.off_first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
+    p.a_scales = m.a_scales;
+    p.w_scales = m.w_scales;
+    p.w_sums = m.w_sums;
+    p.offsets = m.offsets;
+    p.out = m.out;
+    p.T = (int32_t)m.T;
+    p.N = m.N;
+    p.E = m.E;
+    p.asym = m.a_fmt == PERQ_FMT_INT4_ASYM;
+    p.shift = (W4 ? 4 : 0) + (A4 ? 4 : 0);
+    p.out_type = m.out_type;
+    p.vec = m.N % 4 == 0;
+    p.idesc = perq_mm::product_desc(true, !p.asym, perq_mm::FEW_ROWS, p.nt);
+    p.tmem_cols = (uint32_t)p.nt;
+    CUtensorMap w, a;
+    if (!codes_map(&w, m.w, W4, (uint64_t)m.E * (uint64_t)m.N, m.d, perq_mm::FEW_ROWS) || !codes_map(&a, m.a, A4, (uint64_t)m.T, m.d, p.nt)) return PERQ_ERR_CUDA;
+    const int64_t clusters = p.split > 1 ? items : std::min<int64_t>(items, sms);
+    return launch_product(perq_mm::few_kernel<W4, A4>, (unsigned)(clusters * p.split), K::threads, smem, p.split, st, w, a, p);
+}
+
+int check_product(const Product &m)
+{
+    if (m.T < 0 || m.T > (1 << 30) || m.N <= 0 || m.N > PERQ_MAX_N || m.d <= 0 || m.d % 32 != 0 || m.d > PERQ_MAX_D) return PERQ_ERR_SHAPE;
+    if (m.E < 1 || m.E > PERQ_MAX_EXPERTS || (int64_t)m.E * m.N > (1ll << 30)) return PERQ_ERR_SHAPE;
+    if (m.a_fmt != PERQ_FMT_INT8 && m.a_fmt != PERQ_FMT_INT4 && m.a_fmt != PERQ_FMT_INT4_ASYM) return PERQ_ERR_FMT;
+    if (m.w_fmt != PERQ_FMT_INT8 && m.w_fmt != PERQ_FMT_INT4) return PERQ_ERR_FMT;
+    if (m.out_type < PERQ_OUT_BF16 || m.out_type > PERQ_OUT_F32) return PERQ_ERR_FMT;
+    return PERQ_OK;
+}
+
+size_t product_workspace(const Product &m)
+{
+    (void)m;
+    return 0;
+}
+
+int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaStream_t st)
+{
+    if (!m.a || !m.a_scales || !m.w || !m.w_scales || !m.out || (m.a_fmt == PERQ_FMT_INT4_ASYM && !m.w_sums)) return PERQ_ERR_NULL;
+    const size_t need = product_workspace(m);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return PERQ_ERR_WORKSPACE;
+    if (!aligned16(m.a) || !aligned16(m.a_scales) || !aligned16(m.w) || !aligned16(m.w_scales) || !aligned16(m.w_sums) || !aligned16(m.out) ||
+        !aligned16(m.offsets) || !aligned16(workspace))
+        return PERQ_ERR_ALIGN;
+    const bool w4 = is_packed(m.w_fmt), a4 = is_packed(m.a_fmt);
+    if (w4) return a4 ? launch_few<true, true>(m, st) : launch_few<true, false>(m, st);
+    return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);
+}
+
+}  // namespace
+
+cudaError_t perq_mm_read_error(unsigned int *flags) { return cudaMemcpyFromSymbol(flags, perq_mm::g_error, sizeof *flags); }
+cudaError_t perq_mm_clear_error()
+{
+    const unsigned int zero = 0;
+    return cudaMemcpyToSymbol(perq_mm::g_error, &zero, sizeof zero);
+}
+
+extern "C" {
+
+int perq_matmul_i8_workspace_bytes(int64_t T, int32_t N, int32_t d, int32_t a_fmt, int32_t w_fmt, size_t *bytes)
+{
+    const Product m = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, T, N, d, 1, a_fmt, w_fmt, PERQ_OUT_BF16};
+    if (int rc = check_product(m)) return rc;
+    if (!bytes) return PERQ_ERR_NULL;
+    *bytes = product_workspace(m);
+    return PERQ_OK;
+}
+
+int perq_matmul_i8(const void *a_codes, const float *a_scales, int32_t a_fmt, const void *w_codes, const float *w_scales, int32_t w_fmt, const int32_t *w_sums,
+                   int64_t T, int32_t N, int32_t d, void *out, int32_t out_type, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const Product m = {a_codes, w_codes, a_scales, w_scales, w_sums, nullptr, out, T, N, d, 1, a_fmt, w_fmt, out_type};
+    if (int rc = check_product(m)) return rc;
+    if (T == 0) return PERQ_OK;
+    return run_product(m, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int perq_grouped_matmul_i8_workspace_bytes(int64_t T, int32_t E, int32_t N, int32_t d, int32_t a_fmt, int32_t w_fmt, size_t *bytes)
+{
+    // (offsets only says that there are some)
+    const Product m = {nullptr, nullptr, nullptr, nullptr, nullptr, reinterpret_cast<const int32_t *>(16), nullptr, T, N, d, E, a_fmt, w_fmt, PERQ_OUT_BF16};
+    if (int rc = check_product(m)) return rc;
+    if (!bytes) return PERQ_ERR_NULL;
+    *bytes = product_workspace(m);
+    return PERQ_OK;
+}
+
+int perq_grouped_matmul_i8(const void *a_codes, const float *a_scales, int32_t a_fmt, const void *w_codes, const float *w_scales, int32_t w_fmt,
+                           const int32_t *w_sums, const int32_t *offsets, int64_t T, int32_t E, int32_t N, int32_t d, void *out, int32_t out_type, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    const Product m = {a_codes, w_codes, a_scales, w_scales, w_sums, offsets, out, T, N, d, E, a_fmt, w_fmt, out_type};
+    if (int rc = check_product(m)) return rc;
+    if (T == 0) return PERQ_OK;
+    if (!offsets) return PERQ_ERR_NULL;
+    return run_product(m, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,378 @@
+// Product of codes for few tokens (or few to an expert): y[t][n] = s_t s_n (sum_k a[t][k] w[n][k] + z_t c_n).
+//
+// Such calls are bound by reading the weights once, so a tile is 128 weight channels on the lanes of tensor memory by NT = 16 .. 128
+// tokens as its columns: one token wastes columns of the tensor core, which has time, and not weights.  A warp loads k-steps by
+// TMA into a ring; one issues the products; 4-bit codes lie packed in the ring and eight warps in between spread them to bytes, in
+// the order even codes, odd codes where both operands are packed (the sum does not mind, as long as both have it), in their
+// own order where only one is.  The accumulator is 32-bit integers, so sums are exact and the same however they are split.
+//
+// Few tiles are split along k over the CTAs of a cluster, which add their partial sums through distributed shared memory: no
+// workspace, no atomics and no second launch.
+//
+// Grouped calls (offsets): expert e has rows offsets[e] .. offsets[e + 1].  Every CTA counts the tiles of all experts itself and
+// takes every gridDim-th one; experts without rows have none, so their weights are not read.
+#pragma once
+
+#include "perq_mm_ptx.cuh"
+
+namespace perq_mm {
+
+constexpr int FEW_ROWS = 128;                 // weight channels of a tile
+constexpr int FEW_SPREADERS = 8;              // warps that spread packed codes
+constexpr uint32_t FEW_TILE = FEW_ROWS * 128; // bytes of 128 channels by 128 codes
+
+struct FewParams {
+    const float *a_scales, *w_scales;
+    const int32_t *w_sums, *offsets;
+    void *out;
+    int32_t T, N, E;
+    int32_t nt;                  // tokens of a tile
+    int32_t n_tiles;             // tiles of N
+    int32_t steps;               // k-steps
+    int32_t split;               // CTAs of the cluster
+    int32_t shift, asym;
+    int32_t out_type;
+    int32_t vec;                 // four results can be stored at once
+    uint32_t idesc;
+    uint32_t loads, spreads;     // stages of the two rings
+    uint32_t w_bytes, a_bytes;   // of a load
+    uint32_t a_spread;           // bytes of the tokens of a spread stage
+    uint32_t off_spread, off_bars, off_first;
+    uint32_t tmem_cols;          // of one accumulator
+};
+
+template <bool W4, bool A4>
+struct Few {
+    static constexpr bool packed = W4 || A4;
+    static constexpr int tiles = packed ? 2 : 1;                              // of 128 codes in a k-step
+    static constexpr int step_codes = 128 * tiles;
+    static constexpr int epilogue = packed ? 4 + FEW_SPREADERS : 4;           // first of four warps
+    static constexpr int threads = (epilogue + 4) * 32;
+};
+
+// Where a tile's tokens and channels are.
+struct FewItem {
+    int32_t expert, t0, t_end, n0;
+};
+__device__ __forceinline__ FewItem few_item(const FewParams &p, const int32_t *first, uint32_t item)
+{
+    FewItem it;
+    if (p.offsets == nullptr) {
+        const uint32_t tiles = (uint32_t)(p.T + p.nt - 1) / (uint32_t)p.nt, n = item / tiles;
+        it.expert = 0;
+        it.t0 = (int32_t)(item - n * tiles) * p.nt;
+        it.t_end = p.T;
+        it.n0 = (int32_t)n * FEW_ROWS;
+        return it;
+    }
+    // the expert whose tiles begin at or before this one: first[e] tiles of tokens lie before expert e
+    int lo = 0, hi = p.E;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((uint32_t)first[mid] * (uint32_t)p.n_tiles <= item) lo = mid; else hi = mid;
+    }
+    const uint32_t tiles = (uint32_t)(first[lo + 1] - first[lo]), local = item - (uint32_t)first[lo] * (uint32_t)p.n_tiles, n = local / tiles;
+    it.expert = lo;
+    const int32_t begin = min(max(__ldg(p.offsets + lo), 0), p.T);
+    it.t0 = begin + (int32_t)(local - n * tiles) * p.nt;
+    it.t_end = min(max(__ldg(p.offsets + lo + 1), 0), p.T);
+    it.n0 = (int32_t)n * FEW_ROWS;
+    return it;
+}
+
+// first[e]: tiles of tokens of the experts before e, by one warp.  (Offsets outside 0 .. T are taken into it.)
+__device__ __forceinline__ void count_tiles(const int32_t *offsets, int E, int32_t T, int32_t nt, int32_t *first, int lane)
+{
+    int32_t before = 0;
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + lane;
+        int32_t n = 0;
+        if (e < E) {
+            const int32_t b = min(max(__ldg(offsets + e), 0), T), c = min(max(__ldg(offsets + e + 1), 0), T);
+            n = c > b ? (c - b + nt - 1) / nt : 0;
+        }
+        int32_t sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (e < E) first[e] = before + sum - n;
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (lane == 0) first[E] = before;
+}
+
+__device__ __forceinline__ void store_one(void *out, int type, size_t at, float v)
+{
+    if (type == OUT_F32) static_cast<float *>(out)[at] = v;
+    else {
+        uint16_t h;
+        if (type == OUT_BF16) asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(v));
+        else asm("cvt.rn.f16.f32 %0, %1;" : "=h"(h) : "f"(v));
+        static_cast<uint16_t *>(out)[at] = h;
+    }
+}
+// Two results in one register, the first in its low half.
+__device__ __forceinline__ uint32_t pack_two(int type, float a, float b)
+{
+    uint32_t r;
+    if (type == OUT_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+
+struct TokenScale {
+    float s, z;
+};
+__device__ __forceinline__ TokenScale token_scale(const float *scales, int asym, int32_t t)
+{
+    TokenScale r;
+    r.s = __ldg(scales + (asym ? 2 * (size_t)t : (size_t)t));
+    r.z = asym ? __ldg(scales + 2 * (size_t)t + 1) : 0.0f;
+    return r;
+}
+
+// Packed rows of 128 bytes (256 codes) at `src` become two operand tiles at `dst` and `dst + tile`.  BOTH: even codes to the first,
+// odd ones to the second, in place; else in their order.  Lanes 0 .. 7 have the chunks of one row, which lie in eight
+// different groups of banks whichever way they are swizzled; in their order the second half of the row writes its odd chunk
+// first, for the same reason.
+template <bool BOTH>
+__device__ __forceinline__ void spread_rows(uint32_t src, uint32_t dst, uint32_t tile, int rows, int tid)
+{
+    for (int i = tid; i < rows * 8; i += FEW_SPREADERS * 32) {
+        const uint32_t r = (uint32_t)i >> 3, c = (uint32_t)i & 7u;
+        const uint4 v = lds128(src + (uint32_t)i * 16u);
+        const uint4 lo = make_uint4(codes_lo(v.x), codes_lo(v.y), codes_lo(v.z), codes_lo(v.w));
+        const uint4 hi = make_uint4(codes_hi(v.x), codes_hi(v.y), codes_hi(v.z), codes_hi(v.w));
+        if (BOTH) {
+            const uint32_t at = dst + operand_at(r, c);
+            sts128(at, lo);
+            sts128(at + tile, hi);
+        } else {
+            const uint4 x = make_uint4(__byte_perm(lo.x, hi.x, 0x5140), __byte_perm(lo.x, hi.x, 0x7362), __byte_perm(lo.y, hi.y, 0x5140),
+                                       __byte_perm(lo.y, hi.y, 0x7362));
+            const uint4 y = make_uint4(__byte_perm(lo.z, hi.z, 0x5140), __byte_perm(lo.z, hi.z, 0x7362), __byte_perm(lo.w, hi.w, 0x5140),
+                                       __byte_perm(lo.w, hi.w, 0x7362));
+            const uint32_t to = dst + (c >> 2) * tile, k = 2u * (c & 3u);
+            const bool second = (c >> 2) != 0u;
+            sts128(to + operand_at(r, second ? k + 1u : k), second ? y : x);
+            sts128(to + operand_at(r, second ? k : k + 1u), second ? x : y);
+        }
+    }
+}
+
+template <bool W4, bool A4>
+__global__ void __launch_bounds__(Few<W4, A4>::threads, 1)
+few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap a_map, const FewParams p)
+{
+    using K = Few<W4, A4>;
+    extern __shared__ unsigned char raw[];
+    unsigned char *const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(smem);
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    int32_t *const first = reinterpret_cast<int32_t *>(smem + p.off_first);           // [E + 1]
+    volatile uint32_t *const slot = reinterpret_cast<volatile uint32_t *>(smem + p.off_bars);
+    // barriers: loads full and empty, spread full and empty, accumulators full and empty (two)
+    const uint32_t l_full = base + p.off_bars + 16, l_empty = l_full + 8 * p.loads, s_full = l_empty + 8 * p.loads, s_empty = s_full + 8 * p.spreads,
+                   d_full = s_empty + 8 * p.spreads, d_empty = d_full + 16;
+    if (tid == 0) {
+        prefetch_map(&w_map);
+        prefetch_map(&a_map);
+        for (uint32_t i = 0; i < p.loads; ++i) {
+            mbar_init(l_full + 8 * i, 1);
+            // let go by the warps that spread it and, where an operand is used as it was loaded, by the tensor core
+            mbar_init(l_empty + 8 * i, (K::packed ? FEW_SPREADERS : 0) + (W4 && A4 ? 0 : 1));
+        }
+        for (uint32_t i = 0; i < p.spreads; ++i) {
+            mbar_init(s_full + 8 * i, FEW_SPREADERS);
+            mbar_init(s_empty + 8 * i, 1);
+        }
+        for (uint32_t i = 0; i < 2; ++i) {
+            mbar_init(d_full + 8 * i, 1);
+            mbar_init(d_empty + 8 * i, 4);
+        }
+        mbar_init_fence();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + p.off_bars), "r"(2 * p.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    griddep_wait();
+    griddep_launch();
+    if (warp == 2 && p.offsets != nullptr) count_tiles(p.offsets, p.E, p.T, p.nt, first, lane);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+
+    const uint32_t tmem = *slot;
+    const uint32_t rank = p.split > 1 ? cluster_rank() : 0u;
+    const uint32_t clusters = gridDim.x / (uint32_t)p.split;
+    const uint32_t token_tiles = p.offsets ? (uint32_t)first[p.E] : (uint32_t)(p.T + p.nt - 1) / (uint32_t)p.nt;
+    const uint32_t items = token_tiles * (uint32_t)p.n_tiles, begin = blockIdx.x / (uint32_t)p.split;
+    const uint32_t step0 = (uint32_t)p.steps * rank / (uint32_t)p.split, step1 = (uint32_t)p.steps * (rank + 1u) / (uint32_t)p.split;
+    const uint32_t a_tile = (uint32_t)p.nt * 128u, spread_bytes = p.off_spread ? (W4 ? 2u * FEW_TILE : 0u) + p.a_spread : 0u;
+    const uint32_t load_bytes = p.w_bytes + p.a_bytes;
+    auto load_at = [&](uint32_t s) { return base + s * load_bytes; };
+    auto spread_at = [&](uint32_t s) { return base + p.off_spread + s * spread_bytes; };
+    auto give_up = [&]() { atomicOr(&g_error, ERROR_FEW); };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t n = 0;
+            bool ok = true;
+            for (uint32_t item = begin; item < items && ok; item += clusters) {
+                const FewItem it = few_item(p, first, item);
+                const int w_row = it.expert * p.N + it.n0;
+                for (uint32_t k = step0; k < step1; ++k, ++n) {
+                    const uint32_t s = n % p.loads, bar = l_full + 8 * s;
+                    if (n >= p.loads && !mbar_wait(l_empty + 8 * s, (n / p.loads - 1u) & 1u)) { give_up(); ok = false; break; }
+                    mbar_expect_tx(bar, load_bytes);
+                    const uint32_t to = load_at(s);
+                    if (W4) tma_load(to, &w_map, (int)(k * 128u), w_row, bar);
+                    else
+                        for (int h = 0; h < K::tiles; ++h) tma_load(to + h * FEW_TILE, &w_map, (int)(k * K::step_codes + h * 128u), w_row, bar);
+                    if (A4) tma_load(to + p.w_bytes, &a_map, (int)(k * 128u), it.t0, bar);
+                    else
+                        for (int h = 0; h < K::tiles; ++h)
+                            tma_load(to + p.w_bytes + h * a_tile, &a_map, (int)(k * K::step_codes + h * 128u), it.t0, bar);
+                }
+            }
+            // nothing is in flight when the CTA ends, also after a wait that ran out
+            for (uint32_t i = n > p.loads ? n - p.loads : 0u; i < n; ++i) (void)mbar_wait(l_full + 8 * (i % p.loads), (i / p.loads) & 1u);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t n = 0, j = 0;
+            bool ok = true;
+            for (uint32_t item = begin; item < items; item += clusters, ++j) {
+                const uint32_t b = j & 1u;
+                if (j >= 2 && !mbar_wait(d_empty + 8 * b, ((j >> 1) - 1u) & 1u)) ok = false;
+                const uint32_t d = tmem + b * p.tmem_cols;
+                tmem_fence_after();
+                for (uint32_t k = step0; k < step1 && ok; ++k, ++n) {
+                    const uint32_t s = n % p.loads, u = K::packed ? n % p.spreads : 0u;
+                    ok = K::packed ? mbar_wait(s_full + 8 * u, (n / p.spreads) & 1u) : mbar_wait(l_full + 8 * s, (n / p.loads) & 1u);
+                    if (!ok) break;
+                    tmem_fence_after();
+                    const uint32_t w = W4 ? spread_at(u) : load_at(s), a = A4 ? spread_at(u) + (W4 ? 2u * FEW_TILE : 0u) : load_at(s) + p.w_bytes;
+#pragma unroll
+                    for (int h = 0; h < K::tiles; ++h) {
+                        const uint32_t wd = operand_lo(w + h * FEW_TILE), ad = operand_lo(a + h * a_tile);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) product<1>(d, wd + 2 * i, ad + 2 * i, p.idesc, k > step0 || h > 0 || i > 0);
+                    }
+                    if (!(W4 && A4)) commit(l_empty + 8 * s);
+                    if (K::packed) commit(s_empty + 8 * u);
+                }
+                if (!ok) { give_up(); break; }
+                commit(d_full + 8 * b);
+            }
+            // (products in flight end before tensor memory is given back)
+            for (uint32_t i = j > 2 ? j - 2 : 0u; i < j; ++i) (void)mbar_wait(d_full + 8 * (i & 1u), (i >> 1) & 1u);
+        }
+        __syncwarp();
+    } else if (K::packed && warp >= 4 && warp < 4 + FEW_SPREADERS) {
+        const int st = tid - 128;
+        uint32_t n = 0;
+        bool ok = true;
+        for (uint32_t item = begin; item < items && ok; item += clusters) {
+            for (uint32_t k = step0; k < step1; ++k, ++n) {
+                const uint32_t s = n % p.loads, u = n % p.spreads;
+                ok = mbar_wait(l_full + 8 * s, (n / p.loads) & 1u);
+                if (ok && n >= p.spreads) ok = mbar_wait(s_empty + 8 * u, (n / p.spreads - 1u) & 1u);
+                if (!ok) { give_up(); break; }
+                if (W4) spread_rows<W4 && A4>(load_at(s), spread_at(u), FEW_TILE, FEW_ROWS, st);
+                if (A4) spread_rows<W4 && A4>(load_at(s) + p.w_bytes, spread_at(u) + (W4 ? 2u * FEW_TILE : 0u), a_tile, p.nt, st);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(s_full + 8 * u);
+                    mbar_arrive(l_empty + 8 * s);
+                }
+            }
+        }
+    } else if (warp >= K::epilogue) {
+        const int q = warp & 3;
+        uint32_t j = 0;
+        for (uint32_t item = begin; item < items; item += clusters, ++j) {
+            const uint32_t b = j & 1u;
+            if (!mbar_wait(d_full + 8 * b, (j >> 1) & 1u)) { give_up(); break; }
+            tmem_fence_after();
+            const FewItem it = few_item(p, first, item);
+            const int n = it.n0 + q * 32 + lane;
+            const bool mine = n < p.N;
+            const size_t channel = (size_t)it.expert * (size_t)p.N + (size_t)min(n, p.N - 1);
+            const float s_n = __ldg(p.w_scales + channel), c_n = p.asym ? (float)__ldg(p.w_sums + channel) : 0.0f;
+            const uint32_t from = tmem + b * p.tmem_cols + ((uint32_t)(q * 32) << 16);
+            for (int c = 0; c < p.nt; c += 16) {
+                if (p.split == 1 && it.t0 + c >= it.t_end) break;
+                int32_t u[16];
+                tmem_load16(from + c, u);
+                tmem_wait(u);
+                if (p.split > 1) {                          // partial sums, token by token
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sts32(base + (uint32_t)(((c + i) * FEW_ROWS + q * 32 + lane) * 4), (uint32_t)u[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int t = it.t0 + c + i;
+                        if (t < it.t_end) {
+                            const TokenScale ts = token_scale(p.a_scales, p.asym, t);
+                            if (mine) store_one(p.out, p.out_type, (size_t)t * (size_t)p.N + n, scaled(u[i], p.shift, ts.s, s_n, ts.z, c_n));
+                        }
+                    }
+                }
+            }
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(d_empty + 8 * b);
+        }
+    }
+
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tmem_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * p.tmem_cols) : "memory");
+    }
+    if (p.split > 1) {
+        // every CTA of the cluster adds up a share of the tile's tokens: 32 threads to a token, four channels each
+        cluster_sync();
+        if (begin < items) {
+            const FewItem it = few_item(p, first, begin);
+            const int share = p.nt / p.split;
+            for (int i = tid; i < share * 32; i += K::threads) {
+                const int column = (int)rank * share + (i >> 5), t = it.t0 + column, n = it.n0 + (i & 31) * 4;
+                if (t >= it.t_end || n >= p.N) continue;
+                int32_t v[4] = {0, 0, 0, 0};
+                for (int r = 0; r < p.split; ++r) {
+                    const uint4 u = lds_at_rank(base + (uint32_t)((column * FEW_ROWS + (i & 31) * 4) * 4), (uint32_t)r);
+                    v[0] += (int32_t)u.x; v[1] += (int32_t)u.y; v[2] += (int32_t)u.z; v[3] += (int32_t)u.w;
+                }
+                const TokenScale ts = token_scale(p.a_scales, p.asym, t);
+                const size_t channel = (size_t)it.expert * (size_t)p.N + (size_t)n, at = (size_t)t * (size_t)p.N + (size_t)n;
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const size_t ch = channel + (size_t)min(e, p.N - 1 - n);
+                    y[e] = scaled(v[e], p.shift, ts.s, __ldg(p.w_scales + ch), ts.z, p.asym ? (float)__ldg(p.w_sums + ch) : 0.0f);
+                }
+                if (p.vec) {                                // (N is then a multiple of four)
+                    if (p.out_type == OUT_F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
+                    else
+                        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at) =
+                            make_uint2(pack_two(p.out_type, y[0], y[1]), pack_two(p.out_type, y[2], y[3]));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n + e < p.N) store_one(p.out, p.out_type, at + e, y[e]);
+                }
+            }
+        }
+        cluster_sync();                                     // (the others have read this one's sums)
+    }
+}
+
+}  // namespace perq_mm

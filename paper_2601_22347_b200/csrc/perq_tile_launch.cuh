@@ -2,25 +2,6 @@
 // anonymous namespace (uses its sm_count, allow_smem, ilog2, is_pow2).
 #pragma once
 
-// The driver's encoder of tensor maps, asked for once (the library does not link against libcuda).
-typedef CUresult (*TensorMapEncode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                    const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-TensorMapEncode tensor_map_encode()
-{
-    static std::atomic<void *> cached{nullptr};
-    void *fn = cached.load();
-    if (fn == nullptr) {
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            return nullptr;
-        }
-        cached.store(fn);
-    }
-    return reinterpret_cast<TensorMapEncode>(fn);
-}
-
 // x as rows of 128 channels, read in boxes of 64 channels by `rows`, 128-byte swizzle.
 bool tile_tensor_map(CUtensorMap *map, const void *x, uint64_t pieces, int rows)
 {

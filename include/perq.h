@@ -41,7 +41,7 @@ typedef enum {
     PERQ_FMT_F32_DEBUG = 2, /* no quantisation: the rotated row as fp32 (test hook) */
     PERQ_FMT_FP4 = 3,       /* E2M1 elements, one fp32 scale per token (Appendix B, FP4 activations) */
     PERQ_FMT_INT4_ASYM = 4, /* asymmetric INT4, (scale, zero point) per token (Appendix B, INT4 activations) */
-    PERQ_FMT_INT8 = 5       /* symmetric INT8, one fp32 scale per row: the products' operands only */
+    PERQ_FMT_INT8 = 5       /* symmetric INT8, one fp32 scale per row: perq_rotate_quantize_i8 and the products only */
 } perq_fmt_t;
 
 typedef enum { PERQ_OUT_BF16 = 0, PERQ_OUT_F16 = 1, PERQ_OUT_F32 = 2 } perq_out_t;   /* results of the products */
@@ -322,6 +322,28 @@ int perq_massdiff_perm_device(const float *chan_abs_sum, int32_t d, int32_t b, i
                               void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * perq_rotate_quantize_i8 -- the path with 8-bit codes: rows of tokens, or of weight channels, for the products below.
+ *
+ * Defined by: steps 1 and 2 of perq_rotate_quantize and the symmetric quantiser of Sec. 3 with q = 8, one step per row:
+ *     a = max_i |y_i|,  s = a / 127,  code_i = rne(y_i / s)   (ties to even; a == 0 gives scale 0 and codes 0)
+ * with codes decided in exact arithmetic and s stored as fp32.  y = x' (no rotation) for b == 1.
+ *
+ * x, perm, T, d as for perq_rotate_quantize.  b: 1, or a power of two from 16 to 512 that divides d (larger powers of two that
+ * divide d: PERQ_ERR_UNSUPPORTED).  out_codes int8 [T, d], out_scales float [T].
+ * Deterministic.  Every finite row is served down to subnormals; sqrt(b) |y| has to stay below 2^128.
+ * Errors: NULL, SHAPE, BLOCK, UNSUPPORTED, ALIGN, CUDA.
+ */
+int perq_rotate_quantize_i8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *out_codes,
+                            float *out_scales, void *stream);
+
+/*
+ * perq_code_sums -- sums[r] = sum_k code[r][k] of rows of INT8 or INT4 codes (device int32 [rows]): what the products want of the
+ * weights for asymmetric tokens, made once with them.  fmt: PERQ_FMT_INT8, PERQ_FMT_INT4.  rows == 0 is a no-op; d as above.
+ * Errors: NULL, SHAPE, FMT, ALIGN, CUDA.
+ */
+int perq_code_sums(const void *codes, int32_t fmt, int64_t rows, int32_t d, int32_t *sums, void *stream);
+
+/*
  * perq_matmul_i8 -- the linear layer that reads the path's codes: the product of codes in 8-bit integers with a scale for
  * each token and each weight channel.
  *
@@ -336,11 +358,11 @@ int perq_massdiff_perm_device(const float *chan_abs_sum, int32_t d, int32_t b, i
  * out_type, to nearest even.  Results are the same from run to run and do not depend on which kernel serves the call.
  *
  *   a_codes, a_scales   device: codes and scales of T rows as perq_rotate_quantize writes them for INT4 per token (uint8
- *                       [T, d/2], float [T]) and INT4_ASYM (uint8 [T, d/2], float [T, 2]: step, zero point), or INT8 codes
- *                       (int8 [T, d], float [T])
+ *                       [T, d/2], float [T]) and INT4_ASYM (uint8 [T, d/2], float [T, 2]: step, zero point), or as
+ *                       perq_rotate_quantize_i8 does (int8 [T, d], float [T])
  *   a_fmt               PERQ_FMT_INT8, PERQ_FMT_INT4 or PERQ_FMT_INT4_ASYM
  *   w_codes, w_scales   device: the same of N weight channels (rows [N, d]); w_fmt PERQ_FMT_INT8 or PERQ_FMT_INT4
- *   w_sums              device int32 [N]: c_n; read for INT4_ASYM only (else it may be NULL)
+ *   w_sums              device int32 [N]: c_n, from perq_code_sums; read for INT4_ASYM only (else it may be NULL)
  *   T, N, d             T == 0 is a no-op; T <= 2^30; 1 <= N <= PERQ_MAX_N; d % 32 == 0, d <= PERQ_MAX_D
  *   out                 device [T, N] of out_type (perq_out_t), row stride N, written in full
  *   workspace           device, at least perq_matmul_i8_workspace_bytes(...) bytes (NULL where that is 0).  Its contents

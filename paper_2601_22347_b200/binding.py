@@ -71,7 +71,9 @@ def load() -> C.CDLL:
         lib.perq_matmul_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, C.POINTER(sz)]
         lib.perq_grouped_matmul_i8.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, i64, i32, i32, i32, vp, i32, vp, sz, vp]
         lib.perq_grouped_matmul_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, C.POINTER(sz)]
-        for name in ("perq_matmul_i8", "perq_matmul_i8_workspace_bytes", "perq_grouped_matmul_i8", "perq_grouped_matmul_i8_workspace_bytes"):
+        lib.perq_rotate_quantize_i8.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp]
+        lib.perq_code_sums.argtypes = [vp, i32, i64, i32, vp, vp]
+        for name in ("perq_rotate_quantize_i8", "perq_code_sums", "perq_matmul_i8", "perq_matmul_i8_workspace_bytes", "perq_grouped_matmul_i8", "perq_grouped_matmul_i8_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
         lib.perq_device_error.argtypes = [C.POINTER(C.c_uint32)]
         lib.perq_device_error.restype = C.c_int
@@ -326,6 +328,33 @@ def perq_massdiff_perm(chan_abs_sum_host: np.ndarray, b: int) -> np.ndarray:
     rc = load().perq_massdiff_perm(a.ctypes.data_as(C.c_void_p), a.shape[0], b, perm.ctypes.data_as(C.c_void_p))
     _check(rc, "perq_massdiff_perm")
     return perm
+
+
+def perq_rotate_quantize_i8(x: torch.Tensor, perm: Optional[torch.Tensor], b: int, out_codes: Optional[torch.Tensor] = None,
+                            out_scales: Optional[torch.Tensor] = None, stream=None):
+    """x: bf16 CUDA tensor [T, d] (contiguous); perm: int32 CUDA tensor [d] or None.  Returns (int8 [T, d], fp32 [T, 1])."""
+    assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 2 and x.is_contiguous()
+    assert perm is None or (perm.is_cuda and perm.dtype == torch.int32 and perm.is_contiguous())
+    T, d = x.shape
+    assert perm is None or perm.numel() == d
+    if out_codes is None:
+        out_codes = torch.empty((T, d), dtype=torch.int8, device=x.device)
+    if out_scales is None:
+        out_scales = torch.empty((T, 1), dtype=torch.float32, device=x.device)
+    assert out_codes.is_cuda and out_codes.is_contiguous() and out_codes.dtype == torch.int8 and out_codes.numel() == T * d
+    assert out_scales.is_cuda and out_scales.is_contiguous() and out_scales.dtype == torch.float32 and out_scales.numel() == T
+    _check(load().perq_rotate_quantize_i8(_ptr(x), _ptr(perm), T, d, b, _ptr(out_codes), _ptr(out_scales), _stream(stream)),
+           "perq_rotate_quantize_i8")
+    return out_codes, out_scales
+
+
+def perq_code_sums(codes: torch.Tensor, fmt: int, stream=None) -> torch.Tensor:
+    """Sums of the rows of codes (int8 [.., d], or uint8 [.., d / 2] for INT4): int32 CUDA tensor [..]."""
+    assert codes.is_cuda and codes.is_contiguous() and codes.dtype == (torch.int8 if fmt == PERQ_FMT_INT8 else torch.uint8)
+    d = codes.shape[-1] * (1 if fmt == PERQ_FMT_INT8 else 2)
+    sums = torch.empty(codes.shape[:-1], dtype=torch.int32, device=codes.device)
+    _check(load().perq_code_sums(_ptr(codes), fmt, sums.numel(), d, _ptr(sums), _stream(stream)), "perq_code_sums")
+    return sums
 
 
 def perq_matmul_i8_workspace_bytes(T: int, N: int, d: int, a_fmt: int, w_fmt: int) -> int:

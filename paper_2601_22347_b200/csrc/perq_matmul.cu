@@ -1,12 +1,14 @@
-// C ABI of the products of codes: argument checks, choice of kernel, tensor maps, launches.
+// C ABI of the 8-bit linear layers (rows to 8-bit codes, products of codes): argument checks, choice of kernel, tensor maps, launches.
 // Nothing here allocates device memory or synchronises, except where perq.h says so.
 #include "perq.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "perq_host.cuh"
 #include "perq_mm_few.cuh"
+#include "perq_quant8.cuh"
 
 namespace {
 
@@ -142,6 +144,57 @@ int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaS
     return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);
 }
 
+// Programmatic stream serialization, without clusters.
+template <typename P>
+int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cudaStream_t st, const P &p)
+{
+    if (int rc = allow_smem(kernel, smem)) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return PERQ_ERR_CUDA;
+    }
+    return PERQ_OK;
+}
+
+int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *codes, float *scales, cudaStream_t st)
+{
+    using namespace perq_q8;
+    const int sms = sm_count();
+    if (sms <= 0) return PERQ_ERR_CUDA;
+    Params p;
+    std::memset(&p, 0, sizeof(p));
+    p.x = static_cast<const uint16_t *>(x);
+    p.perm = perm;
+    p.codes = static_cast<int8_t *>(codes);
+    p.scales = scales;
+    p.T = T;
+    p.d = d;
+    p.log2b = ilog2(b);
+    const int pieces = d > MAX_THREADS * LANE_ELEMS ? 2 : 1;
+    p.warps = (d + pieces * WARP_ELEMS - 1) / (pieces * WARP_ELEMS);
+    p.rows = (int)std::min<int64_t>(std::max(1, 8 / p.warps), std::max<int64_t>(1, (T + sms - 1) / sms));
+    // E, the fp32 quotient's own roundings (three of 127 at most), and the maximum's error in it
+    const double e = p.log2b * std::sqrt((double)b) * 0x1p-24;
+    p.near_max = (float)(1.0 - 2.0 * e - 0x1p-22);
+    p.doubt = (float)(0.5 - 127.5 * (2.0 * e + 6.0 * 0x1p-24));
+    p.inv_scale = 1.0 / (127.0 * std::sqrt((double)b));
+    const int threads = p.rows * p.warps * 32;
+    const size_t smem = (size_t)p.rows * (sizeof(RowShared) + (perm ? (size_t)d * 2 : 0));
+    const long long grid = std::min<long long>((T + p.rows - 1) / p.rows, (long long)sms * std::max(1, 1024 / threads));
+    if (pieces == 1) return launch_plain(perm ? quant8_kernel<1, true> : quant8_kernel<1, false>, grid, threads, smem, st, p);
+    return launch_plain(perm ? quant8_kernel<2, true> : quant8_kernel<2, false>, grid, threads, smem, st, p);
+}
+
 }  // namespace
 
 cudaError_t perq_mm_read_error(unsigned int *flags) { return cudaMemcpyFromSymbol(flags, perq_mm::g_error, sizeof *flags); }
@@ -152,6 +205,33 @@ cudaError_t perq_mm_clear_error()
 }
 
 extern "C" {
+
+int perq_rotate_quantize_i8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *out_codes, float *out_scales, void *stream)
+{
+    if (T < 0 || d <= 0 || d % 32 != 0 || d > PERQ_MAX_D) return PERQ_ERR_SHAPE;
+    if (!is_pow2(b) || (b != 1 && b < 16) || b > d || d % b != 0) return PERQ_ERR_BLOCK;
+    if (b > 1 << perq_q8::MAX_LOG2B) return PERQ_ERR_UNSUPPORTED;
+    if (T == 0) return PERQ_OK;
+    if (!x || !out_codes || !out_scales) return PERQ_ERR_NULL;
+    if (!aligned16(x) || !aligned16(perm) || !aligned16(out_codes) || !aligned16(out_scales)) return PERQ_ERR_ALIGN;
+    return launch_quant8(x, perm, T, d, b, out_codes, out_scales, static_cast<cudaStream_t>(stream));
+}
+
+int perq_code_sums(const void *codes, int32_t fmt, int64_t rows, int32_t d, int32_t *sums, void *stream)
+{
+    if (rows < 0 || rows > (1ll << 30) || d <= 0 || d % 32 != 0 || d > PERQ_MAX_D) return PERQ_ERR_SHAPE;
+    if (fmt != PERQ_FMT_INT8 && fmt != PERQ_FMT_INT4) return PERQ_ERR_FMT;
+    if (rows == 0) return PERQ_OK;
+    if (!codes || !sums) return PERQ_ERR_NULL;
+    if (!aligned16(codes) || !aligned16(sums)) return PERQ_ERR_ALIGN;
+    perq_q8::SumParams p;
+    p.codes = codes;
+    p.sums = sums;
+    p.rows = rows;
+    p.packed = is_packed(fmt);
+    p.chunks = d / (p.packed ? 32 : 16);
+    return launch_plain(perq_q8::code_sums_kernel, (rows + 7) / 8, 256, 0, static_cast<cudaStream_t>(stream), p);
+}
 
 int perq_matmul_i8_workspace_bytes(int64_t T, int32_t N, int32_t d, int32_t a_fmt, int32_t w_fmt, size_t *bytes)
 {

@@ -71,3 +71,27 @@ def test_workspace_bytes(lib):
     assert lib.perq_grouped_matmul_i8_workspace_bytes(1, 8, 4096, 4096, 0, 0, C.byref(n)) == OK and n.value == 0
     assert lib.perq_grouped_matmul_i8_workspace_bytes(1, 0, 4096, 4096, 0, 0, C.byref(n)) == SHAPE
     assert lib.perq_grouped_matmul_i8_workspace_bytes(1, 8, 4096, 4096, 0, 0, None) == NULL
+
+
+@pytest.mark.parametrize("change,status", [(dict(T=-1), SHAPE), (dict(d=40), SHAPE), (dict(d=0), SHAPE), (dict(d=65536), SHAPE), (dict(b=8), 3), (dict(b=24), 3),
+                                           (dict(b=0), 3), (dict(d=96, b=64), 3), (dict(b=512, d=256), 3), (dict(b=1024), 10), (dict(b=4096), 10),
+                                           (dict(x=None), NULL), (dict(oc=None), NULL), (dict(os=None), NULL), (dict(x=ODD), ALIGN), (dict(perm=ODD), ALIGN),
+                                           (dict(oc=ODD), ALIGN), (dict(os=ODD), ALIGN), (dict(T=0, x=None), OK)])
+def test_rows_to_8_bit_codes_refused(lib, change, status):
+    v = dict(dict(x=P, perm=None, T=4, d=4096, b=32, oc=P, os=P), **change)
+    assert lib.perq_rotate_quantize_i8(v["x"], v["perm"], v["T"], v["d"], v["b"], v["oc"], v["os"], None) == status
+
+
+def test_code_sums_refused(lib):
+    def call(codes=P, fmt=5, rows=4, d=256, sums=P):
+        return lib.perq_code_sums(codes, fmt, rows, d, sums, None)
+    assert call(fmt=4) == FMT and call(fmt=1) == FMT
+    assert call(rows=-1) == SHAPE and call(d=100) == SHAPE and call(d=40000) == SHAPE
+    assert call(codes=None) == NULL and call(sums=None) == NULL
+    assert call(codes=ODD) == ALIGN and call(sums=ODD) == ALIGN
+    assert call(rows=0, codes=None) == OK
+
+
+def test_8_bit_codes_are_not_a_format_of_the_4_bit_path(lib):
+    assert lib.perq_rotate_quantize(P, None, 4, 4096, 32, 5, 0, P, P, None) == FMT
+    assert lib.perq_out_sizes(4, 4096, 5, 0, None, None) == FMT

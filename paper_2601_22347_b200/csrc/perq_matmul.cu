@@ -7,7 +7,7 @@
 #include <cstring>
 
 #include "perq_host.cuh"
-#include "perq_mm_few.cuh"
+#include "perq_mm_many.cuh"
 #include "perq_quant8.cuh"
 
 namespace {
@@ -115,35 +115,6 @@ int launch_few(const Product &m, cudaStream_t st)
     return launch_product(perq_mm::few_kernel<W4, A4>, (unsigned)(clusters * p.split), K::threads, smem, p.split, st, w, a, p);
 }
 
-int check_product(const Product &m)
-{
-    if (m.T < 0 || m.T > (1 << 30) || m.N <= 0 || m.N > PERQ_MAX_N || m.d <= 0 || m.d % 32 != 0 || m.d > PERQ_MAX_D) return PERQ_ERR_SHAPE;
-    if (m.E < 1 || m.E > PERQ_MAX_EXPERTS || (int64_t)m.E * m.N > (1ll << 30)) return PERQ_ERR_SHAPE;
-    if (m.a_fmt != PERQ_FMT_INT8 && m.a_fmt != PERQ_FMT_INT4 && m.a_fmt != PERQ_FMT_INT4_ASYM) return PERQ_ERR_FMT;
-    if (m.w_fmt != PERQ_FMT_INT8 && m.w_fmt != PERQ_FMT_INT4) return PERQ_ERR_FMT;
-    if (m.out_type < PERQ_OUT_BF16 || m.out_type > PERQ_OUT_F32) return PERQ_ERR_FMT;
-    return PERQ_OK;
-}
-
-size_t product_workspace(const Product &m)
-{
-    (void)m;
-    return 0;
-}
-
-int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaStream_t st)
-{
-    if (!m.a || !m.a_scales || !m.w || !m.w_scales || !m.out || (m.a_fmt == PERQ_FMT_INT4_ASYM && !m.w_sums)) return PERQ_ERR_NULL;
-    const size_t need = product_workspace(m);
-    if (need > 0 && (!workspace || workspace_bytes < need)) return PERQ_ERR_WORKSPACE;
-    if (!aligned16(m.a) || !aligned16(m.a_scales) || !aligned16(m.w) || !aligned16(m.w_scales) || !aligned16(m.w_sums) || !aligned16(m.out) ||
-        !aligned16(m.offsets) || !aligned16(workspace))
-        return PERQ_ERR_ALIGN;
-    const bool w4 = is_packed(m.w_fmt), a4 = is_packed(m.a_fmt);
-    if (w4) return a4 ? launch_few<true, true>(m, st) : launch_few<true, false>(m, st);
-    return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);
-}
-
 // Programmatic stream serialization, without clusters.
 template <typename P>
 int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cudaStream_t st, const P &p)
@@ -164,6 +135,107 @@ int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cu
         return PERQ_ERR_CUDA;
     }
     return PERQ_OK;
+}
+
+// Whether the kernel for many tokens is the better one.
+bool many_is_better(const Product &m, int sms)
+{
+    (void)sms;
+    return m.offsets ? m.T >= 256 * (int64_t)m.E : m.T >= 1024;
+}
+
+// What the kernel for many tokens wants of the workspace: packed operands as bytes, tokens first.
+struct ManySpace {
+    size_t tokens, weights;
+};
+ManySpace many_space(const Product &m)
+{
+    auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+    return {is_packed(m.a_fmt) ? up((size_t)m.T * (size_t)m.d) : 0, is_packed(m.w_fmt) ? up((size_t)m.E * (size_t)m.N * (size_t)m.d) : 0};
+}
+
+int spread(const void *src, void *dst, long long codes, const int32_t *offsets, long long per_expert, int64_t T, int sms, cudaStream_t st)
+{
+    perq_mm::SpreadParams p;
+    p.src = static_cast<const uint4 *>(src);
+    p.dst = static_cast<uint4 *>(dst);
+    p.offsets = offsets;
+    p.chunks = codes / 32;
+    p.per_expert = per_expert / 32;
+    p.T = (int32_t)T;
+    return launch_plain(perq_mm::spread_kernel, std::min<long long>((p.chunks + 255) / 256, 8ll * sms), 256, 0, st, p);
+}
+
+int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_t st)
+{
+    const ManySpace space = many_space(m);
+    const void *tokens = m.a, *weights = m.w;
+    if (space.tokens > 0) {
+        tokens = workspace;
+        if (int rc = spread(m.a, workspace, (long long)m.T * m.d, nullptr, 32, m.T, sms, st)) return rc;
+    }
+    if (space.weights > 0) {
+        weights = workspace + space.tokens;
+        if (int rc = spread(m.w, workspace + space.tokens, (long long)m.E * m.N * m.d, m.offsets, (long long)m.N * m.d, m.T, sms, st)) return rc;
+    }
+    perq_mm::ManyParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.a_scales = m.a_scales;
+    p.w_scales = m.w_scales;
+    p.w_sums = m.w_sums;
+    p.offsets = m.offsets;
+    p.out = m.out;
+    p.T = (int32_t)m.T;
+    p.N = m.N;
+    p.E = m.E;
+    p.n_tiles = (m.N + perq_mm::MANY_CHANNELS - 1) / perq_mm::MANY_CHANNELS;
+    p.steps = (m.d + 127) / 128;
+    p.asym = m.a_fmt == PERQ_FMT_INT4_ASYM;
+    p.shift = (space.tokens ? 4 : 0) + (space.weights ? 4 : 0);
+    p.out_type = m.out_type;
+    p.wide = (size_t)m.N * (m.out_type == PERQ_OUT_F32 ? 4 : 2) % 32 == 0 && (reinterpret_cast<uintptr_t>(m.out) & 31u) == 0;
+    p.idesc = perq_mm::product_desc(!p.asym, true, perq_mm::MANY_TOKENS, perq_mm::MANY_CHANNELS);
+    const int64_t token_tiles = m.offsets ? std::min<int64_t>(m.E, m.T) + m.T / perq_mm::MANY_TOKENS : (m.T + perq_mm::MANY_TOKENS - 1) / perq_mm::MANY_TOKENS;
+    const int64_t items = token_tiles * p.n_tiles;
+    if (items >= (1ll << 31)) return PERQ_ERR_SHAPE;
+    CUtensorMap w, a;
+    if (!codes_map(&w, weights, false, (uint64_t)m.E * (uint64_t)m.N, m.d, 128) || !codes_map(&a, tokens, false, (uint64_t)m.T, m.d, 128)) return PERQ_ERR_CUDA;
+    const size_t smem = 1024 + perq_mm::ManySmem::first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
+    return launch_product(perq_mm::many_kernel, (unsigned)(2 * std::min<int64_t>(items, sms / 2)), perq_mm::MANY_THREADS, smem, 2, st, w, a, p);
+}
+
+int check_product(const Product &m)
+{
+    if (m.T < 0 || m.T > (1 << 30) || m.N <= 0 || m.N > PERQ_MAX_N || m.d <= 0 || m.d % 32 != 0 || m.d > PERQ_MAX_D) return PERQ_ERR_SHAPE;
+    if (m.E < 1 || m.E > PERQ_MAX_EXPERTS || (int64_t)m.E * m.N > (1ll << 30)) return PERQ_ERR_SHAPE;
+    if (m.a_fmt != PERQ_FMT_INT8 && m.a_fmt != PERQ_FMT_INT4 && m.a_fmt != PERQ_FMT_INT4_ASYM) return PERQ_ERR_FMT;
+    if (m.w_fmt != PERQ_FMT_INT8 && m.w_fmt != PERQ_FMT_INT4) return PERQ_ERR_FMT;
+    if (m.out_type < PERQ_OUT_BF16 || m.out_type > PERQ_OUT_F32) return PERQ_ERR_FMT;
+    return PERQ_OK;
+}
+
+size_t product_workspace(const Product &m)
+{
+    const int sms = sm_count();
+    if (m.T == 0 || !many_is_better(m, sms)) return 0;
+    const ManySpace space = many_space(m);
+    return space.tokens + space.weights;
+}
+
+int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaStream_t st)
+{
+    if (!m.a || !m.a_scales || !m.w || !m.w_scales || !m.out || (m.a_fmt == PERQ_FMT_INT4_ASYM && !m.w_sums)) return PERQ_ERR_NULL;
+    const size_t need = product_workspace(m);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return PERQ_ERR_WORKSPACE;
+    if (!aligned16(m.a) || !aligned16(m.a_scales) || !aligned16(m.w) || !aligned16(m.w_scales) || !aligned16(m.w_sums) || !aligned16(m.out) ||
+        !aligned16(m.offsets) || !aligned16(workspace))
+        return PERQ_ERR_ALIGN;
+    const int sms = sm_count();
+    if (sms <= 0) return PERQ_ERR_CUDA;
+    if (many_is_better(m, sms)) return launch_many(m, static_cast<unsigned char *>(workspace), sms, st);
+    const bool w4 = is_packed(m.w_fmt), a4 = is_packed(m.a_fmt);
+    if (w4) return a4 ? launch_few<true, true>(m, st) : launch_few<true, false>(m, st);
+    return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);
 }
 
 int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *codes, float *scales, cudaStream_t st)

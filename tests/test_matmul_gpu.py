@@ -43,7 +43,9 @@ def dense(B, a_fmt, w_fmt, T, N, d, dtype, seed=0):
 # one token, one channel, the shortest rows; a k-step and a tile more or less; every number of columns; rows that end inside a
 # k-step; split sums; several tiles of tokens; enough tiles that a CTA takes several
 SHAPES = [(1, 1, 32), (1, 128, 256), (16, 128, 128), (17, 129, 160), (7, 130, 4096), (33, 257, 96), (64, 100, 288), (128, 128, 512), (129, 1001, 2048),
-          (300, 4096, 1056), (5, 4096, 14336), (2, 70, 32768), (600, 4100, 224)]
+          (300, 4096, 1056), (5, 4096, 14336), (2, 70, 32768), (600, 4100, 224),
+          # many tokens: ragged tiles of both sides, rows shorter than a k-step and longer than the ring, bands of tiles, several tiles to a CTA
+          (1024, 256, 128), (1500, 1001, 96), (1025, 2064, 1056), (5000, 129, 32), (2600, 5000, 160)]
 
 
 @pytest.mark.parametrize("a_fmt,w_fmt", FORMATS)
@@ -54,7 +56,7 @@ def test_dense(B, a_fmt, w_fmt, T, N, d):
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("a_fmt,w_fmt", [(INT8, INT8), (ASYM, INT4)])
-@pytest.mark.parametrize("T,N,d", [(1, 1, 32), (20, 300, 512), (20, 301, 512), (150, 258, 64), (150, 4096, 64), (9, 2048, 4096)])
+@pytest.mark.parametrize("T,N,d", [(1, 1, 32), (20, 300, 512), (20, 301, 512), (150, 258, 64), (150, 4096, 64), (9, 2048, 4096), (1100, 272, 64), (1100, 280, 64), (1100, 257, 64)])
 def test_result_types(B, a_fmt, w_fmt, T, N, d, dtype):
     dense(B, a_fmt, w_fmt, T, N, d, dtype)
 
@@ -74,7 +76,8 @@ def grouped(B, a_fmt, w_fmt, offsets, T, N, d, dtype=F32):
 
 
 OFFSETS = [([0, 1], 1), ([0, 0, 5, 5, 18], 20), ([3, 130, 130, 131, 400, 690], 700), ([0, 1, 10, 64], 64), ([0] * 40 + [7] * 25, 9), ([5, 5, 5], 6),
-           ([0, 500, 500, 501, 502], 502), (list(range(0, 130)), 129)]
+           ([0, 500, 500, 501, 502], 502), (list(range(0, 130)), 129), ([7, 7, 3000, 3001, 3001, 4000], 4005), ([0, 1, 257, 513, 2000], 2000),
+           ([0, 0, 0, 0], 800), ([0, 900], 1024)]
 
 
 @pytest.mark.parametrize("a_fmt,w_fmt", FORMATS)
@@ -98,7 +101,7 @@ def test_bad_offsets_do_not_write_past_the_rows(B):
     """Wrong numbers, never a fault: entries outside the rows, and entries that decrease."""
     a, sa, w, sw, _ = operands(INT8, INT8, 50, 64, 128, 5, 4)
     room = torch.full((150, 64), 77.0, device="cuda")
-    for bad in ([-5, 20, 10, 60, 2 ** 31 - 1], [50, 40, 30, 20, 10], [-2 ** 31, -1, 0, 200, 100]):
+    for bad in ([-5, 20, 10, 60, 2 ** 31 - 1], [50, 40, 30, 20, 10], [-2 ** 31, -1, 0, 200, 100], [0, 50, 0, 50, 0]):
         B.perq_grouped_matmul_i8(a, sa, B.PERQ_FMT_INT8, w.reshape(4, 64, -1), sw.reshape(4, 64), B.PERQ_FMT_INT8,
                                  torch.tensor(bad, dtype=torch.int32, device="cuda"), out=room[50:100])
         torch.cuda.synchronize()

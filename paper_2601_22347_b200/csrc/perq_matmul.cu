@@ -255,10 +255,9 @@ int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int3
     const int pieces = d > MAX_THREADS * LANE_ELEMS ? 2 : 1;
     p.warps = (d + pieces * WARP_ELEMS - 1) / (pieces * WARP_ELEMS);
     p.rows = (int)std::min<int64_t>(std::max(1, 8 / p.warps), std::max<int64_t>(1, (T + sms - 1) / sms));
-    // E, the fp32 quotient's own roundings (three of 127 at most), and the maximum's error in it
     const double e = p.log2b * std::sqrt((double)b) * 0x1p-24;
     p.near_max = (float)(1.0 - 2.0 * e - 0x1p-22);
-    p.doubt = (float)(0.5 - 127.5 * (2.0 * e + 6.0 * 0x1p-24));
+    p.doubt = (float)(1.001 * (2.0 * e + 6.0 * 0x1p-24));
     p.inv_scale = 1.0 / (127.0 * std::sqrt((double)b));
     const int threads = p.rows * p.warps * 32;
     const size_t smem = (size_t)p.rows * (sizeof(RowShared) + (perm ? (size_t)d * 2 : 0));

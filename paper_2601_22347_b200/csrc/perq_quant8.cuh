@@ -6,9 +6,10 @@
 //
 // Codes are those of exact arithmetic.  A stage rounds each value to within 2^-24 of itself, an error vector of at most 2^-24 |v|, and
 // the stages after it are orthogonal but for the factor that they give v itself: log2(b) of them lose |u32 - u| <= log2(b) 2^-24 |u|_2
-// <= E max|u|, E = log2(b) sqrt(b) 2^-24.  The row's maximum is summed again in fp64 wherever |u32| is within 2 E of the largest, and so is
-// every element whose quotient lies that close to the border between two codes (E = 0 without a rotation: then only the fp32 quotient
-// is in doubt).  b = 32, gaussian values: 1.8 elements of a row of 4096.
+// <= E max|u| over the block, E = log2(b) sqrt(b) 2^-24.  The row's maximum is summed again in fp64 wherever |u32| is within 2 E of the
+// largest.  A quotient q = 127 u / max is off by 127 E (block's max) / max for u, and by |q| times E for the maximum and 3 roundings: by
+// the block's largest quotient times 2 E + 6 2^-24 in all.  Elements that lie that close to the border between two codes are summed
+// again in fp64 (b = 32, gaussian values: 1.8 of a row of 4096; with outliers, next to none outside their blocks).
 #pragma once
 
 #include "perq_mm_ptx.cuh"
@@ -33,13 +34,13 @@ struct Params {
     int32_t warps;               // to a row
     int32_t rows;                // of a CTA at a time
     float near_max;              // 1 - 2 E, and a little: |u32| from here on may be the maximum
-    float doubt;                 // |quotient - code| from here on may round the other way
+    float doubt;                 // a block's largest quotient times this: how far its quotients may be off
     double inv_scale;            // 1 / (127 sqrt b)
 };
 
 // What the warps of a row agree on.
 struct alignas(16) RowShared {
-    unsigned long long top;      // exact maximum, the bits of a positive double
+    unsigned long long top[2];   // exact maximum, the bits of a positive double; rows take turns
     float part[32];              // warps' maxima
 };
 
@@ -61,27 +62,59 @@ __device__ __forceinline__ void load_piece(uint32_t (&raw)[8], const uint16_t *s
     }
 }
 
+// Two values that are added and multiplied at once.
+struct __align__(8) Pair {
+    float x, y;
+};
+__device__ __forceinline__ Pair pair_add(Pair a, Pair b)
+{
+    Pair r;
+    asm("{ .reg .b64 p, q, s; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; add.rn.f32x2 s, p, q; mov.b64 {%0, %1}, s; }"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("{ .reg .b64 p, q, s, t; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; mov.b64 s, {%6, %7}; fma.rn.f32x2 t, p, q, s; mov.b64 {%0, %1}, t; }"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float max3(float m, Pair v) { return fmaxf(fmaxf(m, fabsf(v.x)), fabsf(v.y)); }
+__device__ __forceinline__ float warp_max(float v)       // (not negative)
+{
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
+}
+
 // The butterflies of blocks of 2^log2b channels (0: none) over a warp's 512.
-__device__ __forceinline__ void rotate(float (&u)[LANE_ELEMS], int log2b, int lane)
+__device__ __forceinline__ void rotate(Pair (&u)[LANE_ELEMS / 2], int log2b, int lane)
 {
     if (log2b == 0) return;
+    const Pair neg = {-1.0f, -1.0f};
 #pragma unroll
-    for (int h = 1; h < LANE_ELEMS; h *= 2) {
+    for (int i = 0; i < LANE_ELEMS / 2; ++i) {
+        const float a = u[i].x, b = u[i].y;
+        u[i].x = a + b;
+        u[i].y = a - b;
+    }
 #pragma unroll
-        for (int i = 0; i < LANE_ELEMS; ++i) {
+    for (int h = 1; h < LANE_ELEMS / 2; h *= 2) {
+#pragma unroll
+        for (int i = 0; i < LANE_ELEMS / 2; ++i) {
             if ((i & h) == 0) {
-                const float a = u[i], b = u[i + h];
-                u[i] = a + b;
-                u[i + h] = a - b;
+                const Pair a = u[i], b = u[i + h];
+                u[i] = pair_add(a, b);
+                u[i + h] = pair_fma(b, neg, a);
             }
         }
     }
     for (int m = 1; m < 1 << (log2b - 4); m *= 2) {
         const float s = (lane & m) ? -1.0f : 1.0f;
+        const Pair ss = {s, s};
 #pragma unroll
-        for (int i = 0; i < LANE_ELEMS; ++i) {
-            const float v = __shfl_xor_sync(0xffffffffu, u[i], m);
-            u[i] = fmaf(s, u[i], v);                     // (s u exact: one rounding)
+        for (int i = 0; i < LANE_ELEMS / 2; ++i) {
+            const Pair v = {__shfl_xor_sync(0xffffffffu, u[i].x, m), __shfl_xor_sync(0xffffffffu, u[i].y, m)};
+            u[i] = pair_fma(ss, u[i], v);                // (s u exact: one rounding)
         }
     }
 }
@@ -91,6 +124,8 @@ __device__ __forceinline__ double exact_output(const uint32_t (&raw)[8], int i, 
 {
     const int lanes = log2b > 4 ? 1 << (log2b - 4) : 1, k0 = (lane & (lanes - 1)) * LANE_ELEMS;
     double s = 0.0;
+    // bit j: the sign of input k0 + j, the parity of i & (k0 + j)
+    const uint32_t signs = ((i & 1) ? 0xaaaau : 0u) ^ ((i & 2) ? 0xccccu : 0u) ^ ((i & 4) ? 0xf0f0u : 0u) ^ ((i & 8) ? 0xff00u : 0u) ^ ((__popc(i & k0) & 1) ? 0xffffu : 0u);
 #pragma unroll
     for (int j = 0; j < LANE_ELEMS; ++j) {
         const uint32_t w = raw[j >> 1];
@@ -98,8 +133,7 @@ __device__ __forceinline__ double exact_output(const uint32_t (&raw)[8], int i, 
         if (log2b == 0) {
             if (j == i) s = (double)__uint_as_float(f);
         } else {
-            const uint32_t sign = (uint32_t)(__popc(i & (k0 + j)) & 1) << 31;
-            s += (double)__uint_as_float(f ^ sign);
+            s += (double)__uint_as_float(f ^ ((signs << (31 - j)) & 0x80000000u));
         }
     }
     for (int m = 1; m < lanes; m *= 2) s += __shfl_xor_sync(0xffffffffu, s, m);
@@ -165,7 +199,10 @@ __global__ void __launch_bounds__(MAX_THREADS, 1) quant8_kernel(const Params p)
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) load_piece(next[k], p.x + (size_t)t * (size_t)p.d + at[k], valid[k]);
     }
-    for (; t < p.T; t += step) {
+    if (w == 0 && lane == 0) row->top[0] = 0ull;
+    const int block_lanes = p.log2b > 4 ? 1 << (p.log2b - 4) : 1;
+    int turn = 0;
+    for (; t < p.T; t += step, turn ^= 1) {
         uint32_t raw[PIECES][8];
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
@@ -177,7 +214,6 @@ __global__ void __launch_bounds__(MAX_THREADS, 1) quant8_kernel(const Params p)
 #pragma unroll
             for (int i = 0; i < 8; ++i) raw[k][i] = next[k][i];
         }
-        if (w == 0 && lane == 0) row->top = 0ull;
         if (PERM) {
             row_barrier(bar, p.warps);
 #pragma unroll
@@ -190,74 +226,74 @@ __global__ void __launch_bounds__(MAX_THREADS, 1) quant8_kernel(const Params p)
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) load_piece(next[k], p.x + (size_t)(t + step) * (size_t)p.d + at[k], valid[k]);
         }
-        float u[PIECES][LANE_ELEMS], top = 0.0f;
+        Pair u[PIECES][LANE_ELEMS / 2];
+        float block[PIECES], top = 0.0f;                 // largest of the lane's block, of the warp
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u[k][2 * i] = __uint_as_float(raw[k][i] << 16);
-                u[k][2 * i + 1] = __uint_as_float(raw[k][i] & 0xffff0000u);
-            }
+            for (int i = 0; i < 8; ++i) u[k][i] = {__uint_as_float(raw[k][i] << 16), __uint_as_float(raw[k][i] & 0xffff0000u)};
             rotate(u[k], p.log2b, lane);
+            float m = 0.0f;
 #pragma unroll
-            for (int i = 0; i < LANE_ELEMS; ++i) top = fmaxf(top, fabsf(u[k][i]));
+            for (int i = 0; i < LANE_ELEMS / 2; ++i) m = max3(m, u[k][i]);
+            for (int l = 1; l < block_lanes; l *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, l));
+            block[k] = m;
+            top = fmaxf(top, m);
         }
-#pragma unroll
-        for (int m = 16; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+        top = warp_max(top);
         float all = top;
         if (p.warps > 1) {
             if (lane == 0) row->part[w] = top;
             row_barrier(bar, p.warps);
-            all = lane < p.warps ? row->part[lane] : 0.0f;
-#pragma unroll
-            for (int m = 16; m >= 1; m >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, m));
+            all = warp_max(lane < p.warps ? row->part[lane] : 0.0f);
         } else {
             __syncwarp();                                // (row->top is cleared)
         }
-        // the exact maximum
+        // (the other turn's maximum: every warp is past the row that had it)
+        if (w == 0 && lane == 0) row->top[turn ^ 1] = 0ull;
         const float near = all * p.near_max;
         if (top >= near && all > 0.0f) {
             double best = 0.0;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
                 uint32_t mask = 0u;
+                if (block[k] >= near) {
 #pragma unroll
-                for (int i = 0; i < LANE_ELEMS; ++i) mask |= (fabsf(u[k][i]) >= near ? 1u : 0u) << i;
+                    for (int i = 0; i < LANE_ELEMS / 2; ++i) mask |= (fabsf(u[k][i].x) >= near ? 1u << (2 * i) : 0u) | (fabsf(u[k][i].y) >= near ? 2u << (2 * i) : 0u);
+                }
                 each_exact(mask, raw[k], p.log2b, lane, [&](int, double v) { best = fmax(best, fabs(v)); });
             }
-            if (best > 0.0) atomicMax(&row->top, (unsigned long long)__double_as_longlong(best));
+            if (best > 0.0) atomicMax(&row->top[turn], (unsigned long long)__double_as_longlong(best));
         }
         row_barrier(bar, p.warps);
-        const double exact = __longlong_as_double((long long)row->top);
+        const double exact = __longlong_as_double((long long)*reinterpret_cast<volatile unsigned long long *>(&row->top[turn]));
         if (w == 0 && lane == 0) p.scales[t] = (float)(exact * p.inv_scale);
-        // |quotients| <= 127 (1 + 2 E).  Rows so small that 127 / max overflows are settled element by element.
-        const float r = 127.0f / all;
+        // Rows so small that 127 / max overflows are settled element by element.
         const bool tiny = !(all > 0x1p-120f);
-        const float ratio = tiny ? 0.0f : r;
+        const float ratio = tiny ? 0.0f : 127.0f / all;
+        const Pair rr = {ratio, ratio}, magic = {12582912.0f, 12582912.0f}, neg = {-1.0f, -1.0f};     // 1.5 2^23: the low byte of the sum is the code
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
             uint32_t code[4];
             float off = 0.0f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                float g[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    g[i] = fmaf(u[k][4 * c + i], ratio, 12582912.0f);              // 1.5 2^23: the low byte is the code
-                    off = fmaxf(off, fabsf(fmaf(u[k][4 * c + i], ratio, 12582912.0f - g[i])));
-                }
-                const uint32_t lo = __byte_perm(__float_as_uint(g[0]), __float_as_uint(g[1]), 0x0040);
-                const uint32_t hi = __byte_perm(__float_as_uint(g[2]), __float_as_uint(g[3]), 0x0040);
+                const Pair g = pair_fma(u[k][2 * c], rr, magic), h = pair_fma(u[k][2 * c + 1], rr, magic);
+                off = max3(off, pair_fma(u[k][2 * c], rr, pair_fma(g, neg, magic)));
+                off = max3(off, pair_fma(u[k][2 * c + 1], rr, pair_fma(h, neg, magic)));
+                const uint32_t lo = __byte_perm(__float_as_uint(g.x), __float_as_uint(g.y), 0x0040);
+                const uint32_t hi = __byte_perm(__float_as_uint(h.x), __float_as_uint(h.y), 0x0040);
                 code[c] = __byte_perm(lo, hi, 0x5410);
             }
-            const bool some = off >= p.doubt || (tiny && all > 0.0f);
+            const float doubt = 0.5f - 0x1p-23f - block[k] * ratio * p.doubt;
+            const bool some = off >= doubt || (tiny && all > 0.0f);
             if (__any_sync(0xffffffffu, some)) {
                 uint32_t mask = 0u;
                 if (some) {
 #pragma unroll
-                    for (int i = 0; i < LANE_ELEMS; ++i) {
-                        const float q = fmaf(u[k][i], ratio, 12582912.0f) - 12582912.0f;
-                        mask |= (tiny || fabsf(fmaf(u[k][i], ratio, -q)) >= p.doubt ? 1u : 0u) << i;
+                    for (int i = 0; i < LANE_ELEMS / 2; ++i) {
+                        const Pair g = pair_fma(pair_fma(u[k][i], rr, magic), neg, magic), q = pair_fma(u[k][i], rr, g);
+                        mask |= (tiny || fabsf(q.x) >= doubt ? 1u << (2 * i) : 0u) | (tiny || fabsf(q.y) >= doubt ? 2u << (2 * i) : 0u);
                     }
                 }
                 each_exact(mask, raw[k], p.log2b, lane, [&](int e, double v) {
@@ -270,8 +306,6 @@ __global__ void __launch_bounds__(MAX_THREADS, 1) quant8_kernel(const Params p)
             }
             if (valid[k]) *reinterpret_cast<uint4 *>(p.codes + (size_t)t * (size_t)p.d + at[k]) = make_uint4(code[0], code[1], code[2], code[3]);
         }
-        // (part and top are written again by the next row: after its first barrier that all have passed, or here)
-        row_barrier(bar, p.warps);
     }
 }
 

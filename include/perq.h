@@ -402,7 +402,8 @@ int perq_grouped_matmul_i8_workspace_bytes(int64_t T, int32_t E, int32_t N, int3
  * bounded wait inside a kernel ran out (an asynchronous copy that never completed); the
  * kernel then stops early and its outputs are incomplete.  Bits 1 and 2: such a wait inside the
  * permuted and grouped kernels, for an exact maximum (1) or a free buffer (2); bit 3: in the
- * statistic; bits 4 and 5: in the kernels of the products.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
+ * statistic; bits 4 to 6: in the products and the
+ * kernel of 8-bit codes.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
  *
  * perq_device_error_clear -- writes 0 to that word on the current device (synchronously,
  * cudaMemcpyToSymbol), so that a later read reports only what happened since.  Call it with no

@@ -238,6 +238,16 @@ int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaS
     return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);
 }
 
+template <int LOG2B>
+int launch_quant8_b(const perq_q8::Params &p, int pieces, long long grid, int threads, size_t smem, cudaStream_t st)
+{
+    using namespace perq_q8;
+    if (pieces == 2) return launch_plain(p.perm ? quant8_kernel<LOG2B, 2, 2, true> : quant8_kernel<LOG2B, 2, 2, false>, grid, threads, smem, st, p);
+    if (threads <= Size<0>::threads) return launch_plain(p.perm ? quant8_kernel<LOG2B, 0, 1, true> : quant8_kernel<LOG2B, 0, 1, false>, grid, threads, smem, st, p);
+    if (threads <= Size<1>::threads) return launch_plain(p.perm ? quant8_kernel<LOG2B, 1, 1, true> : quant8_kernel<LOG2B, 1, 1, false>, grid, threads, smem, st, p);
+    return launch_plain(p.perm ? quant8_kernel<LOG2B, 2, 1, true> : quant8_kernel<LOG2B, 2, 1, false>, grid, threads, smem, st, p);
+}
+
 int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *codes, float *scales, cudaStream_t st)
 {
     using namespace perq_q8;
@@ -251,19 +261,27 @@ int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int3
     p.scales = scales;
     p.T = T;
     p.d = d;
-    p.log2b = ilog2(b);
+    const int log2b = ilog2(b);
     const int pieces = d > MAX_THREADS * LANE_ELEMS ? 2 : 1;
     p.warps = (d + pieces * WARP_ELEMS - 1) / (pieces * WARP_ELEMS);
     p.rows = (int)std::min<int64_t>(std::max(1, 8 / p.warps), std::max<int64_t>(1, (T + sms - 1) / sms));
-    const double e = p.log2b * std::sqrt((double)b) * 0x1p-24;
+    const double e = log2b * std::sqrt((double)b) * 0x1p-24;
     p.near_max = (float)(1.0 - 2.0 * e - 0x1p-22);
     p.doubt = (float)(1.001 * (2.0 * e + 6.0 * 0x1p-24));
     p.inv_scale = 1.0 / (127.0 * std::sqrt((double)b));
     const int threads = p.rows * p.warps * 32;
-    const size_t smem = (size_t)p.rows * (sizeof(RowShared) + (perm ? (size_t)d * 2 : 0));
-    const long long grid = std::min<long long>((T + p.rows - 1) / p.rows, (long long)sms * std::max(1, 1024 / threads));
-    if (pieces == 1) return launch_plain(perm ? quant8_kernel<1, true> : quant8_kernel<1, false>, grid, threads, smem, st, p);
-    return launch_plain(perm ? quant8_kernel<2, true> : quant8_kernel<2, false>, grid, threads, smem, st, p);
+    const size_t smem = (size_t)p.rows * (sizeof(RowShared) + STAGES * (size_t)d * 2);
+    const int per_sm = threads <= Size<0>::threads ? Size<0>::ctas * Size<0>::threads / threads : threads <= Size<1>::threads ? Size<1>::ctas : 1;
+    const long long grid = std::min<long long>((T + p.rows - 1) / p.rows, (long long)sms * per_sm);
+    switch (log2b) {
+    case 0: return launch_quant8_b<0>(p, pieces, grid, threads, smem, st);
+    case 4: return launch_quant8_b<4>(p, pieces, grid, threads, smem, st);
+    case 5: return launch_quant8_b<5>(p, pieces, grid, threads, smem, st);
+    case 6: return launch_quant8_b<6>(p, pieces, grid, threads, smem, st);
+    case 7: return launch_quant8_b<7>(p, pieces, grid, threads, smem, st);
+    case 8: return launch_quant8_b<8>(p, pieces, grid, threads, smem, st);
+    default: return launch_quant8_b<9>(p, pieces, grid, threads, smem, st);
+    }
 }
 
 }  // namespace

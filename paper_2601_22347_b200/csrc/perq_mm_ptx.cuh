@@ -9,9 +9,10 @@ namespace perq_mm {
 
 constexpr uint32_t WAIT_POLLS = 1u << 22;
 
-// Set (never cleared by kernels) when a bounded wait ran out: bit 4 in the kernel for few tokens, bit 5 in the one for many.
+// Set (never cleared by kernels) when a bounded wait ran out: bit 4 in the product for few tokens, bit 5 in the one for many,
+// bit 6 in the kernel of 8-bit codes.
 static __device__ unsigned int g_error = 0u;
-enum : unsigned int { ERROR_FEW = 1u << 4, ERROR_MANY = 1u << 5 };
+enum : unsigned int { ERROR_FEW = 1u << 4, ERROR_MANY = 1u << 5, ERROR_ROWS = 1u << 6 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

@@ -15,7 +15,7 @@ namespace {
 // Whether a format's codes lie two to a byte.
 inline bool is_packed(int32_t fmt) { return fmt != PERQ_FMT_INT8; }
 
-// Codes [rows, d] in boxes of `box` rows by 128 bytes; 8-bit codes as operands (128-byte swizzle), packed ones as they lie.
+// Codes [rows, d] in boxes of `box` rows by 128 bytes, as operands (128-byte swizzle).
 bool codes_map(CUtensorMap *map, const void *codes, bool packed, uint64_t rows, int d, int box)
 {
     TensorMapEncode encode = tensor_map_encode();
@@ -24,7 +24,7 @@ bool codes_map(CUtensorMap *map, const void *codes, bool packed, uint64_t rows, 
     const cuuint64_t dims[2] = {bytes, rows}, strides[1] = {bytes};
     const cuuint32_t size[2] = {128, (cuuint32_t)box}, step[2] = {1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, size, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  packed ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -81,18 +81,43 @@ int launch_few(const Product &m, cudaStream_t st)
     const int64_t token_tiles = m.offsets ? std::min<int64_t>(m.E, m.T) + m.T / p.nt : (m.T + p.nt - 1) / p.nt;
     const int64_t items = token_tiles * p.n_tiles;
     if (items >= (1ll << 31)) return PERQ_ERR_SHAPE;
-    p.split = 1;
-    while (p.split < 8 && items * p.split * 2 <= sms && p.split * 2 <= p.steps) p.split *= 2;
     p.w_bytes = (W4 ? 1 : K::tiles) * perq_mm::FEW_TILE;
     p.a_bytes = (A4 ? 1 : K::tiles) * (uint32_t)p.nt * 128u;
-    p.a_spread = A4 ? 2u * (uint32_t)p.nt * 128u : 0u;
-    const uint32_t load = p.w_bytes + p.a_bytes, spread = (W4 ? 2u * perq_mm::FEW_TILE : 0u) + p.a_spread;
-    const uint32_t tail = 16 + 8 * 2 * (16 + 4) + 32 + 4 * (m.offsets ? (uint32_t)m.E + 1 : 1);
-    const uint32_t room = (uint32_t)kMaxSmem - 1024 - tail;
-    p.spreads = K::packed ? 2 : 0;
-    p.loads = std::min<uint32_t>(12, (room - p.spreads * spread) / load);
-    p.off_spread = K::packed ? p.loads * load : 0;
-    p.off_bars = p.loads * load + p.spreads * spread;
+    p.spread_bytes = A4 ? 2u * (uint32_t)p.nt * 128u : 0u;
+    p.spreads = K::packed ? 3 : 0;
+    p.tmem_cols = 32;
+    while (p.tmem_cols < 2u * (uint32_t)p.nt + (W4 ? 64u * p.spreads : 0u)) p.tmem_cols *= 2;
+    const uint32_t load = p.w_bytes + p.a_bytes, tail = 16 + 16 * (12 + 4) + 32 + 4 * (m.offsets ? (uint32_t)m.E + 1 : 1);
+    // two CTAs to an SM where tensor memory has room for both and the ring is then long enough, the split that fills the SMs, and room for its sums
+    int per_sm = p.tmem_cols <= 256 ? 2 : 1;
+    uint32_t sums = 0;
+    for (;; per_sm = 1) {
+        p.split = 1;
+        while (p.split < 8 && items * p.split * 2 <= (int64_t)sms * per_sm && p.split * 2 <= p.steps) p.split *= 2;
+        sums = p.split > 1 ? (uint32_t)p.nt * perq_mm::FEW_ROWS * 4u : 0u;
+        auto loads = [&]() {
+            return (uint32_t)std::max(0, std::min(12, ((int)(kMaxSmem / per_sm) - 2048 - (int)(tail + sums + p.spreads * p.spread_bytes)) / (int)load));
+        };
+        p.loads = loads();
+        if (per_sm == 2 && p.loads >= 3) break;
+        if (per_sm == 2) continue;
+        // (8-bit weights with 128 packed tokens are 48 KB a step)
+        if (p.loads < 2 && p.spreads > 2) {
+            p.spreads = 2;
+            p.loads = loads();
+        }
+        if (p.loads < 2 && p.split > 1) {
+            p.split = 1;
+            sums = 0;
+            p.loads = loads();
+        }
+        break;
+    }
+    p.log2_share = ilog2(p.nt / p.split);
+    if (p.loads < 2) return PERQ_ERR_SHAPE;              // (no shape of these kernels)
+    p.off_spread = p.loads * load;
+    p.off_sums = p.off_spread + p.spreads * p.spread_bytes;
+    p.off_bars = p.off_sums + sums;
     p.off_first = p.off_bars + 16 + 16 * (p.loads + p.spreads) + 32;
     const size_t smem = 1024 + p.off_first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
     p.a_scales = m.a_scales;
@@ -108,10 +133,9 @@ int launch_few(const Product &m, cudaStream_t st)
     p.out_type = m.out_type;
     p.vec = m.N % 4 == 0;
     p.idesc = perq_mm::product_desc(true, !p.asym, perq_mm::FEW_ROWS, p.nt);
-    p.tmem_cols = (uint32_t)p.nt;
     CUtensorMap w, a;
     if (!codes_map(&w, m.w, W4, (uint64_t)m.E * (uint64_t)m.N, m.d, perq_mm::FEW_ROWS) || !codes_map(&a, m.a, A4, (uint64_t)m.T, m.d, p.nt)) return PERQ_ERR_CUDA;
-    const int64_t clusters = p.split > 1 ? items : std::min<int64_t>(items, sms);
+    const int64_t clusters = p.split > 1 ? items : std::min<int64_t>(items, (int64_t)sms * per_sm);
     return launch_product(perq_mm::few_kernel<W4, A4>, (unsigned)(clusters * p.split), K::threads, smem, p.split, st, w, a, p);
 }
 
@@ -141,7 +165,7 @@ int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cu
 bool many_is_better(const Product &m, int sms)
 {
     (void)sms;
-    return m.offsets ? m.T >= 256 * (int64_t)m.E : m.T >= 1024;
+    return m.offsets ? m.T >= 64 * (int64_t)m.E : m.T >= 200;
 }
 
 // What the kernel for many tokens wants of the workspace: packed operands as bytes, tokens first.

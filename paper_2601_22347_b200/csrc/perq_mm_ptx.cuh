@@ -118,6 +118,13 @@ __device__ __forceinline__ void product(uint32_t d, uint32_t a, uint32_t b, uint
                      "tcgen05.mma.cta_group::2.kind::i8 [%0], a, b, %3, p; }"
                      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(OPERAND_HI) : "memory");
 }
+// The first operand in tensor memory: a row to a lane, four codes to a column.
+__device__ __forceinline__ void product_from_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile("{ .reg .pred p; .reg .b64 b; setp.ne.b32 p, %4, 0; mov.b64 b, {%2, %5}; "
+                 "tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], b, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(OPERAND_HI) : "memory");
+}
 __device__ __forceinline__ void commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -139,6 +146,14 @@ __device__ __forceinline__ void tmem_wait(int32_t (&u)[16])
                    "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15])
                  :: "memory");
 }
+// 16 columns of this warp's 32 lanes are written; they are there after tmem_store_wait.
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&u)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 :: "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+                    "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------------------ codes
 // Packed codes keep their place in a byte, 16 times their value, which saves the shift and the sign: lo(w) are the even codes

@@ -141,11 +141,11 @@ int launch_few(const Product &m, cudaStream_t st)
 
 // Programmatic stream serialization, without clusters.
 template <typename P>
-int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cudaStream_t st, const P &p)
+int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cudaStream_t st, const P &p, int grid_y = 1)
 {
     if (int rc = allow_smem(kernel, smem)) return rc;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)grid_y);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -168,6 +168,14 @@ bool many_is_better(const Product &m, int sms)
     return m.offsets ? m.T >= 64 * (int64_t)m.E : m.T >= 200;
 }
 
+// Whether its tiles are better 128 channels wide.
+bool narrow_is_better(const Product &m, int sms)
+{
+    (void)sms;
+    const char *v = getenv("PERQ_NARROW");
+    return v && v[0] == '1';
+}
+
 // What the kernel for many tokens wants of the workspace: packed operands as bytes, tokens first.
 struct ManySpace {
     size_t tokens, weights;
@@ -178,29 +186,29 @@ ManySpace many_space(const Product &m)
     return {is_packed(m.a_fmt) ? up((size_t)m.T * (size_t)m.d) : 0, is_packed(m.w_fmt) ? up((size_t)m.E * (size_t)m.N * (size_t)m.d) : 0};
 }
 
-int spread(const void *src, void *dst, long long codes, const int32_t *offsets, long long per_expert, int64_t T, int sms, cudaStream_t st)
-{
-    perq_mm::SpreadParams p;
-    p.src = static_cast<const uint4 *>(src);
-    p.dst = static_cast<uint4 *>(dst);
-    p.offsets = offsets;
-    p.chunks = codes / 32;
-    p.per_expert = per_expert / 32;
-    p.T = (int32_t)T;
-    return launch_plain(perq_mm::spread_kernel, std::min<long long>((p.chunks + 255) / 256, 8ll * sms), 256, 0, st, p);
-}
-
+template <int CHANNELS>
 int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_t st)
 {
     const ManySpace space = many_space(m);
-    const void *tokens = m.a, *weights = m.w;
-    if (space.tokens > 0) {
-        tokens = workspace;
-        if (int rc = spread(m.a, workspace, (long long)m.T * m.d, nullptr, 32, m.T, sms, st)) return rc;
-    }
-    if (space.weights > 0) {
-        weights = workspace + space.tokens;
-        if (int rc = spread(m.w, workspace + space.tokens, (long long)m.E * m.N * m.d, m.offsets, (long long)m.N * m.d, m.T, sms, st)) return rc;
+    const void *tokens = space.tokens ? workspace : m.a, *weights = space.weights ? workspace + space.tokens : m.w;
+    if (space.tokens || space.weights) {
+        perq_mm::SpreadParams p;
+        std::memset(&p, 0, sizeof(p));
+        if (space.tokens) {
+            p.tokens = static_cast<const uint4 *>(m.a);
+            p.tokens_out = reinterpret_cast<uint4 *>(workspace);
+            p.token_chunks = (long long)m.T * m.d / 32;
+        }
+        if (space.weights) {
+            p.weights = static_cast<const uint4 *>(m.w);
+            p.weights_out = reinterpret_cast<uint4 *>(workspace + space.tokens);
+            p.expert_chunks = (long long)m.N * m.d / 32;
+            p.offsets = m.offsets;
+        }
+        p.T = (int32_t)m.T;
+        const int parts = (space.tokens ? 1 : 0) + (space.weights ? m.E : 0);
+        const long long most = std::max(p.token_chunks, p.expert_chunks), ctas = std::min<long long>((most + 1023) / 1024, std::max(1, 16 * sms / parts));
+        if (int rc = launch_plain(perq_mm::spread_kernel, ctas, 256, 0, st, p, parts)) return rc;
     }
     perq_mm::ManyParams p;
     std::memset(&p, 0, sizeof(p));
@@ -212,20 +220,20 @@ int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_
     p.T = (int32_t)m.T;
     p.N = m.N;
     p.E = m.E;
-    p.n_tiles = (m.N + perq_mm::MANY_CHANNELS - 1) / perq_mm::MANY_CHANNELS;
+    p.n_tiles = (m.N + CHANNELS - 1) / CHANNELS;
     p.steps = (m.d + 127) / 128;
     p.asym = m.a_fmt == PERQ_FMT_INT4_ASYM;
     p.shift = (space.tokens ? 4 : 0) + (space.weights ? 4 : 0);
     p.out_type = m.out_type;
     p.wide = (size_t)m.N * (m.out_type == PERQ_OUT_F32 ? 4 : 2) % 32 == 0 && (reinterpret_cast<uintptr_t>(m.out) & 31u) == 0;
-    p.idesc = perq_mm::product_desc(!p.asym, true, perq_mm::MANY_TOKENS, perq_mm::MANY_CHANNELS);
+    p.idesc = perq_mm::product_desc(!p.asym, true, perq_mm::MANY_TOKENS, CHANNELS);
     const int64_t token_tiles = m.offsets ? std::min<int64_t>(m.E, m.T) + m.T / perq_mm::MANY_TOKENS : (m.T + perq_mm::MANY_TOKENS - 1) / perq_mm::MANY_TOKENS;
     const int64_t items = token_tiles * p.n_tiles;
     if (items >= (1ll << 31)) return PERQ_ERR_SHAPE;
     CUtensorMap w, a;
-    if (!codes_map(&w, weights, false, (uint64_t)m.E * (uint64_t)m.N, m.d, 128) || !codes_map(&a, tokens, false, (uint64_t)m.T, m.d, 128)) return PERQ_ERR_CUDA;
-    const size_t smem = 1024 + perq_mm::ManySmem::first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
-    return launch_product(perq_mm::many_kernel, (unsigned)(2 * std::min<int64_t>(items, sms / 2)), perq_mm::MANY_THREADS, smem, 2, st, w, a, p);
+    if (!codes_map(&w, weights, false, (uint64_t)m.E * (uint64_t)m.N, m.d, CHANNELS / 2) || !codes_map(&a, tokens, false, (uint64_t)m.T, m.d, 128)) return PERQ_ERR_CUDA;
+    const size_t smem = 1024 + perq_mm::Many<CHANNELS>::first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
+    return launch_product(perq_mm::many_kernel<CHANNELS>, (unsigned)(2 * std::min<int64_t>(items, sms / 2)), perq_mm::MANY_THREADS, smem, 2, st, w, a, p);
 }
 
 int check_product(const Product &m)
@@ -256,7 +264,10 @@ int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaS
         return PERQ_ERR_ALIGN;
     const int sms = sm_count();
     if (sms <= 0) return PERQ_ERR_CUDA;
-    if (many_is_better(m, sms)) return launch_many(m, static_cast<unsigned char *>(workspace), sms, st);
+    if (many_is_better(m, sms)) {
+        unsigned char *const space = static_cast<unsigned char *>(workspace);
+        return narrow_is_better(m, sms) ? launch_many<128>(m, space, sms, st) : launch_many<256>(m, space, sms, st);
+    }
     const bool w4 = is_packed(m.w_fmt), a4 = is_packed(m.a_fmt);
     if (w4) return a4 ? launch_few<true, true>(m, st) : launch_few<true, false>(m, st);
     return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);

@@ -1,8 +1,8 @@
 // Product of codes for many tokens: y[t][n] = s_t s_n (sum_k a[t][k] w[n][k] + z_t c_n), 8-bit operands.
 //
-// Bound by the tensor cores.  A pair of CTAs (cta_group::2) shares a tile of 256 tokens by 256 channels: each CTA has 128 tokens on the lanes
+// Bound by the tensor cores.  A pair of CTAs (cta_group::2) shares a tile of 256 tokens by 256 (or 128) channels: each CTA has 128 tokens on the lanes
 // of its tensor memory and loads them and half of the channels, so that an SM reads 64 bytes of operands a cycle for 8192 products
-// instead of 96.  Two accumulators: the epilogue of a tile runs under the products of the next.  One CTA to an SM; pairs take every
+// instead of 96.  Two accumulators: the epilogue of a tile, by eight warps, runs under the products of the next.  One CTA to an SM; pairs take every
 // (gridDim / 2)-th tile, in bands of 8 tiles of tokens, so that tiles in flight share operands in L2.
 //
 // Packed operands are spread to bytes before (spread_kernel), in the caller's workspace.
@@ -12,12 +12,11 @@
 
 namespace perq_mm {
 
-constexpr int MANY_TOKENS = 256, MANY_CHANNELS = 256;      // of a tile; either half is a CTA's to load
-constexpr uint32_t MANY_HALF = 128 * 128;                   // bytes of 128 rows by 128 codes
-constexpr uint32_t MANY_STAGE = 2 * MANY_HALF;
-constexpr int MANY_STAGES = 6;
+constexpr int MANY_TOKENS = 256;                            // of a tile; either half is a CTA's to load
+constexpr uint32_t MANY_HALF = 128 * 128;                   // bytes of its 128 tokens by 128 codes
 constexpr int MANY_BAND = 8;
-constexpr int MANY_THREADS = 256;                           // loads, products, two idle, four of the epilogue
+constexpr int MANY_THREADS = 384;                           // warps: loads, products, two idle, eight of the epilogue
+constexpr int MANY_ROOM = 17;                               // words of a lane's 16 results on their way to whole rows
 
 struct ManyParams {
     const float *a_scales, *w_scales;
@@ -30,17 +29,23 @@ struct ManyParams {
     uint32_t idesc;
 };
 
-struct ManySmem {
-    static constexpr uint32_t bars = MANY_STAGES * MANY_STAGE;            // full, empty; accumulators full, empty
-    static constexpr uint32_t slot = bars + 16 * MANY_STAGES + 32;
-    static constexpr uint32_t scales = slot + 16;                         // [2][256] of the channels' scales, [2][256] of their sums
-    static constexpr uint32_t first = scales + 4 * 4 * MANY_CHANNELS;     // [E + 1]
+// CHANNELS of a tile: 256 or 128.
+template <int CHANNELS>
+struct Many {
+    static constexpr uint32_t stage = MANY_HALF + CHANNELS / 2 * 128;
+    static constexpr int stages = CHANNELS == 256 ? 6 : 8;
+    static constexpr uint32_t bars = stages * stage;                      // full, empty; accumulators full, empty
+    static constexpr uint32_t slot = bars + 16 * stages + 32;
+    static constexpr uint32_t scales = slot + 16;                         // [2][CHANNELS] of the channels' scales, [2][CHANNELS] of their sums
+    static constexpr uint32_t rows = scales + 4 * 4 * CHANNELS;           // [8][32][MANY_ROOM] of the epilogue's warps
+    static constexpr uint32_t first = rows + 8 * 32 * MANY_ROOM * 4;      // [E + 1]
 };
 
 struct ManyItem {
     int32_t expert, t0, t_end, n0;
 };
 // Tiles of an expert (or of the call) in bands of MANY_BAND tiles of tokens, tokens first inside a band.
+template <int CHANNELS>
 __device__ __forceinline__ ManyItem many_item(const ManyParams &p, const int32_t *first, uint32_t item)
 {
     ManyItem it;
@@ -66,7 +71,7 @@ __device__ __forceinline__ ManyItem many_item(const ManyParams &p, const int32_t
     const uint32_t band = local / (MANY_BAND * (uint32_t)p.n_tiles), in = local - band * MANY_BAND * (uint32_t)p.n_tiles;
     const uint32_t height = min((uint32_t)MANY_BAND, tiles - band * MANY_BAND), n = in / height;
     it.t0 = begin + (int32_t)(band * MANY_BAND + in - n * height) * MANY_TOKENS;
-    it.n0 = (int32_t)n * MANY_CHANNELS;
+    it.n0 = (int32_t)n * CHANNELS;
     return it;
 }
 
@@ -82,47 +87,40 @@ __device__ __forceinline__ void commit_pair(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t addr, int32_t (&u)[32])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
-                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
-                   "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]),
-                   "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]),
-                   "=r"(u[30]), "=r"(u[31])
-                 : "r"(addr) : "memory");
-}
 __device__ __forceinline__ void store_wide(void *dst, const uint32_t (&w)[8])
 {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
+template <int CHANNELS>
 __global__ void __launch_bounds__(MANY_THREADS, 1)
-many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap a_map, const ManyParams p)
+many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ ManyParams p)
 {
+    using K = Many<CHANNELS>;
+    constexpr uint32_t STAGES = K::stages;
     extern __shared__ unsigned char raw[];
     unsigned char *const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t rank = cluster_rank();
-    int32_t *const first = reinterpret_cast<int32_t *>(smem + ManySmem::first);
-    const uint32_t full = base + ManySmem::bars, empty = full + 8 * MANY_STAGES, d_full = empty + 8 * MANY_STAGES, d_empty = d_full + 16;
+    int32_t *const first = reinterpret_cast<int32_t *>(smem + K::first);
+    const uint32_t full = base + K::bars, empty = full + 8 * STAGES, d_full = empty + 8 * STAGES, d_empty = d_full + 16;
     if (tid == 0) {
         prefetch_map(&w_map);
         prefetch_map(&a_map);
-        for (int i = 0; i < MANY_STAGES; ++i) {
+        for (uint32_t i = 0; i < STAGES; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(d_full + 8 * i, 1);
-            mbar_init(d_empty + 8 * i, 8);               // the epilogue warps of both CTAs
+            mbar_init(d_empty + 8 * i, 16);              // the epilogue warps of both CTAs
         }
         mbar_init_fence();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + ManySmem::slot), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + K::slot), "r"(2u * CHANNELS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     griddep_wait();
@@ -133,7 +131,7 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
     cluster_sync();                                          // (both CTAs' barriers are there)
     tmem_fence_after();
 
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + ManySmem::slot);
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + K::slot);
     const uint32_t token_tiles = p.offsets ? (uint32_t)first[p.E] : (uint32_t)(p.T + MANY_TOKENS - 1) / MANY_TOKENS;
     const uint32_t items = token_tiles * (uint32_t)p.n_tiles, begin = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     auto give_up = [&]() { atomicOr(&g_error, ERROR_MANY); };
@@ -143,19 +141,19 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
             uint32_t n = 0;
             bool ok = true;
             for (uint32_t item = begin; item < items && ok; item += pairs) {
-                const ManyItem it = many_item(p, first, item);
-                const int w_row = it.expert * p.N + it.n0 + (int)rank * 128, a_row = it.t0 + (int)rank * 128;
+                const ManyItem it = many_item<CHANNELS>(p, first, item);
+                const int w_row = it.expert * p.N + it.n0 + (int)rank * (CHANNELS / 2), a_row = it.t0 + (int)rank * 128;
                 for (int k = 0; k < p.steps; ++k, ++n) {
-                    const uint32_t s = n % MANY_STAGES, bar = full + 8 * s, to = base + s * MANY_STAGE;
-                    if (n >= MANY_STAGES && !mbar_wait(empty + 8 * s, (n / MANY_STAGES - 1u) & 1u)) { give_up(); ok = false; break; }
-                    if (rank == 0) mbar_expect_tx(bar, 2 * MANY_STAGE);      // both CTAs' loads
+                    const uint32_t s = n % STAGES, bar = full + 8 * s, to = base + s * K::stage;
+                    if (n >= STAGES && !mbar_wait(empty + 8 * s, (n / STAGES - 1u) & 1u)) { give_up(); ok = false; break; }
+                    if (rank == 0) mbar_expect_tx(bar, 2 * K::stage);      // both CTAs' loads
                     tma_load_pair(to, &a_map, k * 128, a_row, bar);
                     tma_load_pair(to + MANY_HALF, &w_map, k * 128, w_row, bar);
                 }
             }
             // nothing is in flight when the pair ends, also after a wait that ran out (both CTAs' loads count at the first one's barriers)
             if (rank == 0)
-                for (uint32_t i = n > MANY_STAGES ? n - MANY_STAGES : 0u; i < n; ++i) (void)mbar_wait(full + 8 * (i % MANY_STAGES), (i / MANY_STAGES) & 1u);
+                for (uint32_t i = n > STAGES ? n - STAGES : 0u; i < n; ++i) (void)mbar_wait(full + 8 * (i % STAGES), (i / STAGES) & 1u);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -163,15 +161,15 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
             uint32_t n = 0, j = 0;
             bool ok = true;
             for (uint32_t item = begin; item < items; item += pairs, ++j) {
-                const uint32_t b = j & 1u, d = tmem + b * MANY_CHANNELS;
+                const uint32_t b = j & 1u, d = tmem + b * CHANNELS;
                 if (j >= 2 && !mbar_wait(d_empty + 8 * b, ((j >> 1) - 1u) & 1u)) ok = false;
                 tmem_fence_after();
                 for (int k = 0; k < p.steps && ok; ++k, ++n) {
-                    const uint32_t s = n % MANY_STAGES;
-                    ok = mbar_wait(full + 8 * s, (n / MANY_STAGES) & 1u);
+                    const uint32_t s = n % STAGES;
+                    ok = mbar_wait(full + 8 * s, (n / STAGES) & 1u);
                     if (!ok) break;
                     tmem_fence_after();
-                    const uint32_t a = operand_lo(base + s * MANY_STAGE), w = operand_lo(base + s * MANY_STAGE + MANY_HALF);
+                    const uint32_t a = operand_lo(base + s * K::stage), w = operand_lo(base + s * K::stage + MANY_HALF);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) product<2>(d, a + 2 * i, w + 2 * i, p.idesc, k > 0 || i > 0);
                     commit_pair(empty + 8 * s);
@@ -183,58 +181,77 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
         }
         __syncwarp();
     } else if (warp >= 4) {
-        // (a wait that ran out ends no warp's part: the four go on to the barriers that they share, without waiting or storing)
-        const int q = warp & 3, st = tid - 128;
+        // (a wait that ran out ends no warp's part: the eight go on to the barriers that they share, without waiting or storing)
+        const int q = warp & 3, half = (warp - 4) >> 2, st = tid - 128;
+        const int c_begin = half * (CHANNELS / 2), c_end = c_begin + CHANNELS / 2;
+        const uint32_t room = base + K::rows + (uint32_t)((warp - 4) * 32 * MANY_ROOM) * 4u;
         uint32_t j = 0;
         bool ok = true;
         for (uint32_t item = begin; item < items; item += pairs, ++j) {
             const uint32_t b = j & 1u;
-            const ManyItem it = many_item(p, first, item);
-            float *const scale = reinterpret_cast<float *>(smem + ManySmem::scales) + b * MANY_CHANNELS, *const sums = scale + 2 * MANY_CHANNELS;
-            // (the scales of the tile before last are read no more: all four warps have met since)
-            for (int i = st; i < MANY_CHANNELS; i += 128) {
-                const int n = it.n0 + i;
-                const size_t channel = (size_t)it.expert * (size_t)p.N + (size_t)min(n, p.N - 1);
-                scale[i] = __ldg(p.w_scales + channel);
-                sums[i] = p.asym ? (float)__ldg(p.w_sums + channel) : 0.0f;
+            const ManyItem it = many_item<CHANNELS>(p, first, item);
+            const uint32_t scale = base + K::scales + b * CHANNELS * 4u, sums = scale + 2u * CHANNELS * 4u;
+            // (the scales of the tile before last are read no more: all eight warps have met since)
+            for (int i = st; i < CHANNELS; i += 256) {
+                const size_t channel = (size_t)it.expert * (size_t)p.N + (size_t)min(it.n0 + i, p.N - 1);
+                sts32(scale + 4u * (uint32_t)i, __float_as_uint(__ldg(p.w_scales + channel)));
+                if (p.asym) sts32(sums + 4u * (uint32_t)i, __float_as_uint((float)__ldg(p.w_sums + channel)));
             }
             const int t = it.t0 + (int)rank * 128 + q * 32 + lane;
             const bool mine = t < it.t_end;
             const TokenScale ts = token_scale(p.a_scales, p.asym, min(t, p.T - 1));
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            asm volatile("bar.sync 1, 256;" ::: "memory");
             if (ok && !mbar_wait(d_full + 8 * b, (j >> 1) & 1u)) { give_up(); ok = false; }
             tmem_fence_after();
-            const uint32_t from = tmem + b * MANY_CHANNELS + ((uint32_t)(q * 32) << 16);
+            const uint32_t from = tmem + b * CHANNELS + ((uint32_t)(q * 32) << 16);
             const size_t row = (size_t)t * (size_t)p.N;
-            for (int c = 0; c < MANY_CHANNELS && it.n0 + c < p.N; c += 32) {
-                int32_t u[32];
-                tmem_load32(from + c, u);
-                if (!mine || !ok) continue;
-                float y[32];
+            const int rows = min(32, it.t_end - (t - lane));         // of this warp
+            for (int c = c_begin; c < c_end && it.n0 + c < p.N && rows > 0 && ok; c += 16) {
+                int32_t u[16];
+                tmem_load16(from + c, u);
+                float y[16];
+                float4 s_n[4], c_n[4];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) y[i] = scaled(u[i], p.shift, ts.s, scale[c + i], ts.z, sums[c + i]);
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 v = lds128(scale + 4u * (uint32_t)c + 16u * i), z = p.asym ? lds128(sums + 4u * (uint32_t)c + 16u * i) : make_uint4(0, 0, 0, 0);
+                    s_n[i] = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+                    c_n[i] = make_float4(__uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w));
+                }
+                tmem_wait(u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[4 * i] = scaled(u[4 * i], p.shift, ts.s, s_n[i].x, ts.z, c_n[i].x);
+                    y[4 * i + 1] = scaled(u[4 * i + 1], p.shift, ts.s, s_n[i].y, ts.z, c_n[i].y);
+                    y[4 * i + 2] = scaled(u[4 * i + 2], p.shift, ts.s, s_n[i].z, ts.z, c_n[i].z);
+                    y[4 * i + 3] = scaled(u[4 * i + 3], p.shift, ts.s, s_n[i].w, ts.z, c_n[i].w);
+                }
                 const size_t at = row + (size_t)(it.n0 + c);
-                if (p.wide && it.n0 + c + 32 <= p.N) {
-                    uint32_t w[8];
+                uint32_t w[8];
+                if (p.wide && it.n0 + c + 16 <= p.N) {
                     if (p.out_type == OUT_F32) {
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(y[8 * h + i]);
-                            store_wide(static_cast<float *>(p.out) + at + 8 * h, w);
-                        }
-                    } else {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) w[i] = pack_two(p.out_type, y[16 * h + 2 * i], y[16 * h + 2 * i + 1]);
-                            store_wide(static_cast<uint16_t *>(p.out) + at + 16 * h, w);
+                            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(y[8 * h + i]);
+                            if (mine) store_wide(static_cast<float *>(p.out) + at + 8 * h, w);
                         }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = pack_two(p.out_type, y[2 * i], y[2 * i + 1]);
+                        if (mine) store_wide(static_cast<uint16_t *>(p.out) + at, w);
                     }
                 } else {
+                    // rows that cannot be stored 32 bytes at a time go through shared memory: 16 lanes then store adjacent results
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (it.n0 + c + i < p.N) store_one(p.out, p.out_type, at + i, y[i]);
+                    for (int i = 0; i < 16; ++i) sts32(room + (uint32_t)(lane * MANY_ROOM + i) * 4u, __float_as_uint(y[i]));
+                    __syncwarp();
+                    const int n = it.n0 + c + (lane & 15);
+                    for (int r = lane >> 4; r < rows; r += 2) {
+                        float v;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(room + (uint32_t)(r * MANY_ROOM + (lane & 15)) * 4u) : "memory");
+                        if (n < p.N) store_one(p.out, p.out_type, (size_t)(t - lane + r) * (size_t)p.N + (size_t)n, v);
+                    }
+                    __syncwarp();
                 }
             }
             tmem_fence_before();
@@ -248,39 +265,48 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
     cluster_sync();                                          // (neither leaves while the other may arrive at its barriers or use its operands)
     if (warp == 1) {
         tmem_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * CHANNELS) : "memory");
     }
 }
 
-// Packed rows to bytes, 16 times the codes, in their order.  Of grouped weights only the experts that have rows.
+// Packed rows to bytes, 16 times the codes, in their order: tokens (blockIdx.y == 0, where they are packed), and the weights of every expert
+// that has rows, which the product reads next, from L2 where they fit.  The tokens are read for 4 chunks of 16 bytes at once.
 struct SpreadParams {
-    const uint4 *src;
-    uint4 *dst;
-    const int32_t *offsets;      // (weights of experts)
-    long long chunks;            // of 16 packed bytes
-    long long per_expert;
+    const uint4 *tokens, *weights;
+    uint4 *tokens_out, *weights_out;
+    const int32_t *offsets;
+    long long token_chunks, expert_chunks;       // of 16 packed bytes
     int32_t T;
 };
 __global__ void __launch_bounds__(256) spread_kernel(const SpreadParams p)
 {
     griddep_wait();
     griddep_launch();
-    for (long long i = (long long)blockIdx.x * 256 + (int)threadIdx.x; i < p.chunks; i += (long long)gridDim.x * 256) {
-        if (p.offsets != nullptr) {
-            const int e = (int)(i / p.per_expert);
-            if (min(max(__ldg(p.offsets + e), 0), p.T) >= min(max(__ldg(p.offsets + e + 1), 0), p.T)) continue;
-        }
-        const uint4 v = __ldg(p.src + i);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t x[8];
+    const bool tokens = p.tokens != nullptr && blockIdx.y == 0;
+    const int expert = (int)blockIdx.y - (p.tokens != nullptr ? 1 : 0);
+    if (!tokens && p.offsets != nullptr &&
+        min(max(__ldg(p.offsets + expert), 0), p.T) >= min(max(__ldg(p.offsets + expert + 1), 0), p.T)) return;
+    const uint4 *const src = tokens ? p.tokens : p.weights + (size_t)expert * (size_t)p.expert_chunks;
+    uint4 *const dst = tokens ? p.tokens_out : p.weights_out + 2 * (size_t)expert * (size_t)p.expert_chunks;
+    const long long n = tokens ? p.token_chunks : p.expert_chunks, step = (long long)gridDim.x * 256;
+    for (long long i0 = (long long)blockIdx.x * 256 + (int)threadIdx.x; i0 < n; i0 += 4 * step) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i0 + k * step < n) v[k] = __ldg(src + i0 + k * step);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = codes_lo(w[k]), hi = codes_hi(w[k]);
-            x[2 * k] = __byte_perm(lo, hi, 0x5140);
-            x[2 * k + 1] = __byte_perm(lo, hi, 0x7362);
+            if (i0 + k * step >= n) break;
+            const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+            uint32_t x[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t lo = codes_lo(w[i]), hi = codes_hi(w[i]);
+                x[2 * i] = __byte_perm(lo, hi, 0x5140);
+                x[2 * i + 1] = __byte_perm(lo, hi, 0x7362);
+            }
+            store_wide(dst + 2 * (i0 + k * step), x);
         }
-        p.dst[2 * i] = make_uint4(x[0], x[1], x[2], x[3]);
-        p.dst[2 * i + 1] = make_uint4(x[4], x[5], x[6], x[7]);
     }
 }
 

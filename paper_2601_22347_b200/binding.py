@@ -28,9 +28,11 @@ FMT_BY_NAME = {"int4": PERQ_FMT_INT4, "mxfp4": PERQ_FMT_MXFP4, "f32": PERQ_FMT_F
 OUT_BY_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}        # perq_out_t
 
 PERQ_OK = 0
+PERQ_ERR_WORKSPACE = 9
 
 _lib = None
-_rotate_quantize = _swiglu_rotate_quantize = None       # the calls of these two: perq_call.c, or ctypes where that is not built or cannot be loaded
+_rotate_quantize = _swiglu_rotate_quantize = None       # the calls of these: perq_call.c, or ctypes where that is not built or cannot be loaded
+_rotate_quantize_i8 = _matmul_i8 = _grouped_matmul_i8 = None
 
 
 class PerqError(RuntimeError):
@@ -41,7 +43,7 @@ class PerqError(RuntimeError):
 
 def load() -> C.CDLL:
     """Load libperq.so from the package directory (never builds implicitly)."""
-    global _lib, _rotate_quantize, _swiglu_rotate_quantize
+    global _lib, _rotate_quantize, _swiglu_rotate_quantize, _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8
     if _lib is None:
         path = _build.LIB_PATH
         if not os.path.exists(path):
@@ -88,13 +90,16 @@ def load() -> C.CDLL:
                      "perq_token_diagnostics", "perq_validate_perm", "perq_massdiff_perm", "perq_massdiff_perm_device"):
             getattr(lib, name).restype = C.c_int
         _rotate_quantize, _swiglu_rotate_quantize = lib.perq_rotate_quantize, lib.perq_swiglu_rotate_quantize
+        _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8 = lib.perq_rotate_quantize_i8, lib.perq_matmul_i8, lib.perq_grouped_matmul_i8
         try:
             spec = importlib.util.spec_from_file_location(__package__ + "._perq_call", _build.CALL_PATH)
             call = importlib.util.module_from_spec(spec)
             spec.loader.exec_module(call)
             call.bind(C.cast(lib.perq_rotate_quantize, vp).value, C.cast(lib.perq_swiglu_rotate_quantize, vp).value)
+            call.bind_i8(C.cast(lib.perq_rotate_quantize_i8, vp).value, C.cast(lib.perq_matmul_i8, vp).value, C.cast(lib.perq_grouped_matmul_i8, vp).value)
             _rotate_quantize, _swiglu_rotate_quantize = call.rotate_quantize, call.swiglu_rotate_quantize
-        except ImportError:         # (no such file, or none that this interpreter can load)
+            _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8 = call.rotate_quantize_i8, call.matmul_i8, call.grouped_matmul_i8
+        except (ImportError, AttributeError):         # (no such file, none that this interpreter can load, or one without these calls)
             pass
         _lib = lib
     return _lib
@@ -330,21 +335,34 @@ def perq_massdiff_perm(chan_abs_sum_host: np.ndarray, b: int) -> np.ndarray:
     return perm
 
 
+def _here(t: torch.Tensor, dtype: torch.dtype) -> bool:
+    """A contiguous tensor of that type on the current device, where the call runs."""
+    return t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice()
+
+
 def perq_rotate_quantize_i8(x: torch.Tensor, perm: Optional[torch.Tensor], b: int, out_codes: Optional[torch.Tensor] = None,
                             out_scales: Optional[torch.Tensor] = None, stream=None):
     """x: bf16 CUDA tensor [T, d] (contiguous); perm: int32 CUDA tensor [d] or None.  Returns (int8 [T, d], fp32 [T, 1])."""
-    assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 2 and x.is_contiguous()
-    assert perm is None or (perm.is_cuda and perm.dtype == torch.int32 and perm.is_contiguous())
+    assert _here(x, torch.bfloat16) and x.dim() == 2
     T, d = x.shape
-    assert perm is None or perm.numel() == d
+    assert perm is None or (_here(perm, torch.int32) and perm.numel() == d)
     if out_codes is None:
         out_codes = torch.empty((T, d), dtype=torch.int8, device=x.device)
+    else:
+        assert _here(out_codes, torch.int8) and out_codes.numel() == T * d
     if out_scales is None:
         out_scales = torch.empty((T, 1), dtype=torch.float32, device=x.device)
-    assert out_codes.is_cuda and out_codes.is_contiguous() and out_codes.dtype == torch.int8 and out_codes.numel() == T * d
-    assert out_scales.is_cuda and out_scales.is_contiguous() and out_scales.dtype == torch.float32 and out_scales.numel() == T
-    _check(load().perq_rotate_quantize_i8(_ptr(x), _ptr(perm), T, d, b, _ptr(out_codes), _ptr(out_scales), _stream(stream)),
-           "perq_rotate_quantize_i8")
+    else:
+        assert _here(out_scales, torch.float32) and out_scales.numel() == T
+    if _lib is None:
+        load()
+    args = (x.data_ptr(), None if perm is None else perm.data_ptr(), T, d, b, out_codes.data_ptr(), out_scales.data_ptr(), _stream(stream))
+    try:
+        rc = _rotate_quantize_i8(*args)
+    except TypeError:           # (not plain integers: what ctypes makes of them)
+        rc = _lib.perq_rotate_quantize_i8(*args)
+    if rc != PERQ_OK:
+        _check(rc, "perq_rotate_quantize_i8")
     return out_codes, out_scales
 
 
@@ -369,36 +387,43 @@ def perq_grouped_matmul_i8_workspace_bytes(T: int, E: int, N: int, d: int, a_fmt
     return int(n.value)
 
 
-def _check_codes(codes: torch.Tensor, scales: torch.Tensor, fmt: int, sums: Optional[torch.Tensor] = None):
-    assert codes.is_cuda and codes.is_contiguous() and codes.dtype == (torch.int8 if fmt == PERQ_FMT_INT8 else torch.uint8)
-    rows = codes.numel() // max(1, codes.shape[-1])
-    assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.float32
-    assert scales.numel() == rows * (2 if fmt == PERQ_FMT_INT4_ASYM else 1)
-    assert sums is None or (sums.is_cuda and sums.is_contiguous() and sums.dtype == torch.int32 and sums.numel() == rows)
+def _codes_width(codes: torch.Tensor, scales: torch.Tensor, fmt: int, sums: Optional[torch.Tensor]) -> int:
+    """Channels of rows of codes [.., d] (or [.., d / 2]) with their scales and, of weights, their sums."""
+    packed = fmt != PERQ_FMT_INT8
+    assert _here(codes, torch.uint8 if packed else torch.int8) and _here(scales, torch.float32)
+    width = codes.shape[-1]
+    assert scales.numel() * width == codes.numel() * (2 if fmt == PERQ_FMT_INT4_ASYM else 1)
+    assert sums is None or (_here(sums, torch.int32) and sums.numel() * width == codes.numel())
+    return 2 * width if packed else width
 
 
-def _product(name, a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream):
-    _check_codes(a_codes, a_scales, a_fmt)
-    _check_codes(w_codes, w_scales, w_fmt, w_sums)
+# (a workspace is asked for only where the call wants one: few do)
+def _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream):
+    d = _codes_width(a_codes, a_scales, a_fmt, None)
+    assert a_codes.dim() == 2 and _codes_width(w_codes, w_scales, w_fmt, w_sums) == d
     T, N = a_codes.shape[0], w_codes.shape[-2]
-    d = a_codes.shape[1] * (1 if a_fmt == PERQ_FMT_INT8 else 2)
-    assert a_codes.dim() == 2 and w_codes.shape[-1] * (1 if w_fmt == PERQ_FMT_INT8 else 2) == d
     if out is None:
         out = torch.empty((T, N), dtype=out_dtype, device=a_codes.device)
-    assert out.is_cuda and out.is_contiguous() and out.shape == (T, N)
-    lib = load()
-    if workspace is None:
-        n = (perq_matmul_i8_workspace_bytes(T, N, d, a_fmt, w_fmt) if offsets is None else
-             perq_grouped_matmul_i8_workspace_bytes(T, w_codes.shape[0], N, d, a_fmt, w_fmt))
-        workspace = torch.empty(n, dtype=torch.uint8, device=a_codes.device) if n else None
-    head = (_ptr(a_codes), _ptr(a_scales), a_fmt, _ptr(w_codes), _ptr(w_scales), w_fmt, _ptr(w_sums))
-    tail = (_ptr(out), OUT_BY_DTYPE[out.dtype], _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
-    if offsets is None:
-        rc = lib.perq_matmul_i8(*head, T, N, d, *tail)
     else:
-        rc = lib.perq_grouped_matmul_i8(*head, _ptr(offsets), T, w_codes.shape[0], N, d, *tail)
-    _check(rc, name)
-    return out
+        assert _here(out, out.dtype) and out.shape == (T, N)
+    assert workspace is None or _here(workspace, workspace.dtype)
+    if _lib is None:
+        load()
+    sizes = (T, N, d) if offsets is None else (T, w_codes.shape[0], N, d)
+    while True:
+        args = (a_codes.data_ptr(), a_scales.data_ptr(), a_fmt, w_codes.data_ptr(), w_scales.data_ptr(), w_fmt, None if w_sums is None else w_sums.data_ptr(),
+                *(sizes if offsets is None else (offsets.data_ptr(), *sizes)), out.data_ptr(), OUT_BY_DTYPE[out.dtype],
+                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+        try:
+            rc = _matmul_i8(*args) if offsets is None else _grouped_matmul_i8(*args)
+        except TypeError:       # (as above)
+            rc = _lib.perq_matmul_i8(*args) if offsets is None else _lib.perq_grouped_matmul_i8(*args)
+        if rc == PERQ_OK:
+            return out
+        if rc != PERQ_ERR_WORKSPACE or workspace is not None:
+            _check(rc, "perq_matmul_i8" if offsets is None else "perq_grouped_matmul_i8")
+        n = (perq_matmul_i8_workspace_bytes if offsets is None else perq_grouped_matmul_i8_workspace_bytes)(*sizes, a_fmt, w_fmt)
+        workspace = torch.empty(n, dtype=torch.uint8, device=a_codes.device)
 
 
 def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
@@ -406,7 +431,7 @@ def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_
                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """a: codes [T, d] of tokens, w: codes [N, d] of weight channels (int8, or uint8 [.., d / 2] for INT4); returns out [T, N]."""
     assert w_codes.dim() == 2
-    return _product("perq_matmul_i8", a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, None, out, out_dtype, workspace, stream)
+    return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, None, out, out_dtype, workspace, stream)
 
 
 def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
@@ -414,5 +439,5 @@ def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt:
                            out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """As perq_matmul_i8 with w [E, N, d] and rows offsets[e] .. offsets[e + 1] (int32 CUDA tensor [E + 1]) of the tokens for expert e."""
     assert w_codes.dim() == 3
-    assert offsets.is_cuda and offsets.is_contiguous() and offsets.dtype == torch.int32 and offsets.numel() == w_codes.shape[0] + 1
-    return _product("perq_grouped_matmul_i8", a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream)
+    assert _here(offsets, torch.int32) and offsets.numel() == w_codes.shape[0] + 1
+    return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream)

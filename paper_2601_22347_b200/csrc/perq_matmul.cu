@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <tuple>
 
 #include "perq_host.cuh"
 #include "perq_mm_many.cuh"
@@ -54,6 +55,38 @@ int launch_product(void (*kernel)(CUtensorMap, CUtensorMap, P), unsigned grid, i
     return PERQ_OK;
 }
 
+// Clusters of a kernel that the device holds at once (0: it cannot say), asked once for a kernel, device, size and shared memory.
+std::mutex g_clusters_mutex;
+std::map<std::tuple<const void *, int, int, size_t>, int> g_clusters;
+
+template <typename K>
+int max_clusters(K kernel, int threads, size_t smem, int size)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    std::lock_guard<std::mutex> lock(g_clusters_mutex);
+    const auto key = std::make_tuple(reinterpret_cast<const void *>(kernel), dev, size, smem);
+    const auto known = g_clusters.find(key);
+    if (known != g_clusters.end()) return known->second;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)size);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (allow_smem(kernel, smem) != PERQ_OK || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = 0;
+    }
+    g_clusters[key] = n;
+    return n;
+}
+
 // A product: dense ones are grouped ones of one expert that has all rows.
 struct Product {
     const void *a, *w;
@@ -88,32 +121,32 @@ int launch_few(const Product &m, cudaStream_t st)
     p.tmem_cols = 32;
     while (p.tmem_cols < 2u * (uint32_t)p.nt + (W4 ? 64u * p.spreads : 0u)) p.tmem_cols *= 2;
     const uint32_t load = p.w_bytes + p.a_bytes, tail = 16 + 16 * (12 + 4) + 32 + 4 * (m.offsets ? (uint32_t)m.E + 1 : 1);
-    // two CTAs to an SM where tensor memory has room for both and the ring is then long enough, the split that fills the SMs, and room for its sums
-    int per_sm = p.tmem_cols <= 256 ? 2 : 1;
+    // The split that fills the SMs, as far as its clusters fit on the device at once, and room for its sums.  Two CTAs to an SM where there are enough for
+    // that, tensor memory has room for both and the ring is then long enough.
     uint32_t sums = 0;
+    int per_sm = p.tmem_cols <= 256 ? 2 : 1;
     for (;; per_sm = 1) {
-        p.split = 1;
-        while (p.split < 8 && items * p.split * 2 <= (int64_t)sms * per_sm && p.split * 2 <= p.steps) p.split *= 2;
-        sums = p.split > 1 ? (uint32_t)p.nt * perq_mm::FEW_ROWS * 4u : 0u;
         auto loads = [&]() {
+            sums = p.split > 1 ? (uint32_t)std::max(p.nt / 4, p.split) * perq_mm::FEW_ROWS * 16u : 0u;
             return (uint32_t)std::max(0, std::min(12, ((int)(kMaxSmem / per_sm) - 2048 - (int)(tail + sums + p.spreads * p.spread_bytes)) / (int)load));
         };
+        p.split = 1;
+        while (p.split < 8 && items * p.split * 2 <= (int64_t)sms * per_sm && p.split * 2 <= p.steps) p.split *= 2;
+        while (per_sm == 1 && p.split > 2 && items > max_clusters(perq_mm::few_kernel<W4, A4>, K::threads, kMaxSmem / per_sm - 8192, p.split)) p.split /= 2;
         p.loads = loads();
         if (per_sm == 2 && p.loads >= 3) break;
         if (per_sm == 2) continue;
-        // (8-bit weights with 128 packed tokens are 48 KB a step)
-        if (p.loads < 2 && p.spreads > 2) {
+        if (p.loads < 2 && p.spreads > 2) {              // (8-bit weights with 128 packed tokens are 48 KB a step)
             p.spreads = 2;
             p.loads = loads();
         }
         if (p.loads < 2 && p.split > 1) {
             p.split = 1;
-            sums = 0;
             p.loads = loads();
         }
         break;
     }
-    p.log2_share = ilog2(p.nt / p.split);
+    p.log2_share = ilog2(std::max(1, p.nt / 4 / p.split));
     if (p.loads < 2) return PERQ_ERR_SHAPE;              // (no shape of these kernels)
     p.off_spread = p.loads * load;
     p.off_sums = p.off_spread + p.spreads * p.spread_bytes;
@@ -131,7 +164,6 @@ int launch_few(const Product &m, cudaStream_t st)
     p.asym = m.a_fmt == PERQ_FMT_INT4_ASYM;
     p.shift = (W4 ? 4 : 0) + (A4 ? 4 : 0);
     p.out_type = m.out_type;
-    p.vec = m.N % 4 == 0;
     p.idesc = perq_mm::product_desc(true, !p.asym, perq_mm::FEW_ROWS, p.nt);
     CUtensorMap w, a;
     if (!codes_map(&w, m.w, W4, (uint64_t)m.E * (uint64_t)m.N, m.d, perq_mm::FEW_ROWS) || !codes_map(&a, m.a, A4, (uint64_t)m.T, m.d, p.nt)) return PERQ_ERR_CUDA;
@@ -161,19 +193,32 @@ int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cu
     return PERQ_OK;
 }
 
-// Whether the kernel for many tokens is the better one.
+// Whether the kernel for many tokens is the better one (us, CUDA graphs, few / many).
+//   dense, 8-bit weights, d = 4096: 256 x 2048 10.6 / 11.8, 384 x 2048 13.8 / 12.7, 128 x 4096 9.3 / 12.6, 192 x 4096 13.8 / 12.8, 512 x 4096 19.3 / 13.8, 64 x 14336
+//     16.0 / 16.4, 128 x 14336 20.4 / 16.9: from a quarter of the SMs on, which a split by four would fill
+//   4-bit weights, which it wants spread: 256 x 4096 14.0 / 17.5, 512 x 4096 19.5 / 18.6, 768 x 4096 30 / 20, 128 x 14336 20 / 30, 256 x 14336 31 / 30
+//   grouped, 8-bit weights, 32 experts of 2048 x 4096: 24 rows to an expert 48 / 58, 64 57 / 60, 96 68 / 61, 128 76 / 62; 8 of 4096 x 2048: 24 17 / 19, 64 22 / 20
+//   4-bit weights: 8 of 2048 x 2048: 128 25 / 21, 256 35 / 27; 8 of 4096 x 2048: 128 37 / 37, 256 56 / 43; 32 of 2048 x 4096, whose spread weights do not fit in L2:
+//     64 49 / 134, 256 114 / 147
 bool many_is_better(const Product &m, int sms)
 {
-    (void)sms;
-    return m.offsets ? m.T >= 64 * (int64_t)m.E : m.T >= 200;
+    const bool packed = is_packed(m.w_fmt);
+    if (m.offsets) {
+        if (!packed) return m.T >= 64 * (int64_t)m.E;
+        return m.T >= ((int64_t)m.E * m.N * m.d <= 1ll << 26 ? 192 : 512) * (int64_t)m.E;
+    }
+    const int64_t tiles = (m.T + 127) / 128 * ((m.N + 127) / 128);
+    return m.T > 64 && tiles > (packed ? sms : sms / 4);
 }
 
-// Whether its tiles are better 128 channels wide.
-bool narrow_is_better(const Product &m, int sms)
+// Pairs of CTAs that share a tile along k: as many as there is room for.  (One / two / four pairs: 256 x 4096 x 4096 15.0 / 12.9, 512 x 1024 x 4096
+// 14.9 / 12.5 / 11.9, 1536 x 1024 x 9728 28 / 21; with sixteen steps in all it loses: 1024 x 2048 x 2048 10.5 / 11.3.)
+int many_split(const Product &m, int64_t items, int steps, size_t smem)
 {
-    (void)sms;
-    const char *v = getenv("PERQ_NARROW");
-    return v && v[0] == '1';
+    if (m.offsets || steps < 24) return 1;
+    for (int split = 4; split > 1; --split)
+        if (items <= max_clusters(perq_mm::many_kernel, perq_mm::MANY_THREADS, smem, 2 * split)) return split;
+    return 1;
 }
 
 // What the kernel for many tokens wants of the workspace: packed operands as bytes, tokens first.
@@ -186,7 +231,6 @@ ManySpace many_space(const Product &m)
     return {is_packed(m.a_fmt) ? up((size_t)m.T * (size_t)m.d) : 0, is_packed(m.w_fmt) ? up((size_t)m.E * (size_t)m.N * (size_t)m.d) : 0};
 }
 
-template <int CHANNELS>
 int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_t st)
 {
     const ManySpace space = many_space(m);
@@ -220,20 +264,22 @@ int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_
     p.T = (int32_t)m.T;
     p.N = m.N;
     p.E = m.E;
-    p.n_tiles = (m.N + CHANNELS - 1) / CHANNELS;
+    p.n_tiles = (m.N + perq_mm::MANY_CHANNELS - 1) / perq_mm::MANY_CHANNELS;
     p.steps = (m.d + 127) / 128;
     p.asym = m.a_fmt == PERQ_FMT_INT4_ASYM;
     p.shift = (space.tokens ? 4 : 0) + (space.weights ? 4 : 0);
     p.out_type = m.out_type;
     p.wide = (size_t)m.N * (m.out_type == PERQ_OUT_F32 ? 4 : 2) % 32 == 0 && (reinterpret_cast<uintptr_t>(m.out) & 31u) == 0;
-    p.idesc = perq_mm::product_desc(!p.asym, true, perq_mm::MANY_TOKENS, CHANNELS);
+    p.idesc = perq_mm::product_desc(!p.asym, true, perq_mm::MANY_TOKENS, perq_mm::MANY_CHANNELS);
     const int64_t token_tiles = m.offsets ? std::min<int64_t>(m.E, m.T) + m.T / perq_mm::MANY_TOKENS : (m.T + perq_mm::MANY_TOKENS - 1) / perq_mm::MANY_TOKENS;
     const int64_t items = token_tiles * p.n_tiles;
     if (items >= (1ll << 31)) return PERQ_ERR_SHAPE;
     CUtensorMap w, a;
-    if (!codes_map(&w, weights, false, (uint64_t)m.E * (uint64_t)m.N, m.d, CHANNELS / 2) || !codes_map(&a, tokens, false, (uint64_t)m.T, m.d, 128)) return PERQ_ERR_CUDA;
-    const size_t smem = 1024 + perq_mm::Many<CHANNELS>::first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
-    return launch_product(perq_mm::many_kernel<CHANNELS>, (unsigned)(2 * std::min<int64_t>(items, sms / 2)), perq_mm::MANY_THREADS, smem, 2, st, w, a, p);
+    if (!codes_map(&w, weights, false, (uint64_t)m.E * (uint64_t)m.N, m.d, perq_mm::MANY_CHANNELS / 2) || !codes_map(&a, tokens, false, (uint64_t)m.T, m.d, 128)) return PERQ_ERR_CUDA;
+    const size_t smem = 1024 + perq_mm::ManySmem::first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
+    p.split = many_split(m, items, p.steps, smem);
+    const int64_t clusters = p.split > 1 ? items : std::min<int64_t>(items, sms / 2);
+    return launch_product(perq_mm::many_kernel, (unsigned)(2 * p.split * clusters), perq_mm::MANY_THREADS, smem, 2 * p.split, st, w, a, p);
 }
 
 int check_product(const Product &m)
@@ -264,10 +310,7 @@ int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaS
         return PERQ_ERR_ALIGN;
     const int sms = sm_count();
     if (sms <= 0) return PERQ_ERR_CUDA;
-    if (many_is_better(m, sms)) {
-        unsigned char *const space = static_cast<unsigned char *>(workspace);
-        return narrow_is_better(m, sms) ? launch_many<128>(m, space, sms, st) : launch_many<256>(m, space, sms, st);
-    }
+    if (many_is_better(m, sms)) return launch_many(m, static_cast<unsigned char *>(workspace), sms, st);
     const bool w4 = is_packed(m.w_fmt), a4 = is_packed(m.a_fmt);
     if (w4) return a4 ? launch_few<true, true>(m, st) : launch_few<true, false>(m, st);
     return a4 ? launch_few<false, true>(m, st) : launch_few<false, false>(m, st);

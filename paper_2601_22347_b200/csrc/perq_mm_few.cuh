@@ -35,13 +35,12 @@ struct FewParams {
     int32_t split;               // CTAs of the cluster
     int32_t shift, asym;
     int32_t out_type;
-    int32_t vec;                 // four results can be stored at once
     uint32_t idesc;
     uint32_t loads, spreads;     // stages of the two rings
     uint32_t w_bytes, a_bytes;   // of a load
     uint32_t spread_bytes;       // of a spread stage in shared memory (the tokens)
     uint32_t tmem_cols;          // two accumulators, and the spread weights
-    int32_t log2_share;          // columns of a CTA of the cluster
+    int32_t log2_share;          // four columns each: how many a CTA of the cluster adds up (with fewer fours than CTAs, the first ones one each)
     uint32_t off_spread, off_sums, off_bars, off_first;
 };
 
@@ -281,7 +280,7 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (p.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");        // (this CTA's shared memory is there)
+    if (p.split > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");        // (this CTA's shared memory is there)
 
     const uint32_t tmem = *slot;
     const uint32_t token_tiles = p.offsets ? (uint32_t)first[p.E] : (uint32_t)(p.T + p.nt - 1) / (uint32_t)p.nt;
@@ -349,12 +348,13 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
         for (uint32_t item = begin; item < items && ok; item += clusters) {
             for (uint32_t k = step0; k < step1; ++k, ++n, r.next(), u.next()) {
                 if ((n & 1u) != (uint32_t)team) continue;
-                ok = mbar_wait(l_full + 8 * r.stage, r.parity) && mbar_wait(s_empty + 8 * u.stage, u.parity);
+                ok = mbar_wait_warp(l_full + 8 * r.stage, r.parity) && mbar_wait_warp(s_empty + 8 * u.stage, u.parity);
                 if (!ok) { give_up(); break; }
                 const uint32_t from = load_at(r.stage);
                 if (A4) {
                     spread_tokens<W4 && A4>(from + p.w_bytes, spread_at(u.stage), a_tile, p.nt, st);
                     fence_async_smem();
+                    __syncwarp();
                 }
                 if (W4) {
                     tmem_fence_after();
@@ -372,7 +372,7 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
     } else if (warp >= K::epilogue) {
         const int q = warp & 3;
         uint32_t j = 0;
-        if (p.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (p.split > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         for (uint32_t item = begin; item < items; item += clusters, ++j) {
             const uint32_t b = j & 1u;
             const FewItem it = few_item(p, first, item);
@@ -384,21 +384,23 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
                 s_n = __ldg(p.w_scales + channel);
                 c_n = p.asym ? (float)__ldg(p.w_sums + channel) : 0.0f;
             }
-            if (!mbar_wait(d_full + 8 * b, (j >> 1) & 1u)) { give_up(); break; }
+            if (!mbar_wait_warp(d_full + 8 * b, (j >> 1) & 1u)) { give_up(); break; }
             tmem_fence_after();
             const uint32_t from = tmem + b * (uint32_t)p.nt + ((uint32_t)(q * 32) << 16);
             TokenScale ts = {0.0f, 0.0f};
             for (int c = 0; c < columns; c += 16) {
                 int32_t u[16];
+                __syncwarp();
                 tmem_load16(from + c, u);
-                if (p.split > 1) {                          // partial sums: to the CTA that adds up the column
+                if (p.split > 1) {                          // partial sums, four columns of a channel at a time: to the CTA that adds them up
                     tmem_wait(u);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
+                    for (int i = 0; i < 16; i += 4) {
                         if (c + i < columns) {
-                            const uint32_t column = (uint32_t)(c + i), owner = column >> p.log2_share;
-                            const uint32_t at = base + p.off_sums + (((rank << p.log2_share) + (column & ((1u << p.log2_share) - 1u))) * FEW_ROWS + (uint32_t)(q * 32 + lane)) * 4u;
-                            asm volatile("{ .reg .b32 a; mapa.shared::cluster.u32 a, %0, %1; st.shared::cluster.u32 [a], %2; }" ::"r"(at), "r"(owner), "r"(u[i]) : "memory");
+                            const uint32_t four = (uint32_t)(c + i) >> 2, owner = four >> p.log2_share;
+                            const uint32_t at = base + p.off_sums + (((rank << p.log2_share) + (four & ((1u << p.log2_share) - 1u))) * FEW_ROWS + (uint32_t)(q * 32 + lane)) * 16u;
+                            asm volatile("{ .reg .b32 a; mapa.shared::cluster.u32 a, %0, %1; st.shared::cluster.v4.u32 [a], {%2, %3, %4, %5}; }"
+                                         ::"r"(at), "r"(owner), "r"(u[i]), "r"(u[i + 1]), "r"(u[i + 2]), "r"(u[i + 3]) : "memory");
                         }
                     }
                 } else {
@@ -421,53 +423,42 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
     if (p.split == 1) {
         __syncthreads();
     } else {
-        // every CTA of the cluster adds up a share of the tile's tokens: 32 threads to a token, four channels each
-        if (warp < K::epilogue) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        // every CTA of the cluster adds up a share of the tile's tokens, a thread four tokens of a channel
+        if (warp < K::epilogue) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         const bool any = begin < items;
         FewItem it = {0, 0, 0, 0};
         if (any) it = few_item(p, first, begin);
-        const int share = p.nt / p.split, n = it.n0 + (tid & 31) * 4;
-        const size_t channel = (size_t)it.expert * (size_t)p.N + (size_t)n;
-        float s_n[4], c_n[4];
-        TokenScale ts = {0.0f, 0.0f};
-        int t = it.t0 + (int)rank * share + (tid >> 5);
-        if (any && n < p.N && t < it.t_end) {                // (on their way while the others' sums arrive)
-            ts = token_scale(p.a_scales, p.asym, t);
+        const int share = 1 << p.log2_share, row = tid & (FEW_ROWS - 1), n = it.n0 + row;
+        int four = tid / FEW_ROWS;
+        auto token_of = [&](int f) { return it.t0 + (((int)rank << p.log2_share) + f) * 4; };
+        auto here = [&](int f) { return any && n < p.N && f < share && (int)rank * share + f < p.nt / 4 && token_of(f) < it.t_end; };
+        float s_n = 0.0f, c_n = 0.0f;
+        TokenScale ts[4];
+        if (here(four)) {                                    // (on their way while the others' sums arrive)
+            const size_t channel = (size_t)it.expert * (size_t)p.N + (size_t)n;
+            s_n = __ldg(p.w_scales + channel);
+            c_n = p.asym ? (float)__ldg(p.w_sums + channel) : 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const size_t ch = channel + (size_t)min(e, p.N - 1 - n);
-                s_n[e] = __ldg(p.w_scales + ch);
-                c_n[e] = p.asym ? (float)__ldg(p.w_sums + ch) : 0.0f;
-            }
+            for (int e = 0; e < 4; ++e) ts[e] = token_scale(p.a_scales, p.asym, min(token_of(four) + e, it.t_end - 1));
         }
         cluster_sync();
-        if (any && n < p.N) {
-            for (int i = tid >> 5; i < share; i += K::threads / 32) {
-                t = it.t0 + (int)rank * share + i;
-                if (t >= it.t_end) break;
-                if (i >= K::threads / 32) ts = token_scale(p.a_scales, p.asym, t);
-                int32_t v[4] = {0, 0, 0, 0};
-                for (int r = 0; r < p.split; ++r) {
-                    const uint4 u = lds128(base + p.off_sums + (uint32_t)(((r * share + i) * FEW_ROWS + (tid & 31) * 4) * 4));
-                    v[0] += (int32_t)u.x; v[1] += (int32_t)u.y; v[2] += (int32_t)u.z; v[3] += (int32_t)u.w;
-                }
-                const size_t at = (size_t)t * (size_t)p.N + (size_t)n;
-                float y[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = scaled(v[e], p.shift, ts.s, s_n[e], ts.z, c_n[e]);
-                if (p.vec) {                                // (N is then a multiple of four)
-                    if (p.out_type == OUT_F32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
-                    else
-                        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at) =
-                            make_uint2(pack_two(p.out_type, y[0], y[1]), pack_two(p.out_type, y[2], y[3]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n + e < p.N) store_one(p.out, p.out_type, at + e, y[e]);
-                }
+        while (here(four)) {
+            int32_t v[4] = {0, 0, 0, 0};
+            for (int r = 0; r < p.split; ++r) {
+                const uint4 u = lds128(base + p.off_sums + (uint32_t)((((r << p.log2_share) + four) * FEW_ROWS + row) * 16));
+                v[0] += (int32_t)u.x; v[1] += (int32_t)u.y; v[2] += (int32_t)u.z; v[3] += (int32_t)u.w;
             }
+            const int t = token_of(four);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (t + e < it.t_end) store_one(p.out, p.out_type, (size_t)(t + e) * (size_t)p.N + (size_t)n, scaled(v[e], p.shift, ts[e].s, s_n, ts[e].z, c_n));
+            four += K::threads / FEW_ROWS;
+            if (!here(four)) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ts[e] = token_scale(p.a_scales, p.asym, min(token_of(four) + e, it.t_end - 1));
         }
     }
+    __syncwarp();
     if (warp == 1) {
         tmem_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");

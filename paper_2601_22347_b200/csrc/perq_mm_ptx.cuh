@@ -51,6 +51,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
         if (mbar_poll(bar, parity)) return true;
     return false;
 }
+// The same by all lanes of a warp, which go on together and agree: the tensor memory's loads and stores that follow want a converged warp,
+// and nothing says that all lanes see a phase complete in the same poll.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
 
 // As in the kernels of the online path: nothing touches global memory before griddep_wait.
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -64,7 +67,7 @@ __device__ __forceinline__ uint32_t cluster_rank()
 }
 __device__ __forceinline__ void cluster_sync()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 __device__ __forceinline__ uint4 lds_at_rank(uint32_t addr, uint32_t rank)
 {

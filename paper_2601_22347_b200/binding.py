@@ -335,28 +335,34 @@ def perq_massdiff_perm(chan_abs_sum_host: np.ndarray, b: int) -> np.ndarray:
     return perm
 
 
-def _here(t: torch.Tensor, dtype: torch.dtype) -> bool:
-    """A contiguous tensor of that type on the current device, where the call runs."""
-    return t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice()
+# Small calls of these are bound by the host (one row of 4096: 2.6 us in the library, 2.1 for each tensor made here, 0.06 for each
+# attribute asked), so the device is asked for once and a tensor's place, type and layout once each.
+def _on(t: torch.Tensor, device: int, dtype: torch.dtype) -> bool:
+    """A contiguous tensor of that type on that CUDA device."""
+    return t.get_device() == device and t.dtype is dtype and t.is_contiguous()
 
 
 def perq_rotate_quantize_i8(x: torch.Tensor, perm: Optional[torch.Tensor], b: int, out_codes: Optional[torch.Tensor] = None,
                             out_scales: Optional[torch.Tensor] = None, stream=None):
-    """x: bf16 CUDA tensor [T, d] (contiguous); perm: int32 CUDA tensor [d] or None.  Returns (int8 [T, d], fp32 [T, 1])."""
-    assert _here(x, torch.bfloat16) and x.dim() == 2
+    """x: bf16 CUDA tensor [T, d] (contiguous); perm: int32 CUDA tensor [d] or None.  Returns (int8 [T, d], fp32 [T, 1]).
+
+    All tensors are on the current device."""
+    device = torch._C._cuda_getDevice()
+    assert x.get_device() == device and x.dtype is torch.bfloat16 and x.is_contiguous()
     T, d = x.shape
-    assert perm is None or (_here(perm, torch.int32) and perm.numel() == d)
+    assert perm is None or (_on(perm, device, torch.int32) and perm.numel() == d)
     if out_codes is None:
-        out_codes = torch.empty((T, d), dtype=torch.int8, device=x.device)
+        out_codes = x.new_empty((T, d), dtype=torch.int8)
     else:
-        assert _here(out_codes, torch.int8) and out_codes.numel() == T * d
+        assert _on(out_codes, device, torch.int8) and out_codes.numel() == T * d
     if out_scales is None:
-        out_scales = torch.empty((T, 1), dtype=torch.float32, device=x.device)
+        out_scales = x.new_empty((T, 1), dtype=torch.float32)
     else:
-        assert _here(out_scales, torch.float32) and out_scales.numel() == T
+        assert _on(out_scales, device, torch.float32) and out_scales.numel() == T
     if _lib is None:
         load()
-    args = (x.data_ptr(), None if perm is None else perm.data_ptr(), T, d, b, out_codes.data_ptr(), out_scales.data_ptr(), _stream(stream))
+    args = (x.data_ptr(), None if perm is None else perm.data_ptr(), T, d, b, out_codes.data_ptr(), out_scales.data_ptr(),
+            torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
     try:
         rc = _rotate_quantize_i8(*args)
     except TypeError:           # (not plain integers: what ctypes makes of them)
@@ -368,7 +374,7 @@ def perq_rotate_quantize_i8(x: torch.Tensor, perm: Optional[torch.Tensor], b: in
 
 def perq_code_sums(codes: torch.Tensor, fmt: int, stream=None) -> torch.Tensor:
     """Sums of the rows of codes (int8 [.., d], or uint8 [.., d / 2] for INT4): int32 CUDA tensor [..]."""
-    assert codes.is_cuda and codes.is_contiguous() and codes.dtype == (torch.int8 if fmt == PERQ_FMT_INT8 else torch.uint8)
+    assert _on(codes, torch._C._cuda_getDevice(), torch.int8 if fmt == PERQ_FMT_INT8 else torch.uint8)
     d = codes.shape[-1] * (1 if fmt == PERQ_FMT_INT8 else 2)
     sums = torch.empty(codes.shape[:-1], dtype=torch.int32, device=codes.device)
     _check(load().perq_code_sums(_ptr(codes), fmt, sums.numel(), d, _ptr(sums), _stream(stream)), "perq_code_sums")
@@ -387,57 +393,70 @@ def perq_grouped_matmul_i8_workspace_bytes(T: int, E: int, N: int, d: int, a_fmt
     return int(n.value)
 
 
-def _codes_width(codes: torch.Tensor, scales: torch.Tensor, fmt: int, sums: Optional[torch.Tensor]) -> int:
-    """Channels of rows of codes [.., d] (or [.., d / 2]) with their scales and, of weights, their sums."""
-    packed = fmt != PERQ_FMT_INT8
-    assert _here(codes, torch.uint8 if packed else torch.int8) and _here(scales, torch.float32)
-    width = codes.shape[-1]
-    assert scales.numel() * width == codes.numel() * (2 if fmt == PERQ_FMT_INT4_ASYM else 1)
-    assert sums is None or (_here(sums, torch.int32) and sums.numel() * width == codes.numel())
-    return 2 * width if packed else width
-
-
 # (a workspace is asked for only where the call wants one: few do)
-def _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream):
-    d = _codes_width(a_codes, a_scales, a_fmt, None)
-    assert a_codes.dim() == 2 and _codes_width(w_codes, w_scales, w_fmt, w_sums) == d
-    T, N = a_codes.shape[0], w_codes.shape[-2]
+def _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, E, N, out, out_dtype, workspace, stream):
+    device, f32 = torch._C._cuda_getDevice(), torch.float32
+    T, d = a_codes.shape
+    assert a_codes.get_device() == device and a_codes.dtype is (torch.int8 if a_fmt == PERQ_FMT_INT8 else torch.uint8) and a_codes.is_contiguous()
+    assert w_codes.get_device() == device and w_codes.dtype is (torch.int8 if w_fmt == PERQ_FMT_INT8 else torch.uint8) and w_codes.is_contiguous()
+    assert a_scales.get_device() == device and a_scales.dtype is f32 and a_scales.is_contiguous()
+    assert w_scales.get_device() == device and w_scales.dtype is f32 and w_scales.is_contiguous()
+    assert a_scales.numel() == (2 * T if a_fmt == PERQ_FMT_INT4_ASYM else T) and w_scales.numel() == E * N
+    if a_fmt != PERQ_FMT_INT8:
+        d *= 2
+    assert w_codes.shape[-1] == (d if w_fmt == PERQ_FMT_INT8 else d // 2)
+    assert w_sums is None or (_on(w_sums, device, torch.int32) and w_sums.numel() == E * N)
     if out is None:
-        out = torch.empty((T, N), dtype=out_dtype, device=a_codes.device)
+        out = a_scales.new_empty((T, N), dtype=out_dtype)
     else:
-        assert _here(out, out.dtype) and out.shape == (T, N)
-    assert workspace is None or _here(workspace, workspace.dtype)
+        out_dtype = out.dtype
+        assert out.get_device() == device and out.is_contiguous() and out.shape == (T, N)
+    assert workspace is None or (workspace.get_device() == device and workspace.is_contiguous())
     if _lib is None:
         load()
-    sizes = (T, N, d) if offsets is None else (T, w_codes.shape[0], N, d)
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(device)
+    else:
+        stream = _stream(stream)
     while True:
-        args = (a_codes.data_ptr(), a_scales.data_ptr(), a_fmt, w_codes.data_ptr(), w_scales.data_ptr(), w_fmt, None if w_sums is None else w_sums.data_ptr(),
-                *(sizes if offsets is None else (offsets.data_ptr(), *sizes)), out.data_ptr(), OUT_BY_DTYPE[out.dtype],
-                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+        sums = None if w_sums is None else w_sums.data_ptr()
+        space, room = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        if offsets is None:
+            call, plain = _matmul_i8, _lib.perq_matmul_i8
+            args = (a_codes.data_ptr(), a_scales.data_ptr(), a_fmt, w_codes.data_ptr(), w_scales.data_ptr(), w_fmt, sums, T, N, d, out.data_ptr(),
+                    OUT_BY_DTYPE[out_dtype], space, room, stream)
+        else:
+            assert _on(offsets, device, torch.int32)
+            call, plain = _grouped_matmul_i8, _lib.perq_grouped_matmul_i8
+            args = (a_codes.data_ptr(), a_scales.data_ptr(), a_fmt, w_codes.data_ptr(), w_scales.data_ptr(), w_fmt, sums, offsets.data_ptr(), T, E, N, d,
+                    out.data_ptr(), OUT_BY_DTYPE[out_dtype], space, room, stream)
         try:
-            rc = _matmul_i8(*args) if offsets is None else _grouped_matmul_i8(*args)
+            rc = call(*args)
         except TypeError:       # (as above)
-            rc = _lib.perq_matmul_i8(*args) if offsets is None else _lib.perq_grouped_matmul_i8(*args)
+            rc = plain(*args)
         if rc == PERQ_OK:
             return out
         if rc != PERQ_ERR_WORKSPACE or workspace is not None:
             _check(rc, "perq_matmul_i8" if offsets is None else "perq_grouped_matmul_i8")
-        n = (perq_matmul_i8_workspace_bytes if offsets is None else perq_grouped_matmul_i8_workspace_bytes)(*sizes, a_fmt, w_fmt)
+        n = (perq_matmul_i8_workspace_bytes(T, N, d, a_fmt, w_fmt) if offsets is None else
+             perq_grouped_matmul_i8_workspace_bytes(T, E, N, d, a_fmt, w_fmt))
         workspace = torch.empty(n, dtype=torch.uint8, device=a_codes.device)
 
 
 def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
                    w_sums: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """a: codes [T, d] of tokens, w: codes [N, d] of weight channels (int8, or uint8 [.., d / 2] for INT4); returns out [T, N]."""
-    assert w_codes.dim() == 2
-    return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, None, out, out_dtype, workspace, stream)
+    """a: codes [T, d] of tokens, w: codes [N, d] of weight channels (int8, or uint8 [.., d / 2] for INT4); returns out [T, N].
+
+    All tensors are on the current device.  A workspace that the call wants and is not given is made here."""
+    N, _ = w_codes.shape
+    return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, None, 1, N, out, out_dtype, workspace, stream)
 
 
 def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
                            offsets: torch.Tensor, w_sums: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                            out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """As perq_matmul_i8 with w [E, N, d] and rows offsets[e] .. offsets[e + 1] (int32 CUDA tensor [E + 1]) of the tokens for expert e."""
-    assert w_codes.dim() == 3
-    assert _here(offsets, torch.int32) and offsets.numel() == w_codes.shape[0] + 1
-    return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, out, out_dtype, workspace, stream)
+    E, N, _ = w_codes.shape
+    assert offsets.numel() == E + 1
+    return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, E, N, out, out_dtype, workspace, stream)

@@ -320,10 +320,12 @@ template <int LOG2B>
 int launch_quant8_b(const perq_q8::Params &p, int pieces, long long grid, int threads, size_t smem, cudaStream_t st)
 {
     using namespace perq_q8;
-    if (pieces == 2) return launch_plain(p.perm ? quant8_kernel<LOG2B, 2, 2, true> : quant8_kernel<LOG2B, 2, 2, false>, grid, threads, smem, st, p);
-    if (threads <= Size<0>::threads) return launch_plain(p.perm ? quant8_kernel<LOG2B, 0, 1, true> : quant8_kernel<LOG2B, 0, 1, false>, grid, threads, smem, st, p);
-    if (threads <= Size<1>::threads) return launch_plain(p.perm ? quant8_kernel<LOG2B, 1, 1, true> : quant8_kernel<LOG2B, 1, 1, false>, grid, threads, smem, st, p);
-    return launch_plain(p.perm ? quant8_kernel<LOG2B, 2, 1, true> : quant8_kernel<LOG2B, 2, 1, false>, grid, threads, smem, st, p);
+    switch (pieces) {
+    case 1: return launch_plain(p.perm ? quant8_kernel<LOG2B, 1, true> : quant8_kernel<LOG2B, 1, false>, grid, threads, smem, st, p);
+    case 2: return launch_plain(p.perm ? quant8_kernel<LOG2B, 2, true> : quant8_kernel<LOG2B, 2, false>, grid, threads, smem, st, p);
+    case 4: return launch_plain(p.perm ? quant8_kernel<LOG2B, 4, true> : quant8_kernel<LOG2B, 4, false>, grid, threads, smem, st, p);
+    default: return launch_plain(p.perm ? quant8_kernel<LOG2B, 8, true> : quant8_kernel<LOG2B, 8, false>, grid, threads, smem, st, p);
+    }
 }
 
 int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *codes, float *scales, cudaStream_t st)
@@ -340,17 +342,24 @@ int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int3
     p.T = T;
     p.d = d;
     const int log2b = ilog2(b);
-    const int pieces = d > MAX_THREADS * LANE_ELEMS ? 2 : 1;
-    p.warps = (d + pieces * WARP_ELEMS - 1) / (pieces * WARP_ELEMS);
-    p.rows = (int)std::min<int64_t>(std::max(1, 8 / p.warps), std::max<int64_t>(1, (T + sms - 1) / sms));
-    const double e = log2b * std::sqrt((double)b) * 0x1p-24;
+    // as many pieces to a warp as leave the device full: a row costs a warp a fixed part, and several warps a barrier
+    const int all = (d + WARP_ELEMS - 1) / WARP_ELEMS;
+    int pieces = 8;
+    while (pieces > 1 && ((pieces / 2 >= all) || T * ((all + pieces - 1) / pieces) < (int64_t)sms * cta_warps(pieces) * 3 / 4) &&
+           (all + pieces / 2 - 1) / (pieces / 2) <= cta_warps(pieces / 2)) pieces /= 2;
+    p.warps = (all + pieces - 1) / pieces;
+    const size_t fixed = sizeof(Shared) + (perm ? ((size_t)d * 2 + 127) / 128 * 128 : 0), row = (size_t)STAGES * (size_t)d * 2;
+    int rows = (int)std::min<size_t>((size_t)(cta_warps(pieces) / p.warps), (kMaxSmem - fixed) / row);
+    if (p.warps > 1) rows = std::min(rows, 8);               // (a barrier each)
+    p.rows = (int)std::min<int64_t>(rows, std::max<int64_t>(1, (T + sms - 1) / sms));
+    if (p.rows < 1) return PERQ_ERR_SHAPE;                   // (no width up to PERQ_MAX_D)
+    const double e = b == 1 ? 0.0 : (13.0 * b / std::min(16, b / 4) - 1.0) * 0x1p-24;
     p.near_max = (float)(1.0 - 2.0 * e - 0x1p-22);
-    p.doubt = (float)(1.001 * (2.0 * e + 6.0 * 0x1p-24));
+    p.doubt = (float)(1.001 * (2.0 * e + 9.0 * 0x1p-24));
     p.inv_scale = 1.0 / (127.0 * std::sqrt((double)b));
     const int threads = p.rows * p.warps * 32;
-    const size_t smem = (size_t)p.rows * (sizeof(RowShared) + STAGES * (size_t)d * 2);
-    const int per_sm = threads <= Size<0>::threads ? Size<0>::ctas * Size<0>::threads / threads : threads <= Size<1>::threads ? Size<1>::ctas : 1;
-    const long long grid = std::min<long long>((T + p.rows - 1) / p.rows, (long long)sms * per_sm);
+    const size_t smem = fixed + (size_t)p.rows * row;
+    const long long grid = std::min<long long>((T + p.rows - 1) / p.rows, sms);
     switch (log2b) {
     case 0: return launch_quant8_b<0>(p, pieces, grid, threads, smem, st);
     case 4: return launch_quant8_b<4>(p, pieces, grid, threads, smem, st);

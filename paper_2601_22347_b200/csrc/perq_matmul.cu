@@ -323,8 +323,7 @@ int launch_quant8_b(const perq_q8::Params &p, int pieces, long long grid, int th
     switch (pieces) {
     case 1: return launch_plain(p.perm ? quant8_kernel<LOG2B, 1, true> : quant8_kernel<LOG2B, 1, false>, grid, threads, smem, st, p);
     case 2: return launch_plain(p.perm ? quant8_kernel<LOG2B, 2, true> : quant8_kernel<LOG2B, 2, false>, grid, threads, smem, st, p);
-    case 4: return launch_plain(p.perm ? quant8_kernel<LOG2B, 4, true> : quant8_kernel<LOG2B, 4, false>, grid, threads, smem, st, p);
-    default: return launch_plain(p.perm ? quant8_kernel<LOG2B, 8, true> : quant8_kernel<LOG2B, 8, false>, grid, threads, smem, st, p);
+    default: return launch_plain(p.perm ? quant8_kernel<LOG2B, 4, true> : quant8_kernel<LOG2B, 4, false>, grid, threads, smem, st, p);
     }
 }
 
@@ -342,11 +341,10 @@ int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int3
     p.T = T;
     p.d = d;
     const int log2b = ilog2(b);
-    // as many pieces to a warp as leave the device full: a row costs a warp a fixed part, and several warps a barrier
     const int all = (d + WARP_ELEMS - 1) / WARP_ELEMS;
-    int pieces = 8;
-    while (pieces > 1 && ((pieces / 2 >= all) || T * ((all + pieces - 1) / pieces) < (int64_t)sms * cta_warps(pieces) * 3 / 4) &&
-           (all + pieces / 2 - 1) / (pieces / 2) <= cta_warps(pieces / 2)) pieces /= 2;
+    // Pieces of a row to a warp: a row costs a warp a fixed part, so four (us for one / two / four: 16384 x 4096, b = 32, 168 / 95 / 48; 1531 x 9728 45 / 23 / 14,
+    // 64 x 4096 5.5 / 5.3 / 5.2; eight 46, 16, 7), but few permuted rows, whose warps gather, are better spread (1 x 4096 5.0 / 5.4 / 6.1, 64 5.9 / 6.3 / 7.1).
+    const int pieces = all == 1 || (perm && T <= sms && all <= cta_warps(1)) ? 1 : all == 2 ? 2 : 4;
     p.warps = (all + pieces - 1) / pieces;
     const size_t fixed = sizeof(Shared) + (perm ? ((size_t)d * 2 + 127) / 128 * 128 : 0), row = (size_t)STAGES * (size_t)d * 2;
     int rows = (int)std::min<size_t>((size_t)(cta_warps(pieces) / p.warps), (kMaxSmem - fixed) / row);

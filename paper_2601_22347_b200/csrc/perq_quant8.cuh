@@ -14,10 +14,10 @@
 // largest quotient times 2 E + 9 2^-24 in all.  Elements that lie that close to the border between two codes are summed again in fp64
 // (b = 32, gaussian values: 3 of a row of 4096; with outliers, next to none outside their blocks).
 //
-// Such places are rare, so a warp only notes their blocks and settles them eight rows at a time: it rotates the noted blocks again in fp64 from
-// global memory, 32 / (b / 16) at once, stores the rows' scales and writes the blocks' codes anew.  (16384 x 4096, b = 32, 4 warps to a row: exact sums as
-// they came up 70 us, by a warp of its own 60 .. 88 us.)  A warp has up to eight pieces of 512 channels of a row in registers, so rows of up to 4096
-// need no barrier; longer ones, and rows too few to fill the device so, have several warps, which meet at one barrier a row and two for every eight.
+// Such places are rare, so a warp only notes them and settles them eight rows at a time, 32 / (b / 16) at once, from the inputs in global memory; it stores
+// the rows' scales and mends codes.  (16384 x 4096, b = 32, 4 warps to a row: exact sums as they came up 70 us, by a warp of its own 60 .. 88 us.)  A warp
+// has up to four pieces of 512 channels of a row in registers.  Rows of up to 2048 need no barrier; the warps of longer ones meet at one barrier
+// a row and two for every eight.
 #pragma once
 
 #include "perq_mm_ptx.cuh"
@@ -33,10 +33,10 @@ constexpr int MAX_LOG2B = 9;
 constexpr int MAX_WARPS = 32;                 // of a CTA
 constexpr int STAGES = 2;                     // rows of a group of warps in shared memory: one is read, the next is on its way
 constexpr int BATCH = 8;                      // rows that are settled together
-constexpr int NOTES = 48;                     // of a warp, batch and kind; more: every block that it has of these rows is settled
+constexpr int NOTES = 48;                     // of a warp, batch and kind; more: everything that it has of these rows is settled
 
-// Warps of a CTA, by the pieces that each holds (168, 102 and 64 registers to a thread).
-__host__ __device__ constexpr int cta_warps(int pieces) { return pieces == 8 ? 12 : pieces == 4 ? 20 : 32; }
+// Warps of a CTA, by the pieces that each holds (96 and 64 registers to a thread).
+__host__ __device__ constexpr int cta_warps(int pieces) { return pieces == 4 ? 20 : 32; }
 
 struct Params {
     const uint16_t *x;
@@ -58,7 +58,7 @@ struct Group {
 };
 struct Notes {
     uint32_t count[2];
-    uint32_t note[2][NOTES];                                          // row of the batch << 16 | channel: blocks with the maximum, with codes in doubt
+    uint32_t note[2][NOTES];                                          // row of the batch << 16 | channel: what may be the maximum, codes in doubt
 };
 struct alignas(128) Shared {
     Group group[MAX_WARPS];
@@ -191,16 +191,93 @@ __device__ __forceinline__ void rotate(Pair (&u)[LANE_ELEMS / 2], const uint32_t
     }
 }
 
-__device__ __forceinline__ void note(Notes *notes, int kind, uint32_t row, int c)
+// Notes the elements in `mask` of a lane whose first channel is c.
+__device__ __forceinline__ void note(Notes *notes, int kind, uint32_t mask, uint32_t row, int c)
 {
-    const uint32_t at = atomicAdd(&notes->count[kind], 1u);
-    if (at < NOTES) notes->note[kind][at] = (row << 16) | (uint32_t)c;
+    while (mask != 0u) {
+        const int e = __ffs((int)mask) - 1;
+        mask &= mask - 1u;
+        const uint32_t at = atomicAdd(&notes->count[kind], 1u);
+        if (at < NOTES) notes->note[kind][at] = (row << 16) | (uint32_t)(c + e);
+    }
 }
 
-// n blocks in fp64, 32 / (b / 16) at a time, b / 16 lanes to a block (at least one), 16 channels each.  place_of(i): row number << 16 | a channel of
-// block i; f(number, channel, outputs) is called by every lane that has some, with its first channel.  Rows are read again.
+// Notes what is in doubt of a lane's 16 outputs: quotients from `limit` on away from their codes (0: all; 1: none), outputs from `near` on.  (Inside the
+// unrolled loop over the pieces this was half of its instructions, and twice its time.)
+__device__ __noinline__ void note_lane(Notes *notes, Pair u0, Pair u1, Pair u2, Pair u3, Pair u4, Pair u5, Pair u6, Pair u7, float ratio, float limit, float near,
+                                       uint32_t row, int c)
+{
+    const Pair u[8] = {u0, u1, u2, u3, u4, u5, u6, u7}, rr = pair_of(ratio, ratio), magic = pair_of(12582912.0f, 12582912.0f), neg = pair_of(-1.0f, -1.0f);
+    uint32_t codes = 0u, most = 0u;
+#pragma unroll
+    for (int j = 0; j < LANE_ELEMS / 2; ++j) {
+        float x, y, v, w;
+        split(u[j], v, w);
+        split(pair_fma(u[j], rr, pair_fma(pair_fma(u[j], rr, magic), neg, magic)), x, y);
+        codes |= (fabsf(x) >= limit ? 1u << (2 * j) : 0u) | (fabsf(y) >= limit ? 2u << (2 * j) : 0u);
+        most |= (fabsf(v) >= near ? 1u << (2 * j) : 0u) | (fabsf(w) >= near ? 2u << (2 * j) : 0u);
+    }
+    note(notes, NOTE_CODE, codes, row, c);
+    note(notes, NOTE_MAX, most, row, c);
+}
+
+// 16 adjacent channels of a row as the rotation takes them, raw pairs.  table: places in the row, in bytes (PERM).
+template <bool PERM>
+__device__ __forceinline__ void inputs16(uint32_t (&raw)[8], const uint16_t *row, uint32_t table, int k0)
+{
+    if (PERM) {
+        const uint4 a = perq_mm::lds128(table + 2u * (uint32_t)k0), b = perq_mm::lds128(table + 2u * (uint32_t)k0 + 16u);
+        const uint32_t at[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const unsigned char *const bytes = reinterpret_cast<const unsigned char *>(row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            raw[j] = (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(bytes + (at[j] & 0xffffu))) |
+                     ((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(bytes + (at[j] >> 16))) << 16);
+    } else {
+        const uint4 a = __ldg(reinterpret_cast<const uint4 *>(row + k0)), b = __ldg(reinterpret_cast<const uint4 *>(row + k0) + 1);
+        raw[0] = a.x; raw[1] = a.y; raw[2] = a.z; raw[3] = a.w;
+        raw[4] = b.x; raw[5] = b.y; raw[6] = b.z; raw[7] = b.w;
+    }
+}
+
+// n noted places, 32 / (b / 16) at a time, b / 16 lanes to a place (at least one), 16 inputs each: f(row, channel, exact output) is called by the
+// first of them.
+template <int LOG2B, bool PERM, typename R, typename F>
+__device__ __forceinline__ void settle_places(const uint32_t *places, uint32_t n, uint32_t table, int lane, R row_of, F f)
+{
+    constexpr int lanes = LOG2B > 4 ? 1 << (LOG2B - 4) : 1, at_once = 32 / lanes;
+    for (uint32_t i0 = 0; i0 < n; i0 += at_once) {
+        const uint32_t i = i0 + (uint32_t)lane / lanes;
+        const bool mine = i < n;
+        const uint32_t place = places[mine ? i : 0];
+        const int c = (int)(place & 0xffffu), k0 = c / (lanes * LANE_ELEMS) * (lanes * LANE_ELEMS) + (lane & (lanes - 1)) * LANE_ELEMS;
+        uint32_t raw[8];
+        inputs16<PERM>(raw, row_of(place >> 16), table, k0);
+        double sum[4] = {0.0, 0.0, 0.0, 0.0};                // (four chains: most of the time here is waiting for sums)
+        // bit j: the sign of input k0 + j, the parity of c & (k0 + j) inside the block
+        const uint32_t signs = ((c & 1) ? 0xaaaau : 0u) ^ ((c & 2) ? 0xccccu : 0u) ^ ((c & 4) ? 0xf0f0u : 0u) ^ ((c & 8) ? 0xff00u : 0u) ^
+                               ((__popc(c & k0 & ((1 << LOG2B) - 1)) & 1) ? 0xffffu : 0u);
+#pragma unroll
+        for (int j = 0; j < LANE_ELEMS; ++j) {
+            const uint32_t v = (j & 1) ? (raw[j >> 1] & 0xffff0000u) : (raw[j >> 1] << 16);
+            if (LOG2B == 0) {
+                if (j == (c & 15)) sum[0] = (double)__uint_as_float(v);
+            } else {
+                sum[j & 3] += (double)__uint_as_float(v ^ ((signs << (31 - j)) & 0x80000000u));
+            }
+        }
+        double u = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+        for (int m = 1; m < lanes; m *= 2) u += __shfl_xor_sync(0xffffffffu, u, m);
+        if (mine && (lane & (lanes - 1)) == 0) f(place >> 16, c, u);
+        __syncwarp();
+    }
+}
+
+// n blocks in fp64, 32 / (b / 16) at a time, b / 16 lanes to a block (at least one), 16 channels each.  place_of(i): row of the batch << 16 | a channel
+// of block i (past the row: none); f(row, channel, outputs) is called by every lane that has some, with its first channel.
 template <int LOG2B, bool PERM, typename P, typename R, typename F>
-__device__ __forceinline__ void settle(const Params &p, uint32_t n, int lane, P place_of, R row_of, F f)
+__device__ __forceinline__ void settle_blocks(const Params &p, uint32_t n, uint32_t table, int lane, P place_of, R row_of, F f)
 {
     constexpr int lanes = LOG2B > 4 ? 1 << (LOG2B - 4) : 1, at_once = 32 / lanes;
     for (uint32_t i0 = 0; i0 < n; i0 += at_once) {
@@ -209,13 +286,11 @@ __device__ __forceinline__ void settle(const Params &p, uint32_t n, int lane, P 
         const bool mine = i < n && (int)(place & 0xffffu) < p.d;
         if (!mine) place = 0u;
         const int c = (int)(place & 0xffffu) / (lanes * LANE_ELEMS) * (lanes * LANE_ELEMS) + (lane & (lanes - 1)) * LANE_ELEMS;
-        const uint16_t *const row = row_of(place >> 16);
+        uint32_t raw[8];
+        inputs16<PERM>(raw, row_of(place >> 16), table, c);
         double v[LANE_ELEMS];
 #pragma unroll
-        for (int j = 0; j < LANE_ELEMS; ++j) {
-            const int from = PERM ? min(max(__ldg(p.perm + c + j), 0), p.d - 1) : c + j;
-            v[j] = mine ? (double)__uint_as_float((uint32_t)__ldg(row + from) << 16) : 0.0;
-        }
+        for (int j = 0; j < LANE_ELEMS; ++j) v[j] = (double)__uint_as_float((j & 1) ? (raw[j >> 1] & 0xffff0000u) : (raw[j >> 1] << 16));
         if (LOG2B > 0) {
 #pragma unroll
             for (int h = 1; h < LANE_ELEMS; h *= 2)
@@ -260,35 +335,37 @@ __device__ __forceinline__ void store_codes(int8_t *to, const double (&v)[LANE_E
 }
 
 
-// A warp's share of the rows of a batch, row t0 + r * step the r-th: c0 is its first channel, per_piece from piece to piece.
+// A warp's share of the rows of a batch, row t0 + r * step the r-th.
 template <int LOG2B, int PIECES, bool PERM>
-__device__ __noinline__ void settle_batch(const Params &p, Group *group, Notes *notes, long long t0, long long step, uint32_t rows, int g, int w, int lane)
+__device__ __noinline__ void settle_batch(const Params &p, Group *group, Notes *notes, uint32_t table, long long t0, long long step, uint32_t rows, int g, int w, int lane)
 {
     __syncwarp();
     const uint32_t n_max = *reinterpret_cast<volatile uint32_t *>(&notes->count[NOTE_MAX]), n_code = *reinterpret_cast<volatile uint32_t *>(&notes->count[NOTE_CODE]);
-    constexpr uint32_t block = LOG2B > 4 ? 1u << LOG2B : LANE_ELEMS, blocks = WARP_ELEMS / block * PIECES;
-    const bool all = n_max > NOTES || n_code > NOTES;                 // all its blocks of all rows
+    const bool all = n_max > NOTES || n_code > NOTES;                 // everything that it has of all rows
     auto row_of = [&](uint32_t r) { return p.x + (size_t)(t0 + r * step) * (size_t)p.d; };
-    // block k of this warp's, or none (a channel past the row)
+    auto raise = [&](uint32_t r, double m) {
+        if (m > 0.0) atomicMax(&group->top[r], (unsigned long long)__double_as_longlong(m));
+    };
+    auto top_of = [&](uint32_t r) { return __longlong_as_double((long long)*reinterpret_cast<volatile unsigned long long *>(&group->top[r])); };
+    constexpr uint32_t block = LOG2B > 4 ? 1u << LOG2B : LANE_ELEMS, blocks = WARP_ELEMS / block * PIECES;
     auto own = [&](uint32_t k) {
         const uint32_t r = k / blocks, j = k % blocks * block;
         return (r << 16) | ((j / WARP_ELEMS * (uint32_t)p.warps + (uint32_t)w) * WARP_ELEMS + j % WARP_ELEMS);
     };
-    const uint32_t *const noted_max = notes->note[NOTE_MAX], *const noted_code = notes->note[NOTE_CODE];
-    settle<LOG2B, PERM>(p, all ? rows * blocks : n_max, lane, [&](uint32_t k) { return all ? own(k) : noted_max[k]; }, row_of,
-                        [&](uint32_t r, int, const double (&v)[LANE_ELEMS]) {
-                            const double m = largest(v);
-                            if (m > 0.0) atomicMax(&group->top[r], (unsigned long long)__double_as_longlong(m));
-                        });
+    if (all) settle_blocks<LOG2B, PERM>(p, rows * blocks, table, lane, own, row_of, [&](uint32_t r, int, const double (&v)[LANE_ELEMS]) { raise(r, largest(v)); });
+    else settle_places<LOG2B, PERM>(notes->note[NOTE_MAX], n_max, table, lane, row_of, [&](uint32_t r, int, double u) { raise(r, fabs(u)); });
     row_barrier(g, p.warps);
-    settle<LOG2B, PERM>(p, all ? rows * blocks : n_code, lane, [&](uint32_t k) { return all ? own(k) : noted_code[k]; }, row_of,
-                        [&](uint32_t r, int c, const double (&v)[LANE_ELEMS]) {
-                            const double top = __longlong_as_double((long long)*reinterpret_cast<volatile unsigned long long *>(&group->top[r]));
-                            store_codes(p.codes + (size_t)(t0 + r * step) * (size_t)p.d + c, v, top);
-                        });
+    if (all)
+        settle_blocks<LOG2B, PERM>(p, rows * blocks, table, lane, own, row_of, [&](uint32_t r, int c, const double (&v)[LANE_ELEMS]) {
+            store_codes(p.codes + (size_t)(t0 + r * step) * (size_t)p.d + c, v, top_of(r));
+        });
+    else
+        settle_places<LOG2B, PERM>(notes->note[NOTE_CODE], n_code, table, lane, row_of, [&](uint32_t r, int c, double u) {
+            const double top = top_of(r);
+            if (top > 0.0) p.codes[(size_t)(t0 + r * step) * (size_t)p.d + c] = (int8_t)__double2int_rn(127.0 * u / top);
+        });
     __syncwarp();
-    if (w == 0 && lane < (int)rows)
-        p.scales[t0 + lane * step] = (float)(__longlong_as_double((long long)*reinterpret_cast<volatile unsigned long long *>(&group->top[lane])) * p.inv_scale);
+    if (w == 0 && lane < (int)rows) p.scales[t0 + lane * step] = (float)(top_of((uint32_t)lane) * p.inv_scale);
     row_barrier(g, p.warps);
     if (w == 0 && lane < BATCH) group->top[lane] = 0ull;              // (read and raised again after the next row's barrier)
     if (lane < 2) notes->count[lane] = 0u;
@@ -407,13 +484,13 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
                 *reinterpret_cast<uint4 *>(out + k * per_piece) = make_uint4(code[0], code[1], code[2], code[3]);
                 const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt || (tiny && all > 0.0f);
                 if (doubt || block[k] >= near) {
-                    if (doubt) note(notes, NOTE_CODE, i % BATCH, c0 + k * per_piece);
-                    if (block[k] >= near && (lane & (block_lanes - 1)) == 0) note(notes, NOTE_MAX, i % BATCH, c0 + k * per_piece);
+                    note_lane(notes, u[k][0], u[k][1], u[k][2], u[k][3], u[k][4], u[k][5], u[k][6], u[k][7], ratio, tiny ? 0.0f : doubt ? 0.5f - 0x1p-23f - block[k] * ratio * p.doubt : 1.0f,
+                              near, i % BATCH, c0 + k * per_piece);
                 }
             }
         }
         if (i % BATCH == BATCH - 1 || i + 1 == steps)
-            settle_batch<LOG2B, PIECES, PERM>(p, group, notes, first + (long long)(i / BATCH * BATCH) * step, step, i % BATCH + 1u, g, w, lane);
+            settle_batch<LOG2B, PIECES, PERM>(p, group, notes, table, first + (long long)(i / BATCH * BATCH) * step, step, i % BATCH + 1u, g, w, lane);
     }
 }
 

@@ -120,7 +120,7 @@ int launch_few(const Product &m, cudaStream_t st)
     p.spreads = K::packed ? 3 : 0;
     p.tmem_cols = 32;
     while (p.tmem_cols < 2u * (uint32_t)p.nt + (W4 ? 64u * p.spreads : 0u)) p.tmem_cols *= 2;
-    const uint32_t load = p.w_bytes + p.a_bytes, tail = 16 + 16 * (12 + 4) + 32 + 4 * (m.offsets ? (uint32_t)m.E + 1 : 1);
+    const uint32_t load = p.w_bytes + p.a_bytes, tail = 16 + 16 * (12 + 4) + 32 + 8 * (m.offsets ? (uint32_t)m.E + 1 : 1);
     // The split that fills the SMs, as far as its clusters fit on the device at once, and room for its sums.  Two CTAs to an SM where there are enough for
     // that, tensor memory has room for both and the ring is then long enough.
     uint32_t sums = 0;
@@ -152,7 +152,7 @@ int launch_few(const Product &m, cudaStream_t st)
     p.off_sums = p.off_spread + p.spreads * p.spread_bytes;
     p.off_bars = p.off_sums + sums;
     p.off_first = p.off_bars + 16 + 16 * (p.loads + p.spreads) + 32;
-    const size_t smem = 1024 + p.off_first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
+    const size_t smem = 1024 + p.off_first + 8 * (m.offsets ? (size_t)m.E + 1 : 1);
     p.a_scales = m.a_scales;
     p.w_scales = m.w_scales;
     p.w_sums = m.w_sums;
@@ -276,7 +276,7 @@ int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_
     if (items >= (1ll << 31)) return PERQ_ERR_SHAPE;
     CUtensorMap w, a;
     if (!codes_map(&w, weights, false, (uint64_t)m.E * (uint64_t)m.N, m.d, perq_mm::MANY_CHANNELS / 2) || !codes_map(&a, tokens, false, (uint64_t)m.T, m.d, 128)) return PERQ_ERR_CUDA;
-    const size_t smem = 1024 + perq_mm::ManySmem::first + 4 * (m.offsets ? (size_t)m.E + 1 : 1);
+    const size_t smem = 1024 + perq_mm::ManySmem::first + 8 * (m.offsets ? (size_t)m.E + 1 : 1);
     p.split = many_split(m, items, p.steps, smem);
     const int64_t clusters = p.split > 1 ? items : std::min<int64_t>(items, sms / 2);
     return launch_product(perq_mm::many_kernel, (unsigned)(2 * p.split * clusters), perq_mm::MANY_THREADS, smem, 2 * p.split, st, w, a, p);

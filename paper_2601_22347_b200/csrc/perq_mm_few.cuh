@@ -76,17 +76,18 @@ __device__ __forceinline__ FewItem few_item(const FewParams &p, const int32_t *f
     }
     const uint32_t tiles = (uint32_t)(first[lo + 1] - first[lo]), local = item - (uint32_t)first[lo] * (uint32_t)p.n_tiles, n = local / tiles;
     it.expert = lo;
-    const int32_t begin = min(max(__ldg(p.offsets + lo), 0), p.T);
-    it.t0 = begin + (int32_t)(local - n * tiles) * p.nt;
-    it.t_end = min(max(__ldg(p.offsets + lo + 1), 0), p.T);
+    it.t0 = first[p.E + 1 + lo] + (int32_t)(local - n * tiles) * p.nt;
+    it.t_end = first[p.E + 2 + lo];
     it.n0 = (int32_t)n * FEW_ROWS;
     return it;
 }
 
-// first[e]: tiles of tokens of the experts before e, by one warp.  (Offsets outside 0 .. T are taken into it.)
+// first[e]: tiles of tokens of the experts before e, and behind these E + 1 numbers the offsets, by one warp.  (Offsets outside 0 .. T are
+// taken into it.)
 __device__ __forceinline__ void count_tiles(const int32_t *offsets, int E, int32_t T, int32_t nt, int32_t *first, int lane)
 {
     int32_t before = 0;
+    for (int e = lane; e <= E; e += 32) first[E + 1 + e] = min(max(__ldg(offsets + e), 0), T);
     for (int e0 = 0; e0 < E; e0 += 32) {
         const int e = e0 + lane;
         int32_t n = 0;
@@ -217,7 +218,7 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
     unsigned char *const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-    int32_t *const first = reinterpret_cast<int32_t *>(smem + p.off_first);           // [E + 1]
+    int32_t *const first = reinterpret_cast<int32_t *>(smem + p.off_first);           // [2 (E + 1)], see count_tiles
     volatile uint32_t *const slot = reinterpret_cast<volatile uint32_t *>(smem + p.off_bars);
     // barriers: loads full and empty, spread full and empty, accumulators full and empty (two)
     const uint32_t l_full = base + p.off_bars + 16, l_empty = l_full + 8 * p.loads, s_full = l_empty + 8 * p.loads, s_empty = s_full + 8 * p.spreads,

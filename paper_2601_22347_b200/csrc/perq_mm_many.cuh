@@ -42,7 +42,7 @@ struct ManySmem {
     static constexpr uint32_t slot = bars + 16 * MANY_STAGES + 32;
     static constexpr uint32_t scales = slot + 16;                         // [2][256] of the channels' scales, [2][256] of their sums
     static constexpr uint32_t rows = scales + 4 * 4 * MANY_CHANNELS;      // [8][32][MANY_ROOM] of the epilogue's warps
-    static constexpr uint32_t first = rows + 8 * 32 * MANY_ROOM * 4;      // [E + 1]
+    static constexpr uint32_t first = rows + 8 * 32 * MANY_ROOM * 4;      // [2 (E + 1)], see count_tiles
 };
 
 struct ManyItem {
@@ -68,8 +68,8 @@ __device__ __forceinline__ ManyItem many_item(const ManyParams &p, const int32_t
         tiles = (uint32_t)(first[lo + 1] - first[lo]);
         local = item - (uint32_t)first[lo] * (uint32_t)p.n_tiles;
         it.expert = lo;
-        begin = min(max(__ldg(p.offsets + lo), 0), p.T);
-        it.t_end = min(max(__ldg(p.offsets + lo + 1), 0), p.T);
+        begin = first[p.E + 1 + lo];
+        it.t_end = first[p.E + 2 + lo];
     }
     const uint32_t band = local / (MANY_BAND * (uint32_t)p.n_tiles), in = local - band * MANY_BAND * (uint32_t)p.n_tiles;
     const uint32_t height = min((uint32_t)MANY_BAND, tiles - band * MANY_BAND), n = in / height;

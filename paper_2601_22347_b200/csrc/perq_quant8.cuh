@@ -14,10 +14,10 @@
 // largest quotient times 2 E + 9 2^-24 in all.  Elements that lie that close to the border between two codes are summed again in fp64
 // (b = 32, gaussian values: 3 of a row of 4096; with outliers, next to none outside their blocks).
 //
-// Such places are rare, so a warp only notes them and settles them eight rows at a time, 32 / (b / 16) at once, from the inputs in global memory; it stores
+// Such places are rare, so a warp only notes them and settles them sixteen rows at a time, 32 / (b / 16) at once, from the inputs in global memory; it stores
 // the rows' scales and mends codes.  (16384 x 4096, b = 32, 4 warps to a row: exact sums as they came up 70 us, by a warp of its own 60 .. 88 us.)  A warp
 // has up to four pieces of 512 channels of a row in registers.  Rows of up to 2048 need no barrier; the warps of longer ones meet at one barrier
-// a row and two for every eight.
+// a row and two for every sixteen.
 #pragma once
 
 #include "perq_mm_ptx.cuh"
@@ -32,11 +32,11 @@ constexpr int WARP_ELEMS = 32 * LANE_ELEMS;
 constexpr int MAX_LOG2B = 9;
 constexpr int MAX_WARPS = 32;                 // of a CTA
 constexpr int STAGES = 2;                     // rows of a group of warps in shared memory: one is read, the next is on its way
-constexpr int BATCH = 8;                      // rows that are settled together
-constexpr int NOTES = 48;                     // of a warp, batch and kind; more: everything that it has of these rows is settled
+constexpr int BATCH = 16;                     // rows that are settled together
+constexpr int NOTES = 64;                     // of a warp, batch and kind; more: everything that it has of these rows is settled
 
-// Warps of a CTA, by the pieces that each holds (96 and 64 registers to a thread).
-__host__ __device__ constexpr int cta_warps(int pieces) { return pieces == 4 ? 20 : 32; }
+// Warps of a CTA, by the pieces that each holds (120 and 64 registers to a thread; four pieces in 96 registers: 42 -> 48 .. 70 us for 16384 x 4096).
+__host__ __device__ constexpr int cta_warps(int pieces) { return pieces == 4 ? 16 : 32; }
 
 struct Params {
     const uint16_t *x;

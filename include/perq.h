@@ -384,8 +384,8 @@ int perq_matmul_i8_workspace_bytes(int64_t T, int32_t N, int32_t d, int32_t a_fm
  *
  *   w_codes             codes of [E, N, d]; w_scales float [E, N]; w_sums int32 [E, N]
  *   offsets             device int32 [E + 1], not decreasing, in 0 .. T.  The host does not look at it, so the call can be
- *                       captured and replayed with other offsets.  Entries outside 0 .. T are taken into it, and where they
- *                       decrease the expert has no rows: wrong numbers, never a fault.
+ *                       captured and replayed with other offsets.  Entries outside 0 .. T are taken into it, and an entry
+ *                       below an earlier one counts as that one: wrong numbers, never a fault.
  *   T                   rows of a_codes and out.  Rows before offsets[0] and from offsets[E] on are neither computed nor written.
  *   E                   1 .. PERQ_MAX_EXPERTS, E * N <= 2^30
  * Everything else as for perq_matmul_i8.

@@ -441,6 +441,8 @@ def _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets
         n = (perq_matmul_i8_workspace_bytes(T, N, d, a_fmt, w_fmt) if offsets is None else
              perq_grouped_matmul_i8_workspace_bytes(T, E, N, d, a_fmt, w_fmt))
         workspace = torch.empty(n, dtype=torch.uint8, device=a_codes.device)
+        if stream != torch._C._cuda_getCurrentRawStream(device):        # (it is let go on return, and its memory is the current stream's)
+            workspace.record_stream(torch.cuda.ExternalStream(stream))
 
 
 def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,

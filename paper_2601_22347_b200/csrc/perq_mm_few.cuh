@@ -82,19 +82,26 @@ __device__ __forceinline__ FewItem few_item(const FewParams &p, const int32_t *f
     return it;
 }
 
-// first[e]: tiles of tokens of the experts before e, and behind these E + 1 numbers the offsets, by one warp.  (Offsets outside 0 .. T are
-// taken into it.)
+// first[e]: tiles of tokens of the experts before e, and behind these E + 1 numbers the offsets, by one warp.  Offsets outside 0 .. T are taken into
+// it, and one below an earlier one counts as that: an expert never has rows of another, and the tiles are no more than the host counts on.
 __device__ __forceinline__ void count_tiles(const int32_t *offsets, int E, int32_t T, int32_t nt, int32_t *first, int lane)
 {
+    int32_t *const at = first + E + 1;
+    int32_t most = 0;
+    for (int e0 = 0; e0 <= E; e0 += 32) {
+        const int e = e0 + lane;
+        int32_t v = e <= E ? min(max(__ldg(offsets + e), 0), T) : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) v = max(v, __shfl_up_sync(0xffffffffu, v, o));
+        v = max(v, most);
+        if (e <= E) at[e] = v;
+        most = __shfl_sync(0xffffffffu, v, 31);
+    }
+    __syncwarp();
     int32_t before = 0;
-    for (int e = lane; e <= E; e += 32) first[E + 1 + e] = min(max(__ldg(offsets + e), 0), T);
     for (int e0 = 0; e0 < E; e0 += 32) {
         const int e = e0 + lane;
-        int32_t n = 0;
-        if (e < E) {
-            const int32_t b = min(max(__ldg(offsets + e), 0), T), c = min(max(__ldg(offsets + e + 1), 0), T);
-            n = c > b ? (c - b + nt - 1) / nt : 0;
-        }
+        const int32_t n = e < E ? (at[e + 1] - at[e] + nt - 1) / nt : 0;
         int32_t sum = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {

@@ -108,6 +108,33 @@ def test_bad_offsets_do_not_write_past_the_rows(B):
         assert (room[:50] == 77).all() and (room[100:] == 77).all()
 
 
+def test_offsets_that_go_back_and_forth_keep_their_first_rows(B):
+    """An entry below an earlier one counts as that one, however many there are: no row belongs to two experts, no tile is counted twice."""
+    E, T, N, d = 1024, 3000, 40, 64
+    for T in (300, 90000):
+        a, sa, w, sw, _ = operands(INT8, INT8, T, N, d, 6, E)
+        room = torch.full((T + 200, N), 77.0, device="cuda")
+        offsets = torch.tensor([0, T] * 512 + [5], dtype=torch.int32, device="cuda")
+        B.perq_grouped_matmul_i8(a, sa, B.PERQ_FMT_INT8, w.reshape(E, N, -1), sw.reshape(E, N), B.PERQ_FMT_INT8, offsets, out=room[100:T + 100])
+        P.compare(room[100:T + 100], *P.product(INT8, a, sa, INT8, w[:N], sw[:N]))
+        assert (room[:100] == 77).all() and (room[T + 100:] == 77).all()
+
+
+@pytest.mark.parametrize("T", [3, 1500])
+def test_a_stream_given_to_the_call(B, T):
+    """The call's own workspace outlives it on a stream that is not the current one."""
+    a, sa, w, sw, cs = operands(ASYM, INT4, T, 1000, 2048, 51)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(6):
+        outs.append(B.perq_matmul_i8(a, sa, B.PERQ_FMT_INT4_ASYM, w, sw, B.PERQ_FMT_INT4, cs, out_dtype=F32, stream=stream))
+        torch.full((T * 2048 + 1000 * 2048 + 4096,), 255, dtype=torch.uint8, device="cuda")      # (would take the workspace's memory)
+    torch.cuda.synchronize()
+    for out in outs:
+        P.compare(out, *P.product(ASYM, a, sa, INT4, w, sw))
+
+
 def test_results_do_not_depend_on_the_run_or_the_batch(B):
     """The sums are exact, so a row's results are the same bits alone, in a batch and grouped."""
     a, sa, w, sw, _ = operands(INT4, INT4, 300, 512, 2048, 11)

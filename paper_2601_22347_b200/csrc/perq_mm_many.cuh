@@ -329,6 +329,7 @@ struct SpreadParams {
     const int32_t *offsets;
     long long token_chunks, expert_chunks;       // of 16 packed bytes
     int32_t T;
+    int32_t wide;                                // the workspace can be written 32 bytes at a time
 };
 __global__ void __launch_bounds__(256) spread_kernel(const SpreadParams p)
 {
@@ -357,7 +358,13 @@ __global__ void __launch_bounds__(256) spread_kernel(const SpreadParams p)
                 x[2 * i] = __byte_perm(lo, hi, 0x5140);
                 x[2 * i + 1] = __byte_perm(lo, hi, 0x7362);
             }
-            store_wide(dst + 2 * (i0 + k * step), x);
+            uint4 *const to = dst + 2 * (i0 + k * step);
+            if (p.wide) {
+                store_wide(to, x);
+            } else {
+                to[0] = make_uint4(x[0], x[1], x[2], x[3]);
+                to[1] = make_uint4(x[4], x[5], x[6], x[7]);
+            }
         }
     }
 }

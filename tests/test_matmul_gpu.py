@@ -225,3 +225,20 @@ def test_two_calls_at_once(B):
     for k, (o, f) in enumerate(((x, (INT4, INT8)), (y, (ASYM, INT4)))):
         P.compare(outs[k][0], *P.product(f[0], o[0], o[1], f[1], o[2], o[3]))
         assert all(torch.equal(v, outs[k][0]) for v in outs[k])
+
+
+@pytest.mark.parametrize("skip", [0, 16, 32, 48])
+@pytest.mark.parametrize("a_fmt,w_fmt", [(INT4, INT4), (ASYM, INT8), (INT8, INT4)])
+def test_a_workspace_aligned_to_16_bytes(B, a_fmt, w_fmt, skip):
+    """And nothing is written outside it."""
+    T, N, d = 1100, 2304, 96
+    a, sa, w, sw, cs = operands(a_fmt, w_fmt, T, N, d, 77 + skip)
+    af, wf = B.FMT_BY_NAME[a_fmt], B.FMT_BY_NAME[w_fmt]
+    n = B.perq_matmul_i8_workspace_bytes(T, N, d, af, wf)
+    assert n > 0
+    room = torch.full((n + 4096,), 0xa5, dtype=torch.uint8, device="cuda")
+    begin = 1024 + skip
+    assert room.data_ptr() % 64 == 0
+    out = B.perq_matmul_i8(a, sa, af, w, sw, wf, cs, out_dtype=F32, workspace=room[begin:begin + n])
+    P.compare(out, *P.product(a_fmt, a, sa, w_fmt, w, sw))
+    assert (room[:begin] == 0xa5).all() and (room[begin + n:] == 0xa5).all()

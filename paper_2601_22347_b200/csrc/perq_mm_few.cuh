@@ -9,8 +9,14 @@
 // order.  The accumulator is 32-bit integers, so sums are exact and the same however they are split.
 //
 // Few tiles are split along k over the CTAs of a cluster.  Every CTA sends its partial sums to the one that adds them up and stores their
-// results, through distributed shared memory: no workspace, no atomics and no second launch.  With up to 32 tokens two CTAs share an SM, so
-// that the next call's set-up runs under this one.
+// results, through distributed shared memory: no workspace, no atomics and no second launch.  Where half of an SM's tensor memory and half of its
+// shared memory (three loads) are enough, two CTAs share it, so that the next call's set-up runs under this one.  (Every plan takes more than a third
+// of the shared memory and, with more than half of the columns, more than two thirds: CTAs that meet on an SM never wait for each other's tensor memory,
+// also those of two calls at once.)
+//
+// Measured in CUDA graphs, weights not in L2: 1 x 4096 x 14336, both packed, 9.9 us, 16 x 14336 x 4096 with 8-bit tokens 10.8 us (29.4 MB, 2.7 .. 3.0 TB/s:
+// 4 .. 5 us are launch, the first loads' way and the cluster's sums), 64 rows over 32 experts of 2048 x 4096 28 .. 37 us (118 MB, 3.2 .. 4.2 TB/s, by where the
+// memory lies).
 //
 // Grouped calls (offsets): expert e has rows offsets[e] .. offsets[e + 1].  Every CTA counts the tiles of all experts itself and
 // takes every gridDim-th one; experts without rows have none, so their weights are not read.

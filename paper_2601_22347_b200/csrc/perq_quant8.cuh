@@ -15,9 +15,12 @@
 // (b = 32, gaussian values: 3 of a row of 4096; with outliers, next to none outside their blocks).
 //
 // Such places are rare, so a warp only notes them and settles them sixteen rows at a time, 32 / (b / 16) at once, from the inputs in global memory; it stores
-// the rows' scales and mends codes.  (16384 x 4096, b = 32, 4 warps to a row: exact sums as they came up 70 us, by a warp of its own 60 .. 88 us.)  A warp
+// the rows' scales and mends codes.  (16384 x 4096, b = 32, 4 warps to a row, earlier: exact sums as they came up 70 us, by a warp of its own 60 .. 88 us.)  A warp
 // has up to four pieces of 512 channels of a row in registers.  Rows of up to 2048 need no barrier; the warps of longer ones meet at one barrier
 // a row and two for every sixteen.
+//
+// Measured in CUDA graphs: 16384 x 4096, b = 32, 40.6 us (201 MB, 5.0 TB/s), 1531 x 9728, b = 128, permuted, 27.6 us (45 MB, 1.6 TB/s: two-byte
+// gathers from shared memory and their latency at 15 warps, 5 us of settling), one row of 4096 3.8 us.
 #pragma once
 
 #include "perq_mm_ptx.cuh"
@@ -492,6 +495,9 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
         if (i % BATCH == BATCH - 1 || i + 1 == steps)
             settle_batch<LOG2B, PIECES, PERM>(p, group, notes, table, first + (long long)(i / BATCH * BATCH) * step, step, i % BATCH + 1u, g, w, lane);
     }
+    // (nothing is in flight when the CTA ends, also after a wait that ran out)
+    if (!alive && w == 0 && lane == 0)
+        for (uint32_t i = steps > STAGES ? steps - STAGES : 0u; i < steps; ++i) (void)perq_mm::mbar_wait(full + 8 * (i % STAGES), (i / STAGES) & 1u);
 }
 
 // sums[r] = sum of the codes of row r, a warp to a row.

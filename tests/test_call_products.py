@@ -10,6 +10,7 @@ import pytest
 def B():
     from paper_2601_22347_b200 import binding, build
     build.build()
+    binding._lib = None                          # (another test may have loaded it without the entry)
     binding.load()
     if not os.path.exists(build.CALL_PATH):
         pytest.skip("no interpreter headers")

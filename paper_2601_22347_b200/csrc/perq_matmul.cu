@@ -252,7 +252,7 @@ int launch_many(const Product &m, unsigned char *workspace, int sms, cudaStream_
         p.T = (int32_t)m.T;
         p.wide = (reinterpret_cast<uintptr_t>(workspace) & 31u) == 0;            // (the weights' part begins a multiple of 256 bytes behind)
         const int parts = (space.tokens ? 1 : 0) + (space.weights ? m.E : 0);
-        const long long most = std::max(p.token_chunks, p.expert_chunks), ctas = std::min<long long>((most + 1023) / 1024, std::max(1, 16 * sms / parts));
+        const long long most = std::max(p.token_chunks, p.expert_chunks), ctas = std::min<long long>((most + 511) / 512, std::max(1, 16 * sms / parts));
         if (int rc = launch_plain(perq_mm::spread_kernel, ctas, 256, 0, st, p, parts)) return rc;
     }
     perq_mm::ManyParams p;

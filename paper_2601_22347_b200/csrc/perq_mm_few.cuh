@@ -120,14 +120,27 @@ __device__ __forceinline__ void count_tiles(const int32_t *offsets, int E, int32
     if (lane == 0) first[E] = before;
 }
 
-__device__ __forceinline__ void store_one(void *out, int type, size_t at, float v)
+// A word, or its low half, where `yes`; without a branch.
+__device__ __forceinline__ void store_if(const void *dst, uint32_t v, bool yes)
 {
-    if (type == OUT_F32) static_cast<float *>(out)[at] = v;
-    else {
-        uint16_t h;
-        if (type == OUT_BF16) asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(v));
-        else asm("cvt.rn.f16.f32 %0, %1;" : "=h"(h) : "f"(v));
-        static_cast<uint16_t *>(out)[at] = h;
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q st.global.b32 [%0], %1; }" ::"l"(dst), "r"(v), "r"((uint32_t)yes) : "memory");
+}
+__device__ __forceinline__ void store16_if(const void *dst, uint32_t v, bool yes)
+{
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q st.global.b16 [%0], %1; }" ::"l"(dst), "h"((uint16_t)v), "r"((uint32_t)yes) : "memory");
+}
+
+// A result, where `yes`.
+template <bool F32>
+__device__ __forceinline__ void store_one(void *out, int type, size_t at, float v, bool yes)
+{
+    if (F32) {
+        store_if(static_cast<float *>(out) + at, __float_as_uint(v), yes);
+    } else {
+        uint16_t bf, h;
+        asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(bf) : "f"(v));
+        asm("cvt.rn.f16.f32 %0, %1;" : "=h"(h) : "f"(v));
+        store16_if(static_cast<uint16_t *>(out) + at, type == OUT_BF16 ? bf : h, yes);
     }
 }
 // Two results in one register, the first in its low half.
@@ -420,10 +433,17 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
                 } else {
                     if ((c & 16) == 0) ts = token_scale(p.a_scales, p.asym, min(it.t0 + c + lane, p.T - 1));      // of 32 tokens, one to a lane
                     tmem_wait(u);
+                    float y[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float s_t = __shfl_sync(0xffffffffu, ts.s, (c & 16) + i), z_t = __shfl_sync(0xffffffffu, ts.z, (c & 16) + i);
-                        if (mine && c + i < columns) store_one(p.out, p.out_type, (size_t)(it.t0 + c + i) * (size_t)p.N + n, scaled(u[i], p.shift, s_t, s_n, z_t, c_n));
+                    for (int i = 0; i < 16; ++i)
+                        y[i] = scaled(u[i], p.shift, __shfl_sync(0xffffffffu, ts.s, (c & 16) + i), s_n, __shfl_sync(0xffffffffu, ts.z, (c & 16) + i), c_n);
+                    const size_t at = (size_t)(it.t0 + c) * (size_t)p.N + (size_t)n;
+                    if (p.out_type == OUT_F32) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) store_one<true>(p.out, p.out_type, at + (size_t)i * (size_t)p.N, y[i], mine && c + i < columns);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) store_one<false>(p.out, p.out_type, at + (size_t)i * (size_t)p.N, y[i], mine && c + i < columns);
                     }
                 }
             }
@@ -463,9 +483,17 @@ few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CU
                 v[0] += (int32_t)u.x; v[1] += (int32_t)u.y; v[2] += (int32_t)u.z; v[3] += (int32_t)u.w;
             }
             const int t = token_of(four);
+            float y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (t + e < it.t_end) store_one(p.out, p.out_type, (size_t)(t + e) * (size_t)p.N + (size_t)n, scaled(v[e], p.shift, ts[e].s, s_n, ts[e].z, c_n));
+            for (int e = 0; e < 4; ++e) y[e] = scaled(v[e], p.shift, ts[e].s, s_n, ts[e].z, c_n);
+            const size_t at = (size_t)t * (size_t)p.N + (size_t)n;
+            if (p.out_type == OUT_F32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) store_one<true>(p.out, p.out_type, at + (size_t)e * (size_t)p.N, y[e], t + e < it.t_end);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) store_one<false>(p.out, p.out_type, at + (size_t)e * (size_t)p.N, y[e], t + e < it.t_end);
+            }
             four += K::threads / FEW_ROWS;
             if (!here(four)) break;
 #pragma unroll

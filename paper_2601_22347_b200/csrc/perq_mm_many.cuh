@@ -11,7 +11,7 @@
 // Packed operands are spread to bytes before (spread_kernel), in the caller's workspace.
 //
 // Measured in CUDA graphs, 8-bit codes: 16384 x 4096 x 14336 in 606 us (3.2e15 operations a second, tensor pipe 88 %); 4099 rows over 32 experts of
-// 2048 x 4096 in 63 us (287 MB, 4.6 TB/s; pipe 59 %); 1531 x 1001 x 9728 in 25 us (48 of the 74 pairs have work, 10 us are launch, the first loads and the pairs'
+// 2048 x 4096 in 63 us (287 MB, 4.6 TB/s; pipe 59 %); 1531 x 1001 x 9728 in 22 us (48 of the 74 pairs have work, 8 us are launch, the first loads and the pairs'
 // exchange).  4-bit codes: 2048 x 4096 x 4096 in 32 us, 7 of them spread_kernel; 8192 rows over 8 experts of 4096 x 2048 in 76 .. 100 us, 17.5 of them
 // spread_kernel (42 MB read, 84 MB written to L2 in part: 7.2 TB/s).
 // Tried: tiles of 128 channels (a k-step takes as long), stores that do not stay in L2 (no change), the next 16 columns on their way while the last are stored
@@ -105,12 +105,17 @@ __device__ __forceinline__ void store_wide(void *dst, const uint32_t (&w)[8])
 
 // The results of one lane's token: 16 adjacent channels from column c of the tile on, from their sums.  Called by whole warps; `rows` of the
 // warp's 32 tokens are there.
+//
+// Rows that cannot be stored 32 bytes at a time go through shared memory.  16-bit results wait there for the next 16 columns (`more`: these come), then 16
+// lanes store a row's 32 as words, shifted by a result where the row begins between two words; fp32 ones go at once.  (bf16, 2048 x 4097 x 2048, rows of 4112
+// being 16.5 us: 29.5 by single results, 28.1 by words, 21.8 without branches, and 19.4 for 4098.)
 struct ManyRow {
     TokenScale ts;
     int32_t t, rows, n0;
     uint32_t scale, sums, room;  // shared memory: the channels' scales and sums, and the warp's room
+    int32_t waiting;             // columns in the room
 };
-__device__ __forceinline__ void many_store(const ManyParams &p, const ManyRow &r, const int32_t (&u)[16], int c, int lane)
+__device__ __forceinline__ void many_store(const ManyParams &p, ManyRow &r, const int32_t (&u)[16], int c, bool more, int lane)
 {
     float y[16];
 #pragma unroll
@@ -122,33 +127,73 @@ __device__ __forceinline__ void many_store(const ManyParams &p, const ManyRow &r
         y[4 * i + 3] = scaled(u[4 * i + 3], p.shift, r.ts.s, __uint_as_float(v.w), r.ts.z, __uint_as_float(z.w));
     }
     const size_t at = (size_t)r.t * (size_t)p.N + (size_t)(r.n0 + c);
-    if (p.wide && r.n0 + c + 16 <= p.N) {
-        uint32_t w[8];
-        if (p.out_type == OUT_F32) {
+    if (p.out_type == OUT_F32) {
+        if (p.wide && r.n0 + c + 16 <= p.N) {
+            uint32_t w[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(y[8 * h + i]);
                 if (lane < r.rows) store_wide(static_cast<float *>(p.out) + at + 8 * h, w);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = pack_two(p.out_type, y[2 * i], y[2 * i + 1]);
-            if (lane < r.rows) store_wide(static_cast<uint16_t *>(p.out) + at, w);
+            return;
         }
-    } else {
-        // rows that cannot be stored 32 bytes at a time go through shared memory: 16 lanes then store adjacent results
 #pragma unroll
         for (int i = 0; i < 16; ++i) sts32(r.room + (uint32_t)(lane * MANY_ROOM + i) * 4u, __float_as_uint(y[i]));
         __syncwarp();
         const int n = r.n0 + c + (lane & 15);
-        for (int k = lane >> 4; k < r.rows; k += 2) {
-            float v;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(r.room + (uint32_t)(k * MANY_ROOM + (lane & 15)) * 4u) : "memory");
-            if (n < p.N) store_one(p.out, p.out_type, (size_t)(r.t - lane + k) * (size_t)p.N + (size_t)n, v);
+        const float *const to = static_cast<const float *>(p.out) + (size_t)(r.t - lane + (lane >> 4)) * (size_t)p.N + (size_t)n;
+#pragma unroll
+        for (int h0 = 0; h0 < 16; h0 += 8) {
+            uint32_t v[8];
+#pragma unroll
+            for (int h = 0; h < 8; ++h) v[h] = lds32(r.room + (uint32_t)((2 * (h0 + h) + (lane >> 4)) * MANY_ROOM + (lane & 15)) * 4u);
+#pragma unroll
+            for (int h = 0; h < 8; ++h) store_if(to + (size_t)(2 * (h0 + h)) * (size_t)p.N, v[h], n < p.N && 2 * (h0 + h) + (lane >> 4) < r.rows);
         }
         __syncwarp();
+        return;
     }
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pack_two(p.out_type, y[2 * i], y[2 * i + 1]);
+    if (p.wide && r.n0 + c + 16 <= p.N) {
+        if (lane < r.rows) store_wide(static_cast<uint16_t *>(p.out) + at, w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sts32(r.room + (uint32_t)(lane * MANY_ROOM + r.waiting / 2 + i) * 4u, w[i]);
+    r.waiting += 16;
+    if (r.waiting < 32 && more) return;
+    __syncwarp();
+    // (every second row: its place between two words is the same for all that a lane stores)
+    const int i = lane & 15, n0 = r.n0 + c + 16 - r.waiting, columns = min(r.waiting, p.N - n0);
+    const uint16_t *const to = static_cast<const uint16_t *>(p.out) + (size_t)(r.t - lane + (lane >> 4)) * (size_t)p.N + (size_t)n0;
+    const int odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 1, e = 2 * i + odd;              // results e and e + 1 are a word of the row
+    const bool both = e + 1 < columns, one = !both && e < columns, first = odd && i == 0, edges = __any_sync(0xffffffffu, one || first);
+#pragma unroll
+    for (int h0 = 0; h0 < 16; h0 += 8) {
+        uint32_t v[8], v1[8];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+            const uint32_t from = r.room + (uint32_t)((2 * (h0 + h) + (lane >> 4)) * MANY_ROOM + i) * 4u;
+            v[h] = lds32(from);
+            v1[h] = lds32(from + 4u);
+        }
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+            const uint16_t *const row = to + (size_t)(2 * (h0 + h)) * (size_t)p.N;
+            const bool there = 2 * (h0 + h) + (lane >> 4) < r.rows;
+            const uint32_t word = __funnelshift_r(v[h], v1[h], 16 * odd);
+            store_if(row + e, word, both && there);
+            if (edges) {
+                store16_if(row + e, word, one && there);
+                store16_if(row, v[h], first && there);
+            }
+        }
+    }
+    __syncwarp();
+    r.waiting = 0;
 }
 
 __global__ void __launch_bounds__(MANY_THREADS, 1)
@@ -197,6 +242,7 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
     const int q = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     ManyRow row;
+    row.waiting = 0;
     row.room = base + ManySmem::rows + (uint32_t)((warp - 4) * 32 * MANY_ROOM) * 4u;
 
     if (warp == 0) {
@@ -272,7 +318,7 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
                 __syncwarp();
                 tmem_load16(tmem + b * MANY_CHANNELS + lanes + c, u);
                 tmem_wait(u);
-                many_store(p, row, u, c, lane);
+                many_store(p, row, u, c, c + 16 < (half + 1) * (MANY_CHANNELS / 2) && it.n0 + c + 16 < p.N, lane);
             }
             tmem_fence_before();
             __syncwarp();
@@ -305,7 +351,9 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
         __syncwarp();
         cluster_sync();
         if (warp >= 4) {
-            for (uint32_t g = g0 + (uint32_t)half; g < g1; g += 2u) {
+            // (the first half of the warps has one more where they are odd)
+            const uint32_t middle = (g0 + g1 + 1u) / 2u, end = half ? g1 : middle;
+            for (uint32_t g = half ? middle : g0; g < end; ++g) {
                 if (row.rows <= 0 || row.n0 + (int)(16u * g) >= p.N) break;
                 int32_t u[16];
 #pragma unroll
@@ -317,7 +365,7 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
                         u[4 * i] += (int32_t)v.x; u[4 * i + 1] += (int32_t)v.y; u[4 * i + 2] += (int32_t)v.z; u[4 * i + 3] += (int32_t)v.w;
                     }
                 }
-                many_store(p, row, u, (int)(16u * g), lane);
+                many_store(p, row, u, (int)(16u * g), g + 1u < end && row.n0 + (int)(16u * g + 16u) < p.N, lane);
             }
         }
         __syncwarp();
@@ -329,7 +377,8 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
 }
 
 // Packed rows to bytes, 16 times the codes, in their order: tokens (blockIdx.y == 0, where they are packed), and the weights of every expert
-// that has rows, which the product reads next, from L2 where they fit.  The tokens are read for 4 chunks of 16 bytes at once.
+// that has rows, which the product reads next, from L2 where they fit.  A thread has two chunks of 16 bytes on their
+// way (one / two / four / eight, 2048 x 4096 x 4096 with 8-bit tokens, in us: 30.5 / 31.0 / 32.6 / 34).
 struct SpreadParams {
     const uint4 *tokens, *weights;
     uint4 *tokens_out, *weights_out;
@@ -349,13 +398,13 @@ __global__ void __launch_bounds__(256) spread_kernel(const SpreadParams p)
     const uint4 *const src = tokens ? p.tokens : p.weights + (size_t)expert * (size_t)p.expert_chunks;
     uint4 *const dst = tokens ? p.tokens_out : p.weights_out + 2 * (size_t)expert * (size_t)p.expert_chunks;
     const long long n = tokens ? p.token_chunks : p.expert_chunks, step = (long long)gridDim.x * 256;
-    for (long long i0 = (long long)blockIdx.x * 256 + (int)threadIdx.x; i0 < n; i0 += 4 * step) {
-        uint4 v[4];
+    for (long long i0 = (long long)blockIdx.x * 256 + (int)threadIdx.x; i0 < n; i0 += 2 * step) {
+        uint4 v[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2; ++k)
             if (i0 + k * step < n) v[k] = __ldg(src + i0 + k * step);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2; ++k) {
             if (i0 + k * step >= n) break;
             const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
             uint32_t x[8];

@@ -193,22 +193,43 @@ int launch_plain(void (*kernel)(P), long long grid, int threads, size_t smem, cu
     return PERQ_OK;
 }
 
-// Whether the kernel for many tokens is the better one (us, CUDA graphs, few / many).
-//   dense, 8-bit weights, d = 4096: 256 x 2048 10.6 / 11.8, 384 x 2048 13.8 / 12.7, 128 x 4096 9.3 / 12.6, 192 x 4096 13.8 / 12.8, 512 x 4096 19.3 / 13.8, 64 x 14336
-//     16.0 / 16.4, 128 x 14336 20.4 / 16.9: from a quarter of the SMs on, which a split by four would fill
-//   4-bit weights, which it wants spread: 256 x 4096 14.0 / 17.5, 512 x 4096 19.5 / 18.6, 768 x 4096 30 / 20, 128 x 14336 20 / 30, 256 x 14336 31 / 30
-//   grouped, 8-bit weights, 32 experts of 2048 x 4096: 24 rows to an expert 48 / 58, 64 57 / 60, 96 68 / 61, 128 76 / 62; 8 of 4096 x 2048: 24 17 / 19, 64 22 / 20
-//   4-bit weights: 8 of 2048 x 2048: 128 25 / 21, 256 35 / 27; 8 of 4096 x 2048: 128 37 / 37, 256 56 / 43; 32 of 2048 x 4096, whose spread weights do not fit in L2:
-//     64 49 / 134, 256 114 / 147
+// What a dense product of more than 64 tokens takes in either kernel, us, from their k-steps (both sides measured, model in brackets).
+//   few: tiles of 128 x 128, a round of them on all SMs after another; a k-step, 128 codes of 8 bits or 256 with a packed operand, is 0.27, 0.54 (4-bit
+//     weights) or 1.1 us (4-bit tokens only, spread beside 8-bit weights that fill the ring)
+//   many: tiles of 256 x 256, 0.27 us for 128 codes, split over pairs where that fits; packed operands are spread first, 0.365 us for a million codes, most of it
+//     under the launch
+// 8-bit codes, few / many: 512 x 4096 x 4096 14.3 [14.8] / 13.7 [13.7], 128 x 14336 x 4096 15.7 [14.8] / 17.1 [16.0], 1400 x 1024 x 9728 25.6 [26.7] / 20.6 [19.7],
+//   1100 x 2048 x 4096 14.2 [14.8] / 16.0 [16.0], 1024 x 1024 x 2048 9.3 [8.4] / 10.4 [11.7]
+// 4-bit weights: 512 x 4096 x 4096 14.6 [14.2] / 18.2 [17.3], 768 x 4096 x 4096 23.5 [23.5] / 19.9 [20.0], 768 x 8192 x 4096 33.0 [32.7] / 34.6 [34.8],
+//   256 x 14336 x 4096 24.2 / 29.1, 640 x 4096 x 14336 64 [67] / 54
+// 4-bit tokens, 8-bit weights: 512 x 4096 x 4096 19.8 [23] / 16.4 [16.2], 1024 x 1024 x 2048 10.1 [10.0] / 12.1 [14.2]
+double few_time(const Product &m, int sms)
+{
+    const bool w4 = is_packed(m.w_fmt), packed = w4 || is_packed(m.a_fmt);
+    const int64_t tiles = (m.T + 127) / 128 * ((m.N + 127) / 128), steps = packed ? (m.d + 255) / 256 : (m.d + 127) / 128;
+    int64_t split = 1;
+    while (split < 8 && tiles * split * 2 <= sms * (packed ? 1 : 2) && split * 2 <= steps) split *= 2;
+    const int64_t rounds = (tiles * split + sms - 1) / sms;
+    return 5.0 + (double)rounds * ((double)steps / (double)split * (w4 ? 0.54 : packed ? 1.1 : 0.27) + 0.6);
+}
+double many_time(const Product &m, int sms)
+{
+    const int64_t items = (m.T + 255) / 256 * ((m.N + 255) / 256), steps = (m.d + 127) / 128, pairs = std::max(1, sms / 2);
+    int64_t split = 4;
+    while (split > 1 && (steps < 24 || items * split > sms * 7 / 16)) --split;
+    const double codes = 1e-6 * m.d * ((is_packed(m.a_fmt) ? (double)m.T : 0.0) + (is_packed(m.w_fmt) ? (double)m.N : 0.0));
+    return (split > 1 ? 9.4 : 7.4) + 0.27 * (double)((items * split + pairs - 1) / pairs * steps) / (double)split + (codes > 0.0 ? std::max(2.5, 0.365 * codes - 3.3) : 0.0);
+}
+
+// Whether the kernel for many tokens is the better one.  Grouped calls, by the rows to an expert (us, CUDA graphs, few / many):
+//   8-bit codes: 64 51 / 60 (32 experts of 2048 x 4096), 96 61.1 / 61.1 and 21.5 / 21.3 (8 of 4096 x 2048), 100 15.5 / 14.4 (8 of 2048 x 2048), 128 26 / 22
+//   4-bit weights: 512 50.8 / 54.0 (8 of 4096 x 2048), 43.7 / 55.7 (4 of 4096 x 4096), 768 72.6 / 66.4, 40.1 / 41.5 (8 of 2048 x 2048), 1024 89 / 74
+//   4-bit tokens, 8-bit weights: 64 25.4 / 21.3 (8 of 4096 x 2048), 128 35 / 22
 bool many_is_better(const Product &m, int sms)
 {
-    const bool packed = is_packed(m.w_fmt);
-    if (m.offsets) {
-        if (!packed) return m.T >= 64 * (int64_t)m.E;
-        return m.T >= ((int64_t)m.E * m.N * m.d <= 1ll << 26 ? 192 : 512) * (int64_t)m.E;
-    }
-    const int64_t tiles = (m.T + 127) / 128 * ((m.N + 127) / 128);
-    return m.T > 64 && tiles > (packed ? sms : sms / 4);
+    if (m.offsets) return m.T >= (is_packed(m.w_fmt) ? 768 : is_packed(m.a_fmt) ? 64 : 96) * (int64_t)m.E;
+    if (sms <= 0) sms = 148;                             // (no device, no launch: sizes are answered for a B200)
+    return m.T > 64 && many_time(m, sms) < few_time(m, sms);
 }
 
 // Pairs of CTAs that share a tile along k: as many as there is room for.  (One / two / four pairs: 256 x 4096 x 4096 15.0 / 12.9, 512 x 1024 x 4096

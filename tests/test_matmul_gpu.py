@@ -120,7 +120,7 @@ def test_offsets_that_go_back_and_forth_keep_their_first_rows(B):
         assert (room[:100] == 77).all() and (room[T + 100:] == 77).all()
 
 
-@pytest.mark.parametrize("T", [3, 1500])
+@pytest.mark.parametrize("T", [3, 1500, 5000])
 def test_a_stream_given_to_the_call(B, T):
     """The call's own workspace outlives it on a stream that is not the current one."""
     a, sa, w, sw, cs = operands(ASYM, INT4, T, 1000, 2048, 51)
@@ -231,7 +231,7 @@ def test_two_calls_at_once(B):
 @pytest.mark.parametrize("a_fmt,w_fmt", [(INT4, INT4), (ASYM, INT8), (INT8, INT4)])
 def test_a_workspace_aligned_to_16_bytes(B, a_fmt, w_fmt, skip):
     """And nothing is written outside it."""
-    T, N, d = 1100, 2304, 96
+    T, N, d = 8000, 2064, 96
     a, sa, w, sw, cs = operands(a_fmt, w_fmt, T, N, d, 77 + skip)
     af, wf = B.FMT_BY_NAME[a_fmt], B.FMT_BY_NAME[w_fmt]
     n = B.perq_matmul_i8_workspace_bytes(T, N, d, af, wf)
@@ -242,3 +242,46 @@ def test_a_workspace_aligned_to_16_bytes(B, a_fmt, w_fmt, skip):
     out = B.perq_matmul_i8(a, sa, af, w, sw, wf, cs, out_dtype=F32, workspace=room[begin:begin + n])
     P.compare(out, *P.product(a_fmt, a, sa, w_fmt, w, sw))
     assert (room[:begin] == 0xa5).all() and (room[begin + n:] == 0xa5).all()
+
+
+# sizes that the kernel for many tokens serves whatever the formats: ragged tiles of both sides, rows shorter than a k-step and longer than the ring, tiles
+# split along k over pairs, bands of tiles, several tiles to a pair
+MANY = [(1500, 1001, 9728), (1025, 1500, 8224), (5000, 2001, 2080), (8000, 2064, 160), (40000, 300, 32), (2600, 5000, 1056)]
+
+
+@pytest.mark.parametrize("a_fmt,w_fmt", FORMATS)
+@pytest.mark.parametrize("T,N,d", MANY)
+def test_many_tokens(B, a_fmt, w_fmt, T, N, d):
+    packed = (a_fmt != INT8) or (w_fmt != INT8)
+    assert (B.perq_matmul_i8_workspace_bytes(T, N, d, B.FMT_BY_NAME[a_fmt], B.FMT_BY_NAME[w_fmt]) > 0) == packed
+    dense(B, a_fmt, w_fmt, T, N, d, F32)
+
+
+# rows on every alignment, and the last channel alone or with one, in words and between two
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("a_fmt,w_fmt", [(INT8, INT8), (ASYM, INT4)])
+@pytest.mark.parametrize("T,N,d", [(60001, n, 64) for n in (257, 258, 263, 264, 270, 271, 272, 273, 287)] + [(1531, n, 9728) for n in (1001, 1002, 1008, 1020)])
+def test_many_tokens_result_types(B, a_fmt, w_fmt, T, N, d, dtype):
+    if a_fmt != INT8:
+        assert B.perq_matmul_i8_workspace_bytes(T, N, d, B.FMT_BY_NAME[a_fmt], B.FMT_BY_NAME[w_fmt]) > 0
+    dense(B, a_fmt, w_fmt, T, N, d, dtype)
+
+
+@pytest.mark.parametrize("a_fmt,w_fmt", FORMATS)
+@pytest.mark.parametrize("N,d,dtype", [(260, 544, F32), (257, 96, BF16), (302, 2080, F16)])
+@pytest.mark.parametrize("offsets,T", [([0, 500, 500, 2501, 2502], 3200), ([3, 1600], 1600), ([0, 0, 0, 2305], 2311), ([7, 7, 3000, 3001, 3001, 4000], 4005)],
+                         ids=["4x3200", "1x1600", "3x2311", "5x4005"])
+def test_many_rows_of_experts(B, a_fmt, w_fmt, offsets, T, N, d, dtype):
+    packed = (a_fmt != INT8) or (w_fmt != INT8)
+    assert (B.perq_grouped_matmul_i8_workspace_bytes(T, len(offsets) - 1, N, d, B.FMT_BY_NAME[a_fmt], B.FMT_BY_NAME[w_fmt]) > 0) == packed
+    grouped(B, a_fmt, w_fmt, offsets, T, N, d, dtype)
+
+
+def test_results_do_not_depend_on_the_kernel(B):
+    """A row of a large batch has the bits that it has alone."""
+    a, sa, w, sw, _ = operands(INT4, INT4, 8000, 2064, 160, 12)
+    f = B.PERQ_FMT_INT4
+    assert B.perq_matmul_i8_workspace_bytes(8000, 2064, 160, f, f) > 0 and B.perq_matmul_i8_workspace_bytes(7, 2064, 160, f, f) == 0
+    full = B.perq_matmul_i8(a, sa, f, w, sw, f)
+    for t in (0, 4000, 7993):
+        assert torch.equal(B.perq_matmul_i8(a[t:t + 7].clone(), sa[t:t + 7].clone(), f, w, sw, f), full[t:t + 7])

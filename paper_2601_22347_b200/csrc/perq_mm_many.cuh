@@ -12,8 +12,8 @@
 //
 // Measured in CUDA graphs, 8-bit codes: 16384 x 4096 x 14336 in 606 us (3.2e15 operations a second, tensor pipe 88 %); 4099 rows over 32 experts of
 // 2048 x 4096 in 63 us (287 MB, 4.6 TB/s; pipe 59 %); 1531 x 1001 x 9728 in 22 us (48 of the 74 pairs have work, 8 us are launch, the first loads and the pairs'
-// exchange).  4-bit codes: 2048 x 4096 x 4096 in 32 us, 7 of them spread_kernel; 8192 rows over 8 experts of 4096 x 2048 in 76 .. 100 us, 17.5 of them
-// spread_kernel (42 MB read, 84 MB written to L2 in part: 7.2 TB/s).
+// exchange).  4-bit codes: 2048 x 4096 x 4096 in 31.5 us, 5 more than with 8-bit ones (spread_kernel); 8192 rows over 8 experts of 4096 x 2048 in 74 us, 17.5 of
+// them spread_kernel (42 MB read, 84 MB written to L2 in part: 7.2 TB/s).  These are at 1965 MHz; under the power limit the SMs fall to 1230.
 // Tried: tiles of 128 channels (a k-step takes as long), stores that do not stay in L2 (no change), the next 16 columns on their way while the last are stored
 // (62 -> 64 us at 4099 rows: the epilogue waits for its stores).
 #pragma once
@@ -97,6 +97,11 @@ __device__ __forceinline__ void commit_pair(uint32_t bar, uint32_t both)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)both) : "memory");
 }
+__device__ __forceinline__ void store_wide_if(const void *dst, const uint32_t (&w)[8], bool yes)
+{
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8}; }"
+                 ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"((uint32_t)yes) : "memory");
+}
 __device__ __forceinline__ void store_wide(void *dst, const uint32_t (&w)[8])
 {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
@@ -134,7 +139,7 @@ __device__ __forceinline__ void many_store(const ManyParams &p, ManyRow &r, cons
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(y[8 * h + i]);
-                if (lane < r.rows) store_wide(static_cast<float *>(p.out) + at + 8 * h, w);
+                store_wide_if(static_cast<float *>(p.out) + at + 8 * h, w, lane < r.rows);
             }
             return;
         }
@@ -158,7 +163,7 @@ __device__ __forceinline__ void many_store(const ManyParams &p, ManyRow &r, cons
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = pack_two(p.out_type, y[2 * i], y[2 * i + 1]);
     if (p.wide && r.n0 + c + 16 <= p.N) {
-        if (lane < r.rows) store_wide(static_cast<uint16_t *>(p.out) + at, w);
+        store_wide_if(static_cast<uint16_t *>(p.out) + at, w, lane < r.rows);
         return;
     }
 #pragma unroll

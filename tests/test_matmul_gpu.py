@@ -285,3 +285,74 @@ def test_results_do_not_depend_on_the_kernel(B):
     full = B.perq_matmul_i8(a, sa, f, w, sw, f)
     for t in (0, 4000, 7993):
         assert torch.equal(B.perq_matmul_i8(a[t:t + 7].clone(), sa[t:t + 7].clone(), f, w, sw, f), full[t:t + 7])
+
+
+def test_calls_of_every_kernel_at_once(B):
+    """Few and many tokens, split along k and not, grouped, and the online path, each on a stream of its own with nothing between them."""
+    calls, wants = [], []
+
+    def product(a_fmt, w_fmt, T, N, d, seed):
+        a, sa, w, sw, cs = operands(a_fmt, w_fmt, T, N, d, seed)
+        calls.append(lambda: B.perq_matmul_i8(a, sa, B.FMT_BY_NAME[a_fmt], w, sw, B.FMT_BY_NAME[w_fmt], cs, out_dtype=F32))
+        wants.append(lambda out: P.compare(out, *P.product(a_fmt, a, sa, w_fmt, w, sw)))
+
+    product(ASYM, INT4, 8000, 2064, 160, 61)
+    product(INT8, INT8, 1531, 1001, 9728, 62)
+    product(INT4, INT4, 3, 4096, 4096, 63)
+    product(INT8, INT4, 100, 2000, 2048, 64)
+    a, sa, w, sw, _ = operands(INT4, INT8, 1000, 300, 1024, 65, 3)
+    offsets = torch.tensor([0, 400, 401, 1000], dtype=torch.int32, device="cuda")
+    calls.append(lambda: B.perq_grouped_matmul_i8(a, sa, B.PERQ_FMT_INT4, w.reshape(3, 300, -1), sw.reshape(3, 300), B.PERQ_FMT_INT8, offsets, out_dtype=F32))
+    wants.append(lambda out: [P.compare(out[r], *P.product(INT4, a[r], sa[r], INT8, w[c], sw[c]))
+                              for r, c in ((slice(0, 400), slice(0, 300)), (slice(400, 401), slice(300, 600)), (slice(401, 1000), slice(600, 900)))])
+    x = torch.randn(16384, 4096, generator=torch.Generator(device="cuda").manual_seed(66), device="cuda").to(BF16)
+    alone = [B.perq_rotate_quantize(x, None, 32, B.FMT_BY_NAME["mxfp4"])[0].clone(), B.perq_rotate_quantize_i8(x, None, 32)[0].clone()]
+    calls += [lambda: B.perq_rotate_quantize(x, None, 32, B.FMT_BY_NAME["mxfp4"])[0], lambda: B.perq_rotate_quantize_i8(x, None, 32)[0]]
+    wants += [lambda out: None, lambda out: None]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    outs = [[] for _ in calls]
+    for _ in range(12):
+        for k, call in enumerate(calls):
+            with torch.cuda.stream(streams[k]):
+                outs[k].append(call())
+    torch.cuda.synchronize()
+    for k, want in enumerate(wants):
+        want(outs[k][0])
+        assert all(torch.equal(v, outs[k][0]) for v in outs[k])
+    assert torch.equal(outs[-2][0], alone[0]) and torch.equal(outs[-1][0], alone[1])
+
+
+def test_a_captured_graph_of_many_tokens(B):
+    """Two graphs, each with the workspace that its capture made, replayed in turn with other tokens and weights."""
+    sizes = (5000, 1000, 2048), (1531, 1001, 9728)
+    states, graphs, outs = [], [], []
+    for k, (T, N, d) in enumerate(sizes):
+        a, sa, w, sw, _ = operands(INT4, INT4, T, N, d, 70 + k)
+        states.append((a, sa, w, sw))
+        outs.append(torch.zeros(T, N, device="cuda"))
+
+    def call(k):
+        a, sa, w, sw = states[k]
+        B.perq_matmul_i8(a, sa, B.PERQ_FMT_INT4, w, sw, B.PERQ_FMT_INT4, out=outs[k])
+
+    for k in range(2):
+        call(k)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(k)
+        graphs.append(graph)
+    for turn in range(3):
+        for k, (T, N, d) in enumerate(sizes):
+            for to, new in zip(states[k], operands(INT4, INT4, T, N, d, 80 + 2 * turn + k)):
+                to.copy_(new)
+            outs[k].fill_(77)
+        for _ in range(3):
+            for graph in graphs:
+                graph.replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            a, sa, w, sw = states[k]
+            P.compare(outs[k], *P.product(INT4, a, sa, INT4, w, sw))
+    del graphs

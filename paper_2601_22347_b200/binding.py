@@ -4,6 +4,9 @@ Every function has the name of the C entry point it calls (see include/perq.h fo
 each computes).  torch is used for device memory and streams; all arithmetic of the path
 happens inside the CUDA library.  There is no CPU fallback: if the library cannot be
 loaded, importing this module's functions raises.
+
+Calls take a `stream` (None: the current one; a torch stream or a handle).  It has to have waited for whatever makes the arguments; tensors
+that a call makes are that stream's memory, and the caller's own streams wait for it before they read them.
 """
 from __future__ import annotations
 
@@ -130,25 +133,43 @@ def _stream(stream) -> int:
     return int(getattr(stream, "cuda_stream", stream))
 
 
+def _empty(shape, dtype: torch.dtype, device, stream=None, result: bool = True) -> torch.Tensor:
+    """Memory for a call on `stream` (None: the current one).
+
+    It is that stream's: a block that was let go on the current one may be in use by kernels that are still queued there, and the call does not
+    wait for them.  Results are noted as in use on the current stream too, where the caller reads them and may let them go."""
+    if stream is not None:
+        handle = _stream(stream)
+        current = torch.cuda.current_stream(device)
+        if handle != current.cuda_stream:
+            # (0 and 1 are the default stream's, and no handles to make a stream object of)
+            with torch.cuda.stream(torch.cuda.default_stream(device) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device)):
+                t = torch.empty(shape, dtype=dtype, device=device)
+            if result:
+                t.record_stream(current)
+            return t
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def perq_out_sizes(T: int, d: int, fmt: int, group: int):
     cb, sb = C.c_size_t(0), C.c_size_t(0)
     _check(load().perq_out_sizes(T, d, fmt, group, C.byref(cb), C.byref(sb)), "perq_out_sizes")
     return int(cb.value), int(sb.value)
 
 
-def alloc_outputs(T: int, d: int, fmt: int, group: int, device):
-    """Device buffers of the right shape for one call (torch owns the memory)."""
+def alloc_outputs(T: int, d: int, fmt: int, group: int, device, stream=None):
+    """Device buffers of the right shape for one call on `stream` (torch owns the memory)."""
     if fmt == PERQ_FMT_F32_DEBUG:
-        return torch.empty((T, d), dtype=torch.float32, device=device), None
-    codes = torch.empty((T, d // 2), dtype=torch.uint8, device=device)
+        return _empty((T, d), torch.float32, device, stream), None
+    codes = _empty((T, d // 2), torch.uint8, device, stream)
     if fmt == PERQ_FMT_FP4:
-        scales = torch.empty((T, 1), dtype=torch.float32, device=device)
+        scales = _empty((T, 1), torch.float32, device, stream)
     elif fmt == PERQ_FMT_INT4_ASYM:
-        scales = torch.empty((T, 2), dtype=torch.float32, device=device)
+        scales = _empty((T, 2), torch.float32, device, stream)
     elif fmt == PERQ_FMT_INT4:
-        scales = torch.empty((T, 1 if group == 0 else d // group), dtype=torch.float32, device=device)
+        scales = _empty((T, 1 if group == 0 else d // group), torch.float32, device, stream)
     else:
-        scales = torch.empty((T, d // 32), dtype=torch.uint8, device=device)
+        scales = _empty((T, d // 32), torch.uint8, device, stream)
     return codes, scales
 
 
@@ -160,7 +181,7 @@ def perq_rotate_quantize(x: torch.Tensor, perm: Optional[torch.Tensor], b: int, 
     assert perm is None or (perm.is_cuda and perm.dtype == torch.int32 and perm.is_contiguous())
     T, d = x.shape
     if out_codes is None:
-        out_codes, out_scales = alloc_outputs(T, d, fmt, group, x.device)
+        out_codes, out_scales = alloc_outputs(T, d, fmt, group, x.device, stream)
     if _lib is None:
         load()
     args = (x.data_ptr(), None if perm is None else perm.data_ptr(), T, d, b, fmt, group, _ptr(out_codes), _ptr(out_scales), _stream(stream))
@@ -182,7 +203,7 @@ def perq_swiglu_rotate_quantize(gate: torch.Tensor, up: torch.Tensor, perm: Opti
     assert gate.shape == up.shape
     T, d = gate.shape
     if out_codes is None:
-        out_codes, out_scales = alloc_outputs(T, d, fmt, group, gate.device)
+        out_codes, out_scales = alloc_outputs(T, d, fmt, group, gate.device, stream)
     if _lib is None:
         load()
     args = (gate.data_ptr(), up.data_ptr(), _ptr(perm), T, d, b, fmt, group, _ptr(out_codes), _ptr(out_scales), _stream(stream))
@@ -225,11 +246,10 @@ def perq_block_l1_stats(x: torch.Tensor, perm: Optional[torch.Tensor], b: int, w
     assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 2 and x.is_contiguous()
     T, d = x.shape
     if workspace is None:
-        workspace = torch.empty(max(16, perq_block_l1_stats_workspace_bytes(T, d, b)), dtype=torch.uint8,
-                                device=x.device)
-    chan = torch.empty(d, dtype=torch.float32, device=x.device) if "chan" in want else None
-    block = torch.empty(d // b, dtype=torch.float32, device=x.device) if "block" in want else None
-    token = torch.empty(T, dtype=torch.float32, device=x.device) if "token" in want else None
+        workspace = _empty(max(16, perq_block_l1_stats_workspace_bytes(T, d, b)), torch.uint8, x.device, stream, result=False)
+    chan = _empty(d, torch.float32, x.device, stream) if "chan" in want else None
+    block = _empty(d // b, torch.float32, x.device, stream) if "block" in want else None
+    token = _empty(T, torch.float32, x.device, stream) if "token" in want else None
     rc = load().perq_block_l1_stats(_ptr(x), _ptr(perm), T, d, b, _ptr(chan), _ptr(block), _ptr(token),
                                     _ptr(workspace), workspace.numel(), _stream(stream))
     _check(rc, "perq_block_l1_stats")
@@ -259,7 +279,7 @@ def perq_token_diagnostics(x: torch.Tensor, perm: Optional[torch.Tensor], b: int
     assert perm is None or (perm.is_cuda and perm.dtype == torch.int32 and perm.is_contiguous())
     T, d = x.shape
     if out is None:
-        out = torch.empty((T, 5), dtype=torch.float32, device=x.device)
+        out = _empty((T, 5), torch.float32, x.device, stream)
     _check(load().perq_token_diagnostics(_ptr(x), _ptr(perm), T, d, b, _ptr(out), _stream(stream)),
            "perq_token_diagnostics")
     return out
@@ -268,7 +288,7 @@ def perq_token_diagnostics(x: torch.Tensor, perm: Optional[torch.Tensor], b: int
 def perq_validate_perm(perm: torch.Tensor, stream=None) -> torch.Tensor:
     """Returns a 1-element int32 CUDA tensor: 0 valid, bit0 out of range, bit1 duplicate."""
     assert perm.is_cuda and perm.dtype == torch.int32 and perm.is_contiguous()
-    status = torch.empty(1, dtype=torch.int32, device=perm.device)
+    status = _empty(1, torch.int32, perm.device, stream)
     _check(load().perq_validate_perm(_ptr(perm), perm.numel(), _ptr(status), _stream(stream)), "perq_validate_perm")
     return status
 
@@ -291,9 +311,9 @@ def perq_massdiff_perm_device(chan_abs_sum: torch.Tensor, b: int, perm: Optional
     assert chan_abs_sum.is_cuda and chan_abs_sum.dtype == torch.float32 and chan_abs_sum.is_contiguous()
     d = chan_abs_sum.numel()
     if perm is None:
-        perm = torch.empty(d, dtype=torch.int32, device=chan_abs_sum.device)
+        perm = _empty(d, torch.int32, chan_abs_sum.device, stream)
     if workspace is None:
-        workspace = torch.empty(d * 4, dtype=torch.uint8, device=chan_abs_sum.device)
+        workspace = _empty(d * 4, torch.uint8, chan_abs_sum.device, stream, result=False)
     _check(load().perq_massdiff_perm_device(_ptr(chan_abs_sum), d, b, _ptr(perm), _ptr(workspace),
                                             workspace.numel() * workspace.element_size(), _stream(stream)),
            "perq_massdiff_perm_device")
@@ -305,7 +325,7 @@ def perq_chan_abs_max(x: torch.Tensor, out: Optional[torch.Tensor] = None, strea
     assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 2 and x.is_contiguous()
     T, d = x.shape
     if out is None:
-        out = torch.empty(d, dtype=torch.float32, device=x.device)
+        out = _empty(d, torch.float32, x.device, stream)
     _check(load().perq_chan_abs_max(_ptr(x), T, d, _ptr(out), _stream(stream)), "perq_chan_abs_max")
     return out
 
@@ -352,11 +372,11 @@ def perq_rotate_quantize_i8(x: torch.Tensor, perm: Optional[torch.Tensor], b: in
     T, d = x.shape
     assert perm is None or (_on(perm, device, torch.int32) and perm.numel() == d)
     if out_codes is None:
-        out_codes = x.new_empty((T, d), dtype=torch.int8)
+        out_codes = x.new_empty((T, d), dtype=torch.int8) if stream is None else _empty((T, d), torch.int8, x.device, stream)
     else:
         assert _on(out_codes, device, torch.int8) and out_codes.numel() == T * d
     if out_scales is None:
-        out_scales = x.new_empty((T, 1), dtype=torch.float32)
+        out_scales = x.new_empty((T, 1), dtype=torch.float32) if stream is None else _empty((T, 1), torch.float32, x.device, stream)
     else:
         assert _on(out_scales, device, torch.float32) and out_scales.numel() == T
     if _lib is None:
@@ -376,7 +396,7 @@ def perq_code_sums(codes: torch.Tensor, fmt: int, stream=None) -> torch.Tensor:
     """Sums of the rows of codes (int8 [.., d], or uint8 [.., d / 2] for INT4): int32 CUDA tensor [..]."""
     assert _on(codes, torch._C._cuda_getDevice(), torch.int8 if fmt == PERQ_FMT_INT8 else torch.uint8)
     d = codes.shape[-1] * (1 if fmt == PERQ_FMT_INT8 else 2)
-    sums = torch.empty(codes.shape[:-1], dtype=torch.int32, device=codes.device)
+    sums = _empty(codes.shape[:-1], torch.int32, codes.device, stream)
     _check(load().perq_code_sums(_ptr(codes), fmt, sums.numel(), d, _ptr(sums), _stream(stream)), "perq_code_sums")
     return sums
 
@@ -407,29 +427,26 @@ def _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets
     assert w_codes.shape[-1] == (d if w_fmt == PERQ_FMT_INT8 else d // 2)
     assert w_sums is None or (_on(w_sums, device, torch.int32) and w_sums.numel() == E * N)
     if out is None:
-        out = a_scales.new_empty((T, N), dtype=out_dtype)
+        out = a_scales.new_empty((T, N), dtype=out_dtype) if stream is None else _empty((T, N), out_dtype, a_scales.device, stream)
     else:
         out_dtype = out.dtype
         assert out.get_device() == device and out.is_contiguous() and out.shape == (T, N)
     assert workspace is None or (workspace.get_device() == device and workspace.is_contiguous())
     if _lib is None:
         load()
-    if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(device)
-    else:
-        stream = _stream(stream)
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
     while True:
         sums = None if w_sums is None else w_sums.data_ptr()
         space, room = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
         if offsets is None:
             call, plain = _matmul_i8, _lib.perq_matmul_i8
             args = (a_codes.data_ptr(), a_scales.data_ptr(), a_fmt, w_codes.data_ptr(), w_scales.data_ptr(), w_fmt, sums, T, N, d, out.data_ptr(),
-                    OUT_BY_DTYPE[out_dtype], space, room, stream)
+                    OUT_BY_DTYPE[out_dtype], space, room, handle)
         else:
             assert _on(offsets, device, torch.int32)
             call, plain = _grouped_matmul_i8, _lib.perq_grouped_matmul_i8
             args = (a_codes.data_ptr(), a_scales.data_ptr(), a_fmt, w_codes.data_ptr(), w_scales.data_ptr(), w_fmt, sums, offsets.data_ptr(), T, E, N, d,
-                    out.data_ptr(), OUT_BY_DTYPE[out_dtype], space, room, stream)
+                    out.data_ptr(), OUT_BY_DTYPE[out_dtype], space, room, handle)
         try:
             rc = call(*args)
         except TypeError:       # (as above)
@@ -440,9 +457,7 @@ def _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets
             _check(rc, "perq_matmul_i8" if offsets is None else "perq_grouped_matmul_i8")
         n = (perq_matmul_i8_workspace_bytes(T, N, d, a_fmt, w_fmt) if offsets is None else
              perq_grouped_matmul_i8_workspace_bytes(T, E, N, d, a_fmt, w_fmt))
-        workspace = torch.empty(n, dtype=torch.uint8, device=a_codes.device)
-        if stream != torch._C._cuda_getCurrentRawStream(device):        # (it is let go on return, and its memory is the current stream's)
-            workspace.record_stream(torch.cuda.ExternalStream(stream))
+        workspace = _empty(n, torch.uint8, a_codes.device, stream, result=False)       # (let go on return)
 
 
 def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,

@@ -163,7 +163,7 @@ def test_blocks_let_go_on_the_current_stream_are_left_alone():
     import products as P
     from paper_2601_22347_b200 import binding as B, build
     build.build()
-    T, N, d = 1500, 1000, 2048
+    T, N, d = 5000, 1000, 2048
     gen = torch.Generator().manual_seed(3)
     a, sa = P.random_codes(P.INT4, T, d, gen)
     w, sw = P.random_codes(P.INT4, N, d, gen)

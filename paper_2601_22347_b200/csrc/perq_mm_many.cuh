@@ -314,6 +314,7 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
             row.n0 = it.n0;
             row.rows = min(32, it.t_end - (row.t - lane));
             row.ts = token_scale(p.a_scales, p.asym, min(row.t, p.T - 1));
+            __syncwarp();                                    // (the barrier wants whole warps, and lane 0 comes from the arrival below)
             asm volatile("bar.sync 1, 256;" ::: "memory");
             if (ok && !mbar_wait_warp(d_full + 8 * b, (j >> 1) & 1u)) { give_up(); ok = false; }
             if (split > 1) break;                            // (one tile to a cluster: see below)
@@ -373,8 +374,8 @@ many_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ C
                 many_store(p, row, u, (int)(16u * g), g + 1u < end && row.n0 + (int)(16u * g + 16u) < p.N, lane);
             }
         }
-        __syncwarp();
     }
+    __syncwarp();
     if (warp == 1) {
         tmem_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * MANY_CHANNELS) : "memory");

@@ -10,8 +10,8 @@
 // terms no larger than the largest output of their n (Parseval), it loses at most 8 + 2 units of 2^-24 of that (12 are counted).  A butterfly adds half
 // a unit of rounding and up to doubles what was lost before; no value on the way exceeds the block's largest output.  In all |u32 - u| <= E max|u| over the
 // block, E = (13 b / n - 1) 2^-24 with n = min(16, b / 4).  The row's maximum is summed again in fp64 wherever |u32| is within 2 E of the largest.
-// A quotient q = 127 u / max is off by 127 E (block's max) / max for u, and by |q| times E for the maximum, a unit for its reciprocal and 3 roundings: by the block's
-// largest quotient times 2 E + 9 2^-24 in all.  Elements that lie that close to the border between two codes are summed again in fp64
+// A quotient q = 127 u / max is off by 127 E (block's max) / max for u, and by |q| times E for the maximum, a unit for its reciprocal (at most 2^-23 of it, for
+// maxima up to 2^126) and 3 roundings: by the block's largest quotient times 2 E + 9 2^-24 in all.  Elements that lie that close to the border between two codes are summed again in fp64
 // (b = 32, gaussian values: 3 of a row of 4096; with outliers, next to none outside their blocks).
 //
 // Such places are rare, so a warp only notes them and settles them sixteen rows at a time, 32 / (b / 16) at once, from the inputs in global memory; it stores
@@ -463,13 +463,14 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
             __syncwarp();
         }
         if (w == 0 && lane == 0) load(i + STAGES);       // (all of the row's warps have read it)
-        // Rows so small that 127 / max overflows are settled block by block.
-        const bool tiny = !(all > 0x1p-120f);
+        // Rows so small that 127 / max overflows, or so large that 1 / max is no normal number (a unit of it is then more than 2^-23 of it), are settled
+        // block by block.
+        const bool odd = !(all > 0x1p-120f && all <= 0x1p126f);
         float ratio;
         asm("rcp.approx.f32 %0, %1;" : "=f"(ratio) : "f"(all));          // (off by a unit at most)
-        ratio = tiny ? 0.0f : 127.0f * ratio;
+        ratio = odd ? 0.0f : 127.0f * ratio;
         const Pair rr = pair_of(ratio, ratio);
-        const float near = tiny ? (all > 0.0f ? 0.0f : 1.0f) : all * p.near_max;
+        const float near = odd ? (all > 0.0f ? 0.0f : 1.0f) : all * p.near_max;
         int8_t *const out = p.codes + (size_t)(first + (long long)i * step) * (size_t)p.d + c0;
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
@@ -485,9 +486,9 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
             }
             if (c0 + k * per_piece < p.d) {
                 *reinterpret_cast<uint4 *>(out + k * per_piece) = make_uint4(code[0], code[1], code[2], code[3]);
-                const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt || (tiny && all > 0.0f);
+                const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt || (odd && all > 0.0f);
                 if (doubt || block[k] >= near) {
-                    note_lane(notes, u[k][0], u[k][1], u[k][2], u[k][3], u[k][4], u[k][5], u[k][6], u[k][7], ratio, tiny ? 0.0f : doubt ? 0.5f - 0x1p-23f - block[k] * ratio * p.doubt : 1.0f,
+                    note_lane(notes, u[k][0], u[k][1], u[k][2], u[k][3], u[k][4], u[k][5], u[k][6], u[k][7], ratio, odd ? 0.0f : doubt ? 0.5f - 0x1p-23f - block[k] * ratio * p.doubt : 1.0f,
                               near, i % BATCH, c0 + k * per_piece);
                 }
             }

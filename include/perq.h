@@ -23,7 +23,7 @@
  *     call was enqueued: the host-buffer entry point has then already queued its copy to
  *     the device, perq_block_l1_stats its first kernel; the outputs are undefined.
  *   - Device pointers must be 16-byte aligned.  Rows are dense (row stride = d).
- *   - Inputs are assumed finite.  NaN/Inf give unspecified codes but never a fault.
+ *   - Inputs are assumed finite.  NaN/Inf give unspecified codes but never a fault (perq_rotate_quantize_i8 shows them).
  */
 #ifndef PERQ_H
 #define PERQ_H
@@ -330,7 +330,8 @@ int perq_massdiff_perm_device(const float *chan_abs_sum, int32_t d, int32_t b, i
  *
  * x, perm, T, d as for perq_rotate_quantize.  b: 1, or a power of two from 16 to 512 that divides d (larger powers of two that
  * divide d: PERQ_ERR_UNSUPPORTED).  out_codes int8 [T, d], out_scales float [T].
- * Deterministic.  Every finite row is served down to subnormals; sqrt(b) |y| has to stay below 2^128.
+ * Deterministic.  Every finite row is served, down to subnormals and up to the largest numbers of bf16.  A row with an infinity or a NaN
+ * has codes 0 and the scale that the formula gives, infinite or NaN, so that its results in the products are not finite either.
  * Errors: NULL, SHAPE, BLOCK, UNSUPPORTED, ALIGN, CUDA.
  */
 int perq_rotate_quantize_i8(const void *x, const int32_t *perm, int64_t T, int32_t d, int32_t b, void *out_codes,

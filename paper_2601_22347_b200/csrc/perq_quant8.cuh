@@ -57,7 +57,7 @@ struct Params {
 
 struct Group {
     unsigned long long full[STAGES];                                  // barriers: the row is there
-    unsigned long long top[BATCH];                                    // exact maxima, the bits of positive doubles
+    unsigned long long top[BATCH];                                    // exact maxima, their bits
 };
 struct Notes {
     uint32_t count[2];
@@ -109,14 +109,21 @@ __device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+// (maxima are NaN where anything is: a row that is not finite is not lost)
 __device__ __forceinline__ float max3(float m, Pair v)
 {
     float x, y, r;
     split(v, x, y);
-    asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(x), "f"(y));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(x), "f"(y));
     return r;
 }
-__device__ __forceinline__ float warp_max(float v)       // (not negative)
+__device__ __forceinline__ float max2(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float warp_max(float v)       // (not negative; max2's NaN is above infinity as a number of bits)
 {
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }
@@ -205,7 +212,7 @@ __device__ __forceinline__ void note(Notes *notes, int kind, uint32_t mask, uint
     }
 }
 
-// Notes what is in doubt of a lane's 16 outputs: quotients from `limit` on away from their codes (0: all; 1: none), outputs from `near` on.  (Inside the
+// Notes what is in doubt of a lane's 16 outputs: quotients from `limit` on away from their codes (0: all; 1: none), outputs from `near` on; NaN always.  (Inside the
 // unrolled loop over the pieces this was half of its instructions, and twice its time.)
 __device__ __noinline__ void note_lane(Notes *notes, Pair u0, Pair u1, Pair u2, Pair u3, Pair u4, Pair u5, Pair u6, Pair u7, float ratio, float limit, float near,
                                        uint32_t row, int c)
@@ -217,8 +224,8 @@ __device__ __noinline__ void note_lane(Notes *notes, Pair u0, Pair u1, Pair u2, 
         float x, y, v, w;
         split(u[j], v, w);
         split(pair_fma(u[j], rr, pair_fma(pair_fma(u[j], rr, magic), neg, magic)), x, y);
-        codes |= (fabsf(x) >= limit ? 1u << (2 * j) : 0u) | (fabsf(y) >= limit ? 2u << (2 * j) : 0u);
-        most |= (fabsf(v) >= near ? 1u << (2 * j) : 0u) | (fabsf(w) >= near ? 2u << (2 * j) : 0u);
+        codes |= (fabsf(x) < limit ? 0u : 1u << (2 * j)) | (fabsf(y) < limit ? 0u : 2u << (2 * j));
+        most |= (fabsf(v) < near ? 0u : 1u << (2 * j)) | (fabsf(w) < near ? 0u : 2u << (2 * j));
     }
     note(notes, NOTE_CODE, codes, row, c);
     note(notes, NOTE_MAX, most, row, c);
@@ -315,21 +322,26 @@ __device__ __forceinline__ void settle_blocks(const Params &p, uint32_t n, uint3
         if (mine) f(place >> 16, c, v);
     }
 }
-__device__ __forceinline__ double largest(const double (&v)[LANE_ELEMS])
+// The bits of |v|, which are ordered as the numbers are, with NaN above infinity.
+__device__ __forceinline__ unsigned long long size_bits(double v) { return (unsigned long long)__double_as_longlong(v) & 0x7fffffffffffffffull; }
+__device__ __forceinline__ unsigned long long largest(const double (&v)[LANE_ELEMS])
 {
-    double m = 0.0;
+    unsigned long long m = 0ull;
 #pragma unroll
-    for (int j = 0; j < LANE_ELEMS; ++j) m = fmax(m, fabs(v[j]));
+    for (int j = 0; j < LANE_ELEMS; ++j) m = max(m, size_bits(v[j]));
     return m;
 }
+// A row's maximum that codes can be counted from; where it is not, they are 0.
+__device__ __forceinline__ bool counts(double top) { return top > 0.0 && top < __longlong_as_double(0x7ff0000000000000ll); }
 // rne(127 v / top) by the reciprocal, off by less than 2^-44: where that could matter, and on borders, by the quotient.
 __device__ __forceinline__ void store_codes(int8_t *to, const double (&v)[LANE_ELEMS], double top)
 {
-    const double r = top > 0.0 ? 127.0 / top : 0.0;
+    const bool some = counts(top);
+    const double r = some ? 127.0 / top : 0.0;
     uint32_t code[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int j = 0; j < LANE_ELEMS; ++j) {
-        const double t = v[j] * r;
+        const double t = some ? v[j] * r : 0.0;
         int q = __double2int_rn(t);
         if (fabs(t - (double)q) > 0.5 - 0x1p-40) q = __double2int_rn(127.0 * v[j] / top);
         code[j >> 2] |= ((uint32_t)q & 0xffu) << (8 * (j & 3));
@@ -346,8 +358,8 @@ __device__ __noinline__ void settle_batch(const Params &p, Group *group, Notes *
     const uint32_t n_max = *reinterpret_cast<volatile uint32_t *>(&notes->count[NOTE_MAX]), n_code = *reinterpret_cast<volatile uint32_t *>(&notes->count[NOTE_CODE]);
     const bool all = n_max > NOTES || n_code > NOTES;                 // everything that it has of all rows
     auto row_of = [&](uint32_t r) { return p.x + (size_t)(t0 + r * step) * (size_t)p.d; };
-    auto raise = [&](uint32_t r, double m) {
-        if (m > 0.0) atomicMax(&group->top[r], (unsigned long long)__double_as_longlong(m));
+    auto raise = [&](uint32_t r, unsigned long long m) {
+        if (m != 0ull) atomicMax(&group->top[r], m);
     };
     auto top_of = [&](uint32_t r) { return __longlong_as_double((long long)*reinterpret_cast<volatile unsigned long long *>(&group->top[r])); };
     constexpr uint32_t block = LOG2B > 4 ? 1u << LOG2B : LANE_ELEMS, blocks = WARP_ELEMS / block * PIECES;
@@ -356,7 +368,7 @@ __device__ __noinline__ void settle_batch(const Params &p, Group *group, Notes *
         return (r << 16) | ((j / WARP_ELEMS * (uint32_t)p.warps + (uint32_t)w) * WARP_ELEMS + j % WARP_ELEMS);
     };
     if (all) settle_blocks<LOG2B, PERM>(p, rows * blocks, table, lane, own, row_of, [&](uint32_t r, int, const double (&v)[LANE_ELEMS]) { raise(r, largest(v)); });
-    else settle_places<LOG2B, PERM>(notes->note[NOTE_MAX], n_max, table, lane, row_of, [&](uint32_t r, int, double u) { raise(r, fabs(u)); });
+    else settle_places<LOG2B, PERM>(notes->note[NOTE_MAX], n_max, table, lane, row_of, [&](uint32_t r, int, double u) { raise(r, size_bits(u)); });
     row_barrier(g, p.warps);
     if (all)
         settle_blocks<LOG2B, PERM>(p, rows * blocks, table, lane, own, row_of, [&](uint32_t r, int c, const double (&v)[LANE_ELEMS]) {
@@ -365,7 +377,7 @@ __device__ __noinline__ void settle_batch(const Params &p, Group *group, Notes *
     else
         settle_places<LOG2B, PERM>(notes->note[NOTE_CODE], n_code, table, lane, row_of, [&](uint32_t r, int c, double u) {
             const double top = top_of(r);
-            if (top > 0.0) p.codes[(size_t)(t0 + r * step) * (size_t)p.d + c] = (int8_t)__double2int_rn(127.0 * u / top);
+            p.codes[(size_t)(t0 + r * step) * (size_t)p.d + c] = counts(top) ? (int8_t)__double2int_rn(127.0 * u / top) : (int8_t)0;
         });
     __syncwarp();
     if (w == 0 && lane < (int)rows) p.scales[t0 + lane * step] = (float)(top_of((uint32_t)lane) * p.inv_scale);
@@ -449,9 +461,9 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
 #pragma unroll
             for (int j = 0; j < LANE_ELEMS / 2; ++j) m = max3(m, u[k][j]);
 #pragma unroll
-            for (int l = 1; l < block_lanes; l *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, l));
+            for (int l = 1; l < block_lanes; l *= 2) m = max2(m, __shfl_xor_sync(0xffffffffu, m, l));
             block[k] = m;
-            top = fmaxf(top, m);
+            top = max2(top, m);
         }
         top = warp_max(top);
         float all = top;
@@ -464,13 +476,13 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
         }
         if (w == 0 && lane == 0) load(i + STAGES);       // (all of the row's warps have read it)
         // Rows so small that 127 / max overflows, or so large that 1 / max is no normal number (a unit of it is then more than 2^-23 of it), are settled
-        // block by block.
+        // block by block, and so are those whose sums are not finite.
         const bool odd = !(all > 0x1p-120f && all <= 0x1p126f);
         float ratio;
         asm("rcp.approx.f32 %0, %1;" : "=f"(ratio) : "f"(all));          // (off by a unit at most)
         ratio = odd ? 0.0f : 127.0f * ratio;
         const Pair rr = pair_of(ratio, ratio);
-        const float near = odd ? (all > 0.0f ? 0.0f : 1.0f) : all * p.near_max;
+        const float near = odd ? (all != 0.0f ? 0.0f : 1.0f) : all * p.near_max;
         int8_t *const out = p.codes + (size_t)(first + (long long)i * step) * (size_t)p.d + c0;
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
@@ -486,7 +498,7 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
             }
             if (c0 + k * per_piece < p.d) {
                 *reinterpret_cast<uint4 *>(out + k * per_piece) = make_uint4(code[0], code[1], code[2], code[3]);
-                const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt || (odd && all > 0.0f);
+                const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt || (odd && all != 0.0f);
                 if (doubt || block[k] >= near) {
                     note_lane(notes, u[k][0], u[k][1], u[k][2], u[k][3], u[k][4], u[k][5], u[k][6], u[k][7], ratio, odd ? 0.0f : doubt ? 0.5f - 0x1p-23f - block[k] * ratio * p.doubt : 1.0f,
                               near, i % BATCH, c0 + k * per_piece);

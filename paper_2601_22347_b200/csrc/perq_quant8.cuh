@@ -477,7 +477,8 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
         if (w == 0 && lane == 0) load(i + STAGES);       // (all of the row's warps have read it)
         // Rows so small that 127 / max overflows, or so large that 1 / max is no normal number (a unit of it is then more than 2^-23 of it), are settled
         // block by block, and so are those whose sums are not finite.
-        const bool odd = !(all > 0x1p-120f && all <= 0x1p126f);
+        // (One comparison of bits, which also finds NaN: 16384 x 4096, b = 32, 41.9 us with two of numbers, 41.0 so.)
+        const bool odd = __float_as_uint(all) - (__float_as_uint(0x1p-120f) + 1u) >= __float_as_uint(0x1p126f) - __float_as_uint(0x1p-120f);
         float ratio;
         asm("rcp.approx.f32 %0, %1;" : "=f"(ratio) : "f"(all));          // (off by a unit at most)
         ratio = odd ? 0.0f : 127.0f * ratio;
@@ -498,8 +499,8 @@ __global__ void __launch_bounds__(cta_warps(PIECES) * 32, 1) quant8_kernel(const
             }
             if (c0 + k * per_piece < p.d) {
                 *reinterpret_cast<uint4 *>(out + k * per_piece) = make_uint4(code[0], code[1], code[2], code[3]);
-                const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt || (odd && all != 0.0f);
-                if (doubt || block[k] >= near) {
+                const bool doubt = off >= 0.5f - 0x1p-23f - block[k] * ratio * p.doubt;
+                if (doubt || !(block[k] < near)) {
                     note_lane(notes, u[k][0], u[k][1], u[k][2], u[k][3], u[k][4], u[k][5], u[k][6], u[k][7], ratio, odd ? 0.0f : doubt ? 0.5f - 0x1p-23f - block[k] * ratio * p.doubt : 1.0f,
                               near, i % BATCH, c0 + k * per_piece);
                 }

@@ -13,9 +13,12 @@ def test_roundings_of_a_quotient():
     """Rows whose maximum is between the borders go by fp32: a unit of the reciprocal (rcp.approx is off by one at most; below 2^-126 units do not
     get smaller, so they are a larger part of it) and three roundings have to stay within what the doubt about a code allows."""
     kernel = body(source("perq_quant8.cuh"), "quant8_kernel(const")
-    ordinary = re.search(r"const bool odd = !\(all > (0x1p-?\d+f) && all <= (0x1p\d+f)\);", kernel)
+    bits = r"__float_as_uint\((%s)\)"
+    lowest, highest = bits % r"0x1p-\d+f", bits % r"0x1p\d+f"
+    ordinary = re.search(r"const bool odd = __float_as_uint\(all\) - \(%s \+ 1u\) >= %s - %s;" % (lowest, highest, lowest), kernel)
     assert ordinary, "no upper border"
     low, high = power(ordinary.group(1)), power(ordinary.group(2))
+    assert ordinary.group(3) == ordinary.group(1)
     allowed = Fraction(re.search(r"p\.doubt = \(float\)\(1\.001 \* \(2\.0 \* e \+ (\d+)\.0 \* 0x1p-24\)\);", source("perq_matmul.cu")).group(1)) / 2 ** 24
     unit, half = Fraction(1, 2 ** 149), Fraction(1, 2 ** 24)
     for e in range(-133, 128):

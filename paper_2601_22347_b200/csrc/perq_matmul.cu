@@ -322,6 +322,30 @@ size_t product_workspace(const Product &m)
     return space.tokens + space.weights;
 }
 
+// A workspace for m.T tokens that serves fewer too.  Which dense calls go to the kernel for many tokens is no matter of tokens alone (in 4-bit codes of
+// 4096 x 4096 1024 tokens do, 1025 to 1152 do not), so the largest tile of 128 tokens is looked for that has such calls.  The first call of a tile is the
+// likeliest: the other kernel takes as long for all of them, and this one no less for more.  (From above, so it is found at once for most large calls; 10 ns a
+// tile where it is not.)
+size_t workspace_up_to(Product m)
+{
+    const int sms = sm_count();
+    const int64_t T = m.T;
+    auto space = [&]() {
+        const ManySpace s = many_space(m);
+        return s.tokens + s.weights;
+    };
+    if (T == 0 || space() == 0) return 0;
+    if (m.offsets || T <= 64) return many_is_better(m, sms) ? space() : 0;
+    for (int64_t first = (T - 1) / 128 * 128 + 1; first > 0; first -= 128) {
+        m.T = std::max<int64_t>(first, 65);                  // (64 and fewer go to the other kernel)
+        if (many_is_better(m, sms)) {
+            m.T = std::min(T, first + 127);
+            return space();
+        }
+    }
+    return 0;
+}
+
 int run_product(const Product &m, void *workspace, size_t workspace_bytes, cudaStream_t st)
 {
     if (!m.a || !m.a_scales || !m.w || !m.w_scales || !m.out || (m.a_fmt == PERQ_FMT_INT4_ASYM && !m.w_sums)) return PERQ_ERR_NULL;
@@ -434,7 +458,7 @@ int perq_matmul_i8_workspace_bytes(int64_t T, int32_t N, int32_t d, int32_t a_fm
     const Product m = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, T, N, d, 1, a_fmt, w_fmt, PERQ_OUT_BF16};
     if (int rc = check_product(m)) return rc;
     if (!bytes) return PERQ_ERR_NULL;
-    *bytes = product_workspace(m);
+    *bytes = workspace_up_to(m);
     return PERQ_OK;
 }
 
@@ -453,7 +477,7 @@ int perq_grouped_matmul_i8_workspace_bytes(int64_t T, int32_t E, int32_t N, int3
     const Product m = {nullptr, nullptr, nullptr, nullptr, nullptr, reinterpret_cast<const int32_t *>(16), nullptr, T, N, d, E, a_fmt, w_fmt, PERQ_OUT_BF16};
     if (int rc = check_product(m)) return rc;
     if (!bytes) return PERQ_ERR_NULL;
-    *bytes = product_workspace(m);
+    *bytes = workspace_up_to(m);
     return PERQ_OK;
 }
 

@@ -17,3 +17,18 @@ def oracle():
     from oracle import perq_oracle
     perq_oracle.build()
     return perq_oracle
+
+
+@pytest.fixture(autouse=True)
+def no_device_error(request):
+    """No wait inside a kernel runs out in any GPU test."""
+    if request.node.get_closest_marker("gpu") is None:
+        yield
+        return
+    import torch
+    from paper_2601_22347_b200 import binding, build
+    build.build()
+    binding.perq_device_error_clear()
+    yield
+    torch.cuda.synchronize()
+    assert binding.perq_device_error() == 0

@@ -33,7 +33,7 @@ def needs_build() -> bool:
 
 
 def build_call(force: bool = False) -> bool:
-    """Compile the interpreter's direct entry to the two calls of the online path.  False where there are no headers for it or
+    """Compile the interpreter's direct entry to the calls of the online path and the 8-bit layers.  False where there are no headers for it or
     no compiler: these calls then go through ctypes, and an older file is taken away."""
     src, include = os.path.join(_CSRC, "perq_call.c"), sysconfig.get_paths()["include"]
     if not force and os.path.exists(CALL_PATH) and os.path.getmtime(src) <= os.path.getmtime(CALL_PATH):

@@ -388,8 +388,9 @@ int launch_quant8(const void *x, const int32_t *perm, int64_t T, int32_t d, int3
     p.d = d;
     const int log2b = ilog2(b);
     const int all = (d + WARP_ELEMS - 1) / WARP_ELEMS;
-    // Pieces of a row to a warp: a row costs a warp a fixed part, so four (us for one / two / four: 16384 x 4096, b = 32, 168 / 95 / 48; 1531 x 9728 45 / 23 / 14,
-    // 64 x 4096 5.5 / 5.3 / 5.2; eight 46, 16, 7), but few permuted rows, whose warps gather, are better spread (1 x 4096 5.0 / 5.4 / 6.1, 64 5.9 / 6.3 / 7.1).
+    // Pieces of a row to a warp: a row costs a warp a fixed part, so four, but few permuted rows, whose warps gather, are better spread (us for one / two / four,
+    // gaussian values: 16384 x 4096, b = 32, 174 / 103 / 51, 1531 x 9728, b = 128, 56 / 31 / 25, 148 x 4096 5.3 / 5.0 / 5.0, 1 x 4096 4.3 / 4.4 / 4.4; permuted 1 x 4096
+    // 5.6 / 5.9 / 6.8, 148 6.8 / 6.6 / 7.6, 300 7.7 / 7.5 / 7.5, 1531 x 9728 63 / 46 / 39).
     const int pieces = all == 1 || (perm && T <= sms && all <= cta_warps(1)) ? 1 : all == 2 ? 2 : 4;
     p.warps = (all + pieces - 1) / pieces;
     const size_t fixed = sizeof(Shared) + (perm ? ((size_t)d * 2 + 127) / 128 * 128 : 0), row = (size_t)STAGES * (size_t)d * 2;

@@ -367,8 +367,9 @@ int perq_code_sums(const void *codes, int32_t fmt, int64_t rows, int32_t d, int3
  *   T, N, d             T == 0 is a no-op; T <= 2^30; 1 <= N <= PERQ_MAX_N; d % 32 == 0, d <= PERQ_MAX_D
  *   out                 device [T, N] of out_type (perq_out_t), row stride N, written in full
  *   workspace           device, at least perq_matmul_i8_workspace_bytes(...) bytes (NULL where that is 0).  What is enough for T
- *                       tokens is enough for fewer with the same N, d and formats (and E).  Its contents need not be kept; calls that
- *                       may overlap need one each.
+ *                       tokens is enough for fewer with the same N, d and formats (and E).  Calls of many tokens spread packed
+ *                       operands to bytes there, in each call: T d bytes of tokens, N d of weights (E N d).  Its contents need
+ *                       not be kept; calls that may overlap need one each.
  *
  * Scales that are infinite or NaN give what fp32 arithmetic makes of the formula.  All device pointers 16-byte aligned.
  * Errors: NULL, SHAPE, FMT (formats and out_type), ALIGN, WORKSPACE, CUDA.

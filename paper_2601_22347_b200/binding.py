@@ -473,7 +473,9 @@ def perq_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_
 def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt: int, w_codes: torch.Tensor, w_scales: torch.Tensor, w_fmt: int,
                            offsets: torch.Tensor, w_sums: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                            out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """As perq_matmul_i8 with w [E, N, d] and rows offsets[e] .. offsets[e + 1] (int32 CUDA tensor [E + 1]) of the tokens for expert e."""
+    """As perq_matmul_i8 with w [E, N, d] and rows offsets[e] .. offsets[e + 1] (int32 CUDA tensor [E + 1]) of the tokens for expert e.
+
+    Rows of no expert are not written: in an `out` made here they are whatever its memory holds."""
     E, N, _ = w_codes.shape
     assert offsets.numel() == E + 1
     return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, E, N, out, out_dtype, workspace, stream)

@@ -15,8 +15,8 @@
 // also those of two calls at once.)
 //
 // Measured in CUDA graphs, weights not in L2: 1 x 4096 x 14336, both packed, 9.9 us, 16 x 14336 x 4096 with 8-bit tokens 10.8 us (29.4 MB, 2.7 .. 3.0 TB/s:
-// 4 .. 5 us are launch, the first loads' way and the cluster's sums), 64 rows over 32 experts of 2048 x 4096 28 us (118 MB, 4.2 TB/s), 500 over 8 of
-// 2048 x 2048 11.4 us (15.6 with a branch to each result).
+// 4 .. 5 us are launch, the first loads' way and the cluster's sums; the 16 tokens' 112 tiles in two parts are 224 CTAs on 296 places), 64 rows over 32 experts of
+// 2048 x 4096 28 us (118 MB, 4.2 TB/s; 448 tiles on 296 CTAs: 76 % busy), 500 over 8 of 2048 x 2048 11.4 us (15.6 with a branch to each result).
 //
 // Grouped calls (offsets): expert e has rows offsets[e] .. offsets[e + 1].  Every CTA counts the tiles of all experts itself and
 // takes every gridDim-th one; experts without rows have none, so their weights are not read.

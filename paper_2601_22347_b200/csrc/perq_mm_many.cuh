@@ -13,7 +13,9 @@
 // Measured in CUDA graphs, 8-bit codes: 16384 x 4096 x 14336 in 606 us (3.2e15 operations a second, tensor pipe 88 %); 4099 rows over 32 experts of
 // 2048 x 4096 in 63 us (287 MB, 4.6 TB/s; pipe 59 %); 1531 x 1001 x 9728 in 22 us (48 of the 74 pairs have work, 8 us are launch, the first loads and the pairs'
 // exchange).  4-bit codes: 2048 x 4096 x 4096 in 31.5 us, 5 more than with 8-bit ones (spread_kernel); 8192 rows over 8 experts of 4096 x 2048 in 74 us, 17.5 of
-// them spread_kernel (42 MB read, 84 MB written to L2 in part: 7.2 TB/s).  These are at 1965 MHz; under the power limit the SMs fall to 1230.
+// them spread_kernel (42 MB read, 84 MB written to L2 in part: 7.2 TB/s).  These are at 1965 MHz.  Back to back for seconds, under the power limit: 714 us at
+// 1290 MHz, 77 at 1245 (so the 4099 rows are not bound by DRAM alone: 22 of their 35 tiles of tokens hold 128 rows or fewer, and the pair's second CTA loads others'
+// rows all the same) and 83 at 1710.
 // Tried: tiles of 128 channels (a k-step takes as long), stores that do not stay in L2 (no change), the next 16 columns on their way while the last are stored
 // (62 -> 64 us at 4099 rows: the epilogue waits for its stores).
 #pragma once

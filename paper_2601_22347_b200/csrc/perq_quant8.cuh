@@ -19,8 +19,8 @@
 // has up to four pieces of 512 channels of a row in registers.  Rows of up to 2048 need no barrier; the warps of longer ones meet at one barrier
 // a row and two for every sixteen.
 //
-// Measured in CUDA graphs: 16384 x 4096, b = 32, 40.6 us (201 MB, 5.0 TB/s), 1531 x 9728, b = 128, permuted, 27.6 us (45 MB, 1.6 TB/s: two-byte
-// gathers from shared memory and their latency at 15 warps, 5 us of settling), one row of 4096 3.8 us.
+// Measured in CUDA graphs, rows with outliers: 16384 x 4096, b = 32, 41.0 us (201 MB, 4.9 TB/s), 1531 x 9728, b = 128, permuted, 27.8 us (45 MB, 1.6 TB/s: two-byte
+// gathers from shared memory and their latency at 15 warps, 5 us of settling), one row of 4096 3.7 us.  Gaussian rows, with more codes in doubt: 51 and 39 us.
 #pragma once
 
 #include "perq_mm_ptx.cuh"

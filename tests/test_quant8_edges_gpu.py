@@ -69,7 +69,7 @@ def want(x, perm, b):
 NAN, INF = float("nan"), float("inf")
 
 
-@pytest.mark.parametrize("b,d", [(1, 32), (32, 32), (16, 64), (1, 512), (64, 2048), (512, 2048), (128, 9728), (32, 16384)])
+@pytest.mark.parametrize("b,d", [(1, 32), (32, 32), (16, 64), (1, 512), (32, 544), (64, 2048), (512, 2048), (128, 9728), (32, 16384)])
 @pytest.mark.parametrize("permuted", [False, True])
 def test_rows_that_are_not_finite_say_so(B, b, d, permuted):  # noqa: F811
     """Their scale is what 64 bits make of the largest output, their codes are 0, and the rows between them are as they are without them."""

@@ -138,17 +138,15 @@ def _empty(shape, dtype: torch.dtype, device, stream=None, result: bool = True) 
 
     It is that stream's: a block that was let go on the current one may be in use by kernels that are still queued there, and the call does not
     wait for them.  Results are noted as in use on the current stream too, where the caller reads them and may let them go."""
-    if stream is not None:
-        handle = _stream(stream)
-        current = torch.cuda.current_stream(device)
-        if handle != current.cuda_stream:
-            # (0 and 1 are the default stream's, and no handles to make a stream object of)
-            with torch.cuda.stream(torch.cuda.default_stream(device) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device)):
-                t = torch.empty(shape, dtype=dtype, device=device)
-            if result:
-                t.record_stream(current)
-            return t
-    return torch.empty(shape, dtype=dtype, device=device)
+    handle = None if stream is None else _stream(stream)
+    if handle is None or handle == _stream(None):
+        return torch.empty(shape, dtype=dtype, device=device)
+    # (0 and 1 are the default stream's, and no handles to make a stream object of)
+    with torch.cuda.stream(torch.cuda.default_stream(device) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
 
 
 def perq_out_sizes(T: int, d: int, fmt: int, group: int):

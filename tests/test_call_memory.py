@@ -188,3 +188,50 @@ def test_blocks_let_go_on_the_current_stream_are_left_alone():
     P.compare(result, *P.product(P.INT4, a, sa, P.INT4, w, sw))
     for g, v in zip((*got[0], *got[1], got[2]), (*want[0], *want[1], want[2])):
         assert torch.equal(g, v)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("handle", [0, 1])
+def test_the_default_stream_given_on_another_one(handle):
+    """By its handles, as a number."""
+    from paper_2601_22347_b200 import binding as B, build
+    build.build()
+    x = torch.randn(300, 2048, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda").to(torch.bfloat16)
+    want = B.perq_rotate_quantize_i8(x, None, 32) + B.perq_block_l1_stats(x, None, 32)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = B.perq_rotate_quantize_i8(x, None, 32, stream=handle) + B.perq_block_l1_stats(x, None, 32, stream=handle)
+        empty = B.perq_rotate_quantize_i8(x[:0], None, 32, stream=handle)
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for g, w in zip(got, want)) and empty[0].shape == (0, 2048)
+
+
+@pytest.mark.gpu
+def test_captured_on_a_stream_that_joined_the_capture():
+    """Results and workspace of a call on a second stream of a graph, replayed."""
+    import products as P
+    from paper_2601_22347_b200 import binding as B, build
+    build.build()
+    T, N, d, f = 5000, 1000, 2048, B.PERQ_FMT_INT4
+    assert B.perq_matmul_i8_workspace_bytes(T, N, d, f, f) > 0
+    ops = [t for k in range(2) for t in P.random_codes(P.INT4, (T, N)[k], d, torch.Generator().manual_seed(7 + k))]
+    side, fork, join = torch.cuda.Stream(), torch.cuda.Event(), torch.cuda.Event()
+    B.perq_matmul_i8(ops[0], ops[1], f, ops[2], ops[3], f, out_dtype=torch.float32)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fork.record()
+        side.wait_event(fork)
+        out = B.perq_matmul_i8(ops[0], ops[1], f, ops[2], ops[3], f, out_dtype=torch.float32, stream=side)
+        join.record(side)
+        torch.cuda.current_stream().wait_event(join)
+        twice = out * 2
+    for seed in (20, 30):
+        for k in range(2):
+            for to, new in zip(ops[2 * k:2 * k + 2], P.random_codes(P.INT4, (T, N)[k], d, torch.Generator().manual_seed(seed + k))):
+                to.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        P.compare(out, *P.product(P.INT4, ops[0], ops[1], P.INT4, ops[2], ops[3]))
+        assert torch.equal(twice, 2 * out)
+    del graph

@@ -65,6 +65,8 @@ typedef enum {
 #define PERQ_MAX_D 32768
 #define PERQ_MAX_N 1048576      /* channels of a product (of one expert) */
 #define PERQ_MAX_EXPERTS 1024
+#define PERQ_MAX_SEQUENCES 65536 /* of a call on the cache */
+#define PERQ_MAX_HEADS 1024
 
 /*
  * perq_rotate_quantize -- the online hot path, one fused pass.
@@ -400,13 +402,86 @@ int perq_grouped_matmul_i8_workspace_bytes(int64_t T, int32_t E, int32_t N, int3
                                            size_t *bytes);
 
 /*
+ * The 8-bit cache of keys and values: one token's keys and values are what the path's quantiser makes of rows of D channels, but with
+ * one step for a page's tokens of a head, so that attention reads a byte for a channel and next to nothing for its steps.
+ *
+ *   k_codes, v_codes    device int8 [n_pages, heads, page, D]: pages of a pool
+ *   k_steps, v_steps    device float [n_pages, heads]: value = step * code
+ *   page                tokens of a page: 16, 32, 64 or 128;  D: 64 or 128;  heads <= PERQ_MAX_HEADS
+ *   pages               device int32 [S, width]: position j of sequence i lies in page pages[i, j / page], at place j % page
+ *   offsets             device int32 [S + 1], not decreasing, in 0 .. T: rows offsets[i] .. offsets[i + 1] of a call are sequence i's, n_i of them
+ *   lengths             device int32 [S]: tokens of sequence i, its rows of the call included.  They are its last ones: row r of it has the
+ *                       position lengths[i] - n_i + r.  The same array serves the call that writes a step's tokens and the one that attends.
+ *   b                   block of the keys' rotation (queries' too): 1 (none), or a power of two from 16 to D.  It cancels in the product of a
+ *                       query with a key; values are kept as they come (a rotation of theirs can be merged into the weights around them).
+ *   T, S, width         rows of the call (T <= 2^30; T == 0 or S == 0 is a no-op), S <= PERQ_MAX_SEQUENCES, width * page <= 2^30
+ *
+ * The host looks at none of the device arrays, so calls can be captured and replayed with other sequences.  Offsets and lengths outside their range
+ * (0 .. T; 0 .. width * page) are taken into it, pages outside 0 .. n_pages - 1 are not written and, read, are zeros (perq_cache_read_i8) or any page
+ * (perq_attention_i8): wrong numbers, never a fault.  Rows of the call that are no sequence's are neither read nor written, and rows at positions below 0 (lengths[i] <
+ * n_i) are in no page.  All device pointers 16-byte aligned.
+ *
+ * perq_cache_write_i8 -- rotates, quantises and writes new tokens.
+ *
+ * For each page and head that rows of the call fall into, with y the new keys times I (x) H_b / sqrt(b), or the new values, and a = max |y| over them:
+ *
+ *     step = fp32(a / 127), or, where earlier tokens of the sequence lie in the page, the larger of that and the step there
+ *     new tokens: code = clip(rne(y / step), -127, 127);  earlier ones, where the step has grown: code = clip(rne(code * old step / step), -127, 127)
+ *
+ * decided in exact arithmetic (a step of 0 gives codes 0).  What is in a page behind a sequence's last token stays.  A page whose first token is written starts anew,
+ * whatever its step was.  Values in the cache depend on how its tokens were split over calls, and on nothing else: results are bit-equal from run to run.
+ * A page and head that an infinity or a NaN is written to has codes 0 and a step that is not finite, and so has what attends to it, until its first token is written again.
+ *
+ *   k, v                device, bf16 or f16 (in_type, a perq_out_t) [T, heads, D], tokens k_stride and v_stride elements apart (multiples of 8, at least heads * D)
+ *   No two sequences of a call may have rows in the same page (pages that are only read may be shared).
+ * Errors: NULL, SHAPE, BLOCK, FMT, ALIGN, CUDA.
+ */
+int perq_cache_write_i8(const void *k, const void *v, int32_t in_type, int64_t k_stride, int64_t v_stride, const int32_t *offsets, const int32_t *lengths,
+                        const int32_t *pages, int64_t T, int32_t S, int32_t heads, int32_t D, int32_t b, int32_t page, int64_t n_pages, int32_t width,
+                        void *k_codes, float *k_steps, void *v_codes, float *v_steps, void *stream);
+
+/*
+ * perq_cache_read_i8 -- the tokens lengths[i] - n_i .. lengths[i] - 1 of every sequence: step * code, keys times I (x) H_b / sqrt(b) again, which is its own
+ * inverse; dense [T, heads, D] of out_type each, fp32 until the last rounding.  Rows at positions below 0 are zeros.  Errors: as for writing.
+ */
+int perq_cache_read_i8(const void *k_codes, const float *k_steps, const void *v_codes, const float *v_steps, const int32_t *offsets, const int32_t *lengths,
+                       const int32_t *pages, int64_t T, int32_t S, int32_t heads, int32_t D, int32_t b, int32_t page, int64_t n_pages, int32_t width, void *k,
+                       void *v, int32_t out_type, void *stream);
+
+/*
+ * perq_attention_i8 -- attention of the call's rows over the cache, their own tokens (written before) included:
+ *
+ *     out[t, h] = sum_j p_j v_j,   p = softmax over the visible j of scale * <q[t, h], k_j>
+ *
+ * with k and v the cache's values of head h / group, q rotated as the keys are.  A row at position i sees j <= i; with a window W > 0 of those only j > i - W and
+ * the first tokens j < sinks.  A row that sees nothing is 0.
+ *
+ *   q                   device, bf16 or f16 (in_type) [T, heads * group, D], tokens q_stride elements apart (a multiple of 8, at least heads * group * D)
+ *   heads, group        heads of the cache, and heads of queries to each; heads * group <= PERQ_MAX_HEADS
+ *   most                at least the rows of the longest sequence of the call (T will do; the least is the fastest).  Of a longer one, rows from
+ *                       `most` on are left as they are.
+ *   out                 device, dense [T, heads * group, D] of out_type
+ *   workspace           device, at least perq_attention_i8_workspace_bytes(...) bytes.  What is enough for T, S and most is enough for less of each
+ *                       with the same heads, group and D.  Its contents need not be kept; calls that may overlap need one each.
+ *
+ * Queries are rounded to fp16 after their rotation (with the row's largest between 1 and 2: bf16 without a rotation is kept), probabilities times their values' step to
+ * fp16 (2^-12 relative); sums are fp32 or wider, and added in an order that does not change from run to run.  Values' steps: 0, or 2^-64 to 2^120 (smaller ones count as 0).
+ * Errors: NULL, SHAPE, BLOCK, FMT, ALIGN, WORKSPACE, CUDA.
+ */
+int perq_attention_i8(const void *q, int32_t in_type, int64_t q_stride, const void *k_codes, const float *k_steps, const void *v_codes, const float *v_steps,
+                      const int32_t *offsets, const int32_t *lengths, const int32_t *pages, int64_t T, int32_t S, int32_t heads, int32_t group, int32_t D,
+                      int32_t b, int32_t page, int64_t n_pages, int32_t width, int32_t most, float scale, int32_t window, int32_t sinks, void *out,
+                      int32_t out_type, void *workspace, size_t workspace_bytes, void *stream);
+int perq_attention_i8_workspace_bytes(int64_t T, int32_t S, int32_t heads, int32_t group, int32_t D, int32_t most, size_t *bytes);
+
+/*
  * perq_device_error -- reads (synchronously, cudaMemcpyFromSymbol) the library's device-side
  * error word on the current device into *flags_host.  0 = no error.  Bit 0 is set when a
  * bounded wait inside a kernel ran out (an asynchronous copy that never completed); the
  * kernel then stops early and its outputs are incomplete.  Bits 1 and 2: such a wait inside the
  * permuted and grouped kernels, for an exact maximum (1) or a free buffer (2); bit 3: in the
  * statistic; bits 4 to 6: in the products and the
- * kernel of 8-bit codes.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
+ * kernel of 8-bit codes; bit 7: in the attention of many queries.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
  *
  * perq_device_error_clear -- writes 0 to that word on the current device (synchronously,
  * cudaMemcpyToSymbol), so that a later read reports only what happened since.  Call it with no

@@ -80,6 +80,14 @@ def load() -> C.CDLL:
         lib.perq_code_sums.argtypes = [vp, i32, i64, i32, vp, vp]
         for name in ("perq_rotate_quantize_i8", "perq_code_sums", "perq_matmul_i8", "perq_matmul_i8_workspace_bytes", "perq_grouped_matmul_i8", "perq_grouped_matmul_i8_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
+        cache = [vp, vp, vp, i64, i32, i32, i32, i32, i32, i64, i32]             # offsets, lengths, pages; T, S, heads, D, b, page, n_pages, width
+        lib.perq_cache_write_i8.argtypes = [vp, vp, i32, i64, i64] + cache + [vp, vp, vp, vp, vp]
+        lib.perq_cache_read_i8.argtypes = [vp, vp, vp, vp] + cache + [vp, vp, i32, vp]
+        lib.perq_attention_i8.argtypes = ([vp, i32, i64, vp, vp, vp, vp] + cache[:6] + [i32] + cache[6:] +
+                                          [i32, C.c_float, i32, i32, vp, i32, vp, sz, vp])
+        lib.perq_attention_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, C.POINTER(sz)]
+        for name in ("perq_cache_write_i8", "perq_cache_read_i8", "perq_attention_i8", "perq_attention_i8_workspace_bytes"):
+            getattr(lib, name).restype = C.c_int
         lib.perq_device_error.argtypes = [C.POINTER(C.c_uint32)]
         lib.perq_device_error.restype = C.c_int
         lib.perq_device_error_clear.argtypes = []
@@ -477,3 +485,102 @@ def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt:
     E, N, _ = w_codes.shape
     assert offsets.numel() == E + 1
     return _product(a_codes, a_scales, a_fmt, w_codes, w_scales, w_fmt, w_sums, offsets, E, N, out, out_dtype, workspace, stream)
+
+
+# ------------------------------------------------------------------------------------------------- the 8-bit cache
+def _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages):
+    """The cache's sizes: (S, heads, D, page, n_pages, width)."""
+    assert _on(k_codes, device, torch.int8) and _on(v_codes, device, torch.int8) and _on(k_steps, device, torch.float32) and _on(v_steps, device, torch.float32)
+    assert _on(offsets, device, torch.int32) and _on(lengths, device, torch.int32) and _on(pages, device, torch.int32)
+    n_pages, heads, page, D = k_codes.shape
+    S, width = pages.shape
+    assert v_codes.shape == k_codes.shape and k_steps.shape == (n_pages, heads) and v_steps.shape == (n_pages, heads)
+    assert lengths.numel() == S and offsets.numel() == S + 1
+    return S, heads, D, page, n_pages, width
+
+
+def _token_rows(x: torch.Tensor, device: int) -> bool:
+    """bf16 or f16 rows [T, heads, D] whose heads lie side by side; the rows may be part of longer ones."""
+    return (x.get_device() == device and x.dtype in (torch.bfloat16, torch.float16) and x.dim() == 3 and
+            (x.is_contiguous() or (x.stride(2) == 1 and x.stride(1) == x.shape[2])))
+
+
+def _row_stride(x: torch.Tensor) -> int:
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]             # (a single row's may be anything)
+
+
+def perq_cache_write_i8(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: torch.Tensor, v_steps: torch.Tensor,
+                        offsets: torch.Tensor, lengths: torch.Tensor, pages: torch.Tensor, b: int = 1, stream=None) -> None:
+    """k, v: bf16 or f16 CUDA tensors [T, heads, D] (parts of longer rows too), written into codes int8 [n_pages, heads, page, D] and steps fp32 [n_pages, heads].
+
+    offsets int32 [S + 1], lengths int32 [S] (tokens with the new ones), pages int32 [S, width].  All tensors are on the current device."""
+    device = torch._C._cuda_getDevice()
+    S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
+    T = k.shape[0]
+    assert _token_rows(k, device) and _token_rows(v, device) and k.dtype is v.dtype and k.shape == v.shape and k.shape[1:] == (heads, D)
+    if _lib is None:
+        load()
+    rc = _lib.perq_cache_write_i8(k.data_ptr(), v.data_ptr(), OUT_BY_DTYPE[k.dtype], _row_stride(k), _row_stride(v), offsets.data_ptr(), lengths.data_ptr(),
+                                  pages.data_ptr(), T, S, heads, D, b, page, n_pages, width, k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(),
+                                  v_steps.data_ptr(), torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    if rc != PERQ_OK:
+        _check(rc, "perq_cache_write_i8")
+
+
+def perq_cache_read_i8(k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: torch.Tensor, v_steps: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor,
+                       pages: torch.Tensor, T: int, b: int = 1, out_dtype: torch.dtype = torch.bfloat16, k: Optional[torch.Tensor] = None,
+                       v: Optional[torch.Tensor] = None, stream=None):
+    """The last offsets[i + 1] - offsets[i] tokens of every sequence: (k, v), each [T, heads, D] of out_dtype.
+
+    Rows of no sequence are not written: in outputs made here they are whatever the memory holds."""
+    device = torch._C._cuda_getDevice()
+    S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
+    if k is None:
+        k = _empty((T, heads, D), out_dtype, k_codes.device, stream)
+    if v is None:
+        v = _empty((T, heads, D), k.dtype, k_codes.device, stream)
+    assert _on(k, device, k.dtype) and _on(v, device, k.dtype) and k.shape == (T, heads, D) and v.shape == (T, heads, D)
+    if _lib is None:
+        load()
+    rc = _lib.perq_cache_read_i8(k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(), offsets.data_ptr(), lengths.data_ptr(), pages.data_ptr(), T, S,
+                                 heads, D, b, page, n_pages, width, k.data_ptr(), v.data_ptr(), OUT_BY_DTYPE[k.dtype],
+                                 torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    if rc != PERQ_OK:
+        _check(rc, "perq_cache_read_i8")
+    return k, v
+
+
+def perq_attention_i8_workspace_bytes(T: int, S: int, heads: int, group: int, D: int, most: int) -> int:
+    n = C.c_size_t(0)
+    _check(load().perq_attention_i8_workspace_bytes(T, S, heads, group, D, most, C.byref(n)), "perq_attention_i8_workspace_bytes")
+    return int(n.value)
+
+
+def perq_attention_i8(q: torch.Tensor, k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: torch.Tensor, v_steps: torch.Tensor, offsets: torch.Tensor,
+                      lengths: torch.Tensor, pages: torch.Tensor, most: Optional[int] = None, b: int = 1, scale: Optional[float] = None, window: int = 0,
+                      sinks: int = 0, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q: bf16 or f16 CUDA tensor [T, heads of queries, D] (part of longer rows too); returns out [T, heads of queries, D] of q's type, or out_dtype.
+
+    most: at least the rows of the longest sequence of the call (None: T); scale: of the logits (None: D ** -0.5).  All tensors are on the current device.  A
+    workspace that the call is not given is made here.  Rows of no sequence are not written: in an `out` made here they are whatever its memory holds."""
+    device = torch._C._cuda_getDevice()
+    S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
+    T, all_heads = q.shape[:2]
+    assert _token_rows(q, device) and q.shape[2] == D and all_heads % heads == 0
+    if out is None:
+        out = _empty((T, all_heads, D), out_dtype or q.dtype, q.device, stream)
+    assert out.get_device() == device and out.is_contiguous() and out.shape == (T, all_heads, D)
+    group, most = all_heads // heads, max(1, T if most is None else most)
+    if workspace is None:
+        workspace = _empty(max(16, perq_attention_i8_workspace_bytes(T, S, heads, group, D, most)), torch.uint8, q.device, stream, result=False)   # (let go on return)
+    assert workspace.get_device() == device and workspace.is_contiguous()
+    if _lib is None:
+        load()
+    rc = _lib.perq_attention_i8(q.data_ptr(), OUT_BY_DTYPE[q.dtype], _row_stride(q), k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(),
+                                offsets.data_ptr(), lengths.data_ptr(), pages.data_ptr(), T, S, heads, group, D, b, page, n_pages, width, most,
+                                D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), OUT_BY_DTYPE[out.dtype], workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    if rc != PERQ_OK:
+        _check(rc, "perq_attention_i8")
+    return out

@@ -978,16 +978,18 @@ int perq_validate_perm(const int32_t *perm, int32_t d, int32_t *status_dev, void
 int perq_device_error(uint32_t *flags_host)
 {
     if (!flags_host) return PERQ_ERR_NULL;
-    unsigned int v = 0, products = 0;
-    if (cudaMemcpyFromSymbol(&v, perq::g_perq_device_error, sizeof v) != cudaSuccess || perq_mm_read_error(&products) != cudaSuccess) return PERQ_ERR_CUDA;
-    *flags_host = v | products;
+    unsigned int v = 0, products = 0, cache = 0;
+    if (cudaMemcpyFromSymbol(&v, perq::g_perq_device_error, sizeof v) != cudaSuccess || perq_mm_read_error(&products) != cudaSuccess ||
+        perq_kv_read_error(&cache) != cudaSuccess)
+        return PERQ_ERR_CUDA;
+    *flags_host = v | products | cache;
     return PERQ_OK;
 }
 
 int perq_device_error_clear(void)
 {
     const unsigned int zero = 0;
-    return cudaMemcpyToSymbol(perq::g_perq_device_error, &zero, sizeof zero) == cudaSuccess && perq_mm_clear_error() == cudaSuccess ? PERQ_OK : PERQ_ERR_CUDA;
+    return cudaMemcpyToSymbol(perq::g_perq_device_error, &zero, sizeof zero) == cudaSuccess && perq_mm_clear_error() == cudaSuccess && perq_kv_clear_error() == cudaSuccess ? PERQ_OK : PERQ_ERR_CUDA;
 }
 
 int perq_massdiff_perm_device(const float *chan_abs_sum, int32_t d, int32_t b, int32_t *perm, void *workspace,

@@ -1,0 +1,548 @@
+// Attention over the 8-bit cache for few queries to a sequence: decode steps and drafted tokens.
+//
+// Bound by memory: the visible codes of a (sequence, head of keys) are read once for all queries that share it.  Rows are pairs of a new token and one of the `group`
+// heads of queries that share a head of keys; a unit of work is 16 keys for a tile of 8 or 16 rows.  The CTAs take equal shares of all units, whatever the lengths are
+// (they are known on the device only), and a share's eight warps take its units in turn.  A row whose units belong to several CTAs is put together by join_kernel, in a
+// fixed order.
+//
+// Keys (then, transposed, values) are the first operand of mma.sync m16n8k16, rows the second, so that eight rows cost no more than they have to.  The order of the
+// channels inside a product is free: a lane takes 16 adjacent codes of its keys as they lie in memory, and of its values 16 adjacent channels of four keys.  It copies just
+// what it reads itself (cp.async into its own places), so the copies want no barrier, and 16-byte reads of them meet no conflict.  Codes become fp16 exactly: code ^ 0x80 in the
+// low bits of 1024, minus 1152.
+//
+// logit (base 2) x = s_k f S with S the sum over codes, f the row's factor.  Values' steps go into the exponent: P = 2^(x + log2 s_v - m), so that fp16 P (2^-12 of each) meet exact codes and no row's
+// sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is only moved when something is over 2^8 times larger.  Blocks of values whose step is below 2^-64 (of zeros)
+// count as zeros of that step.
+#pragma once
+
+#include "perq_cache.cuh"
+
+namespace perq_kv {
+
+constexpr int FEW_WARPS = THREADS / 32;
+constexpr int FEW_KEYS = 16;                  // of a unit
+
+struct AttendParams {
+    Sequences q;
+    const uint16_t *x;                        // queries: [T] rows of heads * group * D, row stride
+    long long stride;
+    const int8_t *k_codes, *v_codes;
+    const float *k_steps, *v_steps;
+    void *out;                                // [T, heads * group, D]
+    float *partial;                           // of shares: [2 * CTAs][rows][D + 2]
+    int32_t heads, group;
+    int32_t most;                             // rows of a sequence that are looked at
+    int32_t few_rows;                         // sequences of up to so many (token, head) rows are the kernel's for few queries, the others the one's for many
+    int32_t window, sinks, log2b, f16, out_type;
+    float scale;                              // of logits, times log2 e / sqrt b
+};
+
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy8(uint32_t to, const void *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float log2_of(float x)
+{
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) { return pack16(lo, hi, true); }
+// Two codes in bytes 0 and 2 as fp16.
+__device__ __forceinline__ uint32_t codes_f16(uint32_t w)
+{
+    uint32_t r;
+    asm("{ .reg .b32 t; lop3.b32 t, %1, 0x00ff00ff, 0x64806480, 0x6a; sub.rn.f16x2 %0, t, %2; }" : "=r"(r) : "r"(w), "r"(0x64806480u));
+    return r;
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) { return perq_mm::lds128(at); }
+__device__ __forceinline__ uint2 lds64(uint32_t at)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
+
+// The units of a sequence's tiles: groups of keys 0 .. sunk - 1, then from `low` on.
+struct Units {
+    Rows r;
+    int32_t tokens;                           // rows that are looked at
+    int32_t sunk, low, count;                 // groups of a tile; at least one, so that rows that see nothing are written
+    int32_t tiles;                            // of rows, each once for every head of keys
+};
+template <int ROWS>
+__device__ __forceinline__ Units units_of(const AttendParams &p, int i)
+{
+    Units u;
+    u.r = rows_of(p.q, i);
+    u.tokens = min(u.r.n, p.most);
+    const long long rows = (long long)u.tokens * p.group;
+    u.tiles = rows <= p.few_rows ? ((int)rows + ROWS - 1) / ROWS : 0;
+    const int first = u.r.length - u.r.n, end = max(min(u.r.length, first + u.tokens), 0);
+    u.low = p.window > 0 ? max(first - p.window + 1, 0) / FEW_KEYS : 0;
+    u.sunk = min((min(p.sinks, end) + FEW_KEYS - 1) / FEW_KEYS, u.low);
+    u.count = max(u.sunk + (end + FEW_KEYS - 1) / FEW_KEYS - u.low, 1);
+    return u;
+}
+
+struct Share {
+    long long all, per;                       // units of the call, and of a CTA
+};
+struct Found {
+    int32_t sequence;
+    long long begin;                          // its first unit
+};
+// The units of all sequences, and the sequence of unit `per * number` (none: S).  Called by all threads of the CTA.
+template <int ROWS>
+__device__ __forceinline__ Share share_units(const AttendParams &p, int number, int ctas, Found &f)
+{
+    __shared__ long long sums[FEW_WARPS];
+    __shared__ Found found;
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    long long units = 0;
+    auto mine = [&](int i) {
+        if (i >= p.q.S) return 0ll;
+        const Units u = units_of<ROWS>(p, i);
+        return (long long)u.tiles * u.count * p.heads;
+    };
+    auto total = [&](long long c, long long &up_to) {                  // over the CTA; of the threads up to this one
+        up_to = c;
+#pragma unroll
+        for (int l = 1; l < 32; l *= 2) {
+            const long long v = __shfl_up_sync(0xffffffffu, up_to, l);
+            if (lane >= l) up_to += v;
+        }
+        if (lane == 31) sums[warp] = up_to;
+        __syncthreads();
+        long long all = 0;
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) {
+            if (w < warp) up_to += sums[w];
+            all += sums[w];
+        }
+        __syncthreads();
+        return all;
+    };
+    long long c0 = 0, up0 = 0;
+    for (int base = 0; base < p.q.S; base += THREADS) {
+        long long up_to;
+        const long long c = mine(base + tid), all = total(c, up_to);
+        if (base == 0) {
+            c0 = c;
+            up0 = up_to;
+        }
+        units += all;
+    }
+    Share s;
+    s.all = units;
+    // (a share of at least a unit for each warp)
+    s.per = max((units + ctas - 1) / ctas, (long long)FEW_WARPS);
+    const long long unit = s.per * number;
+    if (tid == 0) found.sequence = p.q.S;
+    __syncthreads();
+    if (unit < units) {
+        long long before = 0;
+        for (int base = 0; base < p.q.S && before <= unit; base += THREADS) {
+            long long c = c0, up_to = up0, all;
+            if (p.q.S > THREADS) {
+                c = mine(base + tid);
+                all = total(c, up_to);
+            } else {
+                all = units;
+            }
+            const long long begin = before + up_to - c;
+            if (unit >= begin && unit < begin + c) {
+                found.sequence = base + tid;
+                found.begin = begin;
+            }
+            before += all;
+        }
+    }
+    __syncthreads();
+    f = found;
+    __syncthreads();
+    return s;
+}
+
+template <int D, int NT>
+struct Few {
+    static constexpr int rows = 8 * NT;
+    static constexpr int parts = D / 64;                               // 16-byte parts of a key to a lane
+    static constexpr int v_bytes = D / 8;                              // of a value
+    static constexpr int k_lane = 2 * parts * 16, lane_bytes = k_lane + 4 * v_bytes;
+    static constexpr int stages = (NT == 1 ? 3 : 6) * (D == 64 ? 2 : 1);          // units of a warp that are on their way or read
+    static constexpr int stage = 32 * lane_bytes, ring = FEW_WARPS * stages * stage;
+    static constexpr int q_row = D + 8;                                // fp16
+    static constexpr int off_q = ring, off_factor = off_q + rows * q_row * 2, off_top = off_factor + rows * 4, off_sum = off_top + FEW_WARPS * rows * 4,
+                         bytes = off_sum + FEW_WARPS * rows * 4;
+    static_assert(FEW_WARPS * rows * D * 4 <= ring, "the warps' sums lie where the copies did");
+};
+
+// Where a share's results lie: sums [rows][D], then the largest and the sum of probabilities of each row.
+template <int D, int NT>
+__device__ __forceinline__ float *share_result(const AttendParams &p, int number, bool from_start)
+{
+    return p.partial + (size_t)(2 * number + (from_start ? 1 : 0)) * (size_t)(8 * NT * (D + 2));
+}
+
+template <int D>
+__device__ __forceinline__ void store_out4(const AttendParams &p, size_t at, float4 v)
+{
+    if (p.out_type == perq_mm::OUT_F32) {
+        *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = v;
+    } else {
+        const bool f16 = p.out_type == perq_mm::OUT_F16;
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at) = make_uint2(pack16(v.x, v.y, f16), pack16(v.z, v.w, f16));
+    }
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __grid_constant__ AttendParams p)
+{
+    using K = Few<D, NT>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const uint32_t base = perq_mm::smem_u32(smem);
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+    uint16_t *const q_room = reinterpret_cast<uint16_t *>(smem + K::off_q);
+    float *const factor = reinterpret_cast<float *>(smem + K::off_factor), *const tops = reinterpret_cast<float *>(smem + K::off_top),
+          *const totals = reinterpret_cast<float *>(smem + K::off_sum), *const sums = reinterpret_cast<float *>(smem);
+    griddep_wait();
+    griddep_launch();
+    Found f;
+    const Share share = share_units<K::rows>(p, (int)blockIdx.x, (int)gridDim.x, f);
+    long long unit = share.per * (long long)blockIdx.x;
+    const long long unit_end = min(unit + share.per, share.all);
+    int i = f.sequence;
+    long long begin = f.begin;
+    const uint32_t mine = base + (uint32_t)(warp * K::stages * K::stage);
+
+    while (unit < unit_end && i < p.q.S) {
+        // the tile of this unit
+        const Units u = units_of<K::rows>(p, i);
+        const long long of_sequence = (long long)u.tiles * u.count * p.heads;
+        if (unit >= begin + of_sequence) {
+            begin += of_sequence;
+            ++i;
+            continue;
+        }
+        const int number = (int)((unit - begin) / u.count), head = number / u.tiles, row0 = (number - head * u.tiles) * K::rows;
+        const long long tile_begin = begin + (long long)number * u.count;
+        const int l0 = (int)(unit - tile_begin), l1 = (int)min((long long)u.count, unit_end - tile_begin), rows = min(K::rows, u.tokens * p.group - row0);
+        const int first = u.r.length - u.r.n;                          // position of the sequence's first row
+        const int token0 = row0 / p.group, token1 = (row0 + rows - 1) / p.group, low_position = first + token0, high_position = first + token1;
+        const int32_t *const table = p.q.pages + (size_t)i * (size_t)p.q.width;
+
+        auto key_of = [&](int l) { return (l < u.sunk ? l : l - u.sunk + u.low) * FEW_KEYS; };
+        // pages and steps of 32 units of this warp, one to a lane
+        const int units = l1 - l0 > warp ? (l1 - l0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
+        int pages[2] = {0, 0};
+        float k_step[2], v_step[2];
+        auto fetch = [&](int batch) {
+            const int n = batch * 32 + lane, l = l0 + warp + n * FEW_WARPS;
+            int page = 0;
+            float ks = 0.0f, vs = 0.0f;
+            if (n < units) {
+                page = min(max(__ldg(table + min(key_of(l) >> p.q.page, p.q.width - 1)), 0), p.q.n_pages - 1);
+                const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
+                ks = __ldg(p.k_steps + block);
+                vs = __ldg(p.v_steps + block);
+            }
+            if (batch & 1) { pages[1] = page; k_step[1] = ks; v_step[1] = vs; } else { pages[0] = page; k_step[0] = ks; v_step[0] = vs; }
+        };
+        auto issue = [&](int n) {
+            if (n < units) {
+                const int page = __shfl_sync(0xffffffffu, n & 32 ? pages[1] : pages[0], n & 31), key = key_of(l0 + warp + n * FEW_WARPS);
+                const size_t at = ((((size_t)page * (size_t)p.heads + (size_t)head) << p.q.page) + (size_t)(key & ((1 << p.q.page) - 1))) * D;
+                const uint32_t to = mine + (uint32_t)(n % K::stages) * K::stage;
+                const int8_t *const k = p.k_codes + at + q * 16, *const v = p.v_codes + at + g * K::v_bytes;
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int c = 0; c < K::parts; ++c) copy16(to + (uint32_t)((r * K::parts + c) * 512 + lane * 16), k + (g + 8 * r) * D + c * 64);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int8_t *const from = v + (2 * q + (r & 1) + 8 * (r >> 1)) * D;
+                    const uint32_t at_v = to + 32 * K::k_lane + (uint32_t)(r * 32 + lane) * K::v_bytes;
+                    if (D == 128) copy16(at_v, from); else copy8(at_v, from);
+                }
+            }
+            copies_end();
+            if ((n & 31) == 16) fetch((n >> 5) + 1);
+        };
+        fetch(0);
+#pragma unroll
+        for (int n = 0; n < K::stages - 1; ++n) issue(n);
+
+        // queries: rotated, scaled to 1 .. 2 by a power of two, fp16
+        {
+            constexpr int lanes = D / LANE;
+            const int row = min(tid / lanes, K::rows - 1), channel = tid % lanes * LANE;
+            const bool there = tid / lanes < rows;
+            uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+            if (there) {
+                const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
+                const uint4 *const from = reinterpret_cast<const uint4 *>(p.x + (size_t)(u.r.begin + token) * (size_t)p.stride + (size_t)(head * p.group + h) * D + channel);
+                lo = __ldg(from);
+                hi = __ldg(from + 1);
+            }
+            float v[LANE], top = 0.0f;
+            unpack(v, lo, hi, p.f16 != 0);
+            rotate(v, p.log2b, lane);
+#pragma unroll
+            for (int k = 0; k < LANE; ++k) top = fmaxf(top, fabsf(v[k]));
+#pragma unroll
+            for (int l = 1; l < lanes; l *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, l));
+            const int e = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
+            const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+            if (tid / lanes < K::rows) {
+#pragma unroll
+                for (int k = 0; k < LANE; k += 2) *reinterpret_cast<uint32_t *>(q_room + row * K::q_row + channel + k) = half2_of(v[k] * down, v[k + 1] * down);
+                if (channel == 0) factor[row] = __uint_as_float((uint32_t)e << 23) * p.scale;
+            }
+        }
+        __syncthreads();
+        uint32_t qb[NT][4 * K::parts][2];
+        float row_factor[NT][2];
+        int position[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int k = 0; k < 4 * K::parts; ++k) {
+                const int channel = 16 * (q + 4 * (k / 4)) + 4 * (k % 4);
+                const uint2 w = *reinterpret_cast<const uint2 *>(q_room + (t * 8 + g) * K::q_row + channel);
+                qb[t][k][0] = __byte_perm(w.x, w.y, 0x5410);           // channels 0 and 2, 1 and 3
+                qb[t][k][1] = __byte_perm(w.x, w.y, 0x7632);
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int row = t * 8 + 2 * q + c;
+                row_factor[t][c] = factor[row];
+                position[t][c] = row < rows ? first + (row0 + row) / p.group : -1;
+            }
+        }
+        float o[NT][D / 16][4], top[NT][2], total[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][j][e] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                top[t][c] = -INFINITY;
+                total[t][c] = 0.0f;
+            }
+        }
+
+        for (int n = 0; n < units; ++n) {
+            issue(n + K::stages - 1);
+            copies_wait<K::stages - 1>();
+            const uint32_t at = mine + (uint32_t)(n % K::stages) * K::stage;
+            const float ks = __shfl_sync(0xffffffffu, n & 32 ? k_step[1] : k_step[0], n & 31), vs = __shfl_sync(0xffffffffu, n & 32 ? v_step[1] : v_step[0], n & 31);
+            float s[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][e] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < K::parts; ++c) {
+                const uint4 a = lds128(at + (uint32_t)(c * 512 + lane * 16)), b = lds128(at + (uint32_t)((K::parts + c) * 512 + lane * 16));
+                const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t a0 = codes_f16(x[k]), a1 = codes_f16(y[k]), a2 = codes_f16(x[k] >> 8), a3 = codes_f16(y[k] >> 8);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma_f16(s[t], a0, a1, a2, a3, qb[t][4 * c + k][0], qb[t][4 * c + k][1]);
+                }
+            }
+            const int key = key_of(l0 + warp + n * FEW_WARPS);
+            const bool none = vs < 0x1p-64f;
+            const float log_step = none ? -64.0f : log2_of(vs), inverse = none ? 0x1p64f : 1.0f / vs;
+            const bool whole = key + FEW_KEYS - 1 <= low_position && (p.window <= 0 || key > high_position - p.window || key + FEW_KEYS <= p.sinks);
+            float over = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int c = e & 1;
+                    float x = fmaf(s[t][e], row_factor[t][c] * ks, log_step);
+                    if (!whole) {
+                        const int j = key + g + 8 * (e >> 1), at_row = position[t][c];
+                        if (j > at_row || (p.window > 0 && j <= at_row - p.window && j >= p.sinks)) x = -INFINITY;
+                    }
+                    s[t][e] = x;
+                    // (-inf minus -inf is no reason)
+                    over = fmaxf(over, x - top[t][c]);
+                }
+            if (__any_sync(0xffffffffu, over > 8.0f)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = fmaxf(s[t][c], s[t][c + 2]);
+#pragma unroll
+                        for (int l = 4; l < 32; l *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, l));
+                        m = fmaxf(m, top[t][c]);
+                        const float alpha = m == -INFINITY ? 1.0f : exp2_of(top[t][c] - m);
+                        top[t][c] = m;
+                        total[t][c] *= alpha;
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j) {
+                            o[t][j][c] *= alpha;
+                            o[t][j][c + 2] *= alpha;
+                        }
+                    }
+            }
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float e[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float m = top[t][k & 1];
+                    e[k] = exp2_of(s[t][k] - (m == -INFINITY ? 0.0f : m));
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float sum = e[c] + e[c + 2];
+                    if (sum != 0.0f) total[t][c] = fmaf(sum, inverse, total[t][c]);          // (a step that is not finite stays with the rows that see it)
+                }
+                pb[t][0] = none ? 0u : transposed(half2_of(e[0], e[1]));
+                pb[t][1] = none ? 0u : transposed(half2_of(e[2], e[3]));
+            }
+            uint32_t v[4][D / 32];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t from = at + 32 * K::k_lane + (uint32_t)(r * 32 + lane) * K::v_bytes;
+                if constexpr (D == 128) {
+                    const uint4 w = lds128(from);
+                    v[r][0] = w.x; v[r][1] = w.y; v[r][2] = w.z; v[r][3] = w.w;
+                } else {
+                    const uint2 w = lds64(from);
+                    v[r][0] = w.x; v[r][1] = w.y;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                constexpr uint32_t pick[4] = {0x0400u, 0x0501u, 0x0602u, 0x0703u};
+                const int w = j / 2, b = 2 * (j % 2);
+                const uint32_t a0 = codes_f16(__byte_perm(v[0][w], v[1][w], pick[b])), a1 = codes_f16(__byte_perm(v[0][w], v[1][w], pick[b + 1]));
+                const uint32_t a2 = codes_f16(__byte_perm(v[2][w], v[3][w], pick[b])), a3 = codes_f16(__byte_perm(v[2][w], v[3][w], pick[b + 1]));
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma_f16(o[t][j], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+            }
+        }
+        copies_wait<0>();
+
+        // the warps' results become one
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int l = 4; l < 32; l *= 2) total[t][c] += __shfl_xor_sync(0xffffffffu, total[t][c], l);
+                if (g == 0) {
+                    tops[warp * K::rows + t * 8 + 2 * q + c] = top[t][c];
+                    totals[warp * K::rows + t * 8 + 2 * q + c] = total[t][c];
+                }
+            }
+        __syncthreads();
+        // (a lane has channels (D / 8) g + 2 j and one more of rows 2 q and 2 q + 1)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float *const to = sums + ((size_t)warp * K::rows + (size_t)(t * 8 + 2 * q + c)) * D + g * K::v_bytes;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) *reinterpret_cast<float2 *>(to + 2 * j) = make_float2(o[t][j][c], o[t][j][c + 2]);
+            }
+        __syncthreads();
+        const bool whole_row = l0 == 0 && l1 == u.count;
+        float *const result = share_result<D, NT>(p, (int)blockIdx.x, l0 == 0);
+        for (int k = tid; k < K::rows * D / 4; k += THREADS) {
+            const int row = k / (D / 4), channel = k % (D / 4) * 4;
+            float m = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < FEW_WARPS; ++w) m = fmaxf(m, tops[w * K::rows + row]);
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < FEW_WARPS; ++w) {
+                const float mw = tops[w * K::rows + row], a = mw == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : exp2_of(mw - m);
+                const float4 x = *reinterpret_cast<const float4 *>(sums + ((size_t)w * K::rows + (size_t)row) * D + channel);
+                l = fmaf(a, totals[w * K::rows + row], l);
+                v.x = fmaf(a, x.x, v.x); v.y = fmaf(a, x.y, v.y); v.z = fmaf(a, x.z, v.z); v.w = fmaf(a, x.w, v.w);
+            }
+            if (whole_row) {
+                if (row >= rows) continue;
+                const float r = l == 0.0f ? 0.0f : 1.0f / l;
+                const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
+                store_out4<D>(p, ((size_t)(u.r.begin + token) * (size_t)(p.heads * p.group) + (size_t)(head * p.group + h)) * D + (size_t)channel,
+                              make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+            } else {
+                *reinterpret_cast<float4 *>(result + row * D + channel) = v;
+                if (channel == 0) {
+                    result[K::rows * D + row] = m;
+                    result[K::rows * D + K::rows + row] = l;
+                }
+            }
+        }
+        __syncthreads();                                               // (before the next tile's copies)
+        unit = tile_begin + l1;
+    }
+}
+
+// Tiles whose units several CTAs had: CTA `b` puts the one together that its boundary, between shares b and b + 1, is the first to cut.
+template <int D, int NT>
+__global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendParams p, int ctas)
+{
+    using K = Few<D, NT>;
+    griddep_wait();
+    griddep_launch();
+    Found f;
+    const Share share = share_units<K::rows>(p, (int)blockIdx.x + 1, ctas, f);
+    const long long boundary = share.per * (long long)(blockIdx.x + 1);
+    if (boundary >= share.all) return;
+    const Units u = units_of<K::rows>(p, f.sequence);
+    const int number = (int)((boundary - f.begin) / u.count), head = number / u.tiles, row0 = (number - head * u.tiles) * K::rows;
+    const long long tile_begin = f.begin + (long long)number * u.count, tile_end = tile_begin + u.count;
+    if (tile_begin == boundary || tile_begin < boundary - share.per) return;
+    const int rows = min(K::rows, u.tokens * p.group - row0), c0 = (int)blockIdx.x, c1 = (int)((tile_end - 1) / share.per);
+    auto result_of = [&](int c) { return share_result<D, NT>(p, c, c == c0); };
+    for (int k = (int)threadIdx.x; k < rows * D / 4; k += THREADS) {
+        const int row = k / (D / 4), channel = k % (D / 4) * 4;
+        float m = -INFINITY, l = 0.0f;
+        for (int c = c0; c <= c1; ++c) m = fmaxf(m, result_of(c)[K::rows * D + row]);
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int c = c0; c <= c1; ++c) {
+            const float *const from = result_of(c);
+            const float mc = from[K::rows * D + row], a = mc == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : exp2_of(mc - m);
+            const float4 x = *reinterpret_cast<const float4 *>(from + row * D + channel);
+            l = fmaf(a, from[K::rows * D + K::rows + row], l);
+            v.x = fmaf(a, x.x, v.x); v.y = fmaf(a, x.y, v.y); v.z = fmaf(a, x.z, v.z); v.w = fmaf(a, x.w, v.w);
+        }
+        const float r = l == 0.0f ? 0.0f : 1.0f / l;
+        const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
+        store_out4<D>(p, ((size_t)(u.r.begin + token) * (size_t)(p.heads * p.group) + (size_t)(head * p.group + h)) * D + (size_t)channel,
+                      make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+    }
+}
+
+}  // namespace perq_kv

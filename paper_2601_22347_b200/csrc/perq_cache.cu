@@ -1,0 +1,255 @@
+// C ABI of the 8-bit cache (writing, reading back) and of the attention over it: argument checks, choice of kernel, launches.
+// Nothing here allocates device memory or synchronises.
+#include "perq.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "perq_attend_many.cuh"
+#include "perq_host.cuh"
+
+namespace {
+
+using namespace perq_kv;
+
+// Programmatic stream serialization as everywhere in the library.
+template <typename... P>
+int launch(void (*kernel)(P...), long long grid, int threads, size_t smem, cudaStream_t st, int grid_y, const P &...p)
+{
+    if (int rc = allow_smem(kernel, smem)) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)grid_y);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return PERQ_ERR_CUDA;
+    }
+    return PERQ_OK;
+}
+
+int check_cache(int64_t T, int32_t S, int32_t heads, int32_t D, int32_t b, int32_t page, int64_t n_pages, int32_t width)
+{
+    if (T < 0 || T > (1 << 30) || S < 0 || S > PERQ_MAX_SEQUENCES || heads < 1 || heads > PERQ_MAX_HEADS || (D != 64 && D != 128)) return PERQ_ERR_SHAPE;
+    if (!is_pow2(page) || page < 16 || page > 128 || n_pages < 1 || n_pages > INT32_MAX || width < 1 || (int64_t)width * page > (1 << 30)) return PERQ_ERR_SHAPE;
+    if (!is_pow2(b) || (b != 1 && b < 16) || b > D) return PERQ_ERR_BLOCK;
+    return PERQ_OK;
+}
+bool row_stride(int64_t stride, int64_t channels) { return stride >= channels && stride % 8 == 0; }
+int check_pointers(const void *const *p, int n)
+{
+    for (int i = 0; i < n; ++i)
+        if (!p[i]) return PERQ_ERR_NULL;
+    for (int i = 0; i < n; ++i)
+        if (!aligned16(p[i])) return PERQ_ERR_ALIGN;
+    return PERQ_OK;
+}
+
+Sequences sequences(const int32_t *offsets, const int32_t *lengths, const int32_t *pages, int64_t T, int32_t S, int32_t width, int64_t n_pages, int32_t page)
+{
+    Sequences q;
+    q.offsets = offsets;
+    q.lengths = lengths;
+    q.pages = pages;
+    q.T = (int32_t)T;
+    q.S = S;
+    q.width = width;
+    q.n_pages = (int32_t)n_pages;
+    q.page = ilog2(page);
+    return q;
+}
+
+template <int D>
+int launch_write(WriteParams &p, int page, cudaStream_t st)
+{
+    // Blocks that rows can fall into: n rows reach into at most n / page + 2, and into no more than n.
+    const int64_t blocks = std::min<int64_t>(p.q.T, p.q.T / page + 2ll * p.q.S);
+    const bool few = p.q.T <= 8ll * p.q.S;
+    const bool one = few || page * D <= 2048;                          // a warp to a block
+    p.parts = one ? (2 * p.heads + THREADS / 32 - 1) / (THREADS / 32) : 2 * p.heads;
+    const int64_t grid = blocks * p.parts;
+    if (grid >= (1ll << 31)) return PERQ_ERR_SHAPE;
+    if (few) return launch(write_kernel<D, 1, 1>, grid, THREADS, 0, st, 1, p);
+    if (one) return launch(write_kernel<D, 1, 4>, grid, THREADS, 0, st, 1, p);
+    switch (page * D / 4096) {
+    case 1: return launch(write_kernel<D, 8, 1>, grid, THREADS, 0, st, 1, p);
+    case 2: return launch(write_kernel<D, 8, 2>, grid, THREADS, 0, st, 1, p);
+    default: return launch(write_kernel<D, 8, 4>, grid, THREADS, 0, st, 1, p);
+    }
+}
+
+// How many CTAs share the units of few queries: what is resident at once.
+int few_ctas(int sms, int nt) { return nt == 1 ? 2 * sms : sms; }
+
+template <int D, int NT>
+int launch_few(const AttendParams &p, int sms, cudaStream_t st)
+{
+    const int ctas = few_ctas(sms, NT);
+    if (int rc = launch(few_kernel<D, NT>, ctas, THREADS, Few<D, NT>::bytes, st, 1, p)) return rc;
+    return launch(join_kernel<D, NT>, ctas - 1, THREADS, 0, st, 1, p, ctas);
+}
+
+// Rows (of tokens and heads) of a sequence up to which the kernel for few queries takes it.
+constexpr int FEW_ROWS = 64;
+
+// CTAs to the keys of a tile of rows: as many as leave no SM without work.
+int many_split(const AttendParams &p, long long items, int sms)
+{
+    const long long key_tiles = (((long long)p.q.width << p.q.page) + MANY_KEYS - 1) / MANY_KEYS;
+    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(sms / items, 16), key_tiles / 4));
+}
+
+template <int D>
+int launch_many(const AttendParams &a, int sms, cudaStream_t st)
+{
+    ManyParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.a = a;
+    p.partial = a.partial;
+    // (sequences of more than a.few_rows rows have at most this many tiles)
+    const long long items = ((long long)a.q.T * a.group / MANY_ROWS + std::min(a.q.S, a.q.T)) * a.heads;
+    p.split = many_split(a, items, sms);
+    if (items * p.split >= (1ll << 31)) return PERQ_ERR_SHAPE;
+    if (int rc = launch(a.q.page == 4 ? many_kernel<D, true> : many_kernel<D, false>, items * p.split, MANY_THREADS, Many<D>::bytes, st, 1, p)) return rc;
+    return p.split > 1 ? launch(many_join_kernel<D>, items, THREADS, 0, st, 4, p) : PERQ_OK;
+}
+
+template <int D>
+int launch_attention(AttendParams &p, int sms, cudaStream_t st)
+{
+    const int64_t rows = (int64_t)std::min<int64_t>(p.q.T, p.most) * p.group;
+    if (rows <= 8) return launch_few<D, 1>(p, sms, st);
+    if (rows <= FEW_ROWS) return launch_few<D, 2>(p, sms, st);
+    // (a single sequence of what may be many rows goes to the kernel for many, so that nothing is launched in vain)
+    p.few_rows = p.q.S == 1 ? 0 : FEW_ROWS;
+    if (p.few_rows > 0)
+        if (int rc = launch_few<D, 2>(p, sms, st)) return rc;
+    return launch_many<D>(p, sms, st);
+}
+
+}  // namespace
+
+cudaError_t perq_kv_read_error(unsigned int *flags) { return cudaMemcpyFromSymbol(flags, perq_mm::g_error, sizeof *flags); }
+cudaError_t perq_kv_clear_error()
+{
+    const unsigned int zero = 0;
+    return cudaMemcpyToSymbol(perq_mm::g_error, &zero, sizeof zero);
+}
+
+extern "C" {
+
+int perq_cache_write_i8(const void *k, const void *v, int32_t in_type, int64_t k_stride, int64_t v_stride, const int32_t *offsets, const int32_t *lengths,
+                        const int32_t *pages, int64_t T, int32_t S, int32_t heads, int32_t D, int32_t b, int32_t page, int64_t n_pages, int32_t width,
+                        void *k_codes, float *k_steps, void *v_codes, float *v_steps, void *stream)
+{
+    if (int rc = check_cache(T, S, heads, D, b, page, n_pages, width)) return rc;
+    if (!row_stride(k_stride, (int64_t)heads * D) || !row_stride(v_stride, (int64_t)heads * D)) return PERQ_ERR_SHAPE;
+    if (in_type != PERQ_OUT_BF16 && in_type != PERQ_OUT_F16) return PERQ_ERR_FMT;
+    if (T == 0 || S == 0) return PERQ_OK;
+    const void *const all[] = {k, v, offsets, lengths, pages, k_codes, k_steps, v_codes, v_steps};
+    if (int rc = check_pointers(all, 9)) return rc;
+    WriteParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = sequences(offsets, lengths, pages, T, S, width, n_pages, page);
+    p.x[0] = static_cast<const uint16_t *>(k);
+    p.x[1] = static_cast<const uint16_t *>(v);
+    p.stride[0] = k_stride;
+    p.stride[1] = v_stride;
+    p.codes[0] = static_cast<int8_t *>(k_codes);
+    p.codes[1] = static_cast<int8_t *>(v_codes);
+    p.steps[0] = k_steps;
+    p.steps[1] = v_steps;
+    p.heads = heads;
+    p.f16 = in_type == PERQ_OUT_F16;
+    p.log2b = ilog2(b);
+    return D == 64 ? launch_write<64>(p, page, static_cast<cudaStream_t>(stream)) : launch_write<128>(p, page, static_cast<cudaStream_t>(stream));
+}
+
+int perq_cache_read_i8(const void *k_codes, const float *k_steps, const void *v_codes, const float *v_steps, const int32_t *offsets, const int32_t *lengths,
+                       const int32_t *pages, int64_t T, int32_t S, int32_t heads, int32_t D, int32_t b, int32_t page, int64_t n_pages, int32_t width, void *k,
+                       void *v, int32_t out_type, void *stream)
+{
+    if (int rc = check_cache(T, S, heads, D, b, page, n_pages, width)) return rc;
+    if (out_type < PERQ_OUT_BF16 || out_type > PERQ_OUT_F32) return PERQ_ERR_FMT;
+    if (T == 0 || S == 0) return PERQ_OK;
+    const void *const all[] = {k, v, offsets, lengths, pages, k_codes, k_steps, v_codes, v_steps};
+    if (int rc = check_pointers(all, 9)) return rc;
+    ReadParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = sequences(offsets, lengths, pages, T, S, width, n_pages, page);
+    p.codes[0] = static_cast<const int8_t *>(k_codes);
+    p.codes[1] = static_cast<const int8_t *>(v_codes);
+    p.steps[0] = k_steps;
+    p.steps[1] = v_steps;
+    p.out[0] = k;
+    p.out[1] = v;
+    p.heads = heads;
+    p.out_type = out_type;
+    p.log2b = ilog2(b);
+    const long long grid = (T + READ_TOKENS - 1) / READ_TOKENS;
+    return launch(D == 64 ? read_kernel<64> : read_kernel<128>, grid, THREADS, 0, static_cast<cudaStream_t>(stream), 2, p);
+}
+
+int perq_attention_i8_workspace_bytes(int64_t T, int32_t S, int32_t heads, int32_t group, int32_t D, int32_t most, size_t *bytes)
+{
+    if (int rc = check_cache(T, S, heads, D, 1, 16, 1, 1)) return rc;
+    if (group < 1 || (int64_t)heads * group > PERQ_MAX_HEADS || most < 1) return PERQ_ERR_SHAPE;
+    if (!bytes) return PERQ_ERR_NULL;
+    int sms = sm_count();
+    if (sms <= 0) sms = 148;                                           // (no device, no launch: sizes are answered for a B200)
+    const int64_t rows = std::min<int64_t>(T, most) * group;
+    const size_t few = (size_t)few_ctas(sms, 1) * 2 * 8, many = rows > FEW_ROWS ? (size_t)sms * MANY_ROWS : 0;
+    *bytes = T == 0 || S == 0 ? 0 : std::max(few, many) * (size_t)(D + 2) * 4;
+    return PERQ_OK;
+}
+
+int perq_attention_i8(const void *q, int32_t in_type, int64_t q_stride, const void *k_codes, const float *k_steps, const void *v_codes, const float *v_steps,
+                      const int32_t *offsets, const int32_t *lengths, const int32_t *pages, int64_t T, int32_t S, int32_t heads, int32_t group, int32_t D,
+                      int32_t b, int32_t page, int64_t n_pages, int32_t width, int32_t most, float scale, int32_t window, int32_t sinks, void *out,
+                      int32_t out_type, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_cache(T, S, heads, D, b, page, n_pages, width)) return rc;
+    if (group < 1 || (int64_t)heads * group > PERQ_MAX_HEADS || !row_stride(q_stride, (int64_t)heads * group * D) || most < 1 || window < 0 || sinks < 0) return PERQ_ERR_SHAPE;
+    if ((in_type != PERQ_OUT_BF16 && in_type != PERQ_OUT_F16) || out_type < PERQ_OUT_BF16 || out_type > PERQ_OUT_F32) return PERQ_ERR_FMT;
+    if (T == 0 || S == 0) return PERQ_OK;
+    const void *const all[] = {q, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages, out};
+    if (int rc = check_pointers(all, 9)) return rc;
+    size_t need = 0;
+    if (int rc = perq_attention_i8_workspace_bytes(T, S, heads, group, D, most, &need)) return rc;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return PERQ_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return PERQ_ERR_ALIGN;
+    const int sms = sm_count();
+    if (sms <= 0) return PERQ_ERR_CUDA;
+    AttendParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = sequences(offsets, lengths, pages, T, S, width, n_pages, page);
+    p.x = static_cast<const uint16_t *>(q);
+    p.stride = q_stride;
+    p.k_codes = static_cast<const int8_t *>(k_codes);
+    p.v_codes = static_cast<const int8_t *>(v_codes);
+    p.k_steps = k_steps;
+    p.v_steps = v_steps;
+    p.out = out;
+    p.partial = static_cast<float *>(workspace);
+    p.heads = heads;
+    p.group = group;
+    p.most = most;
+    p.few_rows = INT32_MAX;
+    p.window = std::min(window, 1 << 30);
+    p.sinks = std::min(sinks, 1 << 30);
+    p.log2b = ilog2(b);
+    p.f16 = in_type == PERQ_OUT_F16;
+    p.out_type = out_type;
+    p.scale = scale * (1.4426950408889634f / std::sqrt((float)b));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return D == 64 ? launch_attention<64>(p, sms, st) : launch_attention<128>(p, sms, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,467 @@
+// An 8-bit cache of keys and values in pages: writing (rotation of the keys, a step for each page and head) and reading back.
+//
+// A block is `page` tokens of one head, int8 [page][D], with one fp32 step s.  New rows y (keys: rotated) give a = max |y| and s' = fp32(a / 127); s is s', or the
+// larger of s' and the block's step where earlier tokens stay in it.  code = rne(y / s), and earlier codes become rne(code s_old / s) where s has grown: the
+// cache costs one read of a block's codes more only when its largest value changes.
+//
+// Bound by memory: a new element is read once (2 bytes) and written once (1 byte).  A lane holds 16 adjacent channels of a token, so that a block of b channels
+// is a butterfly of four stages in registers (packed fp32) and one to three exchanges between lanes.  Eight warps share a block of a prompt and keep its rotated
+// values in registers over the barrier that its maximum needs; for few tokens a warp has a block of its own.
+//
+// Codes are those of exact arithmetic.  A butterfly of L = log2 b stages rounds each sum L times, so |u32 - u| <= L 2^-24 sum |x|, and sum |x| <= sqrt b |x|_2 =
+// |u|_2 <= sqrt b max |u| over the rotation's block: E = 1.01 L sqrt b 2^-24 of its largest (b = 128: 4.8e-6).  What may be the block's maximum (within 2 E of the largest in
+// fp32) is summed again in fp64, and so is an element whose quotient lies within 127 (E + 2^-22) of the border between two codes (b = 128: one in 800), by the
+// lanes that hold its rotation's block.
+#pragma once
+
+#include "perq_mm_ptx.cuh"
+
+namespace perq_kv {
+
+using perq_mm::griddep_launch;
+using perq_mm::griddep_wait;
+
+constexpr int THREADS = 256;
+constexpr int LANE = 16;                      // channels of a lane
+
+// The sequences of a call.
+struct Sequences {
+    const int32_t *offsets, *lengths, *pages;
+    int32_t T, S, width, n_pages, page;       // (page: its log2)
+};
+struct Rows {
+    int32_t begin, n;                         // rows of the call
+    int32_t length;                           // tokens, these included
+};
+// What the host never looks at is taken into its range here: wrong numbers, never a fault.
+__device__ __forceinline__ Rows rows_of(const Sequences &q, int i)
+{
+    Rows r;
+    r.begin = min(max(__ldg(q.offsets + i), 0), q.T);
+    r.n = max(min(max(__ldg(q.offsets + i + 1), 0), q.T) - r.begin, 0);
+    r.length = (int32_t)min((long long)max(__ldg(q.lengths + i), 0), (long long)q.width << q.page);
+    return r;
+}
+// Blocks that a sequence's rows fall into; rows at positions below 0 (fewer tokens than rows) into none.
+__device__ __forceinline__ int blocks_of(const Sequences &q, const Rows &r)
+{
+    const int first = max(r.length - r.n, 0);
+    return r.length > first ? ((r.length - 1) >> q.page) - (first >> q.page) + 1 : 0;
+}
+
+__device__ __forceinline__ float from16(uint32_t h, bool f16)
+{
+    if (!f16) return __uint_as_float(h << 16);
+    float f;
+    asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.f32.f16 %0, t; }" : "=f"(f) : "r"(h));
+    return f;
+}
+// A lane's 16 channels.
+__device__ __forceinline__ void unpack(float (&u)[LANE], const uint4 &lo, const uint4 &hi, bool f16)
+{
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        u[2 * i] = from16(w[i] & 0xffffu, f16);
+        u[2 * i + 1] = from16(w[i] >> 16, f16);
+    }
+}
+// Times the Hadamard matrix of blocks of 2^log2b channels (0: none), without its factor.
+__device__ __forceinline__ void rotate(float (&u)[LANE], int log2b, int lane)
+{
+    if (log2b == 0) return;
+#pragma unroll
+    for (int h = 1; h < LANE; h *= 2)
+#pragma unroll
+        for (int i = 0; i < LANE; ++i)
+            if ((i & h) == 0) {
+                const float a = u[i], b = u[i + h];
+                u[i] = a + b;
+                u[i + h] = a - b;
+            }
+    for (int l = 1; l < 1 << (log2b - 4); l *= 2) {
+        const float s = (lane & l) ? -1.0f : 1.0f;
+#pragma unroll
+        for (int i = 0; i < LANE; ++i) u[i] = fmaf(s, u[i], __shfl_xor_sync(0xffffffffu, u[i], l));      // (s u exact: one rounding)
+    }
+}
+
+// rne(y / s) for |y / s| < 2^31, exactly: the quotient's nearest whole number, mended by what is left.  y has to have 53 - 32 bits to spare, or no ties.
+__device__ __forceinline__ int exact_code(double y, float s)
+{
+    const double w = (double)s;
+    double n = rint(y / w);
+    const double left = fma(-n, w, y), twice = 2.0 * fabs(left);
+    if (twice > w || (twice == w && fmod(n, 2.0) != 0.0)) n += left > 0.0 ? 1.0 : -1.0;
+    return (int)fmin(fmax(n, -127.0), 127.0);
+}
+
+struct WriteParams {
+    Sequences q;
+    const uint16_t *x[2];                     // keys, values: [T] rows of heads * D, row strides
+    long long stride[2];
+    int8_t *codes[2];                         // [n_pages, heads, page, D]
+    float *steps[2];                          // [n_pages, heads]
+    int32_t heads, f16;
+    int32_t log2b;                            // of the keys
+    int32_t parts;                            // CTAs to a block of all heads, keys and values
+};
+
+struct Place {
+    int32_t row, slot, n;                     // its rows of the call, and their first place in the block
+    int32_t page;                             // of the pool, or -1
+};
+// Which sequence's which page the number-th block is.  Called by all threads of the CTA.
+__device__ __forceinline__ Place find_block(const Sequences &q, int number)
+{
+    __shared__ int32_t sums[THREADS / 32];
+    __shared__ Place found;
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) found.n = 0;
+    for (int base = 0, before = 0; base < q.S; base += THREADS) {
+        Rows r = {0, 0, 0};
+        int c = 0;
+        if (base + tid < q.S) {
+            r = rows_of(q, base + tid);
+            c = blocks_of(q, r);
+        }
+        int sum = c;
+#pragma unroll
+        for (int l = 1; l < 32; l *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, l);
+            if (lane >= l) sum += v;
+        }
+        if (lane == 31) sums[warp] = sum;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) sum += sums[w];
+            all += sums[w];
+        }
+        const int at = number - (before + sum - c);
+        if (at >= 0 && at < c) {
+            const int first = r.length - r.n, index = (max(first, 0) >> q.page) + at, from = max(index << q.page, max(first, 0));
+            Place p;
+            p.row = r.begin + (from - first);
+            p.slot = from - (index << q.page);
+            p.n = min((index + 1) << q.page, r.length) - from;
+            p.page = __ldg(q.pages + (size_t)(base + tid) * (size_t)q.width + (size_t)index);
+            if (p.page < 0 || p.page >= q.n_pages) p.page = -1;
+            found = p;
+        }
+        before += all;
+        __syncthreads();
+        if (before > number) break;
+    }
+    __syncthreads();
+    return found;
+}
+
+// WARPS warps have a block (8: the CTA's; 1: a block of each), TOKENS of it at a time, of which each lane keeps HELD lots.
+template <int D, int WARPS, int HELD>
+struct Write {
+    static constexpr int lanes = D / LANE;                             // to a token
+    static constexpr int tokens = WARPS * 32 / lanes;
+};
+
+template <int D, int WARPS, int HELD>
+__global__ void __launch_bounds__(THREADS) write_kernel(const __grid_constant__ WriteParams p)
+{
+    using K = Write<D, WARPS, HELD>;
+    __shared__ float part[THREADS / 32];
+    __shared__ unsigned long long exact[THREADS / 32];
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    griddep_wait();
+    griddep_launch();
+    const int number = (int)(blockIdx.x / (unsigned)p.parts), in = (int)(blockIdx.x % (unsigned)p.parts);
+    const Place at = find_block(p.q, number);
+    if (at.n <= 0 || at.page < 0) return;
+    const int item = WARPS == 1 ? in * (THREADS / 32) + warp : in;
+    if (item >= 2 * p.heads) return;                                   // (whole warps, and then no barrier follows)
+    const int kind = item >= p.heads ? 1 : 0, head = item - kind * p.heads, log2b = kind ? 0 : p.log2b;
+    const bool f16 = p.f16 != 0;
+    const uint16_t *const x = p.x[kind] + (size_t)at.row * (size_t)p.stride[kind] + (size_t)head * D;
+    const size_t block = (size_t)at.page * (size_t)p.heads + (size_t)head;
+    int8_t *const codes = p.codes[kind] + (block << p.q.page) * (size_t)D;
+    float *const step = p.steps[kind] + block;
+    const float before = at.slot > 0 ? __ldg(step) : 0.0f;
+
+    const int share = WARPS == 1 ? lane : tid, mine = share / K::lanes, channel = (share % K::lanes) * LANE;
+    const int lots = (at.n + K::tokens - 1) / K::tokens;
+    const bool held = lots <= HELD;
+    auto load = [&](int lot, float (&u)[LANE]) {
+        const int t = lot * K::tokens + mine;
+        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        if (t < at.n) {
+            const uint4 *const from = reinterpret_cast<const uint4 *>(x + (size_t)t * (size_t)p.stride[kind] + channel);
+            lo = __ldg(from);
+            hi = __ldg(from + 1);
+        }
+        unpack(u, lo, hi, f16);
+    };
+    // The exact u of one element of every token of the warp: this lane's `channel` + i where it asks, else any.
+    auto again = [&](int lot, int i, unsigned asked, bool &answered) -> double {
+        const unsigned group = (K::lanes == 32 ? 0xffffffffu : ((1u << K::lanes) - 1u) << (lane & ~(K::lanes - 1))) & asked;
+        const int leader = group ? __ffs(group) - 1 : lane;
+        const int e = __shfl_sync(0xffffffffu, channel + i, leader);
+        answered = leader == lane && group != 0u;
+        float v[LANE];
+        load(lot, v);
+        double sum = 0.0;
+        if (log2b == 0) {
+#pragma unroll
+            for (int k = 0; k < LANE; ++k)
+                if (k == i) sum = (double)v[k];
+            return sum;                                                // (the leader's own)
+        }
+        const unsigned sign = (unsigned)e & ((1u << log2b) - 1u);
+        // (other rotations' blocks of the token add up what nobody reads)
+#pragma unroll
+        for (int k = 0; k < LANE; ++k) {
+            const bool minus = __popc(sign & (unsigned)(channel + k)) & 1;
+            sum += minus ? -(double)v[k] : (double)v[k];
+        }
+        for (int l = 1; l < 1 << (log2b - 4); l *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, l);
+        return sum;
+    };
+
+    // 1. the largest of the block
+    float u[HELD][LANE], top = 0.0f;
+    auto larger = [&](const float (&v)[LANE]) {
+#pragma unroll
+        for (int i = 0; i < LANE; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(v[i])));
+    };
+    if (held) {
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            if (h < lots) {
+                load(h, u[h]);
+                rotate(u[h], log2b, lane);
+                larger(u[h]);
+            }
+    } else {
+        for (int lot = 0; lot < lots; ++lot) {
+            load(lot, u[0]);
+            rotate(u[0], log2b, lane);
+            larger(u[0]);
+        }
+    }
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+    if (WARPS > 1) {
+        if (lane == 0) {
+            part[warp] = top;
+            exact[warp] = 0ull;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(part[w])));
+    }
+    const float root = sqrtf((float)(1 << log2b));
+    const float e = log2b == 0 ? 0.0f : 1.01f * (float)log2b * root * 0x1p-24f;
+    // Far from the ends of fp32, or everything is summed in fp64.
+    const bool plain = top < 0x1p100f && top > 0x1p-80f;
+    double a = (double)top;
+    if (top != 0.0f && log2b != 0) {
+        const float near = plain ? top * (1.0f - 2.0f * e - 0x1p-22f) : -1.0f;
+        unsigned long long most = 0ull;
+        auto candidates = [&](int lot, const float (&v)[LANE]) {
+            unsigned want = 0u;
+#pragma unroll
+            for (int i = 0; i < LANE; ++i) want |= !(fabsf(v[i]) < near) ? 1u << i : 0u;
+            if (lot * K::tokens + mine >= at.n) want = 0u;
+            for (unsigned asked = __ballot_sync(0xffffffffu, want != 0u); asked != 0u; asked = __ballot_sync(0xffffffffu, want != 0u)) {
+                const int i = want ? __ffs(want) - 1 : 0;
+                bool answered;
+                const double y = again(lot, i, asked, answered);
+                if (answered) {
+                    most = max(most, (unsigned long long)__double_as_longlong(fabs(y)));
+                    want &= want - 1u;
+                }
+            }
+        };
+        if (held) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h)
+                if (h < lots) candidates(h, u[h]);
+        } else {
+            for (int lot = 0; lot < lots; ++lot) {
+                load(lot, u[0]);
+                rotate(u[0], log2b, lane);
+                candidates(lot, u[0]);
+            }
+        }
+#pragma unroll
+        for (int l = 16; l > 0; l /= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, l));
+        if (WARPS > 1) {
+            if (lane == 0) exact[warp] = most;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) most = max(most, exact[w]);
+        }
+        a = __longlong_as_double((long long)most);
+    }
+    const double wide_root = sqrt((double)(1 << log2b));
+    float s = (float)(a / wide_root / 127.0);
+    if (before > s || before != before) s = before;
+    const bool finite = fabsf(s) <= 3.4028235e38f, none = !finite || s == 0.0f;
+
+    // 2. codes
+    const float inverse = (float)(1.0 / ((double)s * wide_root));
+    // (a value of s is at least that of the largest / 127, so |u| inverse stays below 127 and a little)
+    const bool quick = plain && s > 0x1p-100f;
+    const float sure = quick ? 0.5f - 127.5f * (e + 0x1p-22f) : -1.0f;
+    auto store = [&](int lot, const float (&v)[LANE]) {
+        uint32_t c[LANE];
+        unsigned doubt = 0u;
+#pragma unroll
+        for (int i = 0; i < LANE; ++i) {
+            const float q = v[i] * inverse, t = q + 12582912.0f, d = q - (t - 12582912.0f);
+            c[i] = __float_as_uint(t);
+            doubt |= !(fabsf(d) <= sure) ? 1u << i : 0u;
+        }
+        const int t = lot * K::tokens + mine;
+        if (none || t >= at.n) doubt = 0u;
+        for (unsigned asked = __ballot_sync(0xffffffffu, doubt != 0u); asked != 0u; asked = __ballot_sync(0xffffffffu, doubt != 0u)) {
+            const int i = doubt ? __ffs(doubt) - 1 : 0;
+            bool answered;
+            const double y = again(lot, i, asked, answered);
+            if (answered) {
+                const uint32_t code = (uint32_t)exact_code(y / wide_root, s);
+#pragma unroll
+                for (int k = 0; k < LANE; ++k)
+                    if (k == i) c[k] = code;
+                doubt &= doubt - 1u;
+            }
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = none ? 0u : __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
+        if (t < at.n) *reinterpret_cast<uint4 *>(codes + (size_t)(at.slot + t) * D + channel) = make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    if (held) {
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            if (h < lots) store(h, u[h]);
+    } else {
+        for (int lot = 0; lot < lots; ++lot) {
+            load(lot, u[0]);
+            rotate(u[0], log2b, lane);
+            store(lot, u[0]);
+        }
+    }
+    // 3. earlier codes, where the step has grown
+    if (at.slot > 0 && !(s == before)) {
+        const float ratio = before / s;
+        const bool fast = before > 0x1p-80f && s < 0x1p100f;
+        for (int t = mine; t < at.slot; t += K::tokens) {
+            uint4 *const to = reinterpret_cast<uint4 *>(codes + (size_t)t * D + channel);
+            uint4 old = *to;
+            uint32_t *const w = reinterpret_cast<uint32_t *>(&old);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t r = 0u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int code = (int)(int8_t)(w[i] >> (8 * k));
+                    const float q = (float)code * ratio, n = rintf(q);
+                    int v = (int)n;
+                    if (!fast || fabsf(q - n) > 0.5f - 128.0f * 0x1p-22f) v = none ? 0 : exact_code((double)code * (double)before, s);
+                    r |= (uint32_t)(uint8_t)v << (8 * k);
+                }
+                w[i] = none ? 0u : r;
+            }
+            *to = old;
+        }
+    }
+    if ((WARPS == 1 ? lane : tid) == 0) *step = s;
+}
+
+// ------------------------------------------------------------------------------------------------------ reading back
+constexpr int READ_TOKENS = 16;               // of a CTA
+
+struct ReadParams {
+    Sequences q;
+    const int8_t *codes[2];
+    const float *steps[2];
+    void *out[2];                             // [T, heads, D]
+    int32_t heads, out_type, log2b;
+};
+
+__device__ __forceinline__ uint32_t pack16(float x, float y, bool f16)
+{
+    uint32_t r;
+    if (f16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    return r;
+}
+
+// A lane has 16 channels of a token and head; blockIdx.y: keys, values.  The sequence of a row is looked for once a token.
+template <int D>
+__global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ ReadParams p)
+{
+    constexpr int lanes = D / LANE;
+    __shared__ int32_t place[READ_TOKENS], slot[READ_TOKENS];
+    griddep_wait();
+    griddep_launch();
+    const int tid = (int)threadIdx.x, lane = tid & 31, row0 = (int)blockIdx.x * READ_TOKENS, kind = (int)blockIdx.y;
+    if (tid < READ_TOKENS) {
+        // the last sequence that begins at or before the row (offsets do not decrease)
+        const int row = row0 + tid;
+        int lo = 0, hi = p.q.S;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (__ldg(p.q.offsets + mid) <= row) lo = mid; else hi = mid;
+        }
+        const Rows r = rows_of(p.q, lo);
+        int at = -2;                                                   // not a row of any sequence: left as it is
+        slot[tid] = 0;
+        if (row >= r.begin && row < r.begin + r.n) {
+            const int position = r.length - r.n + (row - r.begin);
+            at = position < 0 ? -1 : __ldg(p.q.pages + (size_t)lo * (size_t)p.q.width + (size_t)(position >> p.q.page));
+            if (at < 0 || at >= p.q.n_pages) at = -1;                  // (zeros)
+            slot[tid] = position & ((1 << p.q.page) - 1);
+        }
+        place[tid] = at;
+    }
+    __syncthreads();
+    const int tokens = min(READ_TOKENS, p.q.T - row0), items = tokens * p.heads * lanes, log2b = kind ? 0 : p.log2b;
+    const float factor = 1.0f / sqrtf((float)(1 << log2b));
+    for (int i0 = 0; i0 < items; i0 += THREADS) {
+        const int i = i0 + tid, t = min(i / lanes / p.heads, tokens - 1), head = i / lanes % p.heads, channel = i % lanes * LANE;
+        const int page = i < items ? place[t] : -2;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        float s = 0.0f;
+        if (page >= 0) {
+            const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
+            v = __ldg(reinterpret_cast<const uint4 *>(p.codes[kind] + ((block << p.q.page) + (size_t)slot[t]) * D + channel));
+            s = __ldg(p.steps[kind] + block);
+        }
+        float u[LANE];
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < LANE; ++k) u[k] = (float)(int8_t)(w[k / 4] >> (8 * (k % 4)));
+        rotate(u, log2b, lane);                                        // (whole numbers below 2^14: exact)
+        s *= factor;
+#pragma unroll
+        for (int k = 0; k < LANE; ++k) u[k] *= s;
+        if (page == -2) continue;
+        const size_t at = ((size_t)(row0 + t) * (size_t)p.heads + (size_t)head) * D + (size_t)channel;
+        if (p.out_type == perq_mm::OUT_F32) {
+            float4 *const to = reinterpret_cast<float4 *>(static_cast<float *>(p.out[kind]) + at);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) to[k] = make_float4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+        } else {
+            const bool f16 = p.out_type == perq_mm::OUT_F16;
+            uint32_t o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = pack16(u[2 * k], u[2 * k + 1], f16);
+            uint4 *const to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.out[kind]) + at);
+            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+    }
+}
+
+}  // namespace perq_kv

@@ -17,6 +17,9 @@
 // The device error word of the product kernels (perq_matmul.cu), which perq_device_error reads with the others' own.
 __attribute__((visibility("hidden"))) cudaError_t perq_mm_read_error(unsigned int *flags);
 __attribute__((visibility("hidden"))) cudaError_t perq_mm_clear_error();
+// And that of the attention over the cache (perq_cache.cu).
+__attribute__((visibility("hidden"))) cudaError_t perq_kv_read_error(unsigned int *flags);
+__attribute__((visibility("hidden"))) cudaError_t perq_kv_clear_error();
 
 namespace {
 

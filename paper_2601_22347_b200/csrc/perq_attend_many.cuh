@@ -1,10 +1,11 @@
 // Attention over the 8-bit cache for many queries to a sequence: prompts and chunks of them, on the fifth-generation tensor cores.
 //
-// A CTA has 256 rows (pairs of a token and one of the `group` heads of queries to a head of keys), two tiles of 128, and goes over the keys they see, 128 at a time.  Four warps
-// bring codes in, make them fp16 (exactly) and lay them down as operands, keys and values in turn, in a ring; one thread issues the products: S = Q K^T into tensor memory, then O += P V with P
-// from tensor memory and V's rows as they are (its channels run along N).  Either tile has four warps of its own, a row to a thread: the row's maximum, P = 2^(x + log2 s_v - m)
-// rounded to fp16 over the columns where S was, and the probabilities' sum.  The products of one tile run under the other's exponentials.  O stays in tensor memory; m moves, and
-// O with it, only when something is over 2^8 times larger.
+// A CTA has 256 rows (pairs of a token and one of the `group` heads of queries to a head of keys), two tiles of 128, and goes over the keys they see, 128 at a time.  Bulk copies
+// bring codes in, a page at a time, keys and values in turn; four warps make them fp16 (exactly) and lay them down as operands, in a ring; one warp issues the products: S = Q K^T into tensor memory, then O += P V with P
+// from tensor memory and V's rows as they are (its channels run along N).  Either tile has eight warps of its own, half of a row's columns to a thread: their maximum, P = 2^(x + log2
+// s_v - m) rounded to fp16 over the columns where S was, and the probabilities' sum.  The products of one tile run under the other's exponentials.  O stays in tensor memory; m moves,
+// and O with it, only when something is over 2^8 times larger, which the two warps of 32 rows agree on at a barrier.  (Whole rows to a thread, four warps to a tile: twice the time, as
+// an in-order warp waits 5 to 6 cycles for an instruction and two to a scheduler do not hide it.)
 //
 // Bound by the tensor cores and the exponentials alike: 128 x 128 x 128 products twice are 1024 cycles, the tile's 16384 exponentials as many.
 #pragma once
@@ -13,7 +14,8 @@
 
 namespace perq_kv {
 
-constexpr int MANY_ROWS = 256, MANY_KEYS = 128, MANY_THREADS = 512;
+constexpr int CODES_WARP = 16, MMA_WARP = 20, LOAD_WARP = 21; // warps: 16 of the rows, 4 that make codes fp16, the products', the loads', 2 idle
+constexpr int MANY_ROWS = 256, MANY_KEYS = 128, MANY_THREADS = 768;
 // (perq_attend_few's rows go up to this; both sides measured beside launch_attention)
 enum : unsigned int { ERROR_ATTEND = 1u << 7 };
 
@@ -25,12 +27,12 @@ struct ManyParams {
 
 template <int D>
 struct Many {
-    static constexpr uint32_t tile = 128u * D * 2u;                    // bytes of 128 rows of fp16
-    static constexpr uint32_t half = 128u * 128u;                      // of 64 channels of them
-    static constexpr uint32_t stages = D == 128 ? 5 : 8;
-    static constexpr uint32_t off_ring = 2u * tile, off_steps = off_ring + stages * tile;
+    static constexpr uint32_t tile = 128u * D * 2u, raw = 128u * D;    // bytes of 128 rows of fp16, of codes
+    static constexpr uint32_t half = 128u * 128u;                      // of 64 channels of the former
+    static constexpr uint32_t stages = D == 128 ? 4 : 8, raw_stages = D == 128 ? 2 : 4;
+    static constexpr uint32_t off_ring = 2u * tile, off_raw = off_ring + stages * tile, off_steps = off_raw + raw_stages * raw;
     static constexpr uint32_t off_bars = off_steps + 8u * 8u * 16u;
-    static constexpr uint32_t bars = 2u * stages + 8u + 2u + 2u + 2u + 2u + 1u;   // full, empty; steps; Q, S, P, O of each tile; the end
+    static constexpr uint32_t bars = 2u * stages + 2u * raw_stages + 8u + 2u + 2u + 2u + 2u + 2u + 1u;   // operands, codes: full, empty; steps; Q, S, half of P, P, O of each tile; the end
     static constexpr uint32_t off_slot = off_bars + 8u * bars, bytes = off_slot + 16u + 1024u;
     static constexpr uint32_t columns = 512u;                          // S0, S1, O0, O1
     static constexpr uint32_t o_column = 256u;
@@ -41,22 +43,64 @@ __host__ __device__ constexpr uint32_t f16_desc(int m, int n, bool second_transp
 {
     return (1u << 4) | ((uint32_t)second_transposed << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+// perq_mm's waits, for barriers that only this CTA's threads and copies arrive at.
+__device__ __forceinline__ bool cta_poll(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0u;
+}
+__device__ __forceinline__ bool cta_wait_warp(uint32_t bar, uint32_t parity)
+{
+    bool done = cta_poll(bar, parity);
+    for (uint32_t i = 0; i < perq_mm::WAIT_POLLS && !done; ++i) done = cta_poll(bar, parity);
+    return __all_sync(0xffffffffu, done);
+}
+// By whole warps, of which one lane issues: what describes a product then stays in uniform registers.  (A lane of its own, with the warps that compute exponentials on the
+// same scheduler: 380 cycles to an instruction of 64.)
 __device__ __forceinline__ void product_f16(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
 {
-    asm volatile("{ .reg .pred p; .reg .b64 a, b; setp.ne.b32 p, %4, 0; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5}; "
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }"
+    asm volatile("{ .reg .pred p, q; .reg .b64 a, b; setp.ne.b32 p, %4, 0; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5}; elect.sync _|q, 0xffffffff; "
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }"
                  ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(perq_mm::OPERAND_HI) : "memory");
 }
 __device__ __forceinline__ void product_f16_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
 {
-    asm volatile("{ .reg .pred p; .reg .b64 b; setp.ne.b32 p, %4, 0; mov.b64 b, {%2, %5}; "
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }"
+    asm volatile("{ .reg .pred p, q; .reg .b64 b; setp.ne.b32 p, %4, 0; mov.b64 b, {%2, %5}; elect.sync _|q, 0xffffffff; "
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }"
                  ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(perq_mm::OPERAND_HI) : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar)
+{
+    asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar) : "memory");
 }
 // A tile of [128 rows][64 channels] halves: as an operand whose rows are M or N, and as one whose rows are K (64 channels of N, then those a half further on).
 __device__ __forceinline__ uint32_t rows_operand(uint32_t addr) { return ((addr >> 4) & 0x3fffu) | (1u << 16); }
 template <int D>
 __device__ __forceinline__ uint32_t keys_operand(uint32_t addr) { return ((addr >> 4) & 0x3fffu) | ((Many<D>::half >> 4) << 16); }
+
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t minus_1152(uint32_t v)
+{
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x64806480u));
+    return r;
+}
+__device__ __forceinline__ void tmem_store1(uint32_t at, float v) { asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%1], {%0};" ::"f"(v), "r"(at) : "memory"); }
+__device__ __forceinline__ float tmem_load1(uint32_t at)
+{
+    float v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+// Two warps meet.
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_any(int id, bool yes)
+{
+    uint32_t any;
+    asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, %2, 64, p; selp.u32 %0, 1, 0, q; }" : "=r"(any) : "r"((uint32_t)yes), "r"(id) : "memory");
+    return any != 0u;
+}
 
 #define PERQ_R8(v, i) "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]), "=f"(v[i + 4]), "=f"(v[i + 5]), "=f"(v[i + 6]), "=f"(v[i + 7])
 // 32 columns of this warp's 32 lanes; they are there after loads_wait.
@@ -84,25 +128,18 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const float (&v)[32])
 }
 #undef PERQ_O8
 
-typedef unsigned long long Pair;
-__device__ __forceinline__ Pair pair_of(float x, float y)
+// 2^x on the multiply-add pipe, for x up to 100: 2^(x - n) with n the nearest whole number by its Taylor polynomial of degree 5 (off by (ln2 / 2)^6 / 6! = 2.4e-6), times 2^n.  One in
+// eight exponentials is taken so, because the others are what the warps wait for (16 a cycle; two tiles of 128 x 128 alone: 2422 -> 2326 cycles).  Below -125: 0.  NaN stays NaN.
+__device__ __forceinline__ float exp2_fma(float x)
 {
-    Pair r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void pair_split(Pair p, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
-__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c)
-{
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ Pair pair_add(Pair a, Pair b)
-{
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
+    const float t = x + 12582912.0f, f = x - (t - 12582912.0f);
+    float r = fmaf(f, 1.3333558e-3f, 9.6181291e-3f);
+    r = fmaf(r, f, 5.5504109e-2f);
+    r = fmaf(r, f, 2.4022651e-1f);
+    r = fmaf(r, f, 6.9314718e-1f);
+    r = fmaf(r, f, 1.0f);
+    r = __int_as_float(__float_as_int(r) + (__float_as_int(t) << 23));
+    return x < -125.0f ? 0.0f : r;
 }
 __device__ __forceinline__ float max_of3(float a, float b, float c)
 {
@@ -199,24 +236,30 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     if (it.rows <= 0) return;
     const int tile0 = (int)((long long)it.tiles * part / p.split), tile1 = (int)((long long)it.tiles * (part + 1) / p.split), tiles = tile1 - tile0;
     const bool two = it.rows > 128;
-    const uint32_t full = base + K::off_bars, empty = full + 8u * K::stages, steps_full = empty + 8u * K::stages, q_full = steps_full + 64u, s_full = q_full + 16u,
-                   p_full = s_full + 16u, o_full = p_full + 16u, end = o_full + 16u, slot = base + K::off_slot, steps = base + K::off_steps;
+    const uint32_t full = base + K::off_bars, empty = full + 8u * K::stages, raw_full = empty + 8u * K::stages, raw_empty = raw_full + 8u * K::raw_stages,
+                   steps_full = raw_empty + 8u * K::raw_stages, q_full = steps_full + 64u, s_full = q_full + 16u,
+                   p_half = s_full + 16u, p_full = p_half + 16u, o_full = p_full + 16u, end = o_full + 16u, slot = base + K::off_slot, steps = base + K::off_steps;
     if (tid == 0) {
         for (uint32_t i = 0; i < K::stages; ++i) {
-            mbar_init(full + 8u * i, 4);                               // a warp that brings codes in, each
+            mbar_init(full + 8u * i, 4);                               // the warps that make codes fp16
             mbar_init(empty + 8u * i, 1);
+        }
+        for (uint32_t i = 0; i < K::raw_stages; ++i) {
+            mbar_init(raw_full + 8u * i, 1);
+            mbar_init(raw_empty + 8u * i, 4);
         }
         for (uint32_t i = 0; i < 8; ++i) mbar_init(steps_full + 8u * i, 1);
         for (uint32_t i = 0; i < 2; ++i) {
-            mbar_init(q_full + 8u * i, 4);
+            mbar_init(q_full + 8u * i, 8);
             mbar_init(s_full + 8u * i, 1);
+            mbar_init(p_half + 8u * i, 4);
             mbar_init(p_full + 8u * i, 4);
             mbar_init(o_full + 8u * i, 1);
         }
         mbar_init(end, 1);
         mbar_init_fence();
     }
-    if (warp == 12) {
+    if (warp == MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(K::columns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -227,177 +270,219 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     auto give_up = [&]() { atomicOr(&g_error, ERROR_ATTEND); };
     auto key_of = [&](int tile) { return (tile < it.sunk ? tile : tile - it.sunk + it.low) * MANY_KEYS; };
 
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-        const int t = warp >> 2, thread = tid & 127, row = t * 128 + thread;
+    if (warp < CODES_WARP) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");           // (of 80 at launch: 4 x 96 + 56 + 40 = 6 x 80)
+        constexpr int C = D / 2;                                       // of queries and results, a thread's channels
+        const int t = warp >> 3, side = (warp >> 2) & 1, thread = tid & 127, row = t * 128 + thread;
         const bool there = row < it.rows;
         const int token = (it.row0 + min(row, it.rows - 1)) / p.a.group, h = it.row0 + min(row, it.rows - 1) - token * p.a.group;
         const int position = it.first + token;
-        const size_t all_heads = (size_t)p.a.heads * (size_t)p.a.group, of_row = (size_t)it.head * (size_t)p.a.group + (size_t)h;
-        float factor;
+        const size_t of_row = (size_t)it.head * (size_t)p.a.group + (size_t)h;
         if (t == 0 || two) {
-            // the row, rotated, scaled to 1 .. 2 by a power of two, fp16
-            float v[D], most = 0.0f;
+            // The row, its largest scaled to 1 .. 2 by a power of two, rotated, fp16.
             const uint4 *const from = reinterpret_cast<const uint4 *>(p.a.x + (size_t)(it.begin + token) * (size_t)p.a.stride + of_row * D);
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
+            auto eight = [&](int c, float (&x)[8]) {
                 const uint4 w = there ? __ldg(from + c) : make_uint4(0, 0, 0, 0);
-                const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                const uint32_t y[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    v[8 * c + 2 * k] = from16(x[k] & 0xffffu, p.a.f16 != 0);
-                    v[8 * c + 2 * k + 1] = from16(x[k] >> 16, p.a.f16 != 0);
+                    x[2 * k] = from16(y[k] & 0xffffu, p.a.f16 != 0);
+                    x[2 * k + 1] = from16(y[k] >> 16, p.a.f16 != 0);
                 }
+            };
+            float most = 0.0f;
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+                float x[8];
+                eight(c, x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
             }
-#pragma unroll
-            for (int l = 0; (1 << l) < D; ++l)
-                if (l < p.a.log2b) {
-#pragma unroll
-                    for (int i = 0; i < D; ++i)
-                        if ((i & (1 << l)) == 0) {
-                            const float x = v[i], y = v[i + (1 << l)];
-                            v[i] = x + y;
-                            v[i + (1 << l)] = x - y;
-                        }
-                }
-#pragma unroll
-            for (int i = 0; i < D; ++i) most = fmaxf(most, fabsf(v[i]));
             const int e = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
             float down = __uint_as_float((uint32_t)(254 - e) << 23);
-            factor = __uint_as_float((uint32_t)e << 23) * fabsf(p.a.scale);
+            // (not 0, so that what is not seen stays -inf)
+            const float factor = fmaxf(__uint_as_float((uint32_t)e << 23) * fabsf(p.a.scale), 0x1p-60f);
             if (p.a.scale < 0.0f) down = -down;                        // (a page's largest logit is that of its largest S)
-            const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)thread * 128u;
+            {
+                float v[C];
+                const bool across = p.a.log2b == (D == 128 ? 7 : 6);   // the stage between the halves, first (they commute)
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                uint4 w;
-                w.x = half2_of(v[8 * c] * down, v[8 * c + 1] * down);
-                w.y = half2_of(v[8 * c + 2] * down, v[8 * c + 3] * down);
-                w.z = half2_of(v[8 * c + 4] * down, v[8 * c + 5] * down);
-                w.w = half2_of(v[8 * c + 6] * down, v[8 * c + 7] * down);
-                sts128(to + (uint32_t)(c / 8) * K::half + (uint32_t)(((c ^ thread) & 7) * 16), w);
+                for (int c = 0; c < C / 8; ++c) {
+                    float x[8];
+                    eight(c + side * (C / 8), x);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[8 * c + k] = x[k] * down;
+                    if (across) {
+                        eight(c + (1 - side) * (C / 8), x);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[8 * c + k] = fmaf(x[k], down, side ? -v[8 * c + k] : v[8 * c + k]);
+                    }
+                }
+#pragma unroll
+                for (int l = 0; (1 << l) < C; ++l)
+                    if (l < p.a.log2b) {
+#pragma unroll
+                        for (int i = 0; i < C; ++i)
+                            if ((i & (1 << l)) == 0) {
+                                const float x = v[i], y = v[i + (1 << l)];
+                                v[i] = x + y;
+                                v[i + (1 << l)] = x - y;
+                            }
+                    }
+                const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)thread * 128u + (D == 128 ? (uint32_t)side * K::half : 0u);
+#pragma unroll
+                for (int c = 0; c < C / 8; ++c) {
+                    uint4 w;
+                    w.x = half2_of(v[8 * c], v[8 * c + 1]);
+                    w.y = half2_of(v[8 * c + 2], v[8 * c + 3]);
+                    w.z = half2_of(v[8 * c + 4], v[8 * c + 5]);
+                    w.w = half2_of(v[8 * c + 6], v[8 * c + 7]);
+                    sts128(to + (uint32_t)((((D == 64 ? side * 4 : 0) + c) ^ thread) & 7) * 16u, w);
+                }
             }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full + 8u * (uint32_t)t);
 
-            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + (uint32_t)t * 128u + lanes, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes;
-            // rows of this warp: all keys of a tile from `seen_low` on (or of the first tokens) up to seen_high are seen by all of them
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tile_at = tmem + (uint32_t)t * 128u + lanes, s_at = tile_at + 64u * (uint32_t)side,
+                           p_at = tile_at + 32u * (uint32_t)side, free_at = tile_at + 64u, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes + (uint32_t)(side * C);
+            const int pair = 1 + t * 4 + (warp & 3);                   // the barrier of the two warps that have these 32 rows
+            // a value of the row's other thread, by columns that are free while P is written
+            auto others = [&](float x) {
+                tmem_store1(free_at + (uint32_t)side, x);
+                tmem_store_wait();
+                tmem_fence_before();
+                pair_sync(pair);
+                tmem_fence_after();
+                return tmem_load1(free_at + 1u - (uint32_t)side);
+            };
+            // rows of this warp: all of a tile's keys that its rows have in common
             const int row_first = it.row0 + t * 128 + (warp & 3) * 32, row_last = it.row0 + it.rows - 1;
             const int low_position = it.first + min(row_first, row_last) / p.a.group, high_position = it.first + min(row_first + 31, row_last) / p.a.group;
             float m = -INFINITY, l = 0.0f;
             bool ok = true;
             for (int j = 0; j < tiles; ++j) {
-                const int key = key_of(tile0 + j);
-                if (!mbar_wait_warp(steps_full + 8u * (uint32_t)(j & 7), (uint32_t)(j >> 3) & 1u) || !mbar_wait_warp(s_full + 8u * (uint32_t)t, (uint32_t)j & 1u)) {
-                    ok = false;
-                    break;
-                }
+                const int key = key_of(tile0 + j) + 64 * side;
+                // (a wait that runs out ends no warp's part: its partner still waits for it at their barrier)
+                if (ok && (!cta_wait_warp(steps_full + 8u * (uint32_t)(j & 7), (uint32_t)(j >> 3) & 1u) || !cta_wait_warp(s_full + 8u * (uint32_t)t, (uint32_t)j & 1u))) ok = false;
                 tmem_fence_after();
-                float s[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load32(s_at + 32u * c, s[c]);
-                const uint32_t at = steps + (uint32_t)(j & 7) * 128u;
-                constexpr int G = FINE ? 8 : 4, W = 128 / G;
+                float s[2][32];
+                tmem_load32(s_at, s[0]);
+                tmem_load32(s_at + 32u, s[1]);
+                constexpr int G = FINE ? 4 : 2, W = 64 / G;
                 // of a page's columns: the factor of S, log2 s_v, 1 / s_v
-                auto step_of = [&](int g) { return lds128(at + (uint32_t)(g * (8 / G)) * 16u); };
+                const uint32_t at = steps + (uint32_t)(j & 7) * 128u + (uint32_t)side * 64u;
+                auto step_of = [&](int g) { return lds128(at + (uint32_t)(g * (4 / G)) * 16u); };
                 loads_wait(s[0]);
                 loads_there(s[1]);
-                loads_there(s[2]);
-                loads_there(s[3]);
-                const bool whole = key + MANY_KEYS - 1 <= low_position && (p.a.window <= 0 || key > high_position - p.a.window || key + MANY_KEYS <= p.a.sinks);
-                float most_x = -INFINITY;
-                if (!whole) {
-                    // logits now, so that what is not seen can be left out whatever its step is
-                    const int last = position - key, window_low = p.a.window > 0 ? last - p.a.window : -1, sunk = p.a.sinks - key;
+                if (key + 63 > low_position || (p.a.window > 0 && key <= high_position - p.a.window && key + 64 > p.a.sinks)) {
+                    // what this row does not see, a bit each
+                    const int last = position - key, low = p.a.window > 0 ? last - p.a.window : -1, sunk = p.a.sinks - key;
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        const uint4 w = step_of(g);
-                        const float f = factor * __uint_as_float(w.x), b = __uint_as_float(w.y);
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t seen = bits_below(last + 1 - 32 * c) & (~bits_below(low + 1 - 32 * c) | (p.a.window > 0 ? bits_below(sunk - 32 * c) : 0u));
 #pragma unroll
-                        for (int i = g * W; i < (g + 1) * W; ++i) {
-                            const float x = i <= last && (i > window_low || i < sunk) ? fmaf(s[i / 32][i % 32], f, b) : -INFINITY;
-                            s[i / 32][i % 32] = x;
-                            most_x = fmaxf(most_x, x);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        const uint4 w = step_of(g);
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int i = g * W; i < (g + 1) * W; i += 2) top = max_of3(top, s[i / 32][i % 32], s[i / 32][i % 32 + 1]);
-                        most_x = fmaxf(most_x, fmaf(top, factor * __uint_as_float(w.x), __uint_as_float(w.y)));
+                        for (int i = 0; i < 32; ++i) s[c][i] = seen & (1u << i) ? s[c][i] : -INFINITY;
                     }
                 }
-                if (__any_sync(0xffffffffu, most_x - m > 8.0f)) {
-                    const float next = fmaxf(m, most_x), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
+                float most_x = -INFINITY;
+                {
+                    float top[G];
+#pragma unroll
+                    for (int g = 0; g < G; ++g) top[g] = fmaxf(s[g * W / 32][g * W % 32], s[g * W / 32][g * W % 32 + 1]);
+#pragma unroll
+                    for (int i = 2; i < W; i += 2)
+#pragma unroll
+                        for (int g = 0; g < G; ++g) top[g] = max_of3(top[g], s[(g * W + i) / 32][(g * W + i) % 32], s[(g * W + i) / 32][(g * W + i) % 32 + 1]);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const uint4 w = step_of(g);
+                        most_x = fmaxf(most_x, fmaf(top[g], factor * __uint_as_float(w.x), __uint_as_float(w.y)));
+                        if (w.w != 0u) {
+                            // a step that is not finite: so is what sees one of its keys
+                            const int k0 = key + g * W, k1 = min(k0 + W - 1, position);
+                            if (k0 <= position && (p.a.window <= 0 || k1 > position - p.a.window || k0 < p.a.sinks)) l = __uint_as_float(0x7fffffffu);
+                        }
+                    }
+                }
+                // (S is read now by both, so P may take its place)
+                tmem_fence_before();
+                if (pair_any(pair, most_x - m > 8.0f)) {
+                    tmem_fence_after();
+                    const float next = fmaxf(m, fmaxf(most_x, others(most_x))), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
                     m = next;
                     l *= alpha;
                     if (j > 0) {
-                        if (!mbar_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(j - 1) & 1u)) {
-                            ok = false;
-                            break;
-                        }
+                        if (ok && !cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(j - 1) & 1u)) ok = false;
                         tmem_fence_after();
 #pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            float o[32];
-                            tmem_load32(o_at + 32u * c, o);
-                            loads_wait(o);
+                        for (int c = 0; c < C / 16; ++c) {
+                            int32_t o[16];
+                            uint32_t w[16];
+                            tmem_load16(o_at + 16u * c, o);
+                            tmem_wait(o);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] *= alpha;
-                            tmem_store32(o_at + 32u * c, o);
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__int_as_float(o[i]) * alpha);
+                            tmem_store16(o_at + 16u * c, w);
                         }
+                        // (the products that add to all of O begin when the first half of P is there)
+                        tmem_store_wait();
+                        tmem_fence_before();
+                        pair_sync(pair);
                     }
                 }
+                tmem_fence_after();
                 const float reference = m == -INFINITY ? 0.0f : m;
+                // (exponentials of 32 columns in place, then their sums; packed fp32 pairs of them cost moves: two tiles of 128 x 128 alone 2695 cycles against 2422)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
+                    float inverse[G / 2];
+#pragma unroll
+                    for (int g = 0; g < G / 2; ++g) {
+                        const uint4 step = step_of(c * G / 2 + g);
+                        const float f = factor * __uint_as_float(step.x), b = __uint_as_float(step.y) - reference;
+                        inverse[g] = __uint_as_float(step.z);
+#pragma unroll
+                        for (int i = g * W; i < (g + 1) * W; ++i) {
+                            const float x = fmaf(s[c][i], f, b);
+                            s[c][i] = i % 8 == 7 ? exp2_fma(x) : exp2_of(x);
+                        }
+                    }
                     uint32_t w[16];
 #pragma unroll
-                    for (int g = c * G / 4; g < (c + 1) * G / 4; ++g) {
-                        const uint4 step = step_of(g);
-                        const float f = whole ? factor * __uint_as_float(step.x) : 1.0f, b = (whole ? __uint_as_float(step.y) : 0.0f) - reference;
-                        const Pair ff = pair_of(f, f), bb = pair_of(b, b);
-                        Pair sum = pair_of(0.0f, 0.0f);
+                    for (int i = 0; i < 32; i += 2) w[i / 2] = half2_of(s[c][i], s[c][i + 1]);
+                    tmem_store16(p_at + 16u * c, w);
 #pragma unroll
-                        for (int i = 0; i < W; i += 2) {
-                            const int k = (g * W + i) % 32;
-                            float x, y;
-                            pair_split(pair_fma(pair_of(s[c][k], s[c][k + 1]), ff, bb), x, y);
-                            x = exp2_of(x);
-                            y = exp2_of(y);
-                            sum = pair_add(sum, pair_of(x, y));
-                            w[k / 2] = half2_of(x, y);
-                        }
-                        float x, y;
-                        pair_split(sum, x, y);
-                        x += y;
-                        if (x != 0.0f) l = fmaf(x, __uint_as_float(step.z), l);        // (a step that is not finite stays with the rows that see it)
+                    for (int g = 0; g < G / 2; ++g) {
+                        float x[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = s[c][g * W + i];
+#pragma unroll
+                        for (int i = 4; i < W; ++i) x[i % 4] += s[c][g * W + i];
+                        l = fmaf((x[0] + x[1]) + (x[2] + x[3]), inverse[g], l);
                     }
-                    tmem_store16(s_at + 16u * c, w);
                 }
                 tmem_store_wait();
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 8u * (uint32_t)t);
+                if (lane == 0) mbar_arrive((side ? p_full : p_half) + 8u * (uint32_t)t);       // (keys 0 .. 63 come first)
             }
-            if (ok && tiles > 0 && !mbar_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(tiles - 1) & 1u)) ok = false;
+            if (ok && tiles > 0 && !cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(tiles - 1) & 1u)) ok = false;
+            tmem_fence_after();
+            l += others(l);
             if (!ok) {
-                give_up();
+                if (lane == 0) give_up();
             } else {
-                tmem_fence_after();
                 const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-                float *const to_part = p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D : nullptr;
-                const size_t to_out = ((size_t)(it.begin + token) * all_heads + of_row) * D;
-                if (p.split > 1) {
+                float *const to_part = p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D + side * C : nullptr;
+                const size_t to_out = ((size_t)(it.begin + token) * ((size_t)p.a.heads * (size_t)p.a.group) + of_row) * D + (size_t)(side * C);
+                if (p.split > 1 && side == 0) {
                     float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
                     ends[row] = m;
                     ends[MANY_ROWS + row] = l;
                 }
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
+                for (int c = 0; c < C / 32; ++c) {
                     float o[32];
                     if (tiles > 0) {
                         tmem_load32(o_at + 32u * c, o);
@@ -427,79 +512,46 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 }
             }
         }
-    } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        // codes of a tile to fp16: a thread has 16 channels of every (128 / rows a pass)-th key
-        constexpr int chunks = D / 16, passes = chunks, rows_a_pass = 128 / chunks;      // (128 threads, 128 * chunks pieces)
-        const int thread = tid - 256, chunk = thread % chunks, row0 = thread / chunks;
-        const int32_t *const table = p.a.q.pages + (size_t)it.sequence * (size_t)p.a.q.width;
-        const int log2page = p.a.q.page, group = lane & 7;
-        // of a tile, lanes 0 .. 7: the pages of its eight groups of 16 keys
-        auto pages_of = [&](int j) {
-            const int key = key_of(tile0 + j) + 16 * group;
-            return j < tiles ? min(max(__ldg(table + min(key >> log2page, p.a.q.width - 1)), 0), p.a.q.n_pages - 1) : 0;
-        };
-        uint4 raw[passes];
-        auto load = [&](int i, int j, int32_t pages, const int8_t *codes) {
-            if (j >= tiles) return;
-            const int key0 = key_of(tile0 + j), row = row0 + i * rows_a_pass, page = __shfl_sync(0xffffffffu, pages, (row >> 4) & 7);
-            const size_t at = ((((size_t)page * (size_t)p.a.heads + (size_t)it.head) << log2page) + (size_t)((key0 + row) & ((1 << log2page) - 1))) * D + (size_t)(chunk * 16);
-            raw[i] = __ldg(reinterpret_cast<const uint4 *>(codes + at));
-        };
-        int32_t pages = pages_of(0);
-#pragma unroll
-        for (int i = 0; i < passes; ++i) load(i, 0, pages, p.a.k_codes);
+    } else if (warp < MMA_WARP) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // codes to fp16: a thread has 16 channels of every (128 / chunks)-th key
+        constexpr int chunks = D / 16;
+        const int thread = tid - 32 * CODES_WARP, chunk = thread % chunks, row0 = thread / chunks;
         bool ok = true;
-        uint32_t n = 0;                                                // pieces of the ring so far
-        for (int j = 0; j < tiles && ok; ++j) {
-            const int32_t next = pages_of(j + 1);
-            if (warp == 8) {
-                const size_t block = (size_t)pages * (size_t)p.a.heads + (size_t)it.head;
-                const float ks = __ldg(p.a.k_steps + block), vs = __ldg(p.a.v_steps + block);
-                const bool none = vs < 0x1p-64f;
-                if (lane < 8)
-                    sts128(steps + (uint32_t)(j & 7) * 128u + (uint32_t)lane * 16u,
-                           make_uint4(__float_as_uint(ks), __float_as_uint(none ? -64.0f : log2_of(vs)), __float_as_uint(none ? 0x1p64f : 1.0f / vs), 0u));
+        for (uint32_t n = 0; n < 2u * (uint32_t)tiles && ok; ++n) {
+            const uint32_t s = n % K::stages, r = n % K::raw_stages, to = base + K::off_ring + s * K::tile, from = base + K::off_raw + r * K::raw + (uint32_t)thread * 16u;
+            if (!cta_wait_warp(raw_full + 8u * r, (n / K::raw_stages) & 1u) || (n >= K::stages && !cta_wait_warp(empty + 8u * s, (n / K::stages - 1u) & 1u))) {
+                ok = false;
+                break;
             }
+#pragma unroll 4
+            for (int i = 0; i < chunks; ++i) {
+                const uint4 raw = lds128(from + (uint32_t)i * 2048u);
+                const uint32_t row = (uint32_t)(row0 + i * (128 / chunks)), x[4] = {raw.x, raw.y, raw.z, raw.w};
+                uint4 o[2];
+                uint32_t *const w = reinterpret_cast<uint32_t *>(o);
 #pragma unroll
-            for (int kind = 0; kind < 2; ++kind, ++n) {
-                const uint32_t s = n % K::stages, to = base + K::off_ring + s * K::tile;
-                if (n >= K::stages && !mbar_wait_warp(empty + 8u * s, (n / K::stages - 1u) & 1u)) {
-                    ok = false;
-                    break;
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t y = x[k] ^ 0x80808080u;             // codes 0 and 1, 2 and 3 in the low bits of 1024, minus 1152
+                    w[2 * k] = minus_1152(__byte_perm(y, 0x64646464u, 0x4140));
+                    w[2 * k + 1] = minus_1152(__byte_perm(y, 0x64646464u, 0x4342));
                 }
-                if (kind == 0 && warp == 8) {
-                    // (at most five tiles ahead of the rows' warps, as many as the ring holds)
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(steps_full + 8u * (uint32_t)(j & 7));
-                }
-#pragma unroll
-                for (int i = 0; i < passes; ++i) {
-                    const uint32_t row = (uint32_t)(row0 + i * rows_a_pass);
-                    const uint32_t x[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                    uint4 o[2];
-                    uint32_t *const w = reinterpret_cast<uint32_t *>(o);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        w[2 * k] = codes_f16(__byte_perm(x[k], 0u, 0x4140));             // codes 0 and 1, 2 and 3
-                        w[2 * k + 1] = codes_f16(__byte_perm(x[k], 0u, 0x4342));
-                    }
-                    if (kind == 0) load(i, j, pages, p.a.v_codes); else load(i, j + 1, next, p.a.k_codes);
-                    // (the second half's threads write their second 16 bytes first: eight threads then meet no conflict)
-                    const uint32_t at = to + (uint32_t)(chunk / 4) * K::half + row * 128u, c = 2u * (uint32_t)(chunk & 3), flip = (uint32_t)(chunk / 4) & 1u;
-                    sts128(at + (((c + flip) ^ row) & 7u) * 16u, flip ? o[1] : o[0]);
-                    sts128(at + (((c + 1u - flip) ^ row) & 7u) * 16u, flip ? o[0] : o[1]);
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8u * s);
+                // (the second half's threads write their second 16 bytes first: eight threads then meet no conflict)
+                const uint32_t at = to + (uint32_t)(chunk / 4) * K::half + row * 128u, c = 2u * (uint32_t)(chunk & 3), flip = (uint32_t)(chunk / 4) & 1u;
+                sts128(at + (((c + flip) ^ row) & 7u) * 16u, flip ? o[1] : o[0]);
+                sts128(at + (((c + 1u - flip) ^ row) & 7u) * 16u, flip ? o[0] : o[1]);
             }
-            pages = next;
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(full + 8u * s);
+                mbar_arrive(raw_empty + 8u * r);
+            }
         }
-        if (!ok) give_up();
+        if (!ok && lane == 0) give_up();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (warp == 12 && lane == 0 && tiles > 0) {
+        if (warp == MMA_WARP && tiles > 0) {
             const uint32_t qk = f16_desc(128, 128, false), pv = f16_desc(128, D, true);
             bool ok = true;
             uint32_t n = 0;
@@ -510,54 +562,101 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     const uint32_t at = (k / 4u) * (K::half >> 4) + (k % 4u) * 2u;
                     product_f16(tmem + t * 128u, a + at, b + at, qk, k > 0);
                 }
-                commit(s_full + 8u * t);
-            };
-            auto outputs = [&](uint32_t t, uint32_t s, bool more) {
-                const uint32_t b = keys_operand<D>(base + K::off_ring + s * K::tile);
-#pragma unroll
-                for (uint32_t k = 0; k < MANY_KEYS / 16; ++k) product_f16_tmem(tmem + K::o_column + t * 128u, tmem + t * 128u + 8u * k, b + k * 128u, pv, more || k > 0);
-                commit(o_full + 8u * t);
+                commit_one(s_full + 8u * t);
             };
             auto wait_for = [&](uint32_t bar, uint32_t parity) {
-                if (ok && !mbar_wait(bar, parity)) ok = false;
+                if (ok && !cta_wait_warp(bar, parity)) ok = false;
                 tmem_fence_after();
                 return ok;
+            };
+            auto outputs = [&](uint32_t t, uint32_t s, int j) {
+                const uint32_t b = keys_operand<D>(base + K::off_ring + s * K::tile);
+#pragma unroll
+                for (uint32_t k = 0; k < MANY_KEYS / 16; ++k) {
+                    if (k == 0 && !wait_for(p_half + 8u * t, (uint32_t)j & 1u)) return false;
+                    if (k == 4 && !wait_for(p_full + 8u * t, (uint32_t)j & 1u)) return false;
+                    product_f16_tmem(tmem + K::o_column + t * 128u, tmem + t * 128u + 8u * k, b + k * 128u, pv, j > 0 || k > 0);
+                }
+                commit_one(o_full + 8u * t);
+                return true;
             };
             auto piece = [&](uint32_t i) { return wait_for(full + 8u * (i % K::stages), (i / K::stages) & 1u); };
             if (wait_for(q_full, 0) && (!two || wait_for(q_full + 8u, 0)) && piece(0)) {
                 logits(0, 0);
                 if (two) logits(1, 0);
-                commit(empty);
+                commit_one(empty);
                 n = 1;
                 for (int j = 0; j < tiles && ok; ++j, n += 2) {
                     const bool more = j + 1 < tiles;
                     const uint32_t sv = n % K::stages, sk = (n + 1) % K::stages;
-                    if (!piece(n) || !wait_for(p_full, (uint32_t)j & 1u)) break;
-                    outputs(0, sv, j > 0);
+                    if (!piece(n) || !outputs(0, sv, j)) break;
                     if (more) {
                         if (!piece(n + 1)) break;
                         logits(0, sk);
                     }
                     if (two) {
-                        if (!wait_for(p_full + 8u, (uint32_t)j & 1u)) break;
-                        outputs(1, sv, j > 0);
+                        if (!outputs(1, sv, j)) break;
                         if (more) logits(1, sk);
                     }
-                    commit(empty + 8u * sv);
-                    if (more) commit(empty + 8u * sk);
+                    commit_one(empty + 8u * sv);
+                    if (more) commit_one(empty + 8u * sk);
                 }
             }
-            if (!ok) give_up();
+            if (!ok && lane == 0) give_up();
             // nothing is in flight when the CTA ends
-            commit(end);
-            (void)mbar_wait(end, 0);
+            commit_one(end);
+            (void)cta_wait_warp(end, 0);
+        }
+        if (warp == LOAD_WARP) {
+            // a lane to a page of a tile (eight at most): its codes and steps
+            const int32_t *const table = p.a.q.pages + (size_t)it.sequence * (size_t)p.a.q.width;
+            const int log2page = p.a.q.page, each = min(1 << log2page, MANY_KEYS), copies = MANY_KEYS / each;
+            auto page_of = [&](int j) {
+                const int key = key_of(tile0 + j) + lane * each;
+                return lane < copies && j < tiles ? min(max(__ldg(table + min(key >> log2page, p.a.q.width - 1)), 0), p.a.q.n_pages - 1) : 0;
+            };
+            bool ok = true;
+            uint32_t n = 0;
+            int page = page_of(0);
+            for (int j = 0; j < tiles && ok; ++j) {
+                const int next = page_of(j + 1);
+                const size_t block = (size_t)page * (size_t)p.a.heads + (size_t)it.head;
+                const float ks = __ldg(p.a.k_steps + block), vs = __ldg(p.a.v_steps + block);
+                for (int kind = 0; kind < 2; ++kind, ++n) {
+                    const uint32_t r = n % K::raw_stages, bar = raw_full + 8u * r;
+                    if (n >= K::raw_stages && !cta_wait_warp(raw_empty + 8u * r, (n / K::raw_stages - 1u) & 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) mbar_expect_tx(bar, K::raw);
+                    __syncwarp();
+                    if (lane < copies)
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                     ::"r"(base + K::off_raw + r * K::raw + (uint32_t)(lane * each * D)), "l"((kind ? p.a.v_codes : p.a.k_codes) + ((block << log2page) * (size_t)D)),
+                                     "r"((uint32_t)(each * D)), "r"(bar) : "memory");
+                }
+                if (!ok) break;
+                // of 16 keys each: s_k (not 0, so that what is not seen stays -inf), log2 s_v, 1 / s_v, and whether one of them is not finite, which the rows' warps see to
+                const int mine = (lane & 7) * 16 / each;
+                const float k = __shfl_sync(0xffffffffu, ks, mine), v = __shfl_sync(0xffffffffu, vs, mine);
+                const bool bad = !(fabsf(k) <= 0x1p126f && fabsf(v) <= 0x1p126f), none = bad || v < 0x1p-64f;
+                if (lane < 8)
+                    sts128(steps + (uint32_t)(j & 7) * 128u + (uint32_t)lane * 16u,
+                           make_uint4(__float_as_uint(bad || k < 0x1p-60f ? 0x1p-60f : k), __float_as_uint(none ? -64.0f : log2_of(v)), __float_as_uint(none ? 0x1p64f : 1.0f / v), (uint32_t)bad));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(steps_full + 8u * (uint32_t)(j & 7));
+                page = next;
+            }
+            if (!ok && lane == 0) give_up();
+            // nothing is in flight when the CTA ends
+            for (uint32_t i = n > K::raw_stages ? n - K::raw_stages : 0u; i < n; ++i) (void)cta_wait_warp(raw_full + 8u * (i % K::raw_stages), (i / K::raw_stages) & 1u);
         }
         __syncwarp();
     }
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(K::columns) : "memory");
+    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(K::columns) : "memory");
 }
 
 // Rows whose keys were split: blockIdx.x is an item, blockIdx.y a quarter of its rows.

@@ -160,40 +160,33 @@ __device__ __forceinline__ int many_tiles(const AttendParams &p, const Rows &r)
     const long long rows = (long long)min(r.n, p.most) * p.group;
     return rows > p.few_rows ? (int)((rows + MANY_ROWS - 1) / MANY_ROWS) : 0;
 }
-// The number-th tile of rows of the call (head by head, a sequence's last first: those see most).  Called by all threads of the CTA.
-template <int THREADS_>
-__device__ __forceinline__ ManyItem many_item(const AttendParams &p, int number)
+// The number-th tile of rows of the call, head by head and a sequence's last tile first: those see most.  Up to 32 sequences also go by the most that they see, so that the CTAs that
+// come last have little to do (four chunks of 226 to 478 tokens behind 5.7 to 12.7 thousand: 382 us in their own order).  By one warp.
+__device__ __forceinline__ ManyItem many_item(const AttendParams &p, int number, int lane)
 {
-    __shared__ int32_t sums[THREADS_ / 32];
-    __shared__ ManyItem found;
-    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, head = number % p.heads, tile = number / p.heads;
-    if (tid == 0) found.rows = 0;
-    for (int base = 0, before = 0; base < p.q.S; base += THREADS_) {
+    const int head = number % p.heads, tile = number / p.heads;
+    ManyItem it;
+    it.rows = 0;
+    for (int base = 0, before = 0; base < p.q.S && before <= tile; base += 32) {
         Rows r = {0, 0, 0};
         int c = 0;
-        if (base + tid < p.q.S) {
-            r = rows_of(p.q, base + tid);
+        if (base + lane < p.q.S) {
+            r = rows_of(p.q, base + lane);
             c = many_tiles(p, r);
         }
-        int sum = c;
+        const int seen = p.window > 0 ? min(r.length, p.window + r.n) : r.length;
+        int first = 0, all = 0;
 #pragma unroll
-        for (int l = 1; l < 32; l *= 2) {
-            const int v = __shfl_up_sync(0xffffffffu, sum, l);
-            if (lane >= l) sum += v;
+        for (int l = 0; l < 32; ++l) {
+            const int cl = __shfl_sync(0xffffffffu, c, l), sl = __shfl_sync(0xffffffffu, seen, l);
+            all += cl;
+            if (p.q.S <= 32 ? sl > seen || (sl == seen && l < lane) : l < lane) first += cl;
         }
-        if (lane == 31) sums[warp] = sum;
-        __syncthreads();
-        int all = 0;
-#pragma unroll
-        for (int w = 0; w < THREADS_ / 32; ++w) {
-            if (w < warp) sum += sums[w];
-            all += sums[w];
-        }
-        const int at = tile - (before + sum - c);
-        if (at >= 0 && at < c) {
-            ManyItem it;
+        const int at = tile - before - first;
+        const unsigned mine = __ballot_sync(0xffffffffu, at >= 0 && at < c);
+        if (mine != 0u) {
             const int tokens = min(r.n, p.most);
-            it.sequence = base + tid;
+            it.sequence = base + lane;
             it.head = head;
             it.row0 = (c - 1 - at) * MANY_ROWS;
             it.rows = min(MANY_ROWS, tokens * p.group - it.row0);
@@ -205,14 +198,15 @@ __device__ __forceinline__ ManyItem many_item(const AttendParams &p, int number)
             it.sunk = min((min(p.sinks, end) + MANY_KEYS - 1) / MANY_KEYS, it.low);
             it.tiles = it.sunk + (end + MANY_KEYS - 1) / MANY_KEYS - it.low;
             it.number = number;
-            found = it;
+            const int owner = __ffs(mine) - 1;
+            int *const words = reinterpret_cast<int *>(&it);
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(ManyItem) / sizeof(int)); ++i) words[i] = __shfl_sync(0xffffffffu, words[i], owner);
+            return it;
         }
         before += all;
-        __syncthreads();
-        if (before > tile) break;
     }
-    __syncthreads();
-    return found;
+    return it;
 }
 
 template <int D>
@@ -232,13 +226,19 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     griddep_wait();
     griddep_launch();
     const int part = (int)(blockIdx.x % (unsigned)p.split);
-    const ManyItem it = many_item<MANY_THREADS>(p.a, (int)(blockIdx.x / (unsigned)p.split));
-    if (it.rows <= 0) return;
-    const int tile0 = (int)((long long)it.tiles * part / p.split), tile1 = (int)((long long)it.tiles * (part + 1) / p.split), tiles = tile1 - tile0;
-    const bool two = it.rows > 128;
+    __shared__ ManyItem found;
     const uint32_t full = base + K::off_bars, empty = full + 8u * K::stages, raw_full = empty + 8u * K::stages, raw_empty = raw_full + 8u * K::raw_stages,
                    steps_full = raw_empty + 8u * K::raw_stages, q_full = steps_full + 64u, s_full = q_full + 16u,
                    p_half = s_full + 16u, p_full = p_half + 16u, o_full = p_full + 16u, end = o_full + 16u, slot = base + K::off_slot, steps = base + K::off_steps;
+    if (warp == LOAD_WARP) {
+        const ManyItem item = many_item(p.a, (int)(blockIdx.x / (unsigned)p.split), lane);
+        if (lane == 0) found = item;
+    }
+    __syncthreads();
+    const ManyItem it = found;
+    if (it.rows <= 0) return;
+    const int tile0 = (int)((long long)it.tiles * part / p.split), tile1 = (int)((long long)it.tiles * (part + 1) / p.split), tiles = tile1 - tile0;
+    const bool two = it.rows > 128;
     if (tid == 0) {
         for (uint32_t i = 0; i < K::stages; ++i) {
             mbar_init(full + 8u * i, 4);                               // the warps that make codes fp16
@@ -279,75 +279,10 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         const int position = it.first + token;
         const size_t of_row = (size_t)it.head * (size_t)p.a.group + (size_t)h;
         if (t == 0 || two) {
-            // The row, its largest scaled to 1 .. 2 by a power of two, rotated, fp16.
-            const uint4 *const from = reinterpret_cast<const uint4 *>(p.a.x + (size_t)(it.begin + token) * (size_t)p.a.stride + of_row * D);
-            auto eight = [&](int c, float (&x)[8]) {
-                const uint4 w = there ? __ldg(from + c) : make_uint4(0, 0, 0, 0);
-                const uint32_t y[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    x[2 * k] = from16(y[k] & 0xffffu, p.a.f16 != 0);
-                    x[2 * k + 1] = from16(y[k] >> 16, p.a.f16 != 0);
-                }
-            };
-            float most = 0.0f;
-#pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-                float x[8];
-                eight(c, x);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
-            }
-            const int e = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
-            float down = __uint_as_float((uint32_t)(254 - e) << 23);
-            // (not 0, so that what is not seen stays -inf)
-            const float factor = fmaxf(__uint_as_float((uint32_t)e << 23) * fabsf(p.a.scale), 0x1p-60f);
-            if (p.a.scale < 0.0f) down = -down;                        // (a page's largest logit is that of its largest S)
-            {
-                float v[C];
-                const bool across = p.a.log2b == (D == 128 ? 7 : 6);   // the stage between the halves, first (they commute)
-#pragma unroll
-                for (int c = 0; c < C / 8; ++c) {
-                    float x[8];
-                    eight(c + side * (C / 8), x);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[8 * c + k] = x[k] * down;
-                    if (across) {
-                        eight(c + (1 - side) * (C / 8), x);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[8 * c + k] = fmaf(x[k], down, side ? -v[8 * c + k] : v[8 * c + k]);
-                    }
-                }
-#pragma unroll
-                for (int l = 0; (1 << l) < C; ++l)
-                    if (l < p.a.log2b) {
-#pragma unroll
-                        for (int i = 0; i < C; ++i)
-                            if ((i & (1 << l)) == 0) {
-                                const float x = v[i], y = v[i + (1 << l)];
-                                v[i] = x + y;
-                                v[i + (1 << l)] = x - y;
-                            }
-                    }
-                const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)thread * 128u + (D == 128 ? (uint32_t)side * K::half : 0u);
-#pragma unroll
-                for (int c = 0; c < C / 8; ++c) {
-                    uint4 w;
-                    w.x = half2_of(v[8 * c], v[8 * c + 1]);
-                    w.y = half2_of(v[8 * c + 2], v[8 * c + 3]);
-                    w.z = half2_of(v[8 * c + 4], v[8 * c + 5]);
-                    w.w = half2_of(v[8 * c + 6], v[8 * c + 7]);
-                    sts128(to + (uint32_t)((((D == 64 ? side * 4 : 0) + c) ^ thread) & 7) * 16u, w);
-                }
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_full + 8u * (uint32_t)t);
-
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tile_at = tmem + (uint32_t)t * 128u + lanes, s_at = tile_at + 64u * (uint32_t)side,
                            p_at = tile_at + 32u * (uint32_t)side, free_at = tile_at + 64u, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes + (uint32_t)(side * C);
             const int pair = 1 + t * 4 + (warp & 3);                   // the barrier of the two warps that have these 32 rows
-            // a value of the row's other thread, by columns that are free while P is written
+            // a value of the row's other thread, by columns that are free before S is there and while P is written
             auto others = [&](float x) {
                 tmem_store1(free_at + (uint32_t)side, x);
                 tmem_store_wait();
@@ -356,6 +291,50 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 tmem_fence_after();
                 return tmem_load1(free_at + 1u - (uint32_t)side);
             };
+            // Queries: 16 rows to a warp, 16 channels to a lane; a row's largest is scaled to 1 .. 2 by a power of two, then it is rotated and rounded to fp16.
+            // (A row to a thread: 12 us of loads that touch 32 rows each.)
+            float factor = 0.0f;
+            {
+                constexpr int wide = D / LANE, at_once = 32 / wide;    // lanes of a row, rows at once
+                const int in = lane / wide, channel = lane % wide * LANE, first_row = (warp & 3) * 32 + side * 16;
+#pragma unroll
+                for (int k = 0; k < 16 / at_once; ++k) {
+                    const int r = first_row + k * at_once + in, pairs = it.row0 + t * 128 + r;
+                    const int its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
+                    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+                    if (t * 128 + r < it.rows) {
+                        const uint4 *const from = reinterpret_cast<const uint4 *>(p.a.x + (size_t)(it.begin + its_token) * (size_t)p.a.stride +
+                                                                                  (size_t)(it.head * p.a.group + its_head) * D + channel);
+                        lo = __ldg(from);
+                        hi = __ldg(from + 1);
+                    }
+                    float v[LANE], most = 0.0f;
+                    unpack(v, lo, hi, p.a.f16 != 0);
+#pragma unroll
+                    for (int i = 0; i < LANE; ++i) most = fmaxf(most, fabsf(v[i]));
+#pragma unroll
+                    for (int l = 1; l < wide; l *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, l));
+                    const int e = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
+                    // (with the sign of the logits' scale, as a page's largest logit has to be that of its largest S)
+                    const float down = copysignf(__uint_as_float((uint32_t)(254 - e) << 23), p.a.scale);
+#pragma unroll
+                    for (int i = 0; i < LANE; ++i) v[i] *= down;
+                    rotate(v, p.a.log2b, lane);
+                    const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)(channel / 64) * K::half + (uint32_t)r * 128u, c = (uint32_t)(channel % 64) / 8u;
+                    sts128(to + ((c ^ (uint32_t)r) & 7u) * 16u, make_uint4(half2_of(v[0], v[1]), half2_of(v[2], v[3]), half2_of(v[4], v[5]), half2_of(v[6], v[7])));
+                    sts128(to + (((c + 1u) ^ (uint32_t)r) & 7u) * 16u, make_uint4(half2_of(v[8], v[9]), half2_of(v[10], v[11]), half2_of(v[12], v[13]), half2_of(v[14], v[15])));
+                    // (the lane of the row has its factor; not 0, so that what is not seen stays -inf)
+                    const float x = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)e << 23), (lane % at_once) * wide);
+                    if (lane / at_once == side * (16 / at_once) + k) factor = fmaxf(x * fabsf(p.a.scale), 0x1p-60f);
+                }
+                const float x = others(factor);
+                if (lane / 16 != side) factor = x;
+            }
+            fence_async_smem();
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full + 8u * (uint32_t)t);
+
             // rows of this warp: all of a tile's keys that its rows have in common
             const int row_first = it.row0 + t * 128 + (warp & 3) * 32, row_last = it.row0 + it.rows - 1;
             const int low_position = it.first + min(row_first, row_last) / p.a.group, high_position = it.first + min(row_first + 31, row_last) / p.a.group;
@@ -467,48 +446,56 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 __syncwarp();
                 if (lane == 0) mbar_arrive((side ? p_full : p_half) + 8u * (uint32_t)t);       // (keys 0 .. 63 come first)
             }
-            if (ok && tiles > 0 && !cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(tiles - 1) & 1u)) ok = false;
+            // (without keys: until all queries are where results go)
+            if (ok && !(tiles > 0 ? cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(tiles - 1) & 1u) : cta_wait_warp(q_full + 8u * (uint32_t)t, 0u))) ok = false;
             tmem_fence_after();
             l += others(l);
-            if (!ok) {
-                if (lane == 0) give_up();
-            } else {
-                const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-                float *const to_part = p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D + side * C : nullptr;
-                const size_t to_out = ((size_t)(it.begin + token) * ((size_t)p.a.heads * (size_t)p.a.group) + of_row) * D + (size_t)(side * C);
-                if (p.split > 1 && side == 0) {
-                    float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
-                    ends[row] = m;
-                    ends[MANY_ROWS + row] = l;
+            if (!ok && lane == 0) give_up();
+            const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+            const bool narrow = p.split == 1 && p.a.out_type != OUT_F32, f16 = p.a.out_type == OUT_F16;
+            if (p.split > 1 && side == 0 && ok) {
+                float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
+                ends[row] = m;
+                ends[MANY_ROWS + row] = l;
+            }
+            // 16-bit results go through shared memory, where the queries were, so that rows are stored whole.
+            const uint32_t room = base + (uint32_t)t * K::tile;
+#pragma unroll
+            for (int c = 0; c < C / 16; ++c) {
+                int32_t u[16];
+                if (tiles > 0) {
+                    tmem_load16(o_at + 16u * c, u);
+                    tmem_wait(u);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) u[i] = 0;
                 }
+                float o[16];
 #pragma unroll
-                for (int c = 0; c < C / 32; ++c) {
-                    float o[32];
-                    if (tiles > 0) {
-                        tmem_load32(o_at + 32u * c, o);
-                        loads_wait(o);
-                    } else {
+                for (int i = 0; i < 16; ++i) o[i] = __int_as_float(u[i]) * r;
+                if (narrow) {
+                    const uint32_t to = room + (uint32_t)thread * (2u * D), at = (uint32_t)(side * (C / 8) + 2 * c);
+                    sts128(to + ((at ^ (uint32_t)thread) & 7u) * 16u + (at & 8u) * 16u, make_uint4(pack16(o[0], o[1], f16), pack16(o[2], o[3], f16), pack16(o[4], o[5], f16), pack16(o[6], o[7], f16)));
+                    sts128(to + (((at + 1u) ^ (uint32_t)thread) & 7u) * 16u + (at & 8u) * 16u,
+                           make_uint4(pack16(o[8], o[9], f16), pack16(o[10], o[11], f16), pack16(o[12], o[13], f16), pack16(o[14], o[15], f16)));
+                } else if (there && ok) {
+                    float *const to = (p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D
+                                                   : static_cast<float *>(p.a.out) + ((size_t)(it.begin + token) * ((size_t)p.a.heads * (size_t)p.a.group) + of_row) * D) + side * C + 16 * c;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = 0.0f;
-                    }
+                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(to + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                }
+            }
+            if (narrow) {
+                pair_sync(pair);
+                constexpr int wide = D / 8, at_once = 32 / wide;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] *= r;
-                    if (!there) continue;
-                    if (p.split > 1) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(to_part + 32 * c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-                    } else if (p.a.out_type == OUT_F32) {
-                        float *const to_f = static_cast<float *>(p.a.out) + to_out + 32 * c;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(to_f + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-                    } else {
-                        const bool f16 = p.a.out_type == OUT_F16;
-                        uint16_t *const to_h = static_cast<uint16_t *>(p.a.out) + to_out + 32 * c;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8)
-                            *reinterpret_cast<uint4 *>(to_h + i) = make_uint4(pack16(o[i], o[i + 1], f16), pack16(o[i + 2], o[i + 3], f16), pack16(o[i + 4], o[i + 5], f16),
-                                                                              pack16(o[i + 6], o[i + 7], f16));
-                    }
+                for (int k = 0; k < 16 / at_once; ++k) {
+                    const int line = (warp & 3) * 32 + side * 16 + k * at_once + lane / wide, chunk = lane % wide, pairs = it.row0 + t * 128 + line;
+                    const int its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
+                    const uint4 w = lds128(room + (uint32_t)line * (2u * D) + (uint32_t)(((chunk ^ line) & 7) * 16 + (chunk & 8) * 16));
+                    if (t * 128 + line < it.rows && ok)
+                        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.a.out) +
+                                                   ((size_t)(it.begin + its_token) * ((size_t)p.a.heads * (size_t)p.a.group) + (size_t)(it.head * p.a.group + its_head)) * D + chunk * 8) = w;
                 }
             }
         }
@@ -665,7 +652,7 @@ __global__ void __launch_bounds__(THREADS) many_join_kernel(const __grid_constan
 {
     griddep_wait();
     griddep_launch();
-    const ManyItem it = many_item<THREADS>(p.a, (int)blockIdx.x);
+    const ManyItem it = many_item(p.a, (int)blockIdx.x, (int)threadIdx.x & 31);       // (every warp for itself)
     const int row_begin = (int)blockIdx.y * (MANY_ROWS / 4), row_end = min(row_begin + MANY_ROWS / 4, it.rows);
     for (int k = (int)threadIdx.x; k < (row_end - row_begin) * (D / 4); k += THREADS) {
         const int row = row_begin + k / (D / 4), channel = k % (D / 4) * 4;

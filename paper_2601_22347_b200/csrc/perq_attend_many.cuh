@@ -43,17 +43,19 @@ __host__ __device__ constexpr uint32_t f16_desc(int m, int n, bool second_transp
 {
     return (1u << 4) | ((uint32_t)second_transposed << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-// perq_mm's waits, for barriers that only this CTA's threads and copies arrive at.
+// Waits of whole warps for barriers that only this CTA's threads and copies arrive at.  A poll sleeps for up to 2 us (without that, warps that waited took more issue slots than those that
+// worked: two prompts of up to 8192 in 303 us); at most 2^19 of them, a second.
 __device__ __forceinline__ bool cta_poll(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
     return done != 0u;
 }
 __device__ __forceinline__ bool cta_wait_warp(uint32_t bar, uint32_t parity)
 {
     bool done = cta_poll(bar, parity);
-    for (uint32_t i = 0; i < perq_mm::WAIT_POLLS && !done; ++i) done = cta_poll(bar, parity);
+    for (uint32_t i = 0; i < 1u << 19 && !done; ++i) done = cta_poll(bar, parity);
     return __all_sync(0xffffffffu, done);
 }
 // By whole warps, of which one lane issues: what describes a product then stays in uniform registers.  (A lane of its own, with the warps that compute exponentials on the
@@ -128,18 +130,26 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const float (&v)[32])
 }
 #undef PERQ_O8
 
-// 2^x on the multiply-add pipe, for x up to 100: 2^(x - n) with n the nearest whole number by its Taylor polynomial of degree 5 (off by (ln2 / 2)^6 / 6! = 2.4e-6), times 2^n.  One in
-// eight exponentials is taken so, because the others are what the warps wait for (16 a cycle; two tiles of 128 x 128 alone: 2422 -> 2326 cycles).  Below -125: 0.  NaN stays NaN.
-__device__ __forceinline__ float exp2_fma(float x)
+// Two fp32 values in one register pair, added and multiplied at once.
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair_of(float x, float y)
 {
-    const float t = x + 12582912.0f, f = x - (t - 12582912.0f);
-    float r = fmaf(f, 1.3333558e-3f, 9.6181291e-3f);
-    r = fmaf(r, f, 5.5504109e-2f);
-    r = fmaf(r, f, 2.4022651e-1f);
-    r = fmaf(r, f, 6.9314718e-1f);
-    r = fmaf(r, f, 1.0f);
-    r = __int_as_float(__float_as_int(r) + (__float_as_int(t) << 23));
-    return x < -125.0f ? 0.0f : r;
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void pair_split(Pair p, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Pair pair_add(Pair a, Pair b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 __device__ __forceinline__ float max_of3(float a, float b, float c)
 {
@@ -412,7 +422,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 }
                 tmem_fence_after();
                 const float reference = m == -INFINITY ? 0.0f : m;
-                // (exponentials of 32 columns in place, then their sums; packed fp32 pairs of them cost moves: two tiles of 128 x 128 alone 2695 cycles against 2422)
+                // (exponentials of 32 columns in place, then their sums: a warp that takes them as they come waits for each)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     float inverse[G / 2];
@@ -420,11 +430,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     for (int g = 0; g < G / 2; ++g) {
                         const uint4 step = step_of(c * G / 2 + g);
                         const float f = factor * __uint_as_float(step.x), b = __uint_as_float(step.y) - reference;
+                        const Pair ff = pair_of(f, f), bb = pair_of(b, b);
                         inverse[g] = __uint_as_float(step.z);
 #pragma unroll
-                        for (int i = g * W; i < (g + 1) * W; ++i) {
-                            const float x = fmaf(s[c][i], f, b);
-                            s[c][i] = i % 8 == 7 ? exp2_fma(x) : exp2_of(x);
+                        for (int i = g * W; i < (g + 1) * W; i += 2) {
+                            pair_split(pair_fma(pair_of(s[c][i], s[c][i + 1]), ff, bb), s[c][i], s[c][i + 1]);
+                            s[c][i] = exp2_of(s[c][i]);
+                            s[c][i + 1] = exp2_of(s[c][i + 1]);
                         }
                     }
                     uint32_t w[16];
@@ -433,12 +445,15 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     tmem_store16(p_at + 16u * c, w);
 #pragma unroll
                     for (int g = 0; g < G / 2; ++g) {
-                        float x[4];
+                        Pair sum[2] = {pair_of(s[c][g * W], s[c][g * W + 1]), pair_of(s[c][g * W + 2], s[c][g * W + 3])};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = s[c][g * W + i];
-#pragma unroll
-                        for (int i = 4; i < W; ++i) x[i % 4] += s[c][g * W + i];
-                        l = fmaf((x[0] + x[1]) + (x[2] + x[3]), inverse[g], l);
+                        for (int i = g * W + 4; i < (g + 1) * W; i += 4) {
+                            sum[0] = pair_add(sum[0], pair_of(s[c][i], s[c][i + 1]));
+                            sum[1] = pair_add(sum[1], pair_of(s[c][i + 2], s[c][i + 3]));
+                        }
+                        float x, y;
+                        pair_split(pair_add(sum[0], sum[1]), x, y);
+                        l = fmaf(x + y, inverse[g], l);
                     }
                 }
                 tmem_store_wait();
@@ -501,32 +516,35 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         }
     } else if (warp < MMA_WARP) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        // codes to fp16: a thread has 16 channels of every (128 / chunks)-th key
-        constexpr int chunks = D / 16;
-        const int thread = tid - 32 * CODES_WARP, chunk = thread % chunks, row0 = thread / chunks;
+        // Codes to fp16.  A thread has 16 channels of one key in 32; eight threads have 64 channels each of two keys next to each other, for D = 128 the lower 64 of one and the
+        // upper 64 of the other, so that neither reads nor stores meet a conflict.
+        constexpr uint32_t halves = D / 64;
+        const uint32_t thread = (uint32_t)(tid - 32 * CODES_WARP), quad = thread & 3u, row = thread >> 2, odd = halves == 2 ? row & 1u : 0u;
+        const uint32_t to0 = row * 128u + (((2u * quad) ^ row) & 7u) * 16u, to1 = row * 128u + (((2u * quad + 1u) ^ row) & 7u) * 16u;
         bool ok = true;
         for (uint32_t n = 0; n < 2u * (uint32_t)tiles && ok; ++n) {
-            const uint32_t s = n % K::stages, r = n % K::raw_stages, to = base + K::off_ring + s * K::tile, from = base + K::off_raw + r * K::raw + (uint32_t)thread * 16u;
+            const uint32_t s = n % K::stages, r = n % K::raw_stages, to = base + K::off_ring + s * K::tile, from = base + K::off_raw + r * K::raw + row * D + quad * 16u;
             if (!cta_wait_warp(raw_full + 8u * r, (n / K::raw_stages) & 1u) || (n >= K::stages && !cta_wait_warp(empty + 8u * s, (n / K::stages - 1u) & 1u))) {
                 ok = false;
                 break;
             }
-#pragma unroll 4
-            for (int i = 0; i < chunks; ++i) {
-                const uint4 raw = lds128(from + (uint32_t)i * 2048u);
-                const uint32_t row = (uint32_t)(row0 + i * (128 / chunks)), x[4] = {raw.x, raw.y, raw.z, raw.w};
-                uint4 o[2];
-                uint32_t *const w = reinterpret_cast<uint32_t *>(o);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t y = x[k] ^ 0x80808080u;             // codes 0 and 1, 2 and 3 in the low bits of 1024, minus 1152
-                    w[2 * k] = minus_1152(__byte_perm(y, 0x64646464u, 0x4140));
-                    w[2 * k + 1] = minus_1152(__byte_perm(y, 0x64646464u, 0x4342));
+            for (uint32_t h = 0; h < halves; ++h) {
+                const uint32_t half = h ^ odd, source = from + half * 64u, target = to + half * K::half;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint4 raw = lds128(source + i * (32u * D));
+                    const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
+                    uint32_t w[8];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t y = x[k] ^ 0x80808080u;         // codes 0 and 1, 2 and 3 in the low bits of 1024, minus 1152
+                        w[2 * k] = minus_1152(__byte_perm(y, 0x64646464u, 0x4140));
+                        w[2 * k + 1] = minus_1152(__byte_perm(y, 0x64646464u, 0x4342));
+                    }
+                    sts128(target + to0 + i * 4096u, make_uint4(w[0], w[1], w[2], w[3]));
+                    sts128(target + to1 + i * 4096u, make_uint4(w[4], w[5], w[6], w[7]));
                 }
-                // (the second half's threads write their second 16 bytes first: eight threads then meet no conflict)
-                const uint32_t at = to + (uint32_t)(chunk / 4) * K::half + row * 128u, c = 2u * (uint32_t)(chunk & 3), flip = (uint32_t)(chunk / 4) & 1u;
-                sts128(at + (((c + flip) ^ row) & 7u) * 16u, flip ? o[1] : o[0]);
-                sts128(at + (((c + 1u - flip) ^ row) & 7u) * 16u, flip ? o[0] : o[1]);
             }
             fence_async_smem();
             __syncwarp();

@@ -49,21 +49,20 @@ __device__ __forceinline__ int blocks_of(const Sequences &q, const Rows &r)
     return r.length > first ? ((r.length - 1) >> q.page) - (first >> q.page) + 1 : 0;
 }
 
-__device__ __forceinline__ float from16(uint32_t h, bool f16)
-{
-    if (!f16) return __uint_as_float(h << 16);
-    float f;
-    asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.f32.f16 %0, t; }" : "=f"(f) : "r"(h));
-    return f;
-}
 // A lane's 16 channels.
 __device__ __forceinline__ void unpack(float (&u)[LANE], const uint4 &lo, const uint4 &hi, bool f16)
 {
     const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (f16) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        u[2 * i] = from16(w[i] & 0xffffu, f16);
-        u[2 * i + 1] = from16(w[i] >> 16, f16);
+        for (int i = 0; i < 8; ++i)
+            asm("{ .reg .b16 x, y; mov.b32 {x, y}, %2; cvt.f32.f16 %0, x; cvt.f32.f16 %1, y; }" : "=f"(u[2 * i]), "=f"(u[2 * i + 1]) : "r"(w[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            u[2 * i] = __uint_as_float(w[i] << 16);
+            u[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
     }
 }
 // Times the Hadamard matrix of blocks of 2^log2b channels (0: none), without its factor.

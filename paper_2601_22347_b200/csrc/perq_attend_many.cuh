@@ -2,11 +2,9 @@
 //
 // A CTA has 256 rows (pairs of a token and one of the `group` heads of queries to a head of keys), two tiles of 128, and goes over the keys they see, 128 at a time.  Bulk copies
 // bring codes in, a page at a time, keys and values in turn; four warps make them fp16 (exactly) and lay them down as operands, in a ring; one warp issues the products: S = Q K^T into tensor memory, then O += P V with P
-// from tensor memory and V's rows as they are (its channels run along N).  Either tile has eight warps of its own, half of a row's columns to a thread: their maximum, P = 2^(x + log2
-// s_v - m) rounded to fp16 over the columns where S was, and the probabilities' sum.  The products of one tile run under the other's exponentials.  O stays in tensor memory; m moves,
-// and O with it, only when something is over 2^8 times larger, which the two warps of 32 rows agree on at a barrier.  (Whole rows to a thread, four warps to a tile: twice the time, as
-// an in-order warp waits 5 to 6 cycles for an instruction and two to a scheduler do not hide it.)
-//
+// from tensor memory and V's rows as they are (its channels run along N).  Either tile has four warps of its own, a row to a thread, which take 64 keys at a time: their maximum, P = 2^(x +
+// log2 s_v - m) rounded to fp16 over the columns where S was, and the probabilities' sum.  S has room for 64 keys twice, so the products with the last 64 and for the next run under
+// the exponentials of these.  O stays in tensor memory; m moves, and O with it, only when something is over 2^8 times larger.
 // Bound by the tensor cores and the exponentials alike: 128 x 128 x 128 products twice are 1024 cycles, the tile's 16384 exponentials as many.
 #pragma once
 
@@ -14,8 +12,8 @@
 
 namespace perq_kv {
 
-constexpr int CODES_WARP = 16, MMA_WARP = 20, LOAD_WARP = 21; // warps: 16 of the rows, 4 that make codes fp16, the products', the loads', 2 idle
-constexpr int MANY_ROWS = 256, MANY_KEYS = 128, MANY_THREADS = 768;
+constexpr int CODES_WARP = 8, MMA_WARP = 12, LOAD_WARP = 13; // warps: 8 of the rows, 4 that make codes fp16, the products', the loads', 2 idle
+constexpr int MANY_ROWS = 256, MANY_KEYS = 128, MANY_THREADS = 512;
 // (perq_attend_few's rows go up to this; both sides measured beside launch_attention)
 enum : unsigned int { ERROR_ATTEND = 1u << 7 };
 
@@ -32,7 +30,7 @@ struct Many {
     static constexpr uint32_t stages = D == 128 ? 4 : 8, raw_stages = D == 128 ? 2 : 4;
     static constexpr uint32_t off_ring = 2u * tile, off_raw = off_ring + stages * tile, off_steps = off_raw + raw_stages * raw;
     static constexpr uint32_t off_bars = off_steps + 8u * 8u * 16u;
-    static constexpr uint32_t bars = 2u * stages + 2u * raw_stages + 8u + 2u + 2u + 2u + 2u + 2u + 1u;   // operands, codes: full, empty; steps; Q, S, half of P, P, O of each tile; the end
+    static constexpr uint32_t bars = 2u * stages + 2u * raw_stages + 8u + 2u + 4u + 4u + 2u + 1u;   // operands, codes: full, empty; steps; Q, S and P (twice), O of each tile; the end
     static constexpr uint32_t off_slot = off_bars + 8u * bars, bytes = off_slot + 16u + 1024u;
     static constexpr uint32_t columns = 512u;                          // S0, S1, O0, O1
     static constexpr uint32_t o_column = 256u;
@@ -88,22 +86,6 @@ __device__ __forceinline__ uint32_t minus_1152(uint32_t v)
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x64806480u));
     return r;
 }
-__device__ __forceinline__ void tmem_store1(uint32_t at, float v) { asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%1], {%0};" ::"f"(v), "r"(at) : "memory"); }
-__device__ __forceinline__ float tmem_load1(uint32_t at)
-{
-    float v;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=f"(v) : "r"(at) : "memory");
-    return v;
-}
-// Two warps meet.
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ bool pair_any(int id, bool yes)
-{
-    uint32_t any;
-    asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, %2, 64, p; selp.u32 %0, 1, 0, q; }" : "=r"(any) : "r"((uint32_t)yes), "r"(id) : "memory");
-    return any != 0u;
-}
-
 #define PERQ_R8(v, i) "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]), "=f"(v[i + 4]), "=f"(v[i + 5]), "=f"(v[i + 6]), "=f"(v[i + 7])
 // 32 columns of this warp's 32 lanes; they are there after loads_wait.
 __device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32])
@@ -239,7 +221,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     __shared__ ManyItem found;
     const uint32_t full = base + K::off_bars, empty = full + 8u * K::stages, raw_full = empty + 8u * K::stages, raw_empty = raw_full + 8u * K::raw_stages,
                    steps_full = raw_empty + 8u * K::raw_stages, q_full = steps_full + 64u, s_full = q_full + 16u,
-                   p_half = s_full + 16u, p_full = p_half + 16u, o_full = p_full + 16u, end = o_full + 16u, slot = base + K::off_slot, steps = base + K::off_steps;
+                   p_full = s_full + 32u, o_full = p_full + 32u, end = o_full + 16u, slot = base + K::off_slot, steps = base + K::off_steps;
     if (warp == LOAD_WARP) {
         const ManyItem item = many_item(p.a, (int)(blockIdx.x / (unsigned)p.split), lane);
         if (lane == 0) found = item;
@@ -260,11 +242,12 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         }
         for (uint32_t i = 0; i < 8; ++i) mbar_init(steps_full + 8u * i, 1);
         for (uint32_t i = 0; i < 2; ++i) {
-            mbar_init(q_full + 8u * i, 8);
-            mbar_init(s_full + 8u * i, 1);
-            mbar_init(p_half + 8u * i, 4);
-            mbar_init(p_full + 8u * i, 4);
+            mbar_init(q_full + 8u * i, 4);
             mbar_init(o_full + 8u * i, 1);
+        }
+        for (uint32_t i = 0; i < 4; ++i) {
+            mbar_init(s_full + 8u * i, 1);
+            mbar_init(p_full + 8u * i, 4);
         }
         mbar_init(end, 1);
         mbar_init_fence();
@@ -281,67 +264,57 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     auto key_of = [&](int tile) { return (tile < it.sunk ? tile : tile - it.sunk + it.low) * MANY_KEYS; };
 
     if (warp < CODES_WARP) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");           // (of 80 at launch: 4 x 96 + 56 + 40 = 6 x 80)
-        constexpr int C = D / 2;                                       // of queries and results, a thread's channels
-        const int t = warp >> 3, side = (warp >> 2) & 1, thread = tid & 127, row = t * 128 + thread;
-        const bool there = row < it.rows;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");          // (of 128 at launch: 2 x 176 + 80 + 80 = 4 x 128)
+        const int t = warp >> 2, row = t * 128 + (tid & 127);
         const int token = (it.row0 + min(row, it.rows - 1)) / p.a.group, h = it.row0 + min(row, it.rows - 1) - token * p.a.group;
         const int position = it.first + token;
-        const size_t of_row = (size_t)it.head * (size_t)p.a.group + (size_t)h;
         if (t == 0 || two) {
-            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tile_at = tmem + (uint32_t)t * 128u + lanes, s_at = tile_at + 64u * (uint32_t)side,
-                           p_at = tile_at + 32u * (uint32_t)side, free_at = tile_at + 64u, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes + (uint32_t)(side * C);
-            const int pair = 1 + t * 4 + (warp & 3);                   // the barrier of the two warps that have these 32 rows
-            // a value of the row's other thread, by columns that are free before S is there and while P is written
-            auto others = [&](float x) {
-                tmem_store1(free_at + (uint32_t)side, x);
-                tmem_store_wait();
-                tmem_fence_before();
-                pair_sync(pair);
-                tmem_fence_after();
-                return tmem_load1(free_at + 1u - (uint32_t)side);
-            };
-            // Queries: 16 rows to a warp, 16 channels to a lane; a row's largest is scaled to 1 .. 2 by a power of two, then it is rotated and rounded to fp16.
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes;
+            // Queries: 32 rows to a warp, 16 channels to a lane; a row's largest is scaled to 1 .. 2 by a power of two, then it is rotated and rounded to fp16.
             // (A row to a thread: 12 us of loads that touch 32 rows each.)
             float factor = 0.0f;
             {
                 constexpr int wide = D / LANE, at_once = 32 / wide;    // lanes of a row, rows at once
-                const int in = lane / wide, channel = lane % wide * LANE, first_row = (warp & 3) * 32 + side * 16;
+                const int in = lane / wide, channel = lane % wide * LANE, first_row = (warp & 3) * 32;
+#pragma unroll 1
+                for (int k0 = 0; k0 < 32 / at_once; k0 += 4) {
+                    uint4 lo[4], hi[4];
 #pragma unroll
-                for (int k = 0; k < 16 / at_once; ++k) {
-                    const int r = first_row + k * at_once + in, pairs = it.row0 + t * 128 + r;
-                    const int its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
-                    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                    if (t * 128 + r < it.rows) {
-                        const uint4 *const from = reinterpret_cast<const uint4 *>(p.a.x + (size_t)(it.begin + its_token) * (size_t)p.a.stride +
-                                                                                  (size_t)(it.head * p.a.group + its_head) * D + channel);
-                        lo = __ldg(from);
-                        hi = __ldg(from + 1);
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = t * 128 + first_row + (k0 + k) * at_once + in, its_token = (it.row0 + r) / p.a.group, its_head = it.row0 + r - its_token * p.a.group;
+                        lo[k] = hi[k] = make_uint4(0, 0, 0, 0);
+                        if (r < it.rows) {
+                            const uint4 *const from = reinterpret_cast<const uint4 *>(p.a.x + (size_t)(it.begin + its_token) * (size_t)p.a.stride +
+                                                                                      (size_t)(it.head * p.a.group + its_head) * D + channel);
+                            lo[k] = __ldg(from);
+                            hi[k] = __ldg(from + 1);
+                        }
                     }
-                    float v[LANE], most = 0.0f;
-                    unpack(v, lo, hi, p.a.f16 != 0);
 #pragma unroll
-                    for (int i = 0; i < LANE; ++i) most = fmaxf(most, fabsf(v[i]));
+                    for (int k = 0; k < 4; ++k) {
+                        float v[LANE], most = 0.0f;
+                        unpack(v, lo[k], hi[k], p.a.f16 != 0);
 #pragma unroll
-                    for (int l = 1; l < wide; l *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, l));
-                    const int e = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
-                    // (with the sign of the logits' scale, as a page's largest logit has to be that of its largest S)
-                    const float down = copysignf(__uint_as_float((uint32_t)(254 - e) << 23), p.a.scale);
+                        for (int i = 0; i < LANE; ++i) most = fmaxf(most, fabsf(v[i]));
 #pragma unroll
-                    for (int i = 0; i < LANE; ++i) v[i] *= down;
-                    rotate(v, p.a.log2b, lane);
-                    const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)(channel / 64) * K::half + (uint32_t)r * 128u, c = (uint32_t)(channel % 64) / 8u;
-                    sts128(to + ((c ^ (uint32_t)r) & 7u) * 16u, make_uint4(half2_of(v[0], v[1]), half2_of(v[2], v[3]), half2_of(v[4], v[5]), half2_of(v[6], v[7])));
-                    sts128(to + (((c + 1u) ^ (uint32_t)r) & 7u) * 16u, make_uint4(half2_of(v[8], v[9]), half2_of(v[10], v[11]), half2_of(v[12], v[13]), half2_of(v[14], v[15])));
-                    // (the lane of the row has its factor; not 0, so that what is not seen stays -inf)
-                    const float x = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)e << 23), (lane % at_once) * wide);
-                    if (lane / at_once == side * (16 / at_once) + k) factor = fmaxf(x * fabsf(p.a.scale), 0x1p-60f);
+                        for (int l = 1; l < wide; l *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, l));
+                        const int e = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
+                        // (with the sign of the logits' scale, as a page's largest logit has to be that of its largest S)
+                        const float down = copysignf(__uint_as_float((uint32_t)(254 - e) << 23), p.a.scale);
+#pragma unroll
+                        for (int i = 0; i < LANE; ++i) v[i] *= down;
+                        rotate(v, p.a.log2b, lane);
+                        const uint32_t r = (uint32_t)(first_row + (k0 + k) * at_once + in), c = (uint32_t)(channel % 64) / 8u;
+                        const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)(channel / 64) * K::half + r * 128u;
+                        sts128(to + ((c ^ r) & 7u) * 16u, make_uint4(half2_of(v[0], v[1]), half2_of(v[2], v[3]), half2_of(v[4], v[5]), half2_of(v[6], v[7])));
+                        sts128(to + (((c + 1u) ^ r) & 7u) * 16u, make_uint4(half2_of(v[8], v[9]), half2_of(v[10], v[11]), half2_of(v[12], v[13]), half2_of(v[14], v[15])));
+                        // (the lane of the row has its factor; not 0, so that what is not seen stays -inf)
+                        const float x = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)e << 23), (lane % at_once) * wide);
+                        if (lane / at_once == k0 + k) factor = fmaxf(x * fabsf(p.a.scale), 0x1p-60f);
+                    }
                 }
-                const float x = others(factor);
-                if (lane / 16 != side) factor = x;
             }
             fence_async_smem();
-            tmem_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full + 8u * (uint32_t)t);
 
@@ -350,10 +323,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
             const int low_position = it.first + min(row_first, row_last) / p.a.group, high_position = it.first + min(row_first + 31, row_last) / p.a.group;
             float m = -INFINITY, l = 0.0f;
             bool ok = true;
-            for (int j = 0; j < tiles; ++j) {
-                const int key = key_of(tile0 + j) + 64 * side;
-                // (a wait that runs out ends no warp's part: its partner still waits for it at their barrier)
-                if (ok && (!cta_wait_warp(steps_full + 8u * (uint32_t)(j & 7), (uint32_t)(j >> 3) & 1u) || !cta_wait_warp(s_full + 8u * (uint32_t)t, (uint32_t)j & 1u))) ok = false;
+            for (int u = 0; u < 2 * tiles; ++u) {
+                const int j = u >> 1, side = u & 1, key = key_of(tile0 + j) + 64 * side;
+                const uint32_t s_at = tmem + (uint32_t)(t * 128 + side * 64) + lanes, buffer = 8u * (uint32_t)(2 * t + side);
+                if (!cta_wait_warp(steps_full + 8u * (uint32_t)(j & 7), (uint32_t)(j >> 3) & 1u) || !cta_wait_warp(s_full + buffer, (uint32_t)j & 1u)) {
+                    ok = false;
+                    break;
+                }
                 tmem_fence_after();
                 float s[2][32];
                 tmem_load32(s_at, s[0]);
@@ -361,7 +337,19 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 constexpr int G = FINE ? 4 : 2, W = 64 / G;
                 // of a page's columns: the factor of S, log2 s_v, 1 / s_v
                 const uint32_t at = steps + (uint32_t)(j & 7) * 128u + (uint32_t)side * 64u;
-                auto step_of = [&](int g) { return lds128(at + (uint32_t)(g * (4 / G)) * 16u); };
+                float f[G], b[G], inverse[G];
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint4 w = lds128(at + (uint32_t)(g * (4 / G)) * 16u);
+                    f[g] = factor * __uint_as_float(w.x);
+                    b[g] = __uint_as_float(w.y);
+                    inverse[g] = __uint_as_float(w.z);
+                    if (w.w != 0u) {
+                        // a step that is not finite: so is what sees one of its keys
+                        const int k0 = key + g * W, k1 = min(k0 + W - 1, position);
+                        if (k0 <= position && (p.a.window <= 0 || k1 > position - p.a.window || k0 < p.a.sinks)) l = __uint_as_float(0x7fffffffu);
+                    }
+                }
                 loads_wait(s[0]);
                 loads_there(s[1]);
                 if (key + 63 > low_position || (p.a.window > 0 && key <= high_position - p.a.window && key + 64 > p.a.sinks)) {
@@ -376,36 +364,29 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 }
                 float most_x = -INFINITY;
                 {
-                    float top[G];
+                    // (chains of their own, as each step of one waits for the last)
+                    float top[4];
 #pragma unroll
-                    for (int g = 0; g < G; ++g) top[g] = fmaxf(s[g * W / 32][g * W % 32], s[g * W / 32][g * W % 32 + 1]);
+                    for (int g = 0; g < 4; ++g) top[g] = fmaxf(s[g / 2][16 * (g % 2)], s[g / 2][16 * (g % 2) + 1]);
 #pragma unroll
-                    for (int i = 2; i < W; i += 2)
+                    for (int i = 2; i < 16; i += 2)
 #pragma unroll
-                        for (int g = 0; g < G; ++g) top[g] = max_of3(top[g], s[(g * W + i) / 32][(g * W + i) % 32], s[(g * W + i) / 32][(g * W + i) % 32 + 1]);
+                        for (int g = 0; g < 4; ++g) top[g] = max_of3(top[g], s[g / 2][16 * (g % 2) + i], s[g / 2][16 * (g % 2) + i + 1]);
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        const uint4 w = step_of(g);
-                        most_x = fmaxf(most_x, fmaf(top[g], factor * __uint_as_float(w.x), __uint_as_float(w.y)));
-                        if (w.w != 0u) {
-                            // a step that is not finite: so is what sees one of its keys
-                            const int k0 = key + g * W, k1 = min(k0 + W - 1, position);
-                            if (k0 <= position && (p.a.window <= 0 || k1 > position - p.a.window || k0 < p.a.sinks)) l = __uint_as_float(0x7fffffffu);
-                        }
-                    }
+                    for (int g = 0; g < G; ++g) most_x = fmaxf(most_x, fmaf(FINE ? top[g] : fmaxf(top[2 * g % 4], top[(2 * g + 1) % 4]), f[g], b[g]));
                 }
-                // (S is read now by both, so P may take its place)
-                tmem_fence_before();
-                if (pair_any(pair, most_x - m > 8.0f)) {
-                    tmem_fence_after();
-                    const float next = fmaxf(m, fmaxf(most_x, others(most_x))), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
+                if (__any_sync(0xffffffffu, most_x - m > 8.0f)) {
+                    const float next = fmaxf(m, most_x), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
                     m = next;
                     l *= alpha;
-                    if (j > 0) {
-                        if (ok && !cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(j - 1) & 1u)) ok = false;
+                    if (u > 0) {
+                        if (!cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(u - 1) & 1u)) {
+                            ok = false;
+                            break;
+                        }
                         tmem_fence_after();
 #pragma unroll
-                        for (int c = 0; c < C / 16; ++c) {
+                        for (int c = 0; c < D / 16; ++c) {
                             int32_t o[16];
                             uint32_t w[16];
                             tmem_load16(o_at + 16u * c, o);
@@ -414,24 +395,16 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                             for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__int_as_float(o[i]) * alpha);
                             tmem_store16(o_at + 16u * c, w);
                         }
-                        // (the products that add to all of O begin when the first half of P is there)
-                        tmem_store_wait();
-                        tmem_fence_before();
-                        pair_sync(pair);
                     }
                 }
-                tmem_fence_after();
                 const float reference = m == -INFINITY ? 0.0f : m;
                 // (exponentials of 32 columns in place, then their sums: a warp that takes them as they come waits for each)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    float inverse[G / 2];
 #pragma unroll
                     for (int g = 0; g < G / 2; ++g) {
-                        const uint4 step = step_of(c * G / 2 + g);
-                        const float f = factor * __uint_as_float(step.x), b = __uint_as_float(step.y) - reference;
-                        const Pair ff = pair_of(f, f), bb = pair_of(b, b);
-                        inverse[g] = __uint_as_float(step.z);
+                        const float shift = b[c * G / 2 + g] - reference;
+                        const Pair ff = pair_of(f[c * G / 2 + g], f[c * G / 2 + g]), bb = pair_of(shift, shift);
 #pragma unroll
                         for (int i = g * W; i < (g + 1) * W; i += 2) {
                             pair_split(pair_fma(pair_of(s[c][i], s[c][i + 1]), ff, bb), s[c][i], s[c][i + 1]);
@@ -442,7 +415,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     uint32_t w[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) w[i / 2] = half2_of(s[c][i], s[c][i + 1]);
-                    tmem_store16(p_at + 16u * c, w);
+                    tmem_store16(s_at + 16u * c, w);
 #pragma unroll
                     for (int g = 0; g < G / 2; ++g) {
                         Pair sum[2] = {pair_of(s[c][g * W], s[c][g * W + 1]), pair_of(s[c][g * W + 2], s[c][g * W + 3])};
@@ -453,69 +426,71 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         }
                         float x, y;
                         pair_split(pair_add(sum[0], sum[1]), x, y);
-                        l = fmaf(x + y, inverse[g], l);
+                        l = fmaf(x + y, inverse[c * G / 2 + g], l);
                     }
                 }
                 tmem_store_wait();
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive((side ? p_full : p_half) + 8u * (uint32_t)t);       // (keys 0 .. 63 come first)
+                if (lane == 0) mbar_arrive(p_full + buffer);
             }
             // (without keys: until all queries are where results go)
-            if (ok && !(tiles > 0 ? cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(tiles - 1) & 1u) : cta_wait_warp(q_full + 8u * (uint32_t)t, 0u))) ok = false;
+            if (ok && !cta_wait_warp(tiles > 0 ? end : q_full + 8u * (uint32_t)t, 0u)) ok = false;
             tmem_fence_after();
-            l += others(l);
-            if (!ok && lane == 0) give_up();
-            const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-            const bool narrow = p.split == 1 && p.a.out_type != OUT_F32, f16 = p.a.out_type == OUT_F16;
-            if (p.split > 1 && side == 0 && ok) {
-                float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
-                ends[row] = m;
-                ends[MANY_ROWS + row] = l;
-            }
-            // 16-bit results go through shared memory, where the queries were, so that rows are stored whole.
-            const uint32_t room = base + (uint32_t)t * K::tile;
-#pragma unroll
-            for (int c = 0; c < C / 16; ++c) {
-                int32_t u[16];
-                if (tiles > 0) {
-                    tmem_load16(o_at + 16u * c, u);
-                    tmem_wait(u);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) u[i] = 0;
+            if (!ok) {
+                if (lane == 0) give_up();
+            } else {
+                const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+                const bool narrow = p.split == 1 && p.a.out_type != OUT_F32, f16 = p.a.out_type == OUT_F16, there = row < it.rows;
+                if (p.split > 1) {
+                    float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
+                    ends[row] = m;
+                    ends[MANY_ROWS + row] = l;
                 }
-                float o[16];
+                float *const wide_out = p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D
+                                                    : static_cast<float *>(p.a.out) + ((size_t)(it.begin + token) * ((size_t)p.a.heads * (size_t)p.a.group) +
+                                                                                       (size_t)it.head * (size_t)p.a.group + (size_t)h) * D;
+                // 16-bit results go through shared memory, where the queries were, so that rows are stored whole.
+                const uint32_t room = base + (uint32_t)t * K::tile, thread = (uint32_t)tid & 127u;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] = __int_as_float(u[i]) * r;
+                for (int c = 0; c < D / 16; ++c) {
+                    int32_t u[16];
+                    if (tiles > 0) {
+                        tmem_load16(o_at + 16u * c, u);
+                        tmem_wait(u);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) u[i] = 0;
+                    }
+                    float o[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = __int_as_float(u[i]) * r;
+                    if (narrow) {
+                        const uint32_t to = room + thread * (2u * D) + (uint32_t)(2 * c & 8) * 16u, at = (uint32_t)(2 * c);
+                        sts128(to + ((at ^ thread) & 7u) * 16u, make_uint4(pack16(o[0], o[1], f16), pack16(o[2], o[3], f16), pack16(o[4], o[5], f16), pack16(o[6], o[7], f16)));
+                        sts128(to + (((at + 1u) ^ thread) & 7u) * 16u, make_uint4(pack16(o[8], o[9], f16), pack16(o[10], o[11], f16), pack16(o[12], o[13], f16), pack16(o[14], o[15], f16)));
+                    } else if (there) {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(wide_out + 16 * c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    }
+                }
                 if (narrow) {
-                    const uint32_t to = room + (uint32_t)thread * (2u * D), at = (uint32_t)(side * (C / 8) + 2 * c);
-                    sts128(to + ((at ^ (uint32_t)thread) & 7u) * 16u + (at & 8u) * 16u, make_uint4(pack16(o[0], o[1], f16), pack16(o[2], o[3], f16), pack16(o[4], o[5], f16), pack16(o[6], o[7], f16)));
-                    sts128(to + (((at + 1u) ^ (uint32_t)thread) & 7u) * 16u + (at & 8u) * 16u,
-                           make_uint4(pack16(o[8], o[9], f16), pack16(o[10], o[11], f16), pack16(o[12], o[13], f16), pack16(o[14], o[15], f16)));
-                } else if (there && ok) {
-                    float *const to = (p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D
-                                                   : static_cast<float *>(p.a.out) + ((size_t)(it.begin + token) * ((size_t)p.a.heads * (size_t)p.a.group) + of_row) * D) + side * C + 16 * c;
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(to + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-                }
-            }
-            if (narrow) {
-                pair_sync(pair);
-                constexpr int wide = D / 8, at_once = 32 / wide;
-#pragma unroll
-                for (int k = 0; k < 16 / at_once; ++k) {
-                    const int line = (warp & 3) * 32 + side * 16 + k * at_once + lane / wide, chunk = lane % wide, pairs = it.row0 + t * 128 + line;
-                    const int its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
-                    const uint4 w = lds128(room + (uint32_t)line * (2u * D) + (uint32_t)(((chunk ^ line) & 7) * 16 + (chunk & 8) * 16));
-                    if (t * 128 + line < it.rows && ok)
-                        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.a.out) +
-                                                   ((size_t)(it.begin + its_token) * ((size_t)p.a.heads * (size_t)p.a.group) + (size_t)(it.head * p.a.group + its_head)) * D + chunk * 8) = w;
+                    __syncwarp();
+                    constexpr int wide = D / 8, at_once = 32 / wide;
+#pragma unroll 4
+                    for (int k = 0; k < 32 / at_once; ++k) {
+                        const int line = (warp & 3) * 32 + k * at_once + lane / wide, chunk = lane % wide, pairs = it.row0 + t * 128 + line;
+                        const int its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
+                        const uint4 w = lds128(room + (uint32_t)line * (2u * D) + (uint32_t)(((chunk ^ line) & 7) * 16 + (chunk & 8) * 16));
+                        if (t * 128 + line < it.rows)
+                            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.a.out) +
+                                                       ((size_t)(it.begin + its_token) * ((size_t)p.a.heads * (size_t)p.a.group) + (size_t)(it.head * p.a.group + its_head)) * D + chunk * 8) = w;
+                    }
                 }
             }
         }
     } else if (warp < MMA_WARP) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         // Codes to fp16.  A thread has 16 channels of one key in 32; eight threads have 64 channels each of two keys next to each other, for D = 128 the lower 64 of one and the
         // upper 64 of the other, so that neither reads nor stores meet a conflict.
         constexpr uint32_t halves = D / 64;
@@ -555,60 +530,57 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         }
         if (!ok && lane == 0) give_up();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         if (warp == MMA_WARP && tiles > 0) {
-            const uint32_t qk = f16_desc(128, 128, false), pv = f16_desc(128, D, true);
+            const uint32_t qk = f16_desc(128, 64, false), pv = f16_desc(128, D, true);
             bool ok = true;
-            uint32_t n = 0;
-            auto logits = [&](uint32_t t, uint32_t s) {
-                const uint32_t a = rows_operand(base + t * K::tile), b = rows_operand(base + K::off_ring + s * K::tile);
+            // S of 64 keys (half h of a tile of keys) for a tile of rows, and O of them
+            auto logits = [&](uint32_t t, uint32_t h, uint32_t s) {
+                const uint32_t a = rows_operand(base + t * K::tile), b = rows_operand(base + K::off_ring + s * K::tile + h * 8192u), d = tmem + t * 128u + h * 64u;
 #pragma unroll
                 for (uint32_t k = 0; k < D / 16; ++k) {
                     const uint32_t at = (k / 4u) * (K::half >> 4) + (k % 4u) * 2u;
-                    product_f16(tmem + t * 128u, a + at, b + at, qk, k > 0);
+                    product_f16(d, a + at, b + at, qk, k > 0);
                 }
-                commit_one(s_full + 8u * t);
+                commit_one(s_full + 8u * (2u * t + h));
+            };
+            auto outputs = [&](uint32_t t, uint32_t h, uint32_t s, bool more) {
+                const uint32_t a = tmem + t * 128u + h * 64u, b = keys_operand<D>(base + K::off_ring + s * K::tile + h * 8192u), d = tmem + K::o_column + t * 128u;
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) product_f16_tmem(d, a + 8u * k, b + k * 128u, pv, more || k > 0);
+                commit_one(o_full + 8u * t);
             };
             auto wait_for = [&](uint32_t bar, uint32_t parity) {
                 if (ok && !cta_wait_warp(bar, parity)) ok = false;
                 tmem_fence_after();
                 return ok;
             };
-            auto outputs = [&](uint32_t t, uint32_t s, int j) {
-                const uint32_t b = keys_operand<D>(base + K::off_ring + s * K::tile);
-#pragma unroll
-                for (uint32_t k = 0; k < MANY_KEYS / 16; ++k) {
-                    if (k == 0 && !wait_for(p_half + 8u * t, (uint32_t)j & 1u)) return false;
-                    if (k == 4 && !wait_for(p_full + 8u * t, (uint32_t)j & 1u)) return false;
-                    product_f16_tmem(tmem + K::o_column + t * 128u, tmem + t * 128u + 8u * k, b + k * 128u, pv, j > 0 || k > 0);
-                }
-                commit_one(o_full + 8u * t);
-                return true;
-            };
             auto piece = [&](uint32_t i) { return wait_for(full + 8u * (i % K::stages), (i / K::stages) & 1u); };
+            const uint32_t row_tiles = two ? 2u : 1u;
             if (wait_for(q_full, 0) && (!two || wait_for(q_full + 8u, 0)) && piece(0)) {
-                logits(0, 0);
-                if (two) logits(1, 0);
+                for (uint32_t h = 0; h < 2; ++h)
+                    for (uint32_t t = 0; t < row_tiles; ++t) logits(t, h, 0);
                 commit_one(empty);
-                n = 1;
+                uint32_t n = 1;
                 for (int j = 0; j < tiles && ok; ++j, n += 2) {
                     const bool more = j + 1 < tiles;
                     const uint32_t sv = n % K::stages, sk = (n + 1) % K::stages;
-                    if (!piece(n) || !outputs(0, sv, j)) break;
-                    if (more) {
-                        if (!piece(n + 1)) break;
-                        logits(0, sk);
-                    }
-                    if (two) {
-                        if (!outputs(1, sv, j)) break;
-                        if (more) logits(1, sk);
-                    }
+                    if (!piece(n)) break;
+                    for (uint32_t h = 0; h < 2 && ok; ++h)
+                        for (uint32_t t = 0; t < row_tiles && ok; ++t) {
+                            if (!wait_for(p_full + 8u * (2u * t + h), (uint32_t)j & 1u)) break;
+                            outputs(t, h, sv, j > 0 || h > 0);
+                            if (more) {
+                                if (h == 0 && t == 0 && !piece(n + 1)) break;
+                                logits(t, h, sk);
+                            }
+                        }
                     commit_one(empty + 8u * sv);
                     if (more) commit_one(empty + 8u * sk);
                 }
             }
             if (!ok && lane == 0) give_up();
-            // nothing is in flight when the CTA ends
+            // (all products: the rows' warps wait for it too, and nothing is in flight when the CTA ends)
             commit_one(end);
             (void)cta_wait_warp(end, 0);
         }

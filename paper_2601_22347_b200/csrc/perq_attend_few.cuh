@@ -5,12 +5,15 @@
 // (they are known on the device only), and a share's eight warps take its units in turn.  A row whose units belong to several CTAs is put together by join_kernel, in a
 // fixed order.
 //
-// Keys (then, transposed, values) are the first operand of mma.sync m16n8k16, rows the second, so that eight rows cost no more than they have to.  The order of the
+// Keys (then, transposed, values) are the first operand of mma.sync, rows the second, so that eight rows cost no more than they have to.  The order of the
 // channels inside a product is free: a lane takes 16 adjacent codes of its keys as they lie in memory, and of its values 16 adjacent channels of four keys.  It copies just
-// what it reads itself (cp.async into its own places), so the copies want no barrier, and 16-byte reads of them meet no conflict.  Codes become fp16 exactly: code ^ 0x80 in the
-// low bits of 1024, minus 1152.
+// what it reads itself (cp.async into its own places), so the copies want no barrier, and 16-byte reads of them meet no conflict.
 //
-// logit (base 2) x = s_k f S with S the sum over codes, f the row's factor.  Values' steps go into the exponent: P = 2^(x + log2 s_v - m), so that fp16 P (2^-12 of each) meet exact codes and no row's
+// Logits: keys' codes stay 8-bit integers (m16n8k32).  A query becomes 128 hi + lo of two 8-bit integers, its largest channel 16256, so it is off by 2^-15 of that at most, and S = sum
+// (128 hi + lo) code is exact.  (Codes to fp16 instead: 80 instructions for 16 keys of 128 channels; these products take 8 of the 8 cycles that an fp16 one takes too.)
+// Values' codes become fp16 exactly: code ^ 0x80 in the low bits of 1024, minus 1152.
+//
+// y = s_k f S + log2 s_v - m, base 2, with f the row's factor and m its reference.  Values' steps go into the exponent: P = 2^y, so that fp16 P (2^-12 of each) meet exact codes and no row's
 // sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is only moved when something is over 2^8 times larger.  Blocks of values whose step is below 2^-64 (of zeros)
 // count as zeros of that step.
 #pragma once
@@ -67,6 +70,11 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_i8(int32_t (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t v)
 {
     uint32_t r;
@@ -110,10 +118,32 @@ struct Found {
     int32_t sequence;
     long long begin;                          // its first unit
 };
-// The units of all sequences, and the sequence of unit `per * number` (none: S).  Called by all threads of the CTA.
+// The units of all sequences, and the sequence of unit `per * number` (none: S).  Called by all threads of the CTA; up to 32 sequences are looked at by every warp for itself.
 template <int ROWS>
 __device__ __forceinline__ Share share_units(const AttendParams &p, int number, int ctas, Found &f)
 {
+    if (p.q.S <= 32) {
+        const int lane = (int)threadIdx.x & 31;
+        long long mine = 0;
+        if (lane < p.q.S) {
+            const Units u = units_of<ROWS>(p, lane);
+            mine = (long long)u.tiles * u.count * p.heads;
+        }
+        long long up_to = mine;
+#pragma unroll
+        for (int l = 1; l < 32; l *= 2) {
+            const long long v = __shfl_up_sync(0xffffffffu, up_to, l);
+            if (lane >= l) up_to += v;
+        }
+        Share s;
+        s.all = __shfl_sync(0xffffffffu, up_to, 31);
+        s.per = max((s.all + ctas - 1) / ctas, (long long)FEW_WARPS);
+        const long long unit = s.per * number, begin = up_to - mine;
+        const unsigned here = __ballot_sync(0xffffffffu, unit >= begin && unit < up_to);
+        f.sequence = here ? __ffs(here) - 1 : p.q.S;
+        f.begin = __shfl_sync(0xffffffffu, begin, here ? __ffs(here) - 1 : 0);
+        return s;
+    }
     __shared__ long long sums[FEW_WARPS];
     __shared__ Found found;
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -188,10 +218,9 @@ struct Few {
     static constexpr int parts = D / 64;                               // 16-byte parts of a key to a lane
     static constexpr int v_bytes = D / 8;                              // of a value
     static constexpr int k_lane = 2 * parts * 16, lane_bytes = k_lane + 4 * v_bytes;
-    static constexpr int stages = (NT == 1 ? 3 : 6) * (D == 64 ? 2 : 1);          // units of a warp that are on their way or read
+    static constexpr int stages = D == 64 ? 6 : NT == 1 ? 3 : 6;          // units of a warp that are on their way or read
     static constexpr int stage = 32 * lane_bytes, ring = FEW_WARPS * stages * stage;
-    static constexpr int q_row = D + 8;                                // fp16
-    static constexpr int off_q = ring, off_factor = off_q + rows * q_row * 2, off_top = off_factor + rows * 4, off_sum = off_top + FEW_WARPS * rows * 4,
+    static constexpr int off_q = ring, off_factor = off_q + 2 * rows * D, off_top = off_factor + rows * 4, off_sum = off_top + FEW_WARPS * rows * 4,
                          bytes = off_sum + FEW_WARPS * rows * 4;
     static_assert(FEW_WARPS * rows * D * 4 <= ring, "the warps' sums lie where the copies did");
 };
@@ -215,13 +244,13 @@ __device__ __forceinline__ void store_out4(const AttendParams &p, size_t at, flo
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __grid_constant__ AttendParams p)
+__global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kernel(const __grid_constant__ AttendParams p)
 {
     using K = Few<D, NT>;
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t base = perq_mm::smem_u32(smem);
-    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
-    uint16_t *const q_room = reinterpret_cast<uint16_t *>(smem + K::off_q);
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
+    int8_t *const q_room = reinterpret_cast<int8_t *>(smem + K::off_q);
     float *const factor = reinterpret_cast<float *>(smem + K::off_factor), *const tops = reinterpret_cast<float *>(smem + K::off_top),
           *const totals = reinterpret_cast<float *>(smem + K::off_sum), *const sums = reinterpret_cast<float *>(smem);
     griddep_wait();
@@ -232,7 +261,8 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __g
     const long long unit_end = min(unit + share.per, share.all);
     int i = f.sequence;
     long long begin = f.begin;
-    const uint32_t mine = base + (uint32_t)(warp * K::stages * K::stage);
+    const uint32_t mine = base + (uint32_t)(warp * K::stages * K::stage) + (uint32_t)lane * 16u, mine_v = base + (uint32_t)(warp * K::stages * K::stage + 32 * K::k_lane + lane * K::v_bytes);
+    const uint32_t page_bytes = (uint32_t)(p.heads * D) << p.q.page;                     // of a page in the pool
 
     while (unit < unit_end && i < p.q.S) {
         // the tile of this unit
@@ -247,57 +277,58 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __g
         const long long tile_begin = begin + (long long)number * u.count;
         const int l0 = (int)(unit - tile_begin), l1 = (int)min((long long)u.count, unit_end - tile_begin), rows = min(K::rows, u.tokens * p.group - row0);
         const int first = u.r.length - u.r.n;                          // position of the sequence's first row
-        const int token0 = row0 / p.group, token1 = (row0 + rows - 1) / p.group, low_position = first + token0, high_position = first + token1;
+        const int low_position = first + row0 / p.group, high_position = first + (row0 + rows - 1) / p.group;
         const int32_t *const table = p.q.pages + (size_t)i * (size_t)p.q.width;
+        const size_t of_head = ((size_t)head * D) << p.q.page;
+        const int8_t *const k_base = p.k_codes + of_head + (size_t)(g * D + q * 16), *const v_base = p.v_codes + of_head + (size_t)(2 * q * D + g * K::v_bytes);
 
         auto key_of = [&](int l) { return (l < u.sunk ? l : l - u.sunk + u.low) * FEW_KEYS; };
-        // pages and steps of 32 units of this warp, one to a lane
+        // of 32 units of this warp, one to a lane: pages, s_k, log2 s_v, 1 / s_v
         const int units = l1 - l0 > warp ? (l1 - l0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
-        int pages[2] = {0, 0};
-        float k_step[2], v_step[2];
+        int next_page = 0, later_page = 0;
+        float next_step[3] = {0.0f, 0.0f, 0.0f}, step[3] = {0.0f, 0.0f, 0.0f};
         auto fetch = [&](int batch) {
             const int n = batch * 32 + lane, l = l0 + warp + n * FEW_WARPS;
-            int page = 0;
-            float ks = 0.0f, vs = 0.0f;
             if (n < units) {
-                page = min(max(__ldg(table + min(key_of(l) >> p.q.page, p.q.width - 1)), 0), p.q.n_pages - 1);
-                const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
-                ks = __ldg(p.k_steps + block);
-                vs = __ldg(p.v_steps + block);
+                later_page = min(max(__ldg(table + min(key_of(l) >> p.q.page, p.q.width - 1)), 0), p.q.n_pages - 1);
+                const size_t block = (size_t)later_page * (size_t)p.heads + (size_t)head;
+                const float vs = __ldg(p.v_steps + block);
+                next_step[0] = __ldg(p.k_steps + block);
+                next_step[1] = vs < 0x1p-64f ? -64.0f : log2_of(vs);
+                next_step[2] = vs < 0x1p-64f ? 0x1p64f : 1.0f / vs;
             }
-            if (batch & 1) { pages[1] = page; k_step[1] = ks; v_step[1] = vs; } else { pages[0] = page; k_step[0] = ks; v_step[0] = vs; }
         };
+        int slot_in = 0;                                               // of the ring, for the unit that is issued next
         auto issue = [&](int n) {
             if (n < units) {
-                const int page = __shfl_sync(0xffffffffu, n & 32 ? pages[1] : pages[0], n & 31), key = key_of(l0 + warp + n * FEW_WARPS);
-                const size_t at = ((((size_t)page * (size_t)p.heads + (size_t)head) << p.q.page) + (size_t)(key & ((1 << p.q.page) - 1))) * D;
-                const uint32_t to = mine + (uint32_t)(n % K::stages) * K::stage;
-                const int8_t *const k = p.k_codes + at + q * 16, *const v = p.v_codes + at + g * K::v_bytes;
+                const int its_page = __shfl_sync(0xffffffffu, next_page, n & 31), key = key_of(l0 + warp + n * FEW_WARPS);
+                const size_t at = (size_t)its_page * page_bytes + (size_t)(uint32_t)((key & ((1 << p.q.page) - 1)) * D);
+                const int8_t *const k = k_base + at, *const v = v_base + at;
+                const uint32_t to = mine + (uint32_t)slot_in * K::stage, to_v = mine_v + (uint32_t)slot_in * K::stage;
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
-                    for (int c = 0; c < K::parts; ++c) copy16(to + (uint32_t)((r * K::parts + c) * 512 + lane * 16), k + (g + 8 * r) * D + c * 64);
+                    for (int c = 0; c < K::parts; ++c) copy16(to + (uint32_t)((r * K::parts + c) * 512), k + 8 * r * D + c * 64);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int8_t *const from = v + (2 * q + (r & 1) + 8 * (r >> 1)) * D;
-                    const uint32_t at_v = to + 32 * K::k_lane + (uint32_t)(r * 32 + lane) * K::v_bytes;
-                    if (D == 128) copy16(at_v, from); else copy8(at_v, from);
+                    if (D == 128) copy16(to_v + (uint32_t)(r * 32 * K::v_bytes), v + ((r & 1) + 8 * (r >> 1)) * D);
+                    else copy8(to_v + (uint32_t)(r * 32 * K::v_bytes), v + ((r & 1) + 8 * (r >> 1)) * D);
                 }
+                slot_in = slot_in + 1 == K::stages ? 0 : slot_in + 1;
             }
             copies_end();
-            if ((n & 31) == 16) fetch((n >> 5) + 1);
         };
         fetch(0);
+        next_page = later_page;
 #pragma unroll
         for (int n = 0; n < K::stages - 1; ++n) issue(n);
 
-        // queries: rotated, scaled to 1 .. 2 by a power of two, fp16
+        // queries: rotated, then 128 hi + lo with the largest channel 16256
         {
             constexpr int lanes = D / LANE;
             const int row = min(tid / lanes, K::rows - 1), channel = tid % lanes * LANE;
-            const bool there = tid / lanes < rows;
             uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-            if (there) {
+            if (tid / lanes < rows) {
                 const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
                 const uint4 *const from = reinterpret_cast<const uint4 *>(p.x + (size_t)(u.r.begin + token) * (size_t)p.stride + (size_t)(head * p.group + h) * D + channel);
                 lo = __ldg(from);
@@ -307,30 +338,39 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __g
             unpack(v, lo, hi, p.f16 != 0);
             rotate(v, p.log2b, lane);
 #pragma unroll
-            for (int k = 0; k < LANE; ++k) top = fmaxf(top, fabsf(v[k]));
+            for (int k = 0; k < LANE; ++k) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(v[k])));
 #pragma unroll
-            for (int l = 1; l < lanes; l *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, l));
+            for (int l = 1; l < lanes; l *= 2) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(__shfl_xor_sync(0xffffffffu, top, l)));
+            // (by a power of two first, so that no reciprocal leaves the range; a row that is not finite has a factor that is not)
             const int e = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
-            const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+            const float down = __uint_as_float((uint32_t)(254 - e) << 23), scaled = top * down, up = scaled > 0.0f ? 16256.0f / scaled : 0.0f;
             if (tid / lanes < K::rows) {
+                uint32_t w[2][4] = {};
 #pragma unroll
-                for (int k = 0; k < LANE; k += 2) *reinterpret_cast<uint32_t *>(q_room + row * K::q_row + channel + k) = half2_of(v[k] * down, v[k + 1] * down);
-                if (channel == 0) factor[row] = __uint_as_float((uint32_t)e << 23) * p.scale;
+                for (int k = 0; k < LANE; ++k) {
+                    const int n = __float2int_rn(v[k] * down * up), high = (n + 64) >> 7;
+                    w[0][k / 4] |= (uint32_t)(uint8_t)high << (8 * (k % 4));
+                    w[1][k / 4] |= (uint32_t)(uint8_t)(n - 128 * high) << (8 * (k % 4));
+                }
+#pragma unroll
+                for (int plane = 0; plane < 2; ++plane)
+                    *reinterpret_cast<uint4 *>(q_room + (plane * K::rows + row) * D + channel) = make_uint4(w[plane][0], w[plane][1], w[plane][2], w[plane][3]);
+                if (channel == 0) factor[row] = scaled * (1.0f / 16256.0f) * __uint_as_float((uint32_t)e << 23) * p.scale;
             }
         }
         __syncthreads();
-        uint32_t qb[NT][4 * K::parts][2];
+        uint32_t qb[NT][2][4 * K::parts];                              // [tile][hi, lo]
         float row_factor[NT][2];
         int position[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int k = 0; k < 4 * K::parts; ++k) {
-                const int channel = 16 * (q + 4 * (k / 4)) + 4 * (k % 4);
-                const uint2 w = *reinterpret_cast<const uint2 *>(q_room + (t * 8 + g) * K::q_row + channel);
-                qb[t][k][0] = __byte_perm(w.x, w.y, 0x5410);           // channels 0 and 2, 1 and 3
-                qb[t][k][1] = __byte_perm(w.x, w.y, 0x7632);
-            }
+            for (int plane = 0; plane < 2; ++plane)
+#pragma unroll
+                for (int c = 0; c < K::parts; ++c) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(q_room + (plane * K::rows + t * 8 + g) * D + 16 * (q + 4 * c));
+                    qb[t][plane][4 * c] = w.x; qb[t][plane][4 * c + 1] = w.y; qb[t][plane][4 * c + 2] = w.z; qb[t][plane][4 * c + 3] = w.w;
+                }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int row = t * 8 + 2 * q + c;
@@ -352,52 +392,68 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __g
             }
         }
 
+        int slot = 0;
         for (int n = 0; n < units; ++n) {
+            if ((n & 31) == 0) {
+#pragma unroll
+                for (int k = 0; k < 3; ++k) step[k] = next_step[k];
+            }
+            // (of the next 32 units, well before the first of them is issued)
+            if ((n & 31) == 16) fetch((n >> 5) + 1);
+            if ((n & 31) == 33 - K::stages) next_page = later_page;
             issue(n + K::stages - 1);
             copies_wait<K::stages - 1>();
-            const uint32_t at = mine + (uint32_t)(n % K::stages) * K::stage;
-            const float ks = __shfl_sync(0xffffffffu, n & 32 ? k_step[1] : k_step[0], n & 31), vs = __shfl_sync(0xffffffffu, n & 32 ? v_step[1] : v_step[0], n & 31);
-            float s[NT][4];
+            const uint32_t at = mine + (uint32_t)slot * K::stage, at_v = mine_v + (uint32_t)slot * K::stage;
+            slot = slot + 1 == K::stages ? 0 : slot + 1;
+            const float ks = __shfl_sync(0xffffffffu, step[0], n & 31), log_step = __shfl_sync(0xffffffffu, step[1], n & 31), inverse = __shfl_sync(0xffffffffu, step[2], n & 31);
+            int32_t acc[NT][2][4];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] = 0.0f;
+                for (int e = 0; e < 4; ++e) acc[t][0][e] = acc[t][1][e] = 0;
 #pragma unroll
             for (int c = 0; c < K::parts; ++c) {
-                const uint4 a = lds128(at + (uint32_t)(c * 512 + lane * 16)), b = lds128(at + (uint32_t)((K::parts + c) * 512 + lane * 16));
-                const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+                const uint4 x = lds128(at + (uint32_t)(c * 512)), y = lds128(at + (uint32_t)((K::parts + c) * 512));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t a0 = codes_f16(x[k]), a1 = codes_f16(y[k]), a2 = codes_f16(x[k] >> 8), a3 = codes_f16(y[k] >> 8);
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma_f16(s[t], a0, a1, a2, a3, qb[t][4 * c + k][0], qb[t][4 * c + k][1]);
-                }
+                    for (int plane = 0; plane < 2; ++plane) {
+                        mma_i8(acc[t][plane], x.x, y.x, x.y, y.y, qb[t][plane][4 * c], qb[t][plane][4 * c + 1]);
+                        mma_i8(acc[t][plane], x.z, y.z, x.w, y.w, qb[t][plane][4 * c + 2], qb[t][plane][4 * c + 3]);
+                    }
             }
             const int key = key_of(l0 + warp + n * FEW_WARPS);
-            const bool none = vs < 0x1p-64f;
-            const float log_step = none ? -64.0f : log2_of(vs), inverse = none ? 0x1p64f : 1.0f / vs;
-            const bool whole = key + FEW_KEYS - 1 <= low_position && (p.window <= 0 || key > high_position - p.window || key + FEW_KEYS <= p.sinks);
-            float over = -INFINITY;
+            const bool edge = key + FEW_KEYS - 1 > low_position || (p.window > 0 && key <= high_position - p.window && key + FEW_KEYS > p.sinks);
+            float s[NT][4], over = -INFINITY;
+            auto exponents = [&]() {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    const float ff[2] = {row_factor[t][0] * ks, row_factor[t][1] * ks}, bb[2] = {log_step - top[t][0], log_step - top[t][1]};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int c = e & 1;
-                    float x = fmaf(s[t][e], row_factor[t][c] * ks, log_step);
-                    if (!whole) {
-                        const int j = key + g + 8 * (e >> 1), at_row = position[t][c];
-                        if (j > at_row || (p.window > 0 && j <= at_row - p.window && j >= p.sinks)) x = -INFINITY;
+                    for (int e = 0; e < 4; ++e) {
+                        const int c = e & 1;
+                        s[t][e] = fmaf((float)(128 * acc[t][0][e] + acc[t][1][e]), ff[c], bb[c]);
+                        if (edge) {
+                            const int j = key + g + 8 * (e >> 1), at_row = position[t][c];
+                            if (j > at_row || (p.window > 0 && j <= at_row - p.window && j >= p.sinks)) s[t][e] = -INFINITY;
+                        }
+                        over = fmaxf(over, s[t][e]);
                     }
-                    s[t][e] = x;
-                    // (-inf minus -inf is no reason)
-                    over = fmaxf(over, x - top[t][c]);
                 }
+            };
+            exponents();
+            // (a row that has seen nothing has the reference -inf, so everything is over)
             if (__any_sync(0xffffffffu, over > 8.0f)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float m = fmaxf(s[t][c], s[t][c + 2]);
+                        // logits without the reference
+                        const float ff = row_factor[t][c] * ks;
+                        float m = -INFINITY;
+#pragma unroll
+                        for (int e = c; e < 4; e += 2)
+                            if (s[t][e] != -INFINITY) m = fmaxf(m, fmaf((float)(128 * acc[t][0][e] + acc[t][1][e]), ff, log_step));
 #pragma unroll
                         for (int l = 4; l < 32; l *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, l));
                         m = fmaxf(m, top[t][c]);
@@ -410,33 +466,29 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 2 : 1) few_kernel(const __g
                             o[t][j][c + 2] *= alpha;
                         }
                     }
+                exponents();
             }
             uint32_t pb[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                float e[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float m = top[t][k & 1];
-                    e[k] = exp2_of(s[t][k] - (m == -INFINITY ? 0.0f : m));
-                }
+                for (int e = 0; e < 4; ++e) s[t][e] = exp2_of(s[t][e]);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const float sum = e[c] + e[c + 2];
+                    const float sum = s[t][c] + s[t][c + 2];
                     if (sum != 0.0f) total[t][c] = fmaf(sum, inverse, total[t][c]);          // (a step that is not finite stays with the rows that see it)
                 }
-                pb[t][0] = none ? 0u : transposed(half2_of(e[0], e[1]));
-                pb[t][1] = none ? 0u : transposed(half2_of(e[2], e[3]));
+                pb[t][0] = transposed(half2_of(s[t][0], s[t][1]));
+                pb[t][1] = transposed(half2_of(s[t][2], s[t][3]));
             }
             uint32_t v[4][D / 32];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const uint32_t from = at + 32 * K::k_lane + (uint32_t)(r * 32 + lane) * K::v_bytes;
                 if constexpr (D == 128) {
-                    const uint4 w = lds128(from);
+                    const uint4 w = lds128(at_v + (uint32_t)(r * 32 * K::v_bytes));
                     v[r][0] = w.x; v[r][1] = w.y; v[r][2] = w.z; v[r][3] = w.w;
                 } else {
-                    const uint2 w = lds64(from);
+                    const uint2 w = lds64(at_v + (uint32_t)(r * 32 * K::v_bytes));
                     v[r][0] = w.x; v[r][1] = w.y;
                 }
             }
@@ -514,10 +566,11 @@ template <int D, int NT>
 __global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendParams p, int ctas)
 {
     using K = Few<D, NT>;
-    griddep_wait();
-    griddep_launch();
+    // (what the sequences are is read before the wait: the kernel before this one let it start after its own wait, so whatever made them has ended, and it writes none of it)
     Found f;
     const Share share = share_units<K::rows>(p, (int)blockIdx.x + 1, ctas, f);
+    griddep_wait();
+    griddep_launch();
     const long long boundary = share.per * (long long)(blockIdx.x + 1);
     if (boundary >= share.all) return;
     const Units u = units_of<K::rows>(p, f.sequence);

@@ -86,12 +86,12 @@ int launch_write(WriteParams &p, int page, cudaStream_t st)
 }
 
 // How many CTAs share the units of few queries: what is resident at once.
-int few_ctas(int sms, int nt) { return nt == 1 ? 2 * sms : sms; }
+int few_ctas(int sms, int nt, int D) { return nt == 1 || D == 64 ? 2 * sms : sms; }
 
 template <int D, int NT>
 int launch_few(const AttendParams &p, int sms, cudaStream_t st)
 {
-    const int ctas = few_ctas(sms, NT);
+    const int ctas = few_ctas(sms, NT, D);
     if (int rc = launch(few_kernel<D, NT>, ctas, THREADS, Few<D, NT>::bytes, st, 1, p)) return rc;
     return launch(join_kernel<D, NT>, ctas - 1, THREADS, 0, st, 1, p, ctas);
 }
@@ -205,7 +205,7 @@ int perq_attention_i8_workspace_bytes(int64_t T, int32_t S, int32_t heads, int32
     int sms = sm_count();
     if (sms <= 0) sms = 148;                                           // (no device, no launch: sizes are answered for a B200)
     const int64_t rows = std::min<int64_t>(T, most) * group;
-    const size_t few = (size_t)few_ctas(sms, 1) * 2 * 8, many = rows > FEW_ROWS ? (size_t)sms * MANY_ROWS : 0;
+    const size_t few = std::max((size_t)few_ctas(sms, 1, D) * 8, (size_t)few_ctas(sms, 2, D) * 16) * 2, many = rows > FEW_ROWS ? (size_t)sms * MANY_ROWS : 0;
     *bytes = T == 0 || S == 0 ? 0 : std::max(few, many) * (size_t)(D + 2) * 4;
     return PERQ_OK;
 }

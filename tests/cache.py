@@ -70,8 +70,9 @@ def visible(positions, length, window, sinks):
 def attention(cache, q, offsets, lengths, pages, b, scale, window=0, sinks=0):
     """(out, tolerance before the result's own rounding), [T, heads of queries, D]; rows of no sequence are NaN.
 
-    Roundings that count: a query's channels to fp16 (2^-11 of each where they are rotated, and half of fp16's smallest step, 2^-25, of the row's largest), which move a logit by
-    at most d_j = scale sum |dq| |k_j|; the rotation's, products', sums' and exponential's in fp32, (64 + |x_j|) 2^-22 in all; a probability times its step to
+    Roundings that count: a query's channels, which move a logit by at most d_j = scale sum |dq| |k_j|.  Few rows: to whole multiples of the largest / 16256, so by 2^-15 of it; many
+    rows: to fp16, 2^-11 of each where they are rotated (bf16 and fp16 are kept otherwise), or half of fp16's smallest step, 2^-25, of the largest; the sum of both covers either.  The
+    rotation's, products', sums' and exponential's in fp32, (64 + |x_j|) 2^-22 in all; a probability times its step to
     fp16, 2^-11 of it, or 2^-25 of at least the largest.  out = sum p v / sum p, so it moves by sum p |v| (d + 2^-11) + |out| sum p d and, for the small ones, by at most
     length 2^-25 times the largest value."""
     T, Hq, D = q.shape
@@ -87,7 +88,7 @@ def attention(cache, q, offsets, lengths, pages, b, scale, window=0, sinks=0):
             x = ((qh @ kh.T) * scale).masked_fill(~seen, -math.inf)
             p = torch.nan_to_num(torch.softmax(x, 1), nan=0.0) * seen                    # (a row that sees nothing)
             y = p @ vh
-            dq = (2.0 ** -11 if b > 1 else 0.0) * qh.abs() + 2.0 ** -25 * qh.abs().amax(1, keepdim=True)
+            dq = (2.0 ** -11 if b > 1 else 0.0) * qh.abs() + 2.0 ** -15 * qh.abs().amax(1, keepdim=True)
             d = abs(scale) * (dq @ kh.abs().T) + (64 + torch.where(seen, x.abs(), 0.0) + abs(scale) * (qh.abs() @ kh.abs().T)) * 2.0 ** -22
             out[rows, h] = y
             most = torch.stack([vh[r].abs().amax() if bool(r.any()) else torch.zeros((), dtype=torch.float64) for r in seen]) if window else torch.cummax(

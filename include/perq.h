@@ -407,7 +407,7 @@ int perq_grouped_matmul_i8_workspace_bytes(int64_t T, int32_t E, int32_t N, int3
  *
  *   k_codes, v_codes    device int8 [n_pages, heads, page, D]: pages of a pool
  *   k_steps, v_steps    device float [n_pages, heads]: value = step * code
- *   page                tokens of a page: 16, 32, 64 or 128;  D: 64 or 128;  heads <= PERQ_MAX_HEADS
+ *   page                tokens of a page: 16, 32, 64 or 128;  D: 64 or 128;  heads <= PERQ_MAX_HEADS, n_pages * heads * page < 2^31
  *   pages               device int32 [S, width]: position j of sequence i lies in page pages[i, j / page], at place j % page
  *   offsets             device int32 [S + 1], not decreasing, in 0 .. T: rows offsets[i] .. offsets[i + 1] of a call are sequence i's, n_i of them
  *   lengths             device int32 [S]: tokens of sequence i, its rows of the call included.  They are its last ones: row r of it has the

@@ -6,8 +6,9 @@
 // fixed order.
 //
 // Keys (then, transposed, values) are the first operand of mma.sync, rows the second, so that eight rows cost no more than they have to.  The order of the
-// channels inside a product is free: a lane takes 16 adjacent codes of its keys as they lie in memory, and of its values 16 adjacent channels of four keys.  It copies just
-// what it reads itself (cp.async into its own places), so the copies want no barrier, and 16-byte reads of them meet no conflict.
+// channels inside a product is free: a lane takes 16 adjacent codes of its keys as they lie in memory, and of its values 16 adjacent channels of four keys.  A warp has a ring of its own
+// in shared memory, filled by tensor copies whose 128-byte swizzle, with odd keys taken four further on (key_in), keeps its 16-byte reads free of conflicts.  (Copies of 16 bytes by every
+// lane ended at 4.6 TB/s, also with nothing done to what they brought: 64 sequences of up to 12000 tokens 228 us.)
 //
 // Logits: keys' codes stay 8-bit integers (m16n8k32).  A query becomes 128 hi + lo of two 8-bit integers, its largest channel 16256, so it is off by 2^-15 of that at most, and S = sum
 // (128 hi + lo) code is exact.  (Codes to fp16 instead: 80 instructions for 16 keys of 128 channels; these products take 8 of the 8 cycles that an fp16 one takes too.)
@@ -24,6 +25,8 @@ namespace perq_kv {
 
 constexpr int FEW_WARPS = THREADS / 32;
 constexpr int FEW_KEYS = 16;                  // of a unit
+// Set in perq_mm's error word when a bounded wait ran out.
+enum : unsigned int { ERROR_ATTEND = 1u << 7 };
 
 struct AttendParams {
     Sequences q;
@@ -40,11 +43,14 @@ struct AttendParams {
     float scale;                              // of logits, times log2 e / sqrt b
 };
 
-__device__ __forceinline__ void copy16(uint32_t to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
-__device__ __forceinline__ void copy8(uint32_t to, const void *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// Row g of a product's first operand is this key of eight, so that rows next to each other differ in bit 2 of their place, and even rows hold even keys.
+__device__ __forceinline__ int key_in(int g) { return g ^ ((g & 1) << 2); }
+// Where 16 bytes lie in rows of D with their copies' swizzle (of 128 or 64 bytes).
+template <int D>
+__device__ __forceinline__ uint32_t swizzled(int row, int chunk)
+{
+    return (uint32_t)(row * D + (D == 128 ? (chunk ^ row) & 7 : (chunk ^ (row >> 1)) & 3) * 16);
+}
 __device__ __forceinline__ float exp2_of(float x)
 {
     float r;
@@ -219,9 +225,9 @@ struct Few {
     static constexpr int v_bytes = D / 8;                              // of a value
     static constexpr int k_lane = 2 * parts * 16, lane_bytes = k_lane + 4 * v_bytes;
     static constexpr int stages = D == 64 ? 6 : NT == 1 ? 3 : 6;          // units of a warp that are on their way or read
-    static constexpr int stage = 32 * lane_bytes, ring = FEW_WARPS * stages * stage;
+    static constexpr int stage = 32 * lane_bytes, ring = FEW_WARPS * stages * stage;               // keys, values
     static constexpr int off_q = ring, off_factor = off_q + 2 * rows * D, off_top = off_factor + rows * 4, off_sum = off_top + FEW_WARPS * rows * 4,
-                         bytes = off_sum + FEW_WARPS * rows * 4;
+                         off_bars = off_sum + FEW_WARPS * rows * 4, bytes = off_bars + FEW_WARPS * stages * 8 + 1024;
     static_assert(FEW_WARPS * rows * D * 4 <= ring, "the warps' sums lie where the copies did");
 };
 
@@ -244,15 +250,24 @@ __device__ __forceinline__ void store_out4(const AttendParams &p, size_t at, flo
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kernel(const __grid_constant__ AttendParams p)
+__global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttendParams p)
 {
     using K = Few<D, NT>;
-    extern __shared__ __align__(128) unsigned char smem[];
+    extern __shared__ __align__(128) unsigned char raw[];
+    unsigned char *const smem = raw + ((1024u - (perq_mm::smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = perq_mm::smem_u32(smem);
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
     int8_t *const q_room = reinterpret_cast<int8_t *>(smem + K::off_q);
     float *const factor = reinterpret_cast<float *>(smem + K::off_factor), *const tops = reinterpret_cast<float *>(smem + K::off_top),
           *const totals = reinterpret_cast<float *>(smem + K::off_sum), *const sums = reinterpret_cast<float *>(smem);
+    const uint32_t mine = base + (uint32_t)(warp * K::stages * K::stage), bars = base + K::off_bars + (uint32_t)(warp * K::stages * 8);
+    if (lane == 0) {
+        perq_mm::prefetch_map(&k_map);
+        perq_mm::prefetch_map(&v_map);
+        for (uint32_t k = 0; k < K::stages; ++k) perq_mm::mbar_init(bars + 8u * k, 1);
+        perq_mm::mbar_init_fence();
+    }
+    __syncwarp();
     griddep_wait();
     griddep_launch();
     Found f;
@@ -261,8 +276,15 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
     const long long unit_end = min(unit + share.per, share.all);
     int i = f.sequence;
     long long begin = f.begin;
-    const uint32_t mine = base + (uint32_t)(warp * K::stages * K::stage) + (uint32_t)lane * 16u, mine_v = base + (uint32_t)(warp * K::stages * K::stage + 32 * K::k_lane + lane * K::v_bytes);
-    const uint32_t page_bytes = (uint32_t)(p.heads * D) << p.q.page;                     // of a page in the pool
+    // this lane's places in a unit: 16 channels of a key (and of the one eight further on), channels of four keys' values
+    uint32_t k_at[K::parts], v_at[2];
+#pragma unroll
+    for (int c = 0; c < K::parts; ++c) k_at[c] = swizzled<D>(key_in(g), q + 4 * c);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) v_at[r] = 16u * D + (D == 128 ? swizzled<D>(key_in(2 * q + r), g) : swizzled<D>(key_in(2 * q + r), g / 2) + (uint32_t)(g & 1) * 8u);
+    int slot_in = 0, slot = 0;                                         // of the ring: what is issued, and what is read, next
+    uint32_t parity = 0u;                                              // of the ring's barriers, for what is read
+    bool ok = true;
 
     while (unit < unit_end && i < p.q.S) {
         // the tile of this unit
@@ -279,9 +301,6 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
         const int first = u.r.length - u.r.n;                          // position of the sequence's first row
         const int low_position = first + row0 / p.group, high_position = first + (row0 + rows - 1) / p.group;
         const int32_t *const table = p.q.pages + (size_t)i * (size_t)p.q.width;
-        const size_t of_head = ((size_t)head * D) << p.q.page;
-        const int8_t *const k_base = p.k_codes + of_head + (size_t)(g * D + q * 16), *const v_base = p.v_codes + of_head + (size_t)(2 * q * D + g * K::v_bytes);
-
         auto key_of = [&](int l) { return (l < u.sunk ? l : l - u.sunk + u.low) * FEW_KEYS; };
         // of 32 units of this warp, one to a lane: pages, s_k, log2 s_v, 1 / s_v
         const int units = l1 - l0 > warp ? (l1 - l0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
@@ -298,25 +317,18 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
                 next_step[2] = vs < 0x1p-64f ? 0x1p64f : 1.0f / vs;
             }
         };
-        int slot_in = 0;                                               // of the ring, for the unit that is issued next
         auto issue = [&](int n) {
             if (n < units) {
                 const int its_page = __shfl_sync(0xffffffffu, next_page, n & 31), key = key_of(l0 + warp + n * FEW_WARPS);
-                const size_t at = (size_t)its_page * page_bytes + (size_t)(uint32_t)((key & ((1 << p.q.page) - 1)) * D);
-                const int8_t *const k = k_base + at, *const v = v_base + at;
-                const uint32_t to = mine + (uint32_t)slot_in * K::stage, to_v = mine_v + (uint32_t)slot_in * K::stage;
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int c = 0; c < K::parts; ++c) copy16(to + (uint32_t)((r * K::parts + c) * 512), k + 8 * r * D + c * 64);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (D == 128) copy16(to_v + (uint32_t)(r * 32 * K::v_bytes), v + ((r & 1) + 8 * (r >> 1)) * D);
-                    else copy8(to_v + (uint32_t)(r * 32 * K::v_bytes), v + ((r & 1) + 8 * (r >> 1)) * D);
+                if (lane == 0) {
+                    const uint32_t to = mine + (uint32_t)slot_in * K::stage, bar = bars + 8u * (uint32_t)slot_in;
+                    const int line = ((its_page * p.heads + head) << p.q.page) + (key & ((1 << p.q.page) - 1));
+                    perq_mm::mbar_expect_tx(bar, K::stage);
+                    perq_mm::tma_load(to, &k_map, 0, line, bar);
+                    perq_mm::tma_load(to + 16u * D, &v_map, 0, line, bar);
                 }
                 slot_in = slot_in + 1 == K::stages ? 0 : slot_in + 1;
             }
-            copies_end();
         };
         fetch(0);
         next_page = later_page;
@@ -392,7 +404,6 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
             }
         }
 
-        int slot = 0;
         for (int n = 0; n < units; ++n) {
             if ((n & 31) == 0) {
 #pragma unroll
@@ -401,27 +412,46 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
             // (of the next 32 units, well before the first of them is issued)
             if ((n & 31) == 16) fetch((n >> 5) + 1);
             if ((n & 31) == 33 - K::stages) next_page = later_page;
+            __syncwarp();                                              // (all lanes have read what lay where the next copy goes)
             issue(n + K::stages - 1);
-            copies_wait<K::stages - 1>();
-            const uint32_t at = mine + (uint32_t)slot * K::stage, at_v = mine_v + (uint32_t)slot * K::stage;
+            if (!perq_mm::mbar_wait_warp(bars + 8u * (uint32_t)slot, parity)) ok = false;
+            const uint32_t at = mine + (uint32_t)slot * K::stage;
             slot = slot + 1 == K::stages ? 0 : slot + 1;
+            parity ^= slot == 0 ? 1u : 0u;
+            if (!ok) continue;                                         // (the other copies are waited for all the same)
             const float ks = __shfl_sync(0xffffffffu, step[0], n & 31), log_step = __shfl_sync(0xffffffffu, step[1], n & 31), inverse = __shfl_sync(0xffffffffu, step[2], n & 31);
             int32_t acc[NT][2][4];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[t][0][e] = acc[t][1][e] = 0;
+            // (all that is read of the unit is on its way before the first of it is used)
+            uint4 x[K::parts], y[K::parts];
 #pragma unroll
             for (int c = 0; c < K::parts; ++c) {
-                const uint4 x = lds128(at + (uint32_t)(c * 512)), y = lds128(at + (uint32_t)((K::parts + c) * 512));
+                x[c] = lds128(at + k_at[c]);
+                y[c] = lds128(at + k_at[c] + 8u * D);
+            }
+            uint32_t v[4][D / 32];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (D == 128) {
+                    const uint4 w = lds128(at + v_at[r & 1] + (uint32_t)(r >> 1) * 8u * D);
+                    v[r][0] = w.x; v[r][1] = w.y; v[r][2] = w.z; v[r][3] = w.w;
+                } else {
+                    const uint2 w = lds64(at + v_at[r & 1] + (uint32_t)(r >> 1) * 8u * D);
+                    v[r][0] = w.x; v[r][1] = w.y;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < K::parts; ++c)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int plane = 0; plane < 2; ++plane) {
-                        mma_i8(acc[t][plane], x.x, y.x, x.y, y.y, qb[t][plane][4 * c], qb[t][plane][4 * c + 1]);
-                        mma_i8(acc[t][plane], x.z, y.z, x.w, y.w, qb[t][plane][4 * c + 2], qb[t][plane][4 * c + 3]);
+                        mma_i8(acc[t][plane], x[c].x, y[c].x, x[c].y, y[c].y, qb[t][plane][4 * c], qb[t][plane][4 * c + 1]);
+                        mma_i8(acc[t][plane], x[c].z, y[c].z, x[c].w, y[c].w, qb[t][plane][4 * c + 2], qb[t][plane][4 * c + 3]);
                     }
-            }
             const int key = key_of(l0 + warp + n * FEW_WARPS);
             const bool edge = key + FEW_KEYS - 1 > low_position || (p.window > 0 && key <= high_position - p.window && key + FEW_KEYS > p.sinks);
             float s[NT][4], over = -INFINITY;
@@ -434,7 +464,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
                         const int c = e & 1;
                         s[t][e] = fmaf((float)(128 * acc[t][0][e] + acc[t][1][e]), ff[c], bb[c]);
                         if (edge) {
-                            const int j = key + g + 8 * (e >> 1), at_row = position[t][c];
+                            const int j = key + key_in(g) + 8 * (e >> 1), at_row = position[t][c];
                             if (j > at_row || (p.window > 0 && j <= at_row - p.window && j >= p.sinks)) s[t][e] = -INFINITY;
                         }
                         over = fmaxf(over, s[t][e]);
@@ -481,17 +511,6 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
                 pb[t][0] = transposed(half2_of(s[t][0], s[t][1]));
                 pb[t][1] = transposed(half2_of(s[t][2], s[t][3]));
             }
-            uint32_t v[4][D / 32];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if constexpr (D == 128) {
-                    const uint4 w = lds128(at_v + (uint32_t)(r * 32 * K::v_bytes));
-                    v[r][0] = w.x; v[r][1] = w.y; v[r][2] = w.z; v[r][3] = w.w;
-                } else {
-                    const uint2 w = lds64(at_v + (uint32_t)(r * 32 * K::v_bytes));
-                    v[r][0] = w.x; v[r][1] = w.y;
-                }
-            }
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
                 constexpr uint32_t pick[4] = {0x0400u, 0x0501u, 0x0602u, 0x0703u};
@@ -502,7 +521,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
                 for (int t = 0; t < NT; ++t) mma_f16(o[t][j], a0, a1, a2, a3, pb[t][0], pb[t][1]);
             }
         }
-        copies_wait<0>();
+        if (!ok && lane == 0) atomicOr(&perq_mm::g_error, ERROR_ATTEND);
 
         // the warps' results become one
 #pragma unroll
@@ -556,7 +575,8 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
                 }
             }
         }
-        __syncthreads();                                               // (before the next tile's copies)
+        perq_mm::fence_async_smem();                                   // (before the next tile's copies)
+        __syncthreads();
         unit = tile_begin + l1;
     }
 }

@@ -14,8 +14,6 @@ namespace perq_kv {
 
 constexpr int CODES_WARP = 8, MMA_WARP = 12, LOAD_WARP = 13; // warps: 8 of the rows, 4 that make codes fp16, the products', the loads', 2 idle
 constexpr int MANY_ROWS = 256, MANY_KEYS = 128, MANY_THREADS = 512;
-// (perq_attend_few's rows go up to this; both sides measured beside launch_attention)
-enum : unsigned int { ERROR_ATTEND = 1u << 7 };
 
 struct ManyParams {
     AttendParams a;

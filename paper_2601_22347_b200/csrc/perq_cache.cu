@@ -38,7 +38,7 @@ int launch(void (*kernel)(P...), long long grid, int threads, size_t smem, cudaS
 int check_cache(int64_t T, int32_t S, int32_t heads, int32_t D, int32_t b, int32_t page, int64_t n_pages, int32_t width)
 {
     if (T < 0 || T > (1 << 30) || S < 0 || S > PERQ_MAX_SEQUENCES || heads < 1 || heads > PERQ_MAX_HEADS || (D != 64 && D != 128)) return PERQ_ERR_SHAPE;
-    if (!is_pow2(page) || page < 16 || page > 128 || n_pages < 1 || n_pages > INT32_MAX || width < 1 || (int64_t)width * page > (1 << 30)) return PERQ_ERR_SHAPE;
+    if (!is_pow2(page) || page < 16 || page > 128 || n_pages < 1 || n_pages > INT32_MAX || n_pages * page * heads > INT32_MAX || width < 1 || (int64_t)width * page > (1 << 30)) return PERQ_ERR_SHAPE;
     if (!is_pow2(b) || (b != 1 && b < 16) || b > D) return PERQ_ERR_BLOCK;
     return PERQ_OK;
 }
@@ -88,11 +88,25 @@ int launch_write(WriteParams &p, int page, cudaStream_t st)
 // How many CTAs share the units of few queries: what is resident at once.
 int few_ctas(int sms, int nt, int D) { return nt == 1 || D == 64 ? 2 * sms : sms; }
 
+// Codes as rows of D bytes, in boxes of a unit's keys.
+template <int D>
+bool codes_map(CUtensorMap *map, const void *codes, const AttendParams &p)
+{
+    TensorMapEncode encode = tensor_map_encode();
+    if (encode == nullptr) return false;
+    const cuuint64_t dims[2] = {D, ((cuuint64_t)p.q.n_pages * (cuuint64_t)p.heads) << p.q.page}, strides[1] = {D};
+    const cuuint32_t size[2] = {D, FEW_KEYS}, step[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, size, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, int NT>
 int launch_few(const AttendParams &p, int sms, cudaStream_t st)
 {
     const int ctas = few_ctas(sms, NT, D);
-    if (int rc = launch(few_kernel<D, NT>, ctas, THREADS, Few<D, NT>::bytes, st, 1, p)) return rc;
+    CUtensorMap k, v;
+    if (!codes_map<D>(&k, p.k_codes, p) || !codes_map<D>(&v, p.v_codes, p)) return PERQ_ERR_CUDA;
+    if (int rc = launch(few_kernel<D, NT>, ctas, THREADS, Few<D, NT>::bytes, st, 1, k, v, p)) return rc;
     return launch(join_kernel<D, NT>, ctas - 1, THREADS, 0, st, 1, p, ctas);
 }
 

@@ -581,11 +581,72 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
     }
 }
 
-// Tiles whose units several CTAs had: CTA `b` puts the one together that its boundary, between shares b and b + 1, is the first to cut.
+// Results of parts of a row's keys, weighted: 4 rows of `parts` results, whose sums lie at `sums_of(part)` (row, then channels), and their references and probabilities at `ends_of(part)`
+// ([row], [row + stride]).  `finish(row, channel, v)` gets four channels of a row.  Called by all threads of the CTA, which has 4 * parts + 4 floats and 16 * THREADS bytes of shared memory
+// at `room`.  Loads of eight parts are on their way at once: one after another they were most of the time (a token behind 1000: 8.9 us, two behind 130000 16).
+constexpr int JOIN_ROWS = 4;
+template <int D, typename Sums, typename Ends, typename Finish>
+__device__ __forceinline__ void join_rows(float *room, int parts, int stride, const Sums &sums_of, const Ends &ends_of, const Finish &finish)
+{
+    constexpr int items = JOIN_ROWS * D / 4, lots = THREADS / items;   // of four channels; threads to one
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float *const weights = room + 4 * THREADS, *const inverse = weights + JOIN_ROWS * parts;
+    if (warp < JOIN_ROWS) {
+        float m = -INFINITY, l = 0.0f;
+        for (int c = lane; c < parts; c += 32) {
+            const float x = ends_of(c)[warp];
+            weights[c * JOIN_ROWS + warp] = x;
+            m = fmaxf(m, x);
+        }
+#pragma unroll
+        for (int k = 16; k > 0; k /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+        for (int c = lane; c < parts; c += 32) {
+            const float x = weights[c * JOIN_ROWS + warp], a = x == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : exp2_of(x - m);
+            weights[c * JOIN_ROWS + warp] = a;
+            l = fmaf(a, ends_of(c)[stride + warp], l);
+        }
+#pragma unroll
+        for (int k = 16; k > 0; k /= 2) l += __shfl_xor_sync(0xffffffffu, l, k);
+        if (lane == 0) inverse[warp] = l == 0.0f ? 0.0f : 1.0f / l;
+    }
+    __syncthreads();
+    const int item = tid % items, lot = tid / items, row = item / (D / 4), channel = item % (D / 4) * 4;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int c0 = lot; c0 < parts; c0 += 8 * lots) {
+        float4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = c0 + k * lots;
+            x[k] = c < parts ? *reinterpret_cast<const float4 *>(sums_of(c) + row * D + channel) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = c0 + k * lots;
+            const float a = c < parts ? weights[c * JOIN_ROWS + row] : 0.0f;
+            v.x = fmaf(a, x[k].x, v.x); v.y = fmaf(a, x[k].y, v.y); v.z = fmaf(a, x[k].z, v.z); v.w = fmaf(a, x[k].w, v.w);
+        }
+    }
+    float4 *const others = reinterpret_cast<float4 *>(room);
+    others[tid] = v;
+    __syncthreads();
+    if (lot == 0) {
+#pragma unroll
+        for (int k = 1; k < lots; ++k) {
+            const float4 x = others[item + k * items];
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        const float r = inverse[row];
+        finish(row, channel, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+    }
+}
+inline size_t join_bytes(int parts) { return (size_t)(4 * THREADS + JOIN_ROWS * parts + JOIN_ROWS) * 4; }
+
+// Tiles whose units several CTAs had: CTA (b, y) puts four rows of the one together that its boundary, between shares b and b + 1, is the first to cut.
 template <int D, int NT>
 __global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendParams p, int ctas)
 {
     using K = Few<D, NT>;
+    extern __shared__ __align__(16) float room[];
     // (what the sequences are is read before the wait: the kernel before this one let it start after its own wait, so whatever made them has ended, and it writes none of it)
     Found f;
     const Share share = share_units<K::rows>(p, (int)blockIdx.x + 1, ctas, f);
@@ -594,28 +655,18 @@ __global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ A
     const long long boundary = share.per * (long long)(blockIdx.x + 1);
     if (boundary >= share.all) return;
     const Units u = units_of<K::rows>(p, f.sequence);
-    const int number = (int)((boundary - f.begin) / u.count), head = number / u.tiles, row0 = (number - head * u.tiles) * K::rows;
+    const int number = (int)((boundary - f.begin) / u.count), head = number / u.tiles, row0 = (number - head * u.tiles) * K::rows + (int)blockIdx.y * JOIN_ROWS;
     const long long tile_begin = f.begin + (long long)number * u.count, tile_end = tile_begin + u.count;
     if (tile_begin == boundary || tile_begin < boundary - share.per) return;
-    const int rows = min(K::rows, u.tokens * p.group - row0), c0 = (int)blockIdx.x, c1 = (int)((tile_end - 1) / share.per);
-    auto result_of = [&](int c) { return share_result<D, NT>(p, c, c == c0); };
-    for (int k = (int)threadIdx.x; k < rows * D / 4; k += THREADS) {
-        const int row = k / (D / 4), channel = k % (D / 4) * 4;
-        float m = -INFINITY, l = 0.0f;
-        for (int c = c0; c <= c1; ++c) m = fmaxf(m, result_of(c)[K::rows * D + row]);
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int c = c0; c <= c1; ++c) {
-            const float *const from = result_of(c);
-            const float mc = from[K::rows * D + row], a = mc == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : exp2_of(mc - m);
-            const float4 x = *reinterpret_cast<const float4 *>(from + row * D + channel);
-            l = fmaf(a, from[K::rows * D + K::rows + row], l);
-            v.x = fmaf(a, x.x, v.x); v.y = fmaf(a, x.y, v.y); v.z = fmaf(a, x.z, v.z); v.w = fmaf(a, x.w, v.w);
-        }
-        const float r = l == 0.0f ? 0.0f : 1.0f / l;
-        const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
-        store_out4<D>(p, ((size_t)(u.r.begin + token) * (size_t)(p.heads * p.group) + (size_t)(head * p.group + h)) * D + (size_t)channel,
-                      make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-    }
+    const int rows = u.tokens * p.group - row0, c0 = (int)blockIdx.x, c1 = (int)((tile_end - 1) / share.per);
+    if (rows <= 0) return;
+    auto result_of = [&](int c) { return share_result<D, NT>(p, c0 + c, c == 0) + (int)blockIdx.y * JOIN_ROWS * D; };
+    join_rows<D>(room, c1 - c0 + 1, K::rows, result_of, [&](int c) { return share_result<D, NT>(p, c0 + c, c == 0) + K::rows * D + (int)blockIdx.y * JOIN_ROWS; },
+                 [&](int row, int channel, float4 v) {
+                     if (row >= rows) return;
+                     const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
+                     store_out4<D>(p, ((size_t)(u.r.begin + token) * (size_t)(p.heads * p.group) + (size_t)(head * p.group + h)) * D + (size_t)channel, v);
+                 });
 }
 
 }  // namespace perq_kv

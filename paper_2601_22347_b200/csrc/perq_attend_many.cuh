@@ -264,8 +264,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     if (warp < CODES_WARP) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");          // (of 128 at launch: 2 x 176 + 80 + 80 = 4 x 128)
         const int t = warp >> 2, row = t * 128 + (tid & 127);
-        const int token = (it.row0 + min(row, it.rows - 1)) / p.a.group, h = it.row0 + min(row, it.rows - 1) - token * p.a.group;
-        const int position = it.first + token;
+        const int position = it.first + (it.row0 + min(row, it.rows - 1)) / p.a.group;
         if (t == 0 || two) {
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes;
             // Queries: 32 rows to a warp, 16 channels to a lane; a row's largest is scaled to 1 .. 2 by a power of two, then it is rotated and rounded to fp16.
@@ -439,17 +438,36 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 if (lane == 0) give_up();
             } else {
                 const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-                const bool narrow = p.split == 1 && p.a.out_type != OUT_F32, f16 = p.a.out_type == OUT_F16, there = row < it.rows;
+                const bool f16 = p.a.out_type == OUT_F16;
                 if (p.split > 1) {
                     float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
                     ends[row] = m;
                     ends[MANY_ROWS + row] = l;
                 }
-                float *const wide_out = p.split > 1 ? many_part<D>(p, it.number, part) + (size_t)row * D
-                                                    : static_cast<float *>(p.a.out) + ((size_t)(it.begin + token) * ((size_t)p.a.heads * (size_t)p.a.group) +
-                                                                                       (size_t)it.head * (size_t)p.a.group + (size_t)h) * D;
-                // 16-bit results go through shared memory, where the queries were, so that rows are stored whole.
-                const uint32_t room = base + (uint32_t)t * K::tile, thread = (uint32_t)tid & 127u;
+                // Results go through shared memory, where the queries were, as many bytes of every row at a time as its queries had, so that rows are stored whole.
+                constexpr int line_bytes = 2 * D;
+                const uint32_t room = base + (uint32_t)t * K::tile + (uint32_t)((warp & 3) * 32 * line_bytes);
+                auto to_rows = [&](const uint32_t (&w)[4], int chunk) {
+                    sts128(room + (uint32_t)(lane * line_bytes + ((chunk ^ lane) & 7) * 16 + (chunk & 8) * 16), make_uint4(w[0], w[1], w[2], w[3]));
+                };
+                auto store_rows = [&](auto &&address) {
+                    __syncwarp();
+                    constexpr int wide = line_bytes / 16, at_once = 32 / wide;
+#pragma unroll 4
+                    for (int k = 0; k < 32 / at_once; ++k) {
+                        const int line = k * at_once + lane / wide, chunk = lane % wide, r = t * 128 + (warp & 3) * 32 + line;
+                        const uint4 w = lds128(room + (uint32_t)(line * line_bytes + ((chunk ^ line) & 7) * 16 + (chunk & 8) * 16));
+                        if (r < it.rows) *reinterpret_cast<uint4 *>(address(r) + chunk * 16) = w;
+                    }
+                    __syncwarp();
+                };
+                auto out_row = [&](int r, int bytes) {                 // of the results
+                    const int pairs = it.row0 + r, its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
+                    return static_cast<char *>(p.a.out) +
+                           ((size_t)(it.begin + its_token) * ((size_t)p.a.heads * (size_t)p.a.group) + (size_t)(it.head * p.a.group + its_head)) * (size_t)(D * bytes);
+                };
+                const bool wide = p.split > 1 || p.a.out_type == OUT_F32;
+                constexpr int per = D / 32;                            // 16 fp32 columns each, to a line
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     int32_t u[16];
@@ -463,28 +481,30 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     float o[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[i] = __int_as_float(u[i]) * r;
-                    if (narrow) {
-                        const uint32_t to = room + thread * (2u * D) + (uint32_t)(2 * c & 8) * 16u, at = (uint32_t)(2 * c);
-                        sts128(to + ((at ^ thread) & 7u) * 16u, make_uint4(pack16(o[0], o[1], f16), pack16(o[2], o[3], f16), pack16(o[4], o[5], f16), pack16(o[6], o[7], f16)));
-                        sts128(to + (((at + 1u) ^ thread) & 7u) * 16u, make_uint4(pack16(o[8], o[9], f16), pack16(o[10], o[11], f16), pack16(o[12], o[13], f16), pack16(o[14], o[15], f16)));
-                    } else if (there) {
+                    if (wide) {
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(wide_out + 16 * c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t w[4] = {__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]), __float_as_uint(o[4 * i + 2]), __float_as_uint(o[4 * i + 3])};
+                            to_rows(w, 4 * (c % per) + i);
+                        }
+                        if (c % per == per - 1) {
+                            if (p.split > 1) {
+                                char *const to = reinterpret_cast<char *>(many_part<D>(p, it.number, part) + 16 * (c - per + 1));
+                                store_rows([&](int r) { return to + (size_t)r * (4 * D); });
+                            } else {
+                                store_rows([&](int r) { return out_row(r, 4) + 64 * (c - per + 1); });
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t w[4] = {pack16(o[8 * i], o[8 * i + 1], f16), pack16(o[8 * i + 2], o[8 * i + 3], f16), pack16(o[8 * i + 4], o[8 * i + 5], f16),
+                                                   pack16(o[8 * i + 6], o[8 * i + 7], f16)};
+                            to_rows(w, 2 * c + i);
+                        }
                     }
                 }
-                if (narrow) {
-                    __syncwarp();
-                    constexpr int wide = D / 8, at_once = 32 / wide;
-#pragma unroll 4
-                    for (int k = 0; k < 32 / at_once; ++k) {
-                        const int line = (warp & 3) * 32 + k * at_once + lane / wide, chunk = lane % wide, pairs = it.row0 + t * 128 + line;
-                        const int its_token = pairs / p.a.group, its_head = pairs - its_token * p.a.group;
-                        const uint4 w = lds128(room + (uint32_t)line * (2u * D) + (uint32_t)(((chunk ^ line) & 7) * 16 + (chunk & 8) * 16));
-                        if (t * 128 + line < it.rows)
-                            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.a.out) +
-                                                       ((size_t)(it.begin + its_token) * ((size_t)p.a.heads * (size_t)p.a.group) + (size_t)(it.head * p.a.group + its_head)) * D + chunk * 8) = w;
-                    }
-                }
+                if (!wide) store_rows([&](int r) { return out_row(r, 2); });
             }
         }
     } else if (warp < MMA_WARP) {
@@ -634,25 +654,44 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(K::columns) : "memory");
 }
 
-// Rows whose keys were split: blockIdx.x is an item, blockIdx.y a quarter of its rows.
+// Rows whose keys were split: blockIdx.x is an item, blockIdx.y a part of its rows.  A thread has four channels of a row at a time, and up to four parts of them on their way.
+constexpr int MANY_JOIN = 8;
 template <int D>
 __global__ void __launch_bounds__(THREADS) many_join_kernel(const __grid_constant__ ManyParams p)
 {
+    const ManyItem it = many_item(p.a, (int)blockIdx.x, (int)threadIdx.x & 31);       // (every warp for itself; before the wait, as in join_kernel)
     griddep_wait();
     griddep_launch();
-    const ManyItem it = many_item(p.a, (int)blockIdx.x, (int)threadIdx.x & 31);       // (every warp for itself)
-    const int row_begin = (int)blockIdx.y * (MANY_ROWS / 4), row_end = min(row_begin + MANY_ROWS / 4, it.rows);
+    const int row_begin = (int)blockIdx.y * (MANY_ROWS / MANY_JOIN), row_end = min(row_begin + MANY_ROWS / MANY_JOIN, it.rows);
+    const float *const parts = many_part<D>(p, it.number, 0);
+    constexpr size_t each = (size_t)MANY_ROWS * (D + 2);
     for (int k = (int)threadIdx.x; k < (row_end - row_begin) * (D / 4); k += THREADS) {
         const int row = row_begin + k / (D / 4), channel = k % (D / 4) * 4;
         float m = -INFINITY, l = 0.0f;
-        for (int c = 0; c < p.split; ++c) m = fmaxf(m, many_part<D>(p, it.number, c)[MANY_ROWS * D + row]);
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int c = 0; c < p.split; ++c) {
-            const float *const from = many_part<D>(p, it.number, c);
-            const float mc = from[MANY_ROWS * D + row], a = mc == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : exp2_of(mc - m);
-            const float4 x = *reinterpret_cast<const float4 *>(from + (size_t)row * D + channel);
-            l = fmaf(a, from[MANY_ROWS * D + MANY_ROWS + row], l);
-            v.x = fmaf(a, x.x, v.x); v.y = fmaf(a, x.y, v.y); v.z = fmaf(a, x.z, v.z); v.w = fmaf(a, x.w, v.w);
+        for (int c0 = 0; c0 < p.split; c0 += 4) {
+            float4 x[4];
+            float xm[4], xl[4], next = m;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float *const from = parts + (size_t)min(c0 + c, p.split - 1) * each;
+                x[c] = *reinterpret_cast<const float4 *>(from + (size_t)row * D + channel);
+                xm[c] = c0 + c < p.split ? from[(size_t)MANY_ROWS * D + row] : -INFINITY;
+                xl[c] = from[(size_t)MANY_ROWS * D + MANY_ROWS + row];
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) next = fmaxf(next, xm[c]);
+            const float before = m == -INFINITY ? 0.0f : exp2_of(m - next);
+            v.x *= before; v.y *= before; v.z *= before; v.w *= before;
+            l *= before;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                // (a part that has seen nothing, or nothing but what is not finite, which stays)
+                const float a = xm[c] == -INFINITY ? (c0 + c < p.split && xl[c] != xl[c] ? 1.0f : 0.0f) : exp2_of(xm[c] - next);
+                l = fmaf(a, xl[c], l);
+                v.x = fmaf(a, x[c].x, v.x); v.y = fmaf(a, x[c].y, v.y); v.z = fmaf(a, x[c].z, v.z); v.w = fmaf(a, x[c].w, v.w);
+            }
+            m = next;
         }
         const float r = l == 0.0f ? 0.0f : 1.0f / l;
         const int token = (it.row0 + row) / p.a.group, h = it.row0 + row - token * p.a.group;

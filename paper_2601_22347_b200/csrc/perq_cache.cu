@@ -107,17 +107,19 @@ int launch_few(const AttendParams &p, int sms, cudaStream_t st)
     CUtensorMap k, v;
     if (!codes_map<D>(&k, p.k_codes, p) || !codes_map<D>(&v, p.v_codes, p)) return PERQ_ERR_CUDA;
     if (int rc = launch(few_kernel<D, NT>, ctas, THREADS, Few<D, NT>::bytes, st, 1, k, v, p)) return rc;
-    return launch(join_kernel<D, NT>, ctas - 1, THREADS, 0, st, 1, p, ctas);
+    return launch(join_kernel<D, NT>, ctas - 1, THREADS, join_bytes(ctas), st, 8 * NT / JOIN_ROWS, p, ctas);
 }
 
 // Rows (of tokens and heads) of a sequence up to which the kernel for few queries takes it.
 constexpr int FEW_ROWS = 64;
+constexpr int MANY_PIECES = 4;               // to an SM, of tiles of rows whose keys are split
 
-// CTAs to the keys of a tile of rows: as many as leave no SM without work.
+// CTAs to the keys of a tile of rows.  Few items leave SMs without work, or, with contexts of different lengths, one SM with much more than another: pieces are made until there are four to
+// an SM, none of fewer than four tiles of keys.
 int many_split(const AttendParams &p, long long items, int sms)
 {
     const long long key_tiles = (((long long)p.q.width << p.q.page) + MANY_KEYS - 1) / MANY_KEYS;
-    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(sms / items, 16), key_tiles / 4));
+    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(MANY_PIECES * sms / items, 16), key_tiles / 4));
 }
 
 template <int D>
@@ -132,7 +134,7 @@ int launch_many(const AttendParams &a, int sms, cudaStream_t st)
     p.split = many_split(a, items, sms);
     if (items * p.split >= (1ll << 31)) return PERQ_ERR_SHAPE;
     if (int rc = launch(a.q.page == 4 ? many_kernel<D, true> : many_kernel<D, false>, items * p.split, MANY_THREADS, Many<D>::bytes, st, 1, p)) return rc;
-    return p.split > 1 ? launch(many_join_kernel<D>, items, THREADS, 0, st, 4, p) : PERQ_OK;
+    return p.split > 1 ? launch(many_join_kernel<D>, items, THREADS, 0, st, MANY_JOIN, p) : PERQ_OK;
 }
 
 template <int D>
@@ -219,7 +221,7 @@ int perq_attention_i8_workspace_bytes(int64_t T, int32_t S, int32_t heads, int32
     int sms = sm_count();
     if (sms <= 0) sms = 148;                                           // (no device, no launch: sizes are answered for a B200)
     const int64_t rows = std::min<int64_t>(T, most) * group;
-    const size_t few = std::max((size_t)few_ctas(sms, 1, D) * 8, (size_t)few_ctas(sms, 2, D) * 16) * 2, many = rows > FEW_ROWS ? (size_t)sms * MANY_ROWS : 0;
+    const size_t few = std::max((size_t)few_ctas(sms, 1, D) * 8, (size_t)few_ctas(sms, 2, D) * 16) * 2, many = rows > FEW_ROWS ? (size_t)MANY_PIECES * (size_t)sms * MANY_ROWS : 0;
     *bytes = T == 0 || S == 0 ? 0 : std::max(few, many) * (size_t)(D + 2) * 4;
     return PERQ_OK;
 }

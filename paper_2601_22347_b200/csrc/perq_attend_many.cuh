@@ -39,19 +39,17 @@ __host__ __device__ constexpr uint32_t f16_desc(int m, int n, bool second_transp
 {
     return (1u << 4) | ((uint32_t)second_transposed << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-// Waits of whole warps for barriers that only this CTA's threads and copies arrive at.  A poll sleeps for up to 2 us (without that, warps that waited took more issue slots than those that
-// worked: two prompts of up to 8192 in 303 us); at most 2^19 of them, a second.
+// Waits of whole warps for barriers that only this CTA's threads and copies arrive at.
 __device__ __forceinline__ bool cta_poll(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
-                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0u;
 }
 __device__ __forceinline__ bool cta_wait_warp(uint32_t bar, uint32_t parity)
 {
     bool done = cta_poll(bar, parity);
-    for (uint32_t i = 0; i < 1u << 19 && !done; ++i) done = cta_poll(bar, parity);
+    for (uint32_t i = 0; i < perq_mm::WAIT_POLLS && !done; ++i) done = cta_poll(bar, parity);
     return __all_sync(0xffffffffu, done);
 }
 // By whole warps, of which one lane issues: what describes a product then stays in uniform registers.  (A lane of its own, with the warps that compute exponentials on the

@@ -28,8 +28,8 @@ struct Many {
     static constexpr uint32_t stages = D == 128 ? 4 : 8, raw_stages = D == 128 ? 2 : 4;
     static constexpr uint32_t off_ring = 2u * tile, off_raw = off_ring + stages * tile, off_steps = off_raw + raw_stages * raw;
     static constexpr uint32_t off_bars = off_steps + 8u * 8u * 16u;
-    static constexpr uint32_t bars = 2u * stages + 2u * raw_stages + 8u + 2u + 4u + 4u + 2u + 1u;   // operands, codes: full, empty; steps; Q, S and P (twice), O of each tile; the end
-    static constexpr uint32_t off_slot = off_bars + 8u * bars, bytes = off_slot + 16u + 1024u;
+    static constexpr uint32_t bars = 2u * stages + 2u * raw_stages + 8u + 2u + 4u + 4u + 2u + 2u + 2u + 4u + 1u + 1u;   // operands, codes: full, empty; steps; Q, S and P (twice), O, all of O, results of each tile; works; the next one; the end
+    static constexpr uint32_t off_slot = (off_bars + 8u * bars + 15u) & ~15u, off_next = off_slot + 16u, bytes = off_next + 16u + 1024u;
     static constexpr uint32_t columns = 512u;                          // S0, S1, O0, O1
     static constexpr uint32_t o_column = 256u;
 };
@@ -75,6 +75,25 @@ __device__ __forceinline__ uint32_t rows_operand(uint32_t addr) { return ((addr 
 template <int D>
 __device__ __forceinline__ uint32_t keys_operand(uint32_t addr) { return ((addr >> 4) & 0x3fffu) | ((Many<D>::half >> 4) << 16); }
 
+// The index of a CTA of the grid that has not begun and does not any more, as this one takes its work; -1: there is none left.  (The device gives them out in order, so CTAs that are done
+// early take more; every gridDim-th work to a CTA instead: two prompts of up to 8192 tokens 340 us, 301 with a CTA to a work.)
+__device__ __forceinline__ int next_cta(uint32_t room, uint32_t bar, uint32_t parity, int lane, bool &ok)
+{
+    if (lane == 0) {
+        perq_mm::mbar_expect_tx(bar, 16u);
+        asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(room), "r"(bar) : "memory");
+    }
+    __syncwarp();
+    ok = cta_wait_warp(bar, parity);
+    if (!ok) return -1;
+    uint32_t yes, x, y, z;
+    asm volatile("{ .reg .b128 h; .reg .pred p; ld.shared.b128 h, [%4]; clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h; selp.u32 %0, 1, 0, p; mov.u32 %1, 0; mov.u32 %2, 0; "
+                 "mov.u32 %3, 0; @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, %2, %3, _}, h; }"
+                 : "=r"(yes), "=r"(x), "=r"(y), "=r"(z) : "r"(room) : "memory");
+    perq_mm::fence_async_smem();                                       // (the next answer is written where this one was)
+    __syncwarp();
+    return yes ? (int)x : -1;
+}
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 __device__ __forceinline__ uint32_t minus_1152(uint32_t v)
 {
@@ -141,6 +160,7 @@ struct ManyItem {
     int32_t sequence, head, row0, rows;       // rows of the sequence's (token, head) pairs
     int32_t begin, first;                     // its rows of the call, and the position of the first
     int32_t sunk, low, tiles;                 // tiles of keys: 0 .. sunk - 1, then from `low` on
+    int32_t part, tile0, count;               // where the keys are split: this CTA's part of the tiles
     int32_t number;                           // of the item: where its parts lie
 };
 __device__ __forceinline__ int many_tiles(const AttendParams &p, const Rows &r)
@@ -213,20 +233,10 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     griddep_wait();
     griddep_launch();
-    const int part = (int)(blockIdx.x % (unsigned)p.split);
-    __shared__ ManyItem found;
+    __shared__ ManyItem found[2];
     const uint32_t full = base + K::off_bars, empty = full + 8u * K::stages, raw_full = empty + 8u * K::stages, raw_empty = raw_full + 8u * K::raw_stages,
-                   steps_full = raw_empty + 8u * K::raw_stages, q_full = steps_full + 64u, s_full = q_full + 16u,
-                   p_full = s_full + 32u, o_full = p_full + 32u, end = o_full + 16u, slot = base + K::off_slot, steps = base + K::off_steps;
-    if (warp == LOAD_WARP) {
-        const ManyItem item = many_item(p.a, (int)(blockIdx.x / (unsigned)p.split), lane);
-        if (lane == 0) found = item;
-    }
-    __syncthreads();
-    const ManyItem it = found;
-    if (it.rows <= 0) return;
-    const int tile0 = (int)((long long)it.tiles * part / p.split), tile1 = (int)((long long)it.tiles * (part + 1) / p.split), tiles = tile1 - tile0;
-    const bool two = it.rows > 128;
+                   steps_full = raw_empty + 8u * K::raw_stages, q_full = steps_full + 64u, s_full = q_full + 16u, p_full = s_full + 32u, o_full = p_full + 32u, o_done = o_full + 16u,
+                   stored = o_done + 16u, work_full = stored + 16u, work_empty = work_full + 16u, next_full = work_empty + 16u, end = next_full + 8u, slot = base + K::off_slot, steps = base + K::off_steps;
     if (tid == 0) {
         for (uint32_t i = 0; i < K::stages; ++i) {
             mbar_init(full + 8u * i, 4);                               // the warps that make codes fp16
@@ -240,11 +250,16 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         for (uint32_t i = 0; i < 2; ++i) {
             mbar_init(q_full + 8u * i, 4);
             mbar_init(o_full + 8u * i, 1);
+            mbar_init(o_done + 8u * i, 1);
+            mbar_init(stored + 8u * i, 4);
+            mbar_init(work_full + 8u * i, 1);
+            mbar_init(work_empty + 8u * i, MMA_WARP + 1);             // all that read it
         }
         for (uint32_t i = 0; i < 4; ++i) {
             mbar_init(s_full + 8u * i, 1);
             mbar_init(p_full + 8u * i, 4);
         }
+        mbar_init(next_full, 1);
         mbar_init(end, 1);
         mbar_init_fence();
     }
@@ -257,18 +272,42 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     tmem_fence_after();
     const uint32_t tmem = lds32(slot);
     auto give_up = [&]() { atomicOr(&g_error, ERROR_ATTEND); };
-    auto key_of = [&](int tile) { return (tile < it.sunk ? tile : tile - it.sunk + it.low) * MANY_KEYS; };
+    auto key_of = [](const ManyItem &it, int tile) { return (tile < it.sunk ? tile : tile - it.sunk + it.low) * MANY_KEYS; };
+    // The number-th work of this CTA, which the loads' warp looks for ahead; rows of 0: there are no more.
+    auto work_of = [&](uint32_t number, ManyItem &it) {
+        if (!cta_wait_warp(work_full + 8u * (number & 1u), (number >> 1) & 1u)) {
+            if (lane == 0) give_up();
+            return false;
+        }
+        it = found[number & 1u];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(work_empty + 8u * (number & 1u));
+        return it.rows > 0;
+    };
 
     if (warp < CODES_WARP) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");          // (of 128 at launch: 2 x 176 + 80 + 80 = 4 x 128)
         const int t = warp >> 2, row = t * 128 + (tid & 127);
-        const int position = it.first + (it.row0 + min(row, it.rows - 1)) / p.a.group;
-        if (t == 0 || two) {
-            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_at = tmem + K::o_column + (uint32_t)t * 128u + lanes;
+        ManyItem it;
+        bool ok = true;
+        uint32_t mine = 0u, j0 = 0u, done = 0u;                        // of this tile of rows: works, tiles of keys, works with some, so far
+        uint32_t global0 = 0u, next0 = 0u;                             // tiles of keys of the CTA before this work, and behind it
+        for (uint32_t work = 0; ok && work_of(work, it); ++work) {
+            global0 = next0;
+            next0 += (uint32_t)it.count;
+            if (t * 128 >= it.rows) continue;
+            const int tile0 = it.tile0, tiles = it.count, position = it.first + (it.row0 + min(row, it.rows - 1)) / p.a.group;
+            // (the four warps' rows of queries lie where others' results did)
+            if (mine > 0 && !cta_wait_warp(stored + 8u * (uint32_t)t, (mine - 1u) & 1u)) {
+                ok = false;
+                break;
+            }
+            ++mine;
             // Queries: 32 rows to a warp, 16 channels to a lane; a row's largest is scaled to 1 .. 2 by a power of two, then it is rotated and rounded to fp16.
             // (A row to a thread: 12 us of loads that touch 32 rows each.)
             float factor = 0.0f;
-            {
+            if (tiles > 0) {
                 constexpr int wide = D / LANE, at_once = 32 / wide;    // lanes of a row, rows at once
                 const int in = lane / wide, channel = lane % wide * LANE, first_row = (warp & 3) * 32;
 #pragma unroll 1
@@ -309,19 +348,21 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     }
                 }
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_full + 8u * (uint32_t)t);
+            if (tiles > 0) {
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full + 8u * (uint32_t)t);
+            }
 
             // rows of this warp: all of a tile's keys that its rows have in common
             const int row_first = it.row0 + t * 128 + (warp & 3) * 32, row_last = it.row0 + it.rows - 1;
             const int low_position = it.first + min(row_first, row_last) / p.a.group, high_position = it.first + min(row_first + 31, row_last) / p.a.group;
             float m = -INFINITY, l = 0.0f;
-            bool ok = true;
             for (int u = 0; u < 2 * tiles; ++u) {
-                const int j = u >> 1, side = u & 1, key = key_of(tile0 + j) + 64 * side;
+                const int side = u & 1, key = key_of(it, tile0 + (u >> 1)) + 64 * side;
+                const uint32_t j = j0 + (uint32_t)(u >> 1), global = global0 + (uint32_t)(u >> 1);
                 const uint32_t s_at = tmem + (uint32_t)(t * 128 + side * 64) + lanes, buffer = 8u * (uint32_t)(2 * t + side);
-                if (!cta_wait_warp(steps_full + 8u * (uint32_t)(j & 7), (uint32_t)(j >> 3) & 1u) || !cta_wait_warp(s_full + buffer, (uint32_t)j & 1u)) {
+                if (!cta_wait_warp(steps_full + 8u * (global & 7u), (global >> 3) & 1u) || !cta_wait_warp(s_full + buffer, j & 1u)) {
                     ok = false;
                     break;
                 }
@@ -331,7 +372,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 tmem_load32(s_at + 32u, s[1]);
                 constexpr int G = FINE ? 4 : 2, W = 64 / G;
                 // of a page's columns: the factor of S, log2 s_v, 1 / s_v
-                const uint32_t at = steps + (uint32_t)(j & 7) * 128u + (uint32_t)side * 64u;
+                const uint32_t at = steps + (global & 7u) * 128u + (uint32_t)side * 64u;
                 float f[G], b[G], inverse[G];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
@@ -429,16 +470,17 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + buffer);
             }
-            // (without keys: until all queries are where results go)
-            if (ok && !cta_wait_warp(tiles > 0 ? end : q_full + 8u * (uint32_t)t, 0u)) ok = false;
-            tmem_fence_after();
-            if (!ok) {
-                if (lane == 0) give_up();
-            } else {
+            if (tiles > 0) {
+                if (ok && !cta_wait_warp(o_done + 8u * (uint32_t)t, done & 1u)) ok = false;
+                tmem_fence_after();
+                j0 += (uint32_t)tiles;
+                ++done;
+            }
+            if (ok) {
                 const float r = p.split > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
                 const bool f16 = p.a.out_type == OUT_F16;
                 if (p.split > 1) {
-                    float *const ends = many_part<D>(p, it.number, part) + MANY_ROWS * D;
+                    float *const ends = many_part<D>(p, it.number, it.part) + MANY_ROWS * D;
                     ends[row] = m;
                     ends[MANY_ROWS + row] = l;
                 }
@@ -487,7 +529,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         }
                         if (c % per == per - 1) {
                             if (p.split > 1) {
-                                char *const to = reinterpret_cast<char *>(many_part<D>(p, it.number, part) + 16 * (c - per + 1));
+                                char *const to = reinterpret_cast<char *>(many_part<D>(p, it.number, it.part) + 16 * (c - per + 1));
                                 store_rows([&](int r) { return to + (size_t)r * (4 * D); });
                             } else {
                                 store_rows([&](int r) { return out_row(r, 4) + 64 * (c - per + 1); });
@@ -503,8 +545,10 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                     }
                 }
                 if (!wide) store_rows([&](int r) { return out_row(r, 2); });
+                if (lane == 0) mbar_arrive(stored + 8u * (uint32_t)t);
             }
         }
+        if (!ok && lane == 0) give_up();
     } else if (warp < MMA_WARP) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         // Codes to fp16.  A thread has 16 channels of one key in 32; eight threads have 64 channels each of two keys next to each other, for D = 128 the lower 64 of one and the
@@ -513,7 +557,10 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         const uint32_t thread = (uint32_t)(tid - 32 * CODES_WARP), quad = thread & 3u, row = thread >> 2, odd = halves == 2 ? row & 1u : 0u;
         const uint32_t to0 = row * 128u + (((2u * quad) ^ row) & 7u) * 16u, to1 = row * 128u + (((2u * quad + 1u) ^ row) & 7u) * 16u;
         bool ok = true;
-        for (uint32_t n = 0; n < 2u * (uint32_t)tiles && ok; ++n) {
+        ManyItem it;
+        uint32_t n = 0;                                                // pieces so far
+        for (uint32_t work = 0; ok && work_of(work, it); ++work)
+        for (const uint32_t n_end = n + 2u * (uint32_t)it.count; n < n_end; ++n) {
             const uint32_t s = n % K::stages, r = n % K::raw_stages, to = base + K::off_ring + s * K::tile, from = base + K::off_raw + r * K::raw + row * D + quad * 16u;
             if (!cta_wait_warp(raw_full + 8u * r, (n / K::raw_stages) & 1u) || (n >= K::stages && !cta_wait_warp(empty + 8u * s, (n / K::stages - 1u) & 1u))) {
                 ok = false;
@@ -547,7 +594,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
         if (!ok && lane == 0) give_up();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp == MMA_WARP && tiles > 0) {
+        if (warp == MMA_WARP) {
             const uint32_t qk = f16_desc(128, 64, false), pv = f16_desc(128, D, true);
             bool ok = true;
             // S of 64 keys (half h of a tile of keys) for a tile of rows, and O of them
@@ -572,73 +619,112 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 return ok;
             };
             auto piece = [&](uint32_t i) { return wait_for(full + 8u * (i % K::stages), (i / K::stages) & 1u); };
-            const uint32_t row_tiles = two ? 2u : 1u;
-            if (wait_for(q_full, 0) && (!two || wait_for(q_full + 8u, 0)) && piece(0)) {
-                for (uint32_t h = 0; h < 2; ++h)
-                    for (uint32_t t = 0; t < row_tiles; ++t) logits(t, h, 0);
-                commit_one(empty);
-                uint32_t n = 1;
+            ManyItem it;
+            uint32_t n = 0, j0[2] = {0u, 0u}, done[2] = {0u, 0u};      // pieces; of each tile of rows: tiles of keys, and works with some, so far
+            for (uint32_t work = 0; ok && work_of(work, it); ++work) {
+                const int tiles = it.count;
+                const uint32_t row_tiles = it.rows > 128 ? 2u : 1u;
+                if (tiles == 0) continue;
+                for (uint32_t t = 0; t < row_tiles && ok; ++t) {
+                    if (!wait_for(q_full + 8u * t, done[t] & 1u) || (t == 0 && !piece(n))) break;
+                    logits(t, 0, n % K::stages);
+                    logits(t, 1, n % K::stages);
+                }
+                if (!ok) break;
+                commit_one(empty + 8u * (n % K::stages));
+                ++n;
                 for (int j = 0; j < tiles && ok; ++j, n += 2) {
                     const bool more = j + 1 < tiles;
                     const uint32_t sv = n % K::stages, sk = (n + 1) % K::stages;
                     if (!piece(n)) break;
                     for (uint32_t h = 0; h < 2 && ok; ++h)
                         for (uint32_t t = 0; t < row_tiles && ok; ++t) {
-                            if (!wait_for(p_full + 8u * (2u * t + h), (uint32_t)j & 1u)) break;
+                            if (!wait_for(p_full + 8u * (2u * t + h), (j0[t] + (uint32_t)j) & 1u)) break;
                             outputs(t, h, sv, j > 0 || h > 0);
                             if (more) {
                                 if (h == 0 && t == 0 && !piece(n + 1)) break;
                                 logits(t, h, sk);
+                            } else if (h == 1) {
+                                commit_one(o_done + 8u * t);
                             }
                         }
                     commit_one(empty + 8u * sv);
                     if (more) commit_one(empty + 8u * sk);
                 }
+                --n;                                                   // (the last tile has no keys behind it)
+                for (uint32_t t = 0; t < row_tiles; ++t) {
+                    j0[t] += (uint32_t)tiles;
+                    ++done[t];
+                }
             }
             if (!ok && lane == 0) give_up();
-            // (all products: the rows' warps wait for it too, and nothing is in flight when the CTA ends)
+            // nothing is in flight when the CTA ends
             commit_one(end);
             (void)cta_wait_warp(end, 0);
         }
         if (warp == LOAD_WARP) {
             // a lane to a page of a tile (eight at most): its codes and steps
-            const int32_t *const table = p.a.q.pages + (size_t)it.sequence * (size_t)p.a.q.width;
             const int log2page = p.a.q.page, each = min(1 << log2page, MANY_KEYS), copies = MANY_KEYS / each;
-            auto page_of = [&](int j) {
-                const int key = key_of(tile0 + j) + lane * each;
-                return lane < copies && j < tiles ? min(max(__ldg(table + min(key >> log2page, p.a.q.width - 1)), 0), p.a.q.n_pages - 1) : 0;
-            };
             bool ok = true;
-            uint32_t n = 0;
-            int page = page_of(0);
-            for (int j = 0; j < tiles && ok; ++j) {
-                const int next = page_of(j + 1);
-                const size_t block = (size_t)page * (size_t)p.a.heads + (size_t)it.head;
-                const float ks = __ldg(p.a.k_steps + block), vs = __ldg(p.a.v_steps + block);
-                for (int kind = 0; kind < 2; ++kind, ++n) {
-                    const uint32_t r = n % K::raw_stages, bar = raw_full + 8u * r;
-                    if (n >= K::raw_stages && !cta_wait_warp(raw_empty + 8u * r, (n / K::raw_stages - 1u) & 1u)) {
-                        ok = false;
-                        break;
-                    }
-                    if (lane == 0) mbar_expect_tx(bar, K::raw);
-                    __syncwarp();
-                    if (lane < copies)
-                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                                     ::"r"(base + K::off_raw + r * K::raw + (uint32_t)(lane * each * D)), "l"((kind ? p.a.v_codes : p.a.k_codes) + ((block << log2page) * (size_t)D)),
-                                     "r"((uint32_t)(each * D)), "r"(bar) : "memory");
+            uint32_t n = 0, global = 0;                                // pieces, and tiles of keys, so far
+            int index = (int)blockIdx.x;
+            for (uint32_t work = 0; ok; ++work) {
+                if (work > 0) {
+                    index = next_cta(base + K::off_next, next_full, (work - 1u) & 1u, lane, ok);
+                    if (!ok) break;
                 }
-                if (!ok) break;
-                // of 16 keys each: s_k (not 0, so that what is not seen stays -inf), log2 s_v, 1 / s_v, and whether one of them is not finite, which the rows' warps see to
-                const int mine = (lane & 7) * 16 / each;
-                const float k = __shfl_sync(0xffffffffu, ks, mine), v = __shfl_sync(0xffffffffu, vs, mine);
-                const bool bad = !(fabsf(k) <= 0x1p126f && fabsf(v) <= 0x1p126f), none = bad || v < 0x1p-64f;
-                if (lane < 8)
-                    sts128(steps + (uint32_t)(j & 7) * 128u + (uint32_t)lane * 16u,
-                           make_uint4(__float_as_uint(bad || k < 0x1p-60f ? 0x1p-60f : k), __float_as_uint(none ? -64.0f : log2_of(v)), __float_as_uint(none ? 0x1p64f : 1.0f / v), (uint32_t)bad));
+                ManyItem it;
+                it.rows = 0;
+                if (index >= 0) it = many_item(p.a, index / p.split, lane);
+                it.part = index >= 0 ? index % p.split : 0;
+                it.tile0 = (int)((long long)it.tiles * it.part / p.split);
+                it.count = (int)((long long)it.tiles * (it.part + 1) / p.split) - it.tile0;
+                if (work >= 2 && !cta_wait_warp(work_empty + 8u * (work & 1u), (work / 2u - 1u) & 1u)) {
+                    ok = false;
+                    break;
+                }
+                if (lane == 0) {
+                    found[work & 1u] = it;
+                    mbar_arrive(work_full + 8u * (work & 1u));
+                }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(steps_full + 8u * (uint32_t)(j & 7));
-                page = next;
+                if (it.rows <= 0) break;
+                const int32_t *const table = p.a.q.pages + (size_t)it.sequence * (size_t)p.a.q.width;
+                auto page_of = [&](int j) {
+                    const int key = key_of(it, it.tile0 + j) + lane * each;
+                    return lane < copies && j < it.count ? min(max(__ldg(table + min(key >> log2page, p.a.q.width - 1)), 0), p.a.q.n_pages - 1) : 0;
+                };
+                int page = page_of(0);
+                for (int j = 0; j < it.count && ok; ++j, ++global) {
+                    const int next = page_of(j + 1);
+                    const size_t block = (size_t)page * (size_t)p.a.heads + (size_t)it.head;
+                    const float ks = __ldg(p.a.k_steps + block), vs = __ldg(p.a.v_steps + block);
+                    for (int kind = 0; kind < 2; ++kind, ++n) {
+                        const uint32_t r = n % K::raw_stages, bar = raw_full + 8u * r;
+                        if (n >= K::raw_stages && !cta_wait_warp(raw_empty + 8u * r, (n / K::raw_stages - 1u) & 1u)) {
+                            ok = false;
+                            break;
+                        }
+                        if (lane == 0) mbar_expect_tx(bar, K::raw);
+                        __syncwarp();
+                        if (lane < copies)
+                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                         ::"r"(base + K::off_raw + r * K::raw + (uint32_t)(lane * each * D)),
+                                         "l"((kind ? p.a.v_codes : p.a.k_codes) + ((block << log2page) * (size_t)D)), "r"((uint32_t)(each * D)), "r"(bar) : "memory");
+                    }
+                    if (!ok) break;
+                    // of 16 keys each: s_k (not 0, so that what is not seen stays -inf), log2 s_v, 1 / s_v, and whether one of them is not finite, which the rows' warps see to
+                    const int mine = (lane & 7) * 16 / each;
+                    const float k = __shfl_sync(0xffffffffu, ks, mine), v = __shfl_sync(0xffffffffu, vs, mine);
+                    const bool bad = !(fabsf(k) <= 0x1p126f && fabsf(v) <= 0x1p126f), none = bad || v < 0x1p-64f;
+                    if (lane < 8)
+                        sts128(steps + (global & 7u) * 128u + (uint32_t)lane * 16u,
+                               make_uint4(__float_as_uint(bad || k < 0x1p-60f ? 0x1p-60f : k), __float_as_uint(none ? -64.0f : log2_of(v)), __float_as_uint(none ? 0x1p64f : 1.0f / v),
+                                          (uint32_t)bad));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(steps_full + 8u * (global & 7u));
+                    page = next;
+                }
             }
             if (!ok && lane == 0) give_up();
             // nothing is in flight when the CTA ends

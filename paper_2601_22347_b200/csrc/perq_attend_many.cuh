@@ -75,6 +75,27 @@ __device__ __forceinline__ uint32_t rows_operand(uint32_t addr) { return ((addr 
 template <int D>
 __device__ __forceinline__ uint32_t keys_operand(uint32_t addr) { return ((addr >> 4) & 0x3fffu) | ((Many<D>::half >> 4) << 16); }
 
+// For two barriers, polled before either answer is looked at.
+__device__ __forceinline__ bool cta_wait_warp(uint32_t bar, uint32_t parity, uint32_t bar1, uint32_t parity1)
+{
+    const bool done = cta_poll(bar, parity), done1 = cta_poll(bar1, parity1);
+    if (__all_sync(0xffffffffu, done && done1)) return true;
+    return cta_wait_warp(bar, parity) && cta_wait_warp(bar1, parity1);
+}
+// 2^x on the multiply-add pipe, for x up to 100: 2^(x - n) with n the nearest whole number by its Taylor polynomial of degree 5 (off by (ln2 / 2)^6 / 6! = 2.4e-6), times 2^n.  One in
+// eight exponentials is taken so, because the others are what two warps of a scheduler wait for (16 a cycle and SM): chunks behind long contexts 310 -> 298 us; one in four 310.  Below -125: 0.
+// NaN stays NaN.
+__device__ __forceinline__ float exp2_fma(float x)
+{
+    const float t = x + 12582912.0f, f = x - (t - 12582912.0f);
+    float r = fmaf(f, 1.3333558e-3f, 9.6181291e-3f);
+    r = fmaf(r, f, 5.5504109e-2f);
+    r = fmaf(r, f, 2.4022651e-1f);
+    r = fmaf(r, f, 6.9314718e-1f);
+    r = fmaf(r, f, 1.0f);
+    r = __int_as_float(__float_as_int(r) + (__float_as_int(t) << 23));
+    return x < -125.0f ? 0.0f : r;
+}
 // The index of a CTA of the grid that has not begun and does not any more, as this one takes its work; -1: there is none left.  (The device gives them out in order, so CTAs that are done
 // early take more; every gridDim-th work to a CTA instead: two prompts of up to 8192 tokens 340 us, 301 with a CTA to a work.)
 __device__ __forceinline__ int next_cta(uint32_t room, uint32_t bar, uint32_t parity, int lane, bool &ok)
@@ -86,13 +107,13 @@ __device__ __forceinline__ int next_cta(uint32_t room, uint32_t bar, uint32_t pa
     __syncwarp();
     ok = cta_wait_warp(bar, parity);
     if (!ok) return -1;
-    uint32_t yes, x, y, z;
+    uint32_t yes, x, y, z;           // (y and z are 0)
     asm volatile("{ .reg .b128 h; .reg .pred p; ld.shared.b128 h, [%4]; clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h; selp.u32 %0, 1, 0, p; mov.u32 %1, 0; mov.u32 %2, 0; "
                  "mov.u32 %3, 0; @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, %2, %3, _}, h; }"
                  : "=r"(yes), "=r"(x), "=r"(y), "=r"(z) : "r"(room) : "memory");
     perq_mm::fence_async_smem();                                       // (the next answer is written where this one was)
     __syncwarp();
-    return yes ? (int)x : -1;
+    return yes ? (int)(x + y + z) : -1;
 }
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 __device__ __forceinline__ uint32_t minus_1152(uint32_t v)
@@ -362,7 +383,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 const int side = u & 1, key = key_of(it, tile0 + (u >> 1)) + 64 * side;
                 const uint32_t j = j0 + (uint32_t)(u >> 1), global = global0 + (uint32_t)(u >> 1);
                 const uint32_t s_at = tmem + (uint32_t)(t * 128 + side * 64) + lanes, buffer = 8u * (uint32_t)(2 * t + side);
-                if (!cta_wait_warp(steps_full + 8u * (global & 7u), (global >> 3) & 1u) || !cta_wait_warp(s_full + buffer, j & 1u)) {
+                if (!cta_wait_warp(steps_full + 8u * (global & 7u), (global >> 3) & 1u, s_full + buffer, j & 1u)) {
                     ok = false;
                     break;
                 }
@@ -445,7 +466,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         for (int i = g * W; i < (g + 1) * W; i += 2) {
                             pair_split(pair_fma(pair_of(s[c][i], s[c][i + 1]), ff, bb), s[c][i], s[c][i + 1]);
                             s[c][i] = exp2_of(s[c][i]);
-                            s[c][i + 1] = exp2_of(s[c][i + 1]);
+                            s[c][i + 1] = i % 8 == 6 ? exp2_fma(s[c][i + 1]) : exp2_of(s[c][i + 1]);
                         }
                     }
                     uint32_t w[16];

@@ -11,6 +11,7 @@ that a call makes are that stream's memory, and the caller's own streams wait fo
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import importlib.util
 import os
 from typing import Optional
@@ -36,6 +37,7 @@ PERQ_ERR_WORKSPACE = 9
 _lib = None
 _rotate_quantize = _swiglu_rotate_quantize = None       # the calls of these: perq_call.c, or ctypes where that is not built or cannot be loaded
 _rotate_quantize_i8 = _matmul_i8 = _grouped_matmul_i8 = None
+_cache_write_i8 = _cache_read_i8 = _attention_i8 = None
 
 
 class PerqError(RuntimeError):
@@ -46,7 +48,7 @@ class PerqError(RuntimeError):
 
 def load() -> C.CDLL:
     """Load libperq.so from the package directory (never builds implicitly)."""
-    global _lib, _rotate_quantize, _swiglu_rotate_quantize, _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8
+    global _lib, _rotate_quantize, _swiglu_rotate_quantize, _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8, _cache_write_i8, _cache_read_i8, _attention_i8
     if _lib is None:
         path = _build.LIB_PATH
         if not os.path.exists(path):
@@ -102,14 +104,17 @@ def load() -> C.CDLL:
             getattr(lib, name).restype = C.c_int
         _rotate_quantize, _swiglu_rotate_quantize = lib.perq_rotate_quantize, lib.perq_swiglu_rotate_quantize
         _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8 = lib.perq_rotate_quantize_i8, lib.perq_matmul_i8, lib.perq_grouped_matmul_i8
+        _cache_write_i8, _cache_read_i8, _attention_i8 = lib.perq_cache_write_i8, lib.perq_cache_read_i8, lib.perq_attention_i8
         try:
             spec = importlib.util.spec_from_file_location(__package__ + "._perq_call", _build.CALL_PATH)
             call = importlib.util.module_from_spec(spec)
             spec.loader.exec_module(call)
             call.bind(C.cast(lib.perq_rotate_quantize, vp).value, C.cast(lib.perq_swiglu_rotate_quantize, vp).value)
             call.bind_i8(C.cast(lib.perq_rotate_quantize_i8, vp).value, C.cast(lib.perq_matmul_i8, vp).value, C.cast(lib.perq_grouped_matmul_i8, vp).value)
+            call.bind_cache(C.cast(lib.perq_cache_write_i8, vp).value, C.cast(lib.perq_cache_read_i8, vp).value, C.cast(lib.perq_attention_i8, vp).value)
             _rotate_quantize, _swiglu_rotate_quantize = call.rotate_quantize, call.swiglu_rotate_quantize
             _rotate_quantize_i8, _matmul_i8, _grouped_matmul_i8 = call.rotate_quantize_i8, call.matmul_i8, call.grouped_matmul_i8
+            _cache_write_i8, _cache_read_i8, _attention_i8 = call.cache_write_i8, call.cache_read_i8, call.attention_i8
         except (ImportError, AttributeError):         # (no such file, none that this interpreter can load, or one without these calls)
             pass
         _lib = lib
@@ -490,23 +495,26 @@ def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt:
 # ------------------------------------------------------------------------------------------------- the 8-bit cache
 def _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages):
     """The cache's sizes: (S, heads, D, page, n_pages, width)."""
-    assert _on(k_codes, device, torch.int8) and _on(v_codes, device, torch.int8) and _on(k_steps, device, torch.float32) and _on(v_steps, device, torch.float32)
-    assert _on(offsets, device, torch.int32) and _on(lengths, device, torch.int32) and _on(pages, device, torch.int32)
-    n_pages, heads, page, D = k_codes.shape
+    i8, i32, f32 = torch.int8, torch.int32, torch.float32
+    assert k_codes.get_device() == device and k_codes.dtype is i8 and k_codes.is_contiguous() and v_codes.get_device() == device and v_codes.dtype is i8 and v_codes.is_contiguous()
+    assert k_steps.get_device() == device and k_steps.dtype is f32 and k_steps.is_contiguous() and v_steps.get_device() == device and v_steps.dtype is f32 and v_steps.is_contiguous()
+    assert offsets.get_device() == device and offsets.dtype is i32 and offsets.is_contiguous() and lengths.get_device() == device and lengths.dtype is i32 and lengths.is_contiguous()
+    assert pages.get_device() == device and pages.dtype is i32 and pages.is_contiguous()
+    shape = k_codes.shape
+    n_pages, heads, page, D = shape
     S, width = pages.shape
-    assert v_codes.shape == k_codes.shape and k_steps.shape == (n_pages, heads) and v_steps.shape == (n_pages, heads)
-    assert lengths.numel() == S and offsets.numel() == S + 1
+    assert v_codes.shape == shape and k_steps.shape == (n_pages, heads) and v_steps.shape == (n_pages, heads) and lengths.numel() == S and offsets.numel() == S + 1
     return S, heads, D, page, n_pages, width
 
 
-def _token_rows(x: torch.Tensor, device: int) -> bool:
-    """bf16 or f16 rows [T, heads, D] whose heads lie side by side; the rows may be part of longer ones."""
-    return (x.get_device() == device and x.dtype in (torch.bfloat16, torch.float16) and x.dim() == 3 and
-            (x.is_contiguous() or (x.stride(2) == 1 and x.stride(1) == x.shape[2])))
-
-
-def _row_stride(x: torch.Tensor) -> int:
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]             # (a single row's may be anything)
+# Rows of tokens [T, heads, D] whose heads lie side by side, bf16 or f16; they may be parts of longer rows, so tokens are some elements apart.
+def _row_stride(x: torch.Tensor, device: int) -> int:
+    assert x.get_device() == device and (x.dtype is torch.bfloat16 or x.dtype is torch.float16)
+    T, heads, D = x.shape
+    stride = x.stride()
+    assert heads == 1 or stride[1] == D and stride[2] == 1 or x.is_contiguous()
+    assert stride[2] == 1 or x.is_contiguous()
+    return stride[0] if T > 1 and not x.is_contiguous() else heads * D             # (a single row's may be anything)
 
 
 def perq_cache_write_i8(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: torch.Tensor, v_steps: torch.Tensor,
@@ -517,12 +525,17 @@ def perq_cache_write_i8(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor,
     device = torch._C._cuda_getDevice()
     S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
     T = k.shape[0]
-    assert _token_rows(k, device) and _token_rows(v, device) and k.dtype is v.dtype and k.shape == v.shape and k.shape[1:] == (heads, D)
+    assert k.dtype is v.dtype and k.shape == (T, heads, D) == v.shape
+    k_stride, v_stride = _row_stride(k, device), _row_stride(v, device)
     if _lib is None:
         load()
-    rc = _lib.perq_cache_write_i8(k.data_ptr(), v.data_ptr(), OUT_BY_DTYPE[k.dtype], _row_stride(k), _row_stride(v), offsets.data_ptr(), lengths.data_ptr(),
-                                  pages.data_ptr(), T, S, heads, D, b, page, n_pages, width, k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(),
-                                  v_steps.data_ptr(), torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    args = (k.data_ptr(), v.data_ptr(), OUT_BY_DTYPE[k.dtype], k_stride, v_stride, offsets.data_ptr(), lengths.data_ptr(), pages.data_ptr(), T, S, heads, D, b, page,
+            n_pages, width, k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(),
+            torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    try:
+        rc = _cache_write_i8(*args)
+    except TypeError:           # (not plain integers: what ctypes makes of them)
+        rc = _lib.perq_cache_write_i8(*args)
     if rc != PERQ_OK:
         _check(rc, "perq_cache_write_i8")
 
@@ -535,16 +548,20 @@ def perq_cache_read_i8(k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: to
     Rows of no sequence are not written: in outputs made here they are whatever the memory holds."""
     device = torch._C._cuda_getDevice()
     S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
+    shape = (T, heads, D)
     if k is None:
-        k = _empty((T, heads, D), out_dtype, k_codes.device, stream)
+        k = k_codes.new_empty(shape, dtype=out_dtype) if stream is None else _empty(shape, out_dtype, k_codes.device, stream)
     if v is None:
-        v = _empty((T, heads, D), k.dtype, k_codes.device, stream)
-    assert _on(k, device, k.dtype) and _on(v, device, k.dtype) and k.shape == (T, heads, D) and v.shape == (T, heads, D)
+        v = k_codes.new_empty(shape, dtype=k.dtype) if stream is None else _empty(shape, k.dtype, k_codes.device, stream)
+    assert k.get_device() == device and k.is_contiguous() and k.shape == shape and _on(v, device, k.dtype) and v.shape == shape
     if _lib is None:
         load()
-    rc = _lib.perq_cache_read_i8(k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(), offsets.data_ptr(), lengths.data_ptr(), pages.data_ptr(), T, S,
-                                 heads, D, b, page, n_pages, width, k.data_ptr(), v.data_ptr(), OUT_BY_DTYPE[k.dtype],
-                                 torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    args = (k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(), offsets.data_ptr(), lengths.data_ptr(), pages.data_ptr(), T, S, heads, D, b, page,
+            n_pages, width, k.data_ptr(), v.data_ptr(), OUT_BY_DTYPE[k.dtype], torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    try:
+        rc = _cache_read_i8(*args)
+    except TypeError:           # (as above)
+        rc = _lib.perq_cache_read_i8(*args)
     if rc != PERQ_OK:
         _check(rc, "perq_cache_read_i8")
     return k, v
@@ -554,6 +571,12 @@ def perq_attention_i8_workspace_bytes(T: int, S: int, heads: int, group: int, D:
     n = C.c_size_t(0)
     _check(load().perq_attention_i8_workspace_bytes(T, S, heads, group, D, most, C.byref(n)), "perq_attention_i8_workspace_bytes")
     return int(n.value)
+
+
+# (asked once for the sizes of a device: it takes 1.7 us, and small calls are bound by the host)
+@functools.lru_cache(maxsize=1024)
+def _attention_space(device: int, T: int, S: int, heads: int, group: int, D: int, most: int) -> int:
+    return max(16, perq_attention_i8_workspace_bytes(T, S, heads, group, D, most))
 
 
 def perq_attention_i8(q: torch.Tensor, k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: torch.Tensor, v_steps: torch.Tensor, offsets: torch.Tensor,
@@ -566,21 +589,31 @@ def perq_attention_i8(q: torch.Tensor, k_codes: torch.Tensor, k_steps: torch.Ten
     workspace that the call is not given is made here.  Rows of no sequence are not written: in an `out` made here they are whatever its memory holds."""
     device = torch._C._cuda_getDevice()
     S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
-    T, all_heads = q.shape[:2]
-    assert _token_rows(q, device) and q.shape[2] == D and all_heads % heads == 0
+    shape = q.shape
+    T, all_heads, channels = shape
+    assert channels == D and all_heads % heads == 0
+    q_stride, group = _row_stride(q, device), all_heads // heads
     if out is None:
-        out = _empty((T, all_heads, D), out_dtype or q.dtype, q.device, stream)
-    assert out.get_device() == device and out.is_contiguous() and out.shape == (T, all_heads, D)
-    group, most = all_heads // heads, max(1, T if most is None else most)
-    if workspace is None:
-        workspace = _empty(max(16, perq_attention_i8_workspace_bytes(T, S, heads, group, D, most)), torch.uint8, q.device, stream, result=False)   # (let go on return)
-    assert workspace.get_device() == device and workspace.is_contiguous()
+        out = q.new_empty(shape, dtype=out_dtype) if stream is None else _empty(shape, out_dtype or q.dtype, q.device, stream)
+    else:
+        assert out.get_device() == device and out.is_contiguous() and out.shape == shape
+    if most is None:
+        most = T or 1
     if _lib is None:
         load()
-    rc = _lib.perq_attention_i8(q.data_ptr(), OUT_BY_DTYPE[q.dtype], _row_stride(q), k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(),
-                                offsets.data_ptr(), lengths.data_ptr(), pages.data_ptr(), T, S, heads, group, D, b, page, n_pages, width, most,
-                                D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), OUT_BY_DTYPE[out.dtype], workspace.data_ptr(),
-                                workspace.numel() * workspace.element_size(), torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    if workspace is None:
+        n = _attention_space(device, T, S, heads, group, D, most)
+        workspace = k_codes.new_empty(n) if stream is None else _empty(n, torch.uint8, q.device, stream, result=False)       # (let go on return)
+    else:
+        assert workspace.get_device() == device and workspace.is_contiguous()
+        n = workspace.numel() * workspace.element_size()
+    args = (q.data_ptr(), OUT_BY_DTYPE[q.dtype], q_stride, k_codes.data_ptr(), k_steps.data_ptr(), v_codes.data_ptr(), v_steps.data_ptr(), offsets.data_ptr(), lengths.data_ptr(),
+            pages.data_ptr(), T, S, heads, group, D, b, page, n_pages, width, most, D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), OUT_BY_DTYPE[out.dtype],
+            workspace.data_ptr(), n, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    try:
+        rc = _attention_i8(*args)
+    except TypeError:           # (as above)
+        rc = _lib.perq_attention_i8(*args)
     if rc != PERQ_OK:
         _check(rc, "perq_attention_i8")
     return out

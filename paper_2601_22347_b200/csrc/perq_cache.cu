@@ -76,12 +76,12 @@ int launch_write(WriteParams &p, int page, cudaStream_t st)
     p.parts = one ? (2 * p.heads + THREADS / 32 - 1) / (THREADS / 32) : 2 * p.heads;
     const int64_t grid = blocks * p.parts;
     if (grid >= (1ll << 31)) return PERQ_ERR_SHAPE;
-    if (few) return launch(write_kernel<D, 1, 1>, grid, THREADS, 0, st, 1, p);
-    if (one) return launch(write_kernel<D, 1, 4>, grid, THREADS, 0, st, 1, p);
+    if (few) return launch(write_kernel<D, 1, 1, 4, false>, grid, THREADS, 0, st, 1, p);
+    if (one) return launch(write_kernel<D, 1, 4, 16, true>, grid, THREADS, 0, st, 1, p);
     switch (page * D / 4096) {
-    case 1: return launch(write_kernel<D, 8, 1>, grid, THREADS, 0, st, 1, p);
-    case 2: return launch(write_kernel<D, 8, 2>, grid, THREADS, 0, st, 1, p);
-    default: return launch(write_kernel<D, 8, 4>, grid, THREADS, 0, st, 1, p);
+    case 1: return launch(write_kernel<D, 8, 1, 16, true>, grid, THREADS, 0, st, 1, p);
+    case 2: return launch(write_kernel<D, 8, 2, 16, true>, grid, THREADS, 0, st, 1, p);
+    default: return launch(write_kernel<D, 16, 2, 16, true>, grid, 512, 0, st, 1, p);
     }
 }
 

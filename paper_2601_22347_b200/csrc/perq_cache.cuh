@@ -10,7 +10,7 @@
 //
 // Codes are those of exact arithmetic.  A butterfly of L = log2 b stages rounds each sum L times, so |u32 - u| <= L 2^-24 sum |x|, and sum |x| <= sqrt b |x|_2 =
 // |u|_2 <= sqrt b max |u| over the rotation's block: E = 1.01 L sqrt b 2^-24 of its largest (b = 128: 4.8e-6).  What may be the block's maximum (within 2 E of the largest in
-// fp32) is summed again in fp64, and so is an element whose quotient lies within 127 (E + 2^-22) of the border between two codes (b = 128: one in 800), by the
+// fp32) is summed again in fp64, and so is an element whose quotient lies within 127 (E + 2^-21) of the border between two codes (b = 128: one in 800), by the
 // lanes that hold its rotation's block.
 #pragma once
 
@@ -49,39 +49,46 @@ __device__ __forceinline__ int blocks_of(const Sequences &q, const Rows &r)
     return r.length > first ? ((r.length - 1) >> q.page) - (first >> q.page) + 1 : 0;
 }
 
-// A lane's 16 channels.
-__device__ __forceinline__ void unpack(float (&u)[LANE], const uint4 &lo, const uint4 &hi, bool f16)
+// A lane's C channels, two to a word.
+template <int C>
+__device__ __forceinline__ void unpack(float (&u)[C], const uint32_t (&w)[C / 2], bool f16)
 {
-    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     if (f16) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < C / 2; ++i)
             asm("{ .reg .b16 x, y; mov.b32 {x, y}, %2; cvt.f32.f16 %0, x; cvt.f32.f16 %1, y; }" : "=f"(u[2 * i]), "=f"(u[2 * i + 1]) : "r"(w[i]));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < C / 2; ++i) {
             u[2 * i] = __uint_as_float(w[i] << 16);
             u[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
 }
+__device__ __forceinline__ void unpack(float (&u)[LANE], const uint4 &lo, const uint4 &hi, bool f16)
+{
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    unpack<LANE>(u, w, f16);
+}
 // Times the Hadamard matrix of blocks of 2^log2b channels (0: none), without its factor.
-__device__ __forceinline__ void rotate(float (&u)[LANE], int log2b, int lane)
+template <int C>
+__device__ __forceinline__ void rotate(float (&u)[C], int log2b, int lane)
 {
     if (log2b == 0) return;
 #pragma unroll
-    for (int h = 1; h < LANE; h *= 2)
+    for (int h = 1; h < C; h *= 2)
 #pragma unroll
-        for (int i = 0; i < LANE; ++i)
+        for (int i = 0; i < C; ++i)
             if ((i & h) == 0) {
                 const float a = u[i], b = u[i + h];
                 u[i] = a + b;
                 u[i + h] = a - b;
             }
-    for (int l = 1; l < 1 << (log2b - 4); l *= 2) {
+#pragma unroll 1
+    for (int l = 1; l < (1 << log2b) / C; l *= 2) {
         const float s = (lane & l) ? -1.0f : 1.0f;
 #pragma unroll
-        for (int i = 0; i < LANE; ++i) u[i] = fmaf(s, u[i], __shfl_xor_sync(0xffffffffu, u[i], l));      // (s u exact: one rounding)
+        for (int i = 0; i < C; ++i) u[i] = fmaf(s, u[i], __shfl_xor_sync(0xffffffffu, u[i], l));      // (s u exact: one rounding)
     }
 }
 
@@ -103,21 +110,60 @@ struct WriteParams {
     float *steps[2];                          // [n_pages, heads]
     int32_t heads, f16;
     int32_t log2b;                            // of the keys
-    int32_t parts;                            // CTAs to a block of all heads, keys and values
+    int32_t parts;                            // CTAs to a page's blocks, for all heads' keys and values
 };
 
 struct Place {
     int32_t row, slot, n;                     // its rows of the call, and their first place in the block
-    int32_t page;                             // of the pool, or -1
+    int32_t entry;                            // its place in the sequence's row of the table, read when it is wanted
+    int32_t sequence;
 };
 // Which sequence's which page the number-th block is.  Called by all threads of the CTA.
+template <int SIZE>
 __device__ __forceinline__ Place find_block(const Sequences &q, int number)
 {
-    __shared__ int32_t sums[THREADS / 32];
+    __shared__ int32_t sums[SIZE / 32];
     __shared__ Place found;
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto place_of = [&](int i, const Rows &r, int at) {
+        const int first = r.length - r.n, index = (max(first, 0) >> q.page) + at, from = max(index << q.page, max(first, 0));
+        Place p;
+        p.row = r.begin + (from - first);
+        p.slot = from - (index << q.page);
+        p.n = min((index + 1) << q.page, r.length) - from;
+        p.entry = index;
+        p.sequence = i;
+        return p;
+    };
+    if (q.S <= 32) {
+        // (every warp for itself)
+        Rows r = {0, 0, 0};
+        int c = 0;
+        if (lane < q.S) {
+            r = rows_of(q, lane);
+            c = blocks_of(q, r);
+        }
+        int sum = c;
+#pragma unroll
+        for (int l = 1; l < 32; l *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, l);
+            if (lane >= l) sum += v;
+        }
+        const int at = number - (sum - c);
+        const unsigned here = __ballot_sync(0xffffffffu, at >= 0 && at < c);
+        Place p = {0, 0, 0, 0, 0};
+        if (here == 0u) return p;
+        if (at >= 0 && at < c) p = place_of(lane, r, at);
+        const int owner = __ffs(here) - 1;
+        p.row = __shfl_sync(0xffffffffu, p.row, owner);
+        p.slot = __shfl_sync(0xffffffffu, p.slot, owner);
+        p.n = __shfl_sync(0xffffffffu, p.n, owner);
+        p.entry = __shfl_sync(0xffffffffu, p.entry, owner);
+        p.sequence = owner;
+        return p;
+    }
     if (tid == 0) found.n = 0;
-    for (int base = 0, before = 0; base < q.S; base += THREADS) {
+    for (int base = 0, before = 0; base < q.S; base += SIZE) {
         Rows r = {0, 0, 0};
         int c = 0;
         if (base + tid < q.S) {
@@ -134,20 +180,13 @@ __device__ __forceinline__ Place find_block(const Sequences &q, int number)
         __syncthreads();
         int all = 0;
 #pragma unroll
-        for (int w = 0; w < THREADS / 32; ++w) {
+        for (int w = 0; w < SIZE / 32; ++w) {
             if (w < warp) sum += sums[w];
             all += sums[w];
         }
         const int at = number - (before + sum - c);
         if (at >= 0 && at < c) {
-            const int first = r.length - r.n, index = (max(first, 0) >> q.page) + at, from = max(index << q.page, max(first, 0));
-            Place p;
-            p.row = r.begin + (from - first);
-            p.slot = from - (index << q.page);
-            p.n = min((index + 1) << q.page, r.length) - from;
-            p.page = __ldg(q.pages + (size_t)(base + tid) * (size_t)q.width + (size_t)index);
-            if (p.page < 0 || p.page >= q.n_pages) p.page = -1;
-            found = p;
+            found = place_of(base + tid, r, at);
         }
         before += all;
         __syncthreads();
@@ -157,95 +196,100 @@ __device__ __forceinline__ Place find_block(const Sequences &q, int number)
     return found;
 }
 
-// WARPS warps have a block (8: the CTA's; 1: a block of each), TOKENS of it at a time, of which each lane keeps HELD lots.
-template <int D, int WARPS, int HELD>
+// WARPS warps have a block (8 or 16: the CTA's; 1: a block of each), `tokens` of it at a time, of which each lane keeps HELD lots of C channels.  ALL: those are all that there can be.
+// (C is 16 for prompts.  For few tokens it is 4: instructions that are met for the first time are most of such a call, and a quarter of them is unrolled.)
+template <int D, int WARPS, int HELD, int C>
 struct Write {
-    static constexpr int lanes = D / LANE;                             // to a token
+    static constexpr int lanes = D / C;                                // to a token
+    static constexpr int threads = WARPS == 16 ? 512 : THREADS;
     static constexpr int tokens = WARPS * 32 / lanes;
 };
 
-template <int D, int WARPS, int HELD>
-__global__ void __launch_bounds__(THREADS) write_kernel(const __grid_constant__ WriteParams p)
+template <int D, int WARPS, int HELD, int C, bool ALL>
+__global__ void __launch_bounds__(WARPS == 16 ? 512 : THREADS, HELD == 4 || WARPS == 16 ? 2 : 4) write_kernel(const __grid_constant__ WriteParams p)
 {
-    using K = Write<D, WARPS, HELD>;
-    __shared__ float part[THREADS / 32];
-    __shared__ unsigned long long exact[THREADS / 32];
+    using K = Write<D, WARPS, HELD, C>;
+    __shared__ float part[K::threads / 32];
+    __shared__ unsigned long long exact[K::threads / 32];
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
     griddep_wait();
     griddep_launch();
     const int number = (int)(blockIdx.x / (unsigned)p.parts), in = (int)(blockIdx.x % (unsigned)p.parts);
-    const Place at = find_block(p.q, number);
-    if (at.n <= 0 || at.page < 0) return;
-    const int item = WARPS == 1 ? in * (THREADS / 32) + warp : in;
+    const Place at = find_block<K::threads>(p.q, number);
+    if (at.n <= 0) return;
+    // (on its way while the tokens are read and rotated)
+    const int page = __ldg(p.q.pages + (size_t)at.sequence * (size_t)p.q.width + (size_t)at.entry);
+    const int item = WARPS == 1 ? in * (K::threads / 32) + warp : in;
     if (item >= 2 * p.heads) return;                                   // (whole warps, and then no barrier follows)
     const int kind = item >= p.heads ? 1 : 0, head = item - kind * p.heads, log2b = kind ? 0 : p.log2b;
     const bool f16 = p.f16 != 0;
     const uint16_t *const x = p.x[kind] + (size_t)at.row * (size_t)p.stride[kind] + (size_t)head * D;
-    const size_t block = (size_t)at.page * (size_t)p.heads + (size_t)head;
-    int8_t *const codes = p.codes[kind] + (block << p.q.page) * (size_t)D;
-    float *const step = p.steps[kind] + block;
-    const float before = at.slot > 0 ? __ldg(step) : 0.0f;
-
-    const int share = WARPS == 1 ? lane : tid, mine = share / K::lanes, channel = (share % K::lanes) * LANE;
+    const int share = WARPS == 1 ? lane : tid, mine = share / K::lanes, channel = (share % K::lanes) * C;
     const int lots = (at.n + K::tokens - 1) / K::tokens;
-    const bool held = lots <= HELD;
-    auto load = [&](int lot, float (&u)[LANE]) {
+    const bool held = ALL || lots <= HELD;                             // (else every pass reads and rotates again)
+    auto load = [&](int lot, float (&u)[C]) {
         const int t = lot * K::tokens + mine;
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        uint32_t w[C / 2] = {};
         if (t < at.n) {
-            const uint4 *const from = reinterpret_cast<const uint4 *>(x + (size_t)t * (size_t)p.stride[kind] + channel);
-            lo = __ldg(from);
-            hi = __ldg(from + 1);
+            const uint16_t *const from = x + (size_t)t * (size_t)p.stride[kind] + channel;
+            if constexpr (C == 16) {
+                const uint4 lo = __ldg(reinterpret_cast<const uint4 *>(from)), hi = __ldg(reinterpret_cast<const uint4 *>(from) + 1);
+                w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+            } else {
+                const uint2 lo = __ldg(reinterpret_cast<const uint2 *>(from));
+                w[0] = lo.x; w[1] = lo.y;
+            }
         }
-        unpack(u, lo, hi, f16);
+        unpack<C>(u, w, f16);
     };
-    // The exact u of one element of every token of the warp: this lane's `channel` + i where it asks, else any.
-    auto again = [&](int lot, int i, unsigned asked, bool &answered) -> double {
-        const unsigned group = (K::lanes == 32 ? 0xffffffffu : ((1u << K::lanes) - 1u) << (lane & ~(K::lanes - 1))) & asked;
-        const int leader = group ? __ffs(group) - 1 : lane;
-        const int e = __shfl_sync(0xffffffffu, channel + i, leader);
-        answered = leader == lane && group != 0u;
-        float v[LANE];
-        load(lot, v);
-        double sum = 0.0;
-        if (log2b == 0) {
+    // The lanes' elements that have a bit in `want` (C of a lot, lots from lot0 on) are summed again in fp64, by the lanes that have their token: take(lot, i, u) gets each.
+    auto settle = [&](int lot0, unsigned long long want, auto &&take) {
+        for (unsigned asked = __ballot_sync(0xffffffffu, want != 0ull); asked != 0u; asked = __ballot_sync(0xffffffffu, want != 0ull)) {
+            const unsigned group = ((K::lanes == 32 ? 0xffffffffu : ((1u << (K::lanes & 31)) - 1u) << (lane & ~(K::lanes - 1)))) & asked;
+            const int leader = group ? __ffs(group) - 1 : lane, bit = want ? __ffsll((long long)want) - 1 : 0;
+            const int lot = lot0 + __shfl_sync(0xffffffffu, bit / C, leader);
+            const unsigned e = (unsigned)__shfl_sync(0xffffffffu, channel + bit % C, leader) & ((1u << log2b) - 1u);
+            float v[C];
+            load(lot, v);
+            double sum = 0.0;
+            // (other rotations' blocks of the token add up what nobody reads)
 #pragma unroll
-            for (int k = 0; k < LANE; ++k)
-                if (k == i) sum = (double)v[k];
-            return sum;                                                // (the leader's own)
-        }
-        const unsigned sign = (unsigned)e & ((1u << log2b) - 1u);
-        // (other rotations' blocks of the token add up what nobody reads)
+            for (int k = 0; k < C; ++k) sum += __popc(e & (unsigned)(channel + k)) & 1 ? -(double)v[k] : (double)v[k];
+            for (int l = 1; l < (1 << log2b) / C; l *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, l);
+            if (log2b == 0) {
 #pragma unroll
-        for (int k = 0; k < LANE; ++k) {
-            const bool minus = __popc(sign & (unsigned)(channel + k)) & 1;
-            sum += minus ? -(double)v[k] : (double)v[k];
+                for (int k = 0; k < C; ++k)
+                    if (k == bit % C) sum = (double)v[k];
+            }
+            if (leader == lane && want != 0ull) {
+                take(lot, bit % C, sum);
+                want &= want - 1ull;
+            }
         }
-        for (int l = 1; l < 1 << (log2b - 4); l *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, l);
-        return sum;
     };
 
     // 1. the largest of the block
-    float u[HELD][LANE], top = 0.0f;
-    auto larger = [&](const float (&v)[LANE]) {
-#pragma unroll
-        for (int i = 0; i < LANE; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(v[i])));
-    };
-    if (held) {
+    float u[HELD][C], top = 0.0f, tops[HELD];
+    for (int lot0 = 0; lot0 < lots; lot0 += HELD) {
 #pragma unroll
         for (int h = 0; h < HELD; ++h)
-            if (h < lots) {
-                load(h, u[h]);
+            if (lot0 + h < lots) load(lot0 + h, u[h]);
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            if (lot0 + h < lots) {
                 rotate(u[h], log2b, lane);
-                larger(u[h]);
+                tops[h] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < C; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(tops[h]) : "f"(fabsf(u[h][i])), "f"(fabsf(u[h][i + 1])));
+                asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(tops[h]));
             }
-    } else {
-        for (int lot = 0; lot < lots; ++lot) {
-            load(lot, u[0]);
-            rotate(u[0], log2b, lane);
-            larger(u[0]);
-        }
+        if (ALL) break;
     }
+    if (page < 0 || page >= p.q.n_pages) return;                       // (the whole block's: no barrier is missed)
+    const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
+    int8_t *const codes = p.codes[kind] + (block << p.q.page) * (size_t)D;
+    float *const step = p.steps[kind] + block;
+    const float before = at.slot > 0 ? __ldg(step) : 0.0f;
     top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
     if (WARPS > 1) {
         if (lane == 0) {
@@ -253,10 +297,10 @@ __global__ void __launch_bounds__(THREADS) write_kernel(const __grid_constant__ 
             exact[warp] = 0ull;
         }
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(part[w])));
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(part[lane % WARPS])));
     }
-    const float root = sqrtf((float)(1 << log2b));
+    const double wide_root = (log2b & 1 ? 1.4142135623730951 : 1.0) * (double)(1 << (log2b >> 1));        // sqrt b
+    const float root = (float)wide_root;
     const float e = log2b == 0 ? 0.0f : 1.01f * (float)log2b * root * 0x1p-24f;
     // Far from the ends of fp32, or everything is summed in fp64.
     const bool plain = top < 0x1p100f && top > 0x1p-80f;
@@ -264,110 +308,109 @@ __global__ void __launch_bounds__(THREADS) write_kernel(const __grid_constant__ 
     if (top != 0.0f && log2b != 0) {
         const float near = plain ? top * (1.0f - 2.0f * e - 0x1p-22f) : -1.0f;
         unsigned long long most = 0ull;
-        auto candidates = [&](int lot, const float (&v)[LANE]) {
-            unsigned want = 0u;
+        for (int lot0 = 0; lot0 < lots; lot0 += HELD) {
+            unsigned long long want = 0ull;
 #pragma unroll
-            for (int i = 0; i < LANE; ++i) want |= !(fabsf(v[i]) < near) ? 1u << i : 0u;
-            if (lot * K::tokens + mine >= at.n) want = 0u;
-            for (unsigned asked = __ballot_sync(0xffffffffu, want != 0u); asked != 0u; asked = __ballot_sync(0xffffffffu, want != 0u)) {
-                const int i = want ? __ffs(want) - 1 : 0;
-                bool answered;
-                const double y = again(lot, i, asked, answered);
-                if (answered) {
-                    most = max(most, (unsigned long long)__double_as_longlong(fabs(y)));
-                    want &= want - 1u;
+            for (int h = 0; h < HELD; ++h) {
+                if (lot0 + h >= lots) break;
+                if (!held) {
+                    load(lot0 + h, u[h]);
+                    rotate(u[h], log2b, lane);
+                }
+                if ((!held || !(tops[h] < near)) && (lot0 + h) * K::tokens + mine < at.n) {
+                    unsigned bits = 0u;
+#pragma unroll
+                    for (int i = 0; i < C; ++i) bits |= !(fabsf(u[h][i]) < near) ? 1u << i : 0u;
+                    want |= (unsigned long long)bits << (C * h);
                 }
             }
-        };
-        if (held) {
-#pragma unroll
-            for (int h = 0; h < HELD; ++h)
-                if (h < lots) candidates(h, u[h]);
-        } else {
-            for (int lot = 0; lot < lots; ++lot) {
-                load(lot, u[0]);
-                rotate(u[0], log2b, lane);
-                candidates(lot, u[0]);
-            }
+            settle(lot0, want, [&](int, int, double y) { most = max(most, (unsigned long long)__double_as_longlong(fabs(y))); });
+            if (ALL) break;
         }
-#pragma unroll
-        for (int l = 16; l > 0; l /= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, l));
+        // (numbers of bits, as none is negative: the upper halves' largest, then the lower ones' of those that have it)
+        auto largest = [](unsigned long long v) {
+            const unsigned high = __reduce_max_sync(0xffffffffu, (unsigned)(v >> 32));
+            return (unsigned long long)high << 32 | __reduce_max_sync(0xffffffffu, (unsigned)(v >> 32) == high ? (unsigned)v : 0u);
+        };
+        most = largest(most);
         if (WARPS > 1) {
             if (lane == 0) exact[warp] = most;
             __syncthreads();
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) most = max(most, exact[w]);
+            most = largest(exact[lane % WARPS]);
         }
         a = __longlong_as_double((long long)most);
     }
-    const double wide_root = sqrt((double)(1 << log2b));
-    float s = (float)(a / wide_root / 127.0);
+    // a / sqrt b / 127: by a product that is off by 2^-51 at most, unless that could decide how it is rounded to fp32 (or fp32's ends are near).  Divisions in fp64 are 60 instructions each.
+    const double about = a * (1.0 / 127.0) * (log2b & 1 ? 0.70710678118654752 : 1.0) * __longlong_as_double((long long)(1023 - (log2b >> 1)) << 52);
+    const uint32_t rest = (uint32_t)__double_as_longlong(about) & 0x1fffffffu;
+    float s = plain && rest - 0x0ffffff0u > 0x20u ? (float)about : (float)(a / wide_root / 127.0);
     if (before > s || before != before) s = before;
     const bool finite = fabsf(s) <= 3.4028235e38f, none = !finite || s == 0.0f;
 
     // 2. codes
-    const float inverse = (float)(1.0 / ((double)s * wide_root));
+    const float inverse = 1.0f / (s * root);                           // (off by 3 2^-24, and a quotient by one more)
     // (a value of s is at least that of the largest / 127, so |u| inverse stays below 127 and a little)
     const bool quick = plain && s > 0x1p-100f;
-    const float sure = quick ? 0.5f - 127.5f * (e + 0x1p-22f) : -1.0f;
-    auto store = [&](int lot, const float (&v)[LANE]) {
-        uint32_t c[LANE];
-        unsigned doubt = 0u;
+    const float sure = quick ? 0.5f - 127.5f * (e + 0x1p-21f) : -1.0f;
+    for (int lot0 = 0; lot0 < lots; lot0 += HELD) {
+        unsigned long long doubt = 0ull;
 #pragma unroll
-        for (int i = 0; i < LANE; ++i) {
-            const float q = v[i] * inverse, t = q + 12582912.0f, d = q - (t - 12582912.0f);
-            c[i] = __float_as_uint(t);
-            doubt |= !(fabsf(d) <= sure) ? 1u << i : 0u;
-        }
-        const int t = lot * K::tokens + mine;
-        if (none || t >= at.n) doubt = 0u;
-        for (unsigned asked = __ballot_sync(0xffffffffu, doubt != 0u); asked != 0u; asked = __ballot_sync(0xffffffffu, doubt != 0u)) {
-            const int i = doubt ? __ffs(doubt) - 1 : 0;
-            bool answered;
-            const double y = again(lot, i, asked, answered);
-            if (answered) {
-                const uint32_t code = (uint32_t)exact_code(y / wide_root, s);
+        for (int h = 0; h < HELD; ++h) {
+            if (lot0 + h >= lots) break;
+            if (!held) {
+                load(lot0 + h, u[h]);
+                rotate(u[h], log2b, lane);
+            }
+            uint32_t c[C];
+            float far = 0.0f;
 #pragma unroll
-                for (int k = 0; k < LANE; ++k)
-                    if (k == i) c[k] = code;
-                doubt &= doubt - 1u;
+            for (int i = 0; i < C; ++i) {
+                const float q = u[h][i] * inverse, t = q + 12582912.0f;
+                u[h][i] = q - (t - 12582912.0f);
+                c[i] = __float_as_uint(t);
+            }
+#pragma unroll
+            for (int i = 0; i < C; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(far) : "f"(fabsf(u[h][i])), "f"(fabsf(u[h][i + 1])));
+            const int t = (lot0 + h) * K::tokens + mine;
+            if (!(far <= sure) && !none && t < at.n) {
+                unsigned bits = 0u;
+#pragma unroll
+                for (int i = 0; i < C; ++i) bits |= !(fabsf(u[h][i]) <= sure) ? 1u << i : 0u;
+                doubt |= (unsigned long long)bits << (C * h);
+            }
+            uint32_t w[C / 4];
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i)
+                w[i] = none ? 0u : __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
+            int8_t *const to = codes + (size_t)(at.slot + t) * D + channel;
+            if (t < at.n) {
+                if constexpr (C == 16) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                else *reinterpret_cast<uint32_t *>(to) = w[0];
             }
         }
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = none ? 0u : __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
-        if (t < at.n) *reinterpret_cast<uint4 *>(codes + (size_t)(at.slot + t) * D + channel) = make_uint4(w[0], w[1], w[2], w[3]);
-    };
-    if (held) {
-#pragma unroll
-        for (int h = 0; h < HELD; ++h)
-            if (h < lots) store(h, u[h]);
-    } else {
-        for (int lot = 0; lot < lots; ++lot) {
-            load(lot, u[0]);
-            rotate(u[0], log2b, lane);
-            store(lot, u[0]);
-        }
+        // (bytes of what this lane has just stored)
+        settle(lot0, doubt, [&](int lot, int i, double y) { codes[(size_t)(at.slot + lot * K::tokens + mine) * D + channel + i] = (int8_t)exact_code(y / wide_root, s); });
+        if (ALL) break;
     }
     // 3. earlier codes, where the step has grown
     if (at.slot > 0 && !(s == before)) {
         const float ratio = before / s;
         const bool fast = before > 0x1p-80f && s < 0x1p100f;
-        for (int t = mine; t < at.slot; t += K::tokens) {
-            uint4 *const to = reinterpret_cast<uint4 *>(codes + (size_t)t * D + channel);
+        // (16 codes to a lane)
+        for (int k = share; k < at.slot * (D / 16); k += WARPS * 32) {
+            uint4 *const to = reinterpret_cast<uint4 *>(codes) + k;
             uint4 old = *to;
             uint32_t *const w = reinterpret_cast<uint32_t *>(&old);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t r = 0u;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int code = (int)(int8_t)(w[i] >> (8 * k));
+#pragma unroll 1
+                for (int b = 0; b < 32; b += 8) {
+                    const int code = (int)(int8_t)(w[i] >> b);
                     const float q = (float)code * ratio, n = rintf(q);
                     int v = (int)n;
                     if (!fast || fabsf(q - n) > 0.5f - 128.0f * 0x1p-22f) v = none ? 0 : exact_code((double)code * (double)before, s);
-                    r |= (uint32_t)(uint8_t)v << (8 * k);
+                    r |= (uint32_t)(uint8_t)v << b;
                 }
                 w[i] = none ? 0u : r;
             }

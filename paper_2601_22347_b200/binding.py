@@ -500,10 +500,9 @@ def _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages):
     assert k_steps.get_device() == device and k_steps.dtype is f32 and k_steps.is_contiguous() and v_steps.get_device() == device and v_steps.dtype is f32 and v_steps.is_contiguous()
     assert offsets.get_device() == device and offsets.dtype is i32 and offsets.is_contiguous() and lengths.get_device() == device and lengths.dtype is i32 and lengths.is_contiguous()
     assert pages.get_device() == device and pages.dtype is i32 and pages.is_contiguous()
-    shape = k_codes.shape
-    n_pages, heads, page, D = shape
+    n_pages, heads, page, D = shape = k_codes.shape
     S, width = pages.shape
-    assert v_codes.shape == shape and k_steps.shape == (n_pages, heads) and v_steps.shape == (n_pages, heads) and lengths.numel() == S and offsets.numel() == S + 1
+    assert v_codes.shape == shape and k_steps.numel() == n_pages * heads == v_steps.numel() and lengths.numel() == S and offsets.numel() == S + 1
     return S, heads, D, page, n_pages, width
 
 

@@ -462,10 +462,15 @@ int perq_cache_read_i8(const void *k_codes, const float *k_steps, const void *v_
  *                       `most` on are left as they are.
  *   out                 device, dense [T, heads * group, D] of out_type
  *   workspace           device, at least perq_attention_i8_workspace_bytes(...) bytes.  What is enough for T, S and most is enough for less of each
- *                       with the same heads, group and D.  Its contents need not be kept; calls that may overlap need one each.
+ *                       with the same heads, group and D; 80 MB are the most (a B200, D = 128, more than 64 rows to a sequence), 2.5 MB for decode steps.  Its contents need not be
+ *                       kept; calls that may overlap need one each.
+ *   scale               of the logits: finite (SHAPE)
  *
- * Queries are rounded to fp16 after their rotation (with the row's largest between 1 and 2: bf16 without a rotation is kept), probabilities times their values' step to
- * fp16 (2^-12 relative); sums are fp32 or wider, and added in an order that does not change from run to run.  Values' steps: 0, or 2^-64 to 2^120 (smaller ones count as 0).
+ * Rotated queries are rounded: of sequences with up to 64 rows (token and query head of one head of the cache) to whole multiples of 1/16256 of the row's largest; of others to fp16
+ * with the row's largest, before its rotation, between 1 and 2 (bf16 and fp16 without a rotation are kept, but for 2^-25 of that).  Probabilities times their values' step are rounded to
+ * fp16 (2^-11 of each); sums are fp32 or wider, and added in an order that does not change from run to run.  A query that is not finite gives a row of NaN.
+ * Steps are not negative.  Keys' below 2^-60 may count as 2^-60, values' below 2^-64 count as 2^-64 (codes of such pages are 0 where perq_cache_write_i8 writes a step of 0), and those
+ * above 2^126 may count as not finite.  Values' steps of one sequence and head should lie within 2^80 of each other (0 counts as 2^-64): probabilities below 2^-45 may be left out beyond.
  * Errors: NULL, SHAPE, BLOCK, FMT, ALIGN, WORKSPACE, CUDA.
  */
 int perq_attention_i8(const void *q, int32_t in_type, int64_t q_stride, const void *k_codes, const float *k_steps, const void *v_codes, const float *v_steps,
@@ -481,7 +486,7 @@ int perq_attention_i8_workspace_bytes(int64_t T, int32_t S, int32_t heads, int32
  * kernel then stops early and its outputs are incomplete.  Bits 1 and 2: such a wait inside the
  * permuted and grouped kernels, for an exact maximum (1) or a free buffer (2); bit 3: in the
  * statistic; bits 4 to 6: in the products and the
- * kernel of 8-bit codes; bit 7: in the attention of many queries.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
+ * kernel of 8-bit codes; bit 7: in the attention over the 8-bit cache.  Kernels only ever set bits; the word keeps them until perq_device_error_clear.
  *
  * perq_device_error_clear -- writes 0 to that word on the current device (synchronously,
  * cudaMemcpyToSymbol), so that a later read reports only what happened since.  Call it with no

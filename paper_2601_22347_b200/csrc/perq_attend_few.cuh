@@ -15,8 +15,8 @@
 // Values' codes become fp16 exactly: code ^ 0x80 in the low bits of 1024, minus 1152.
 //
 // y = s_k f S + log2 s_v - m, base 2, with f the row's factor and m its reference.  Values' steps go into the exponent: P = 2^y, so that fp16 P (2^-12 of each) meet exact codes and no row's
-// sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is only moved when something is over 2^8 times larger.  Blocks of values whose step is below 2^-64 (of zeros)
-// count as zeros of that step.
+// sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is only moved when something is over 2^8 times larger.  Values' steps below 2^-64 (of
+// zeros) count as 2^-64.
 #pragma once
 
 #include "perq_cache.cuh"
@@ -292,7 +292,14 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
         const long long of_sequence = (long long)u.tiles * u.count * p.heads;
         if (unit >= begin + of_sequence) {
             begin += of_sequence;
-            ++i;
+            // (the next one with rows: a padded batch has many without)
+            for (++i; i < p.q.S; i += 32) {
+                const unsigned some = __ballot_sync(0xffffffffu, i + lane < p.q.S && units_of<K::rows>(p, min(i + lane, p.q.S - 1)).tiles > 0);
+                if (some != 0u) {
+                    i += __ffs(some) - 1;
+                    break;
+                }
+            }
             continue;
         }
         const int number = (int)((unit - begin) / u.count), head = number / u.tiles, row0 = (number - head * u.tiles) * K::rows;
@@ -309,10 +316,10 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
         auto fetch = [&](int batch) {
             const int n = batch * 32 + lane, l = l0 + warp + n * FEW_WARPS;
             if (n < units) {
-                later_page = min(max(__ldg(table + min(key_of(l) >> p.q.page, p.q.width - 1)), 0), p.q.n_pages - 1);
+                later_page = min(max(*(table + min(key_of(l) >> p.q.page, p.q.width - 1)), 0), p.q.n_pages - 1);
                 const size_t block = (size_t)later_page * (size_t)p.heads + (size_t)head;
-                const float vs = __ldg(p.v_steps + block);
-                next_step[0] = __ldg(p.k_steps + block);
+                const float vs = *(p.v_steps + block);
+                next_step[0] = *(p.k_steps + block);
                 next_step[1] = vs < 0x1p-64f ? -64.0f : log2_of(vs);
                 next_step[2] = vs < 0x1p-64f ? 0x1p64f : 1.0f / vs;
             }
@@ -343,8 +350,8 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
             if (tid / lanes < rows) {
                 const int token = (row0 + row) / p.group, h = (row0 + row) - token * p.group;
                 const uint4 *const from = reinterpret_cast<const uint4 *>(p.x + (size_t)(u.r.begin + token) * (size_t)p.stride + (size_t)(head * p.group + h) * D + channel);
-                lo = __ldg(from);
-                hi = __ldg(from + 1);
+                lo = *from;
+                hi = *(from + 1);
             }
             float v[LANE], top = 0.0f;
             unpack(v, lo, hi, p.f16 != 0);

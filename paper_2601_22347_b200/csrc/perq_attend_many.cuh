@@ -84,7 +84,7 @@ __device__ __forceinline__ bool cta_wait_warp(uint32_t bar, uint32_t parity, uin
 }
 // 2^x on the multiply-add pipe, for x up to 100: 2^(x - n) with n the nearest whole number by its Taylor polynomial of degree 5 (off by (ln2 / 2)^6 / 6! = 2.4e-6), times 2^n.  One in
 // eight exponentials is taken so, because the others are what two warps of a scheduler wait for (16 a cycle and SM): chunks behind long contexts 310 -> 298 us; one in four 310.  Below -125: 0.
-// NaN stays NaN.
+// (NaN need not stay NaN: rows that have one carry it in their sum.)
 __device__ __forceinline__ float exp2_fma(float x)
 {
     const float t = x + 12582912.0f, f = x - (t - 12582912.0f);
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
             ++mine;
             // Queries: 32 rows to a warp, 16 channels to a lane; a row's largest is scaled to 1 .. 2 by a power of two, then it is rotated and rounded to fp16.
             // (A row to a thread: 12 us of loads that touch 32 rows each.)
-            float factor = 0.0f;
+            float factor = 0.0f, l = 0.0f;                             // (l: of probabilities)
             if (tiles > 0) {
                 constexpr int wide = D / LANE, at_once = 32 / wide;    // lanes of a row, rows at once
                 const int in = lane / wide, channel = lane % wide * LANE, first_row = (warp & 3) * 32;
@@ -341,8 +341,8 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         if (r < it.rows) {
                             const uint4 *const from = reinterpret_cast<const uint4 *>(p.a.x + (size_t)(it.begin + its_token) * (size_t)p.a.stride +
                                                                                       (size_t)(it.head * p.a.group + its_head) * D + channel);
-                            lo[k] = __ldg(from);
-                            hi[k] = __ldg(from + 1);
+                            lo[k] = *from;
+                            hi[k] = *(from + 1);
                         }
                     }
 #pragma unroll
@@ -350,9 +350,9 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         float v[LANE], most = 0.0f;
                         unpack(v, lo[k], hi[k], p.a.f16 != 0);
 #pragma unroll
-                        for (int i = 0; i < LANE; ++i) most = fmaxf(most, fabsf(v[i]));
+                        for (int i = 0; i < LANE; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v[i])));
 #pragma unroll
-                        for (int l = 1; l < wide; l *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, l));
+                        for (int k1 = 1; k1 < wide; k1 *= 2) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(__shfl_xor_sync(0xffffffffu, most, k1)));
                         const int e = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
                         // (with the sign of the logits' scale, as a page's largest logit has to be that of its largest S)
                         const float down = copysignf(__uint_as_float((uint32_t)(254 - e) << 23), p.a.scale);
@@ -363,9 +363,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)(channel / 64) * K::half + r * 128u;
                         sts128(to + ((c ^ r) & 7u) * 16u, make_uint4(half2_of(v[0], v[1]), half2_of(v[2], v[3]), half2_of(v[4], v[5]), half2_of(v[6], v[7])));
                         sts128(to + (((c + 1u) ^ r) & 7u) * 16u, make_uint4(half2_of(v[8], v[9]), half2_of(v[10], v[11]), half2_of(v[12], v[13]), half2_of(v[14], v[15])));
-                        // (the lane of the row has its factor; not 0, so that what is not seen stays -inf)
-                        const float x = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)e << 23), (lane % at_once) * wide);
-                        if (lane / at_once == k0 + k) factor = fmaxf(x * fabsf(p.a.scale), 0x1p-60f);
+                        // (the lane of the row has its factor; not 0, so that what is not seen stays -inf.  A query that is not finite makes the sum of probabilities NaN, unless the row
+                        // sees nothing)
+                        const float top = __shfl_sync(0xffffffffu, most, (lane % at_once) * wide);
+                        if (lane / at_once == k0 + k) {
+                            factor = fmaxf(__uint_as_float(min(max(__float_as_uint(top) >> 23, 1u), 253u) << 23) * fabsf(p.a.scale), 0x1p-60f);
+                            if (!(top <= 3.4028235e38f) && position >= 0) l = __uint_as_float(0x7fffffffu);
+                        }
                     }
                 }
             }
@@ -378,7 +382,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
             // rows of this warp: all of a tile's keys that its rows have in common
             const int row_first = it.row0 + t * 128 + (warp & 3) * 32, row_last = it.row0 + it.rows - 1;
             const int low_position = it.first + min(row_first, row_last) / p.a.group, high_position = it.first + min(row_first + 31, row_last) / p.a.group;
-            float m = -INFINITY, l = 0.0f;
+            float m = -INFINITY;
             for (int u = 0; u < 2 * tiles; ++u) {
                 const int side = u & 1, key = key_of(it, tile0 + (u >> 1)) + 64 * side;
                 const uint32_t j = j0 + (uint32_t)(u >> 1), global = global0 + (uint32_t)(u >> 1);
@@ -713,13 +717,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 const int32_t *const table = p.a.q.pages + (size_t)it.sequence * (size_t)p.a.q.width;
                 auto page_of = [&](int j) {
                     const int key = key_of(it, it.tile0 + j) + lane * each;
-                    return lane < copies && j < it.count ? min(max(__ldg(table + min(key >> log2page, p.a.q.width - 1)), 0), p.a.q.n_pages - 1) : 0;
+                    return lane < copies && j < it.count ? min(max(*(table + min(key >> log2page, p.a.q.width - 1)), 0), p.a.q.n_pages - 1) : 0;
                 };
                 int page = page_of(0);
                 for (int j = 0; j < it.count && ok; ++j, ++global) {
                     const int next = page_of(j + 1);
                     const size_t block = (size_t)page * (size_t)p.a.heads + (size_t)it.head;
-                    const float ks = __ldg(p.a.k_steps + block), vs = __ldg(p.a.v_steps + block);
+                    const float ks = *(p.a.k_steps + block), vs = *(p.a.v_steps + block);
                     for (int kind = 0; kind < 2; ++kind, ++n) {
                         const uint32_t r = n % K::raw_stages, bar = raw_full + 8u * r;
                         if (n >= K::raw_stages && !cta_wait_warp(raw_empty + 8u * r, (n / K::raw_stages - 1u) & 1u)) {

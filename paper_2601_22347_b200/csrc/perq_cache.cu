@@ -129,8 +129,9 @@ int launch_many(const AttendParams &a, int sms, cudaStream_t st)
     std::memset(&p, 0, sizeof(p));
     p.a = a;
     p.partial = a.partial;
-    // (sequences of more than a.few_rows rows have at most this many tiles)
-    const long long items = ((long long)a.q.T * a.group / MANY_ROWS + std::min(a.q.S, a.q.T)) * a.heads;
+    // (n sequences of more than a.few_rows rows each have at most rows / 256 + n tiles, and there are no more of them than fit into the rows)
+    const long long rows = (long long)a.q.T * a.group;
+    const long long items = (rows / MANY_ROWS + std::min<long long>(a.q.S, rows / (a.few_rows + 1))) * a.heads;
     p.split = many_split(a, items, sms);
     if (items * p.split >= (1ll << 31)) return PERQ_ERR_SHAPE;
     if (int rc = launch(a.q.page == 4 ? many_kernel<D, true> : many_kernel<D, false>, items * p.split, MANY_THREADS, Many<D>::bytes, st, 1, p)) return rc;
@@ -232,7 +233,7 @@ int perq_attention_i8(const void *q, int32_t in_type, int64_t q_stride, const vo
                       int32_t out_type, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (int rc = check_cache(T, S, heads, D, b, page, n_pages, width)) return rc;
-    if (group < 1 || (int64_t)heads * group > PERQ_MAX_HEADS || !row_stride(q_stride, (int64_t)heads * group * D) || most < 1 || window < 0 || sinks < 0) return PERQ_ERR_SHAPE;
+    if (group < 1 || (int64_t)heads * group > PERQ_MAX_HEADS || !row_stride(q_stride, (int64_t)heads * group * D) || most < 1 || window < 0 || sinks < 0 || !std::isfinite(scale)) return PERQ_ERR_SHAPE;
     if ((in_type != PERQ_OUT_BF16 && in_type != PERQ_OUT_F16) || out_type < PERQ_OUT_BF16 || out_type > PERQ_OUT_F32) return PERQ_ERR_FMT;
     if (T == 0 || S == 0) return PERQ_OK;
     const void *const all[] = {q, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages, out};

@@ -37,9 +37,9 @@ struct Rows {
 __device__ __forceinline__ Rows rows_of(const Sequences &q, int i)
 {
     Rows r;
-    r.begin = min(max(__ldg(q.offsets + i), 0), q.T);
-    r.n = max(min(max(__ldg(q.offsets + i + 1), 0), q.T) - r.begin, 0);
-    r.length = (int32_t)min((long long)max(__ldg(q.lengths + i), 0), (long long)q.width << q.page);
+    r.begin = min(max(*(q.offsets + i), 0), q.T);
+    r.n = max(min(max(*(q.offsets + i + 1), 0), q.T) - r.begin, 0);
+    r.length = (int32_t)min((long long)max(*(q.lengths + i), 0), (long long)q.width << q.page);
     return r;
 }
 // Blocks that a sequence's rows fall into; rows at positions below 0 (fewer tokens than rows) into none.
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(WARPS == 16 ? 512 : THREADS, HELD == 4 || WARP
     const Place at = find_block<K::threads>(p.q, number);
     if (at.n <= 0) return;
     // (on its way while the tokens are read and rotated)
-    const int page = __ldg(p.q.pages + (size_t)at.sequence * (size_t)p.q.width + (size_t)at.entry);
+    const int page = *(p.q.pages + (size_t)at.sequence * (size_t)p.q.width + (size_t)at.entry);
     const int item = WARPS == 1 ? in * (K::threads / 32) + warp : in;
     if (item >= 2 * p.heads) return;                                   // (whole warps, and then no barrier follows)
     const int kind = item >= p.heads ? 1 : 0, head = item - kind * p.heads, log2b = kind ? 0 : p.log2b;
@@ -233,10 +233,10 @@ __global__ void __launch_bounds__(WARPS == 16 ? 512 : THREADS, HELD == 4 || WARP
         if (t < at.n) {
             const uint16_t *const from = x + (size_t)t * (size_t)p.stride[kind] + channel;
             if constexpr (C == 16) {
-                const uint4 lo = __ldg(reinterpret_cast<const uint4 *>(from)), hi = __ldg(reinterpret_cast<const uint4 *>(from) + 1);
+                const uint4 lo = *reinterpret_cast<const uint4 *>(from), hi = *(reinterpret_cast<const uint4 *>(from) + 1);
                 w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
             } else {
-                const uint2 lo = __ldg(reinterpret_cast<const uint2 *>(from));
+                const uint2 lo = *reinterpret_cast<const uint2 *>(from);
                 w[0] = lo.x; w[1] = lo.y;
             }
         }
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(WARPS == 16 ? 512 : THREADS, HELD == 4 || WARP
     const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
     int8_t *const codes = p.codes[kind] + (block << p.q.page) * (size_t)D;
     float *const step = p.steps[kind] + block;
-    const float before = at.slot > 0 ? __ldg(step) : 0.0f;
+    const float before = at.slot > 0 ? *step : 0.0f;
     top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
     if (WARPS > 1) {
         if (lane == 0) {
@@ -454,14 +454,14 @@ __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ R
         int lo = 0, hi = p.q.S;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (__ldg(p.q.offsets + mid) <= row) lo = mid; else hi = mid;
+            if (*(p.q.offsets + mid) <= row) lo = mid; else hi = mid;
         }
         const Rows r = rows_of(p.q, lo);
         int at = -2;                                                   // not a row of any sequence: left as it is
         slot[tid] = 0;
         if (row >= r.begin && row < r.begin + r.n) {
             const int position = r.length - r.n + (row - r.begin);
-            at = position < 0 ? -1 : __ldg(p.q.pages + (size_t)lo * (size_t)p.q.width + (size_t)(position >> p.q.page));
+            at = position < 0 ? -1 : *(p.q.pages + (size_t)lo * (size_t)p.q.width + (size_t)(position >> p.q.page));
             if (at < 0 || at >= p.q.n_pages) at = -1;                  // (zeros)
             slot[tid] = position & ((1 << p.q.page) - 1);
         }
@@ -477,8 +477,8 @@ __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ R
         float s = 0.0f;
         if (page >= 0) {
             const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
-            v = __ldg(reinterpret_cast<const uint4 *>(p.codes[kind] + ((block << p.q.page) + (size_t)slot[t]) * D + channel));
-            s = __ldg(p.steps[kind] + block);
+            v = *reinterpret_cast<const uint4 *>(p.codes[kind] + ((block << p.q.page) + (size_t)slot[t]) * D + channel);
+            s = *(p.steps[kind] + block);
         }
         float u[LANE];
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};

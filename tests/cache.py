@@ -81,6 +81,8 @@ def attention(cache, q, offsets, lengths, pages, b, scale, window=0, sinks=0):
     out, tolerance = torch.full((T, Hq, D), math.nan, dtype=torch.float64), torch.zeros((T, Hq, D), dtype=torch.float64)
     for i, length in enumerate(lengths):
         rows, length = slice(offsets[i], offsets[i + 1]), max(length, 0)
+        if rows.start == rows.stop:
+            continue
         k, v = (cache.tokens(kind, i, length, pages) for kind in (0, 1))
         seen = visible(torch.arange(lengths[i] - (rows.stop - rows.start), lengths[i]), length, window, sinks)
         for h in range(Hq):

@@ -99,3 +99,8 @@ def test_workspace(lib):
     assert lib.perq_attention_i8_workspace_bytes(1, 1, 8, 0, 64, 1, C.byref(n)) == SHAPE
     assert lib.perq_attention_i8_workspace_bytes(1, 1, 8, 4, 64, 0, C.byref(n)) == SHAPE
     assert lib.perq_attention_i8_workspace_bytes(1, 1, 8, 4, 64, 1, None) == NULL
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 1e39])
+def test_scales_that_are_not_finite(lib, scale):
+    assert attend(lib, scale=scale) == SHAPE

@@ -110,16 +110,28 @@ int launch_few(const AttendParams &p, int sms, cudaStream_t st)
     return launch(join_kernel<D, NT>, ctas - 1, THREADS, join_bytes(ctas), st, 8 * NT / JOIN_ROWS, p, ctas);
 }
 
-// Rows (of tokens and heads) of a sequence up to which the kernel for few queries takes it.
-constexpr int FEW_ROWS = 64;
+// Rows (of tokens and heads) of a sequence up to which the kernel for few queries takes it.  32 sequences of 8000 tokens, 8 heads of 128, few against many: 24 rows 245 and 237 us, 32 rows
+// 250 and 242, 48 rows 360 and 214; two sequences: 32 rows 31 and 32, 48 rows 38 and 32 (behind 500 tokens: 13 and 19, 19 and 19).  Heads of 64: 32 rows 85 and 108, 48 rows 122 and 108.
+constexpr int FEW_ROWS = 32, BOTH_ROWS = 64;
 constexpr int MANY_PIECES = 4;               // to an SM, of tiles of rows whose keys are split
 
-// CTAs to the keys of a tile of rows.  Few items leave SMs without work, or, with contexts of different lengths, one SM with much more than another: pieces are made until there are four to
-// an SM, none of fewer than four tiles of keys.
-int many_split(const AttendParams &p, long long items, int sms)
+// CTAs to the keys of a tile of rows.  Few items leave SMs without work, or, with contexts of different lengths, one SM with much more than another; every piece costs as much as four and a half
+// tiles of keys for its queries and results, and joining them two.  With items alike the call takes whole rounds of pieces, with different ones the CTAs take them as they come: the mean of
+// both is what is compared.  (Two sequences of 8000 tokens, 64 rows: 15 pieces 51 us, 9 of them 32; 8 sequences 98 and 77; 32 sequences of 2000, heads of 64: 4 pieces 46 us, 1 32.)
+int many_split(const AttendParams &p, long long most_items, long long items, int sms)
 {
-    const long long key_tiles = (((long long)p.q.width << p.q.page) + MANY_KEYS - 1) / MANY_KEYS;
-    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(MANY_PIECES * sms / items, 16), key_tiles / 4));
+    long long keys = (long long)p.q.width << p.q.page;
+    if (p.window > 0) keys = std::min(keys, (long long)p.window + p.sinks + std::min(p.q.T, p.most) + 2 * MANY_KEYS);
+    const long long tiles = (keys + MANY_KEYS - 1) / MANY_KEYS, limit = std::min<long long>(std::min<long long>(MANY_PIECES * sms / most_items, 16), tiles);
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s == 1 || s <= limit; ++s) {
+        const double rounds = (double)items * s / sms, cost = 0.5 * (std::ceil(rounds) + rounds + 0.5) * (4.5 + (double)tiles / s) + (s > 1 ? 2.0 : 0.0);
+        if (s > 1 && cost >= least) continue;
+        best = s;
+        least = cost;
+    }
+    return best;
 }
 
 template <int D>
@@ -129,10 +141,10 @@ int launch_many(const AttendParams &a, int sms, cudaStream_t st)
     std::memset(&p, 0, sizeof(p));
     p.a = a;
     p.partial = a.partial;
-    // (n sequences of more than a.few_rows rows each have at most rows / 256 + n tiles, and there are no more of them than fit into the rows)
-    const long long rows = (long long)a.q.T * a.group;
-    const long long items = (rows / MANY_ROWS + std::min<long long>(a.q.S, rows / (a.few_rows + 1))) * a.heads;
-    p.split = many_split(a, items, sms);
+    // (n sequences of more than a.few_rows rows each have at most rows / 256 + n tiles, and there are no more of them than fit into the rows; if they are alike, so many have them)
+    const long long rows = (long long)a.q.T * a.group, n = std::min<long long>(a.q.S, rows / (a.few_rows + 1)), each = (rows + n - 1) / n;
+    const long long items = (rows / MANY_ROWS + n) * a.heads;
+    p.split = many_split(a, items, n * ((each + MANY_ROWS - 1) / MANY_ROWS) * a.heads, sms);
     if (items * p.split >= (1ll << 31)) return PERQ_ERR_SHAPE;
     if (int rc = launch(a.q.page == 4 ? many_kernel<D, true> : many_kernel<D, false>, items * p.split, MANY_THREADS, Many<D>::bytes, st, 1, p)) return rc;
     return p.split > 1 ? launch(many_join_kernel<D>, items, THREADS, 0, st, MANY_JOIN, p) : PERQ_OK;
@@ -141,11 +153,13 @@ int launch_many(const AttendParams &a, int sms, cudaStream_t st)
 template <int D>
 int launch_attention(AttendParams &p, int sms, cudaStream_t st)
 {
-    const int64_t rows = (int64_t)std::min<int64_t>(p.q.T, p.most) * p.group;
+    const int64_t most = std::min<int64_t>(p.q.T, p.most), rows = most * p.group;
     if (rows <= 8) return launch_few<D, 1>(p, sms, st);
-    if (rows <= FEW_ROWS) return launch_few<D, 2>(p, sms, st);
-    // (a single sequence of what may be many rows goes to the kernel for many, so that nothing is launched in vain)
-    p.few_rows = p.q.S == 1 ? 0 : FEW_ROWS;
+    // Up to 64 rows one kernel takes all sequences, by the mean of their rows (32 sequences of up to 5 tokens and 8 heads, 1 to 4 of them by one kernel and 5 by the other: 113 us, 63 by the first).
+    if (rows <= FEW_ROWS || (rows <= BOTH_ROWS && p.q.T * (int64_t)p.group <= (int64_t)FEW_ROWS * p.q.S)) return launch_few<D, 2>(p, sms, st);
+    // Beyond, the kernel for many takes them all if the shortest has more than FEW_ROWS where every row of the call is one's and the others have `most`; that saves two launches: two sequences of
+    // 256 rows behind 500 tokens 27 -> 23 us.  (No result hangs on it.)
+    p.few_rows = rows <= BOTH_ROWS || (p.q.T - (p.q.S - 1) * most) * p.group > FEW_ROWS ? 0 : FEW_ROWS;
     if (p.few_rows > 0)
         if (int rc = launch_few<D, 2>(p, sms, st)) return rc;
     return launch_many<D>(p, sms, st);

@@ -105,3 +105,11 @@ def test_a_padded_batch(B, rows):
     """Sequences without rows before, between and behind those that have some."""
     taken = {3: 900, 40: 80, 41: 133, 300: 2000, 411: 70}
     check(B, [rows if i in taken else 0 for i in range(500)], [taken.get(i, 0) for i in range(500)], 2, 4, 64, 16, 16, BF16, 11)
+
+
+@pytest.mark.parametrize("rows,group", [([9, 9, 9], 4), ([8, 8], 8), ([16, 2, 15, 14], 4), ([5, 5, 1, 5, 5], 8), ([1, 1, 1], 40)])
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 5)])
+def test_one_kernel_for_all(B, rows, group, D, window, sinks):
+    """33 to 64 rows to the longest sequence."""
+    check(B, rows, [n + 113 * i * i for i, n in enumerate(rows)], 2, group, D, 32, 16, BF16, group, window=window, sinks=sinks)

@@ -421,7 +421,8 @@ __global__ void __launch_bounds__(WARPS == 16 ? 512 : THREADS, HELD == 4 || WARP
 }
 
 // ------------------------------------------------------------------------------------------------------ reading back
-constexpr int READ_TOKENS = 16;               // of a CTA
+constexpr int READ_TOKENS = 32;               // of a CTA
+constexpr int READ_AHEAD = 4;
 
 struct ReadParams {
     Sequences q;
@@ -439,7 +440,20 @@ __device__ __forceinline__ uint32_t pack16(float x, float y, bool f16)
     return r;
 }
 
-// A lane has 16 channels of a token and head; blockIdx.y: keys, values.  The sequence of a row is looked for once a token.
+// 32 bytes: in one store where they lie on a multiple of 32, so that no sector is written in halves.
+__device__ __forceinline__ void store32(void *to, const uint32_t *w, bool wide)
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {
+        static_cast<uint4 *>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        static_cast<uint4 *>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
+// A lane has 16 channels of a token and head; blockIdx.y: keys, values.  The sequence of a row is looked for once a token.  Bound by instructions where keys are rotated (eight sequences of up
+// to 4096 tokens, blocks of 128, 5.0 TB/s without the rotation): 3 exchanges of 16 words each, 64 sums.  Conversions of codes run beside that on a pipe of their own; by permuted bytes and a
+// subtraction they cost the one that is wanted (31 -> 42 us), and so do sums of two in one integer (36).
 template <int D>
 __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ ReadParams p)
 {
@@ -470,38 +484,50 @@ __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ R
     __syncthreads();
     const int tokens = min(READ_TOKENS, p.q.T - row0), items = tokens * p.heads * lanes, log2b = kind ? 0 : p.log2b;
     const float factor = 1.0f / sqrtf((float)(1 << log2b));
-    for (int i0 = 0; i0 < items; i0 += THREADS) {
-        const int i = i0 + tid, t = min(i / lanes / p.heads, tokens - 1), head = i / lanes % p.heads, channel = i % lanes * LANE;
-        const int page = i < items ? place[t] : -2;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        float s = 0.0f;
-        if (page >= 0) {
-            const size_t block = (size_t)page * (size_t)p.heads + (size_t)head;
-            v = *reinterpret_cast<const uint4 *>(p.codes[kind] + ((block << p.q.page) + (size_t)slot[t]) * D + channel);
-            s = *(p.steps[kind] + block);
+    const bool wide = (reinterpret_cast<size_t>(p.out[kind]) & 31u) == 0u;
+    for (int i0 = 0; i0 < items; i0 += READ_AHEAD * THREADS) {
+        // (all that is read is on its way before the first of it is used)
+        uint4 v[READ_AHEAD];
+        float s[READ_AHEAD];
+        int page[READ_AHEAD];
+#pragma unroll
+        for (int a = 0; a < READ_AHEAD; ++a) {
+            const int i = i0 + a * THREADS + tid, t = min(i / lanes / p.heads, tokens - 1), head = i / lanes % p.heads, channel = i % lanes * LANE;
+            page[a] = i < items ? place[t] : -2;
+            v[a] = make_uint4(0, 0, 0, 0);
+            s[a] = 0.0f;
+            if (page[a] >= 0) {
+                const size_t block = (size_t)page[a] * (size_t)p.heads + (size_t)head;
+                v[a] = *reinterpret_cast<const uint4 *>(p.codes[kind] + ((block << p.q.page) + (size_t)slot[t]) * D + channel);
+                s[a] = *(p.steps[kind] + block);
+            }
         }
-        float u[LANE];
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int k = 0; k < LANE; ++k) u[k] = (float)(int8_t)(w[k / 4] >> (8 * (k % 4)));
-        rotate(u, log2b, lane);                                        // (whole numbers below 2^14: exact)
-        s *= factor;
+        for (int a = 0; a < READ_AHEAD; ++a) {
+            if (i0 + a * THREADS >= items) break;
+            float u[LANE];
+            const uint32_t w[4] = {v[a].x, v[a].y, v[a].z, v[a].w};
 #pragma unroll
-        for (int k = 0; k < LANE; ++k) u[k] *= s;
-        if (page == -2) continue;
-        const size_t at = ((size_t)(row0 + t) * (size_t)p.heads + (size_t)head) * D + (size_t)channel;
-        if (p.out_type == perq_mm::OUT_F32) {
-            float4 *const to = reinterpret_cast<float4 *>(static_cast<float *>(p.out[kind]) + at);
+            for (int k = 0; k < LANE; ++k) u[k] = (float)(int8_t)(w[k / 4] >> (8 * (k % 4)));
+            rotate(u, log2b, lane);                                    // (whole numbers below 2^14: exact)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) to[k] = make_float4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
-        } else {
-            const bool f16 = p.out_type == perq_mm::OUT_F16;
-            uint32_t o[8];
+            for (int k = 0; k < LANE; ++k) u[k] *= s[a] * factor;
+            if (page[a] == -2) continue;
+            // (rows are dense: the i-th 16 channels from the CTA's first row on)
+            const size_t at = ((size_t)row0 * (size_t)(p.heads * lanes) + (size_t)(i0 + a * THREADS + tid)) * LANE;
+            if (p.out_type == perq_mm::OUT_F32) {
+                float *const to = static_cast<float *>(p.out[kind]) + at;
+                uint32_t o[LANE];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = pack16(u[2 * k], u[2 * k + 1], f16);
-            uint4 *const to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.out[kind]) + at);
-            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
-            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                for (int k = 0; k < LANE; ++k) o[k] = __float_as_uint(u[k]);
+                store32(to, o, wide);
+                store32(to + 8, o + 8, wide);
+            } else {
+                uint32_t o[LANE / 2];
+#pragma unroll
+                for (int k = 0; k < LANE / 2; ++k) o[k] = pack16(u[2 * k], u[2 * k + 1], p.out_type == perq_mm::OUT_F16);
+                store32(static_cast<uint16_t *>(p.out[kind]) + at, o, wide);
+            }
         }
     }
 }

@@ -113,3 +113,19 @@ def test_a_padded_batch(B, rows):
 def test_one_kernel_for_all(B, rows, group, D, window, sinks):
     """33 to 64 rows to the longest sequence."""
     check(B, rows, [n + 113 * i * i for i, n in enumerate(rows)], 2, group, D, 32, 16, BF16, group, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", (BF16, torch.float32), ids=("bf16", "f32"))
+def test_read_into_what_is_aligned_to_16_bytes(B, dtype):
+    gen = torch.Generator()
+    gen.manual_seed(1)
+    cache, pages = filled([50, 90], 3, 64, 16, gen)
+    device, tables = cache.on_gpu(), (C.ints([0, 50, 140]), C.ints([50, 90]), pages.cuda())
+    k, v = B.perq_cache_read_i8(*device, *tables, T=140, b=32, out_dtype=dtype)
+    room = torch.full((2, 140 * 3 * 64 + 16), 7.0, dtype=dtype).cuda()
+    at = 16 // dtype.itemsize
+    parts = [r[at:at + k.numel()].view(k.shape) for r in room]
+    assert parts[0].data_ptr() % 32 == 16
+    B.perq_cache_read_i8(*device, *tables, T=140, b=32, k=parts[0], v=parts[1])
+    assert torch.equal(parts[0], k) and torch.equal(parts[1], v)
+    assert (room[:, :at] == 7).all() and (room[:, at + k.numel():] == 7).all()

@@ -1,11 +1,17 @@
 // Attention over the 8-bit cache for many queries to a sequence: prompts and chunks of them, on the fifth-generation tensor cores.
 //
-// A CTA has 256 rows (pairs of a token and one of the `group` heads of queries to a head of keys), two tiles of 128, and goes over the keys they see, 128 at a time.  Bulk copies
-// bring codes in, a page at a time, keys and values in turn; four warps make them fp16 (exactly) and lay them down as operands, in a ring; one warp issues the products: S = Q K^T into tensor memory, then O += P V with P
-// from tensor memory and V's rows as they are (its channels run along N).  Either tile has four warps of its own, a row to a thread, which take 64 keys at a time: their maximum, P = 2^(x +
-// log2 s_v - m) rounded to fp16 over the columns where S was, and the probabilities' sum.  S has room for 64 keys twice, so the products with the last 64 and for the next run under
-// the exponentials of these.  O stays in tensor memory; m moves, and O with it, only when something is over 2^8 times larger.
-// Bound by the tensor cores and the exponentials alike: 128 x 128 x 128 products twice are 1024 cycles, the tile's 16384 exponentials as many.
+// A work is 256 rows (pairs of a token and one of the `group` heads of queries to a head of keys), two tiles of 128, over the keys they see, 128 at a time.  Bulk copies bring codes in, a page
+// at a time, keys and values in turn; four warps make them fp16 (exactly: code ^ 0x80 in the low bits of 1024, minus 1152) and lay them down as operands, in a ring; one warp issues the
+// products: S = Q K^T into tensor memory, then O += P V with P from tensor memory and V's rows as they are (its channels run along N).  Either tile has four warps of its own, a row to a
+// thread, which take 64 keys at a time: their maximum, P = 2^(x + log2 s_v - m) rounded to fp16 over the columns where S was, and the probabilities' sum in fp32.  S has room for 64 keys
+// twice, so the products with the last 64 and for the next run under the exponentials of these.  O stays in tensor memory; m moves, and O with it, only when something is over 2^8 times
+// larger.  A CTA takes the work of others that have not begun (next_cta), and its loads and conversions run ahead into it.
+//
+// Floors: 4 D operations a pair of a row and a key it sees, at the tensor cores' rate.  Chunks of up to 512 tokens behind 16000, 32 heads of 128: 284 us, 820 TFLOP/s of 1667; two prompts of
+// up to 8192 268, 850.  Bound by the rows' warps, which never wait for the products: 2000 cycles to 64 keys of both tiles, in which the products take 1024 (pipe 42 %): 1020 exponentials (two warps
+// to a scheduler, 16 a cycle and SM), 400 maxima, 185 reading S, 400 waits and polls between steps that depend on each other.  Without the exponentials 11 % less, without the products 8, without
+// the conversions or the maxima 4.  What did not help: two threads to a row and 128 keys (the same); the maximum of P instead of S, with a second try where it was too large (349 -> 399 us); the
+// next S read under the exponentials (303 -> 326, registers); sleeping waits (+4 %); one exponential in four on the multiply-add pipe (310, in eight 298); heads in the inner order (+3 %).
 #pragma once
 
 #include "perq_attend_few.cuh"
@@ -763,38 +769,37 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
     if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(K::columns) : "memory");
 }
 
-// Rows whose keys were split: blockIdx.x is an item, blockIdx.y a part of its rows.  A thread has four channels of a row at a time, and up to four parts of them on their way.
+// Rows whose keys were split: blockIdx.x is an item, blockIdx.y a part of its rows.  A thread has four channels of a row at a time, and AHEAD parts of them on their way (two where there are no
+// more: bound by instructions and latency, 23.5 -> 19.8 us for two parts each of 200 items of 256 rows, all from memory).
 constexpr int MANY_JOIN = 8;
-template <int D>
-__global__ void __launch_bounds__(THREADS) many_join_kernel(const __grid_constant__ ManyParams p)
+template <int D, int AHEAD>
+__device__ __forceinline__ void join_many(const ManyParams &p, const ManyItem &it)
 {
-    const ManyItem it = many_item(p.a, (int)blockIdx.x, (int)threadIdx.x & 31);       // (every warp for itself; before the wait, as in join_kernel)
-    griddep_wait();
-    griddep_launch();
     const int row_begin = (int)blockIdx.y * (MANY_ROWS / MANY_JOIN), row_end = min(row_begin + MANY_ROWS / MANY_JOIN, it.rows);
     const float *const parts = many_part<D>(p, it.number, 0);
     constexpr size_t each = (size_t)MANY_ROWS * (D + 2);
+#pragma unroll 2
     for (int k = (int)threadIdx.x; k < (row_end - row_begin) * (D / 4); k += THREADS) {
         const int row = row_begin + k / (D / 4), channel = k % (D / 4) * 4;
         float m = -INFINITY, l = 0.0f;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int c0 = 0; c0 < p.split; c0 += 4) {
-            float4 x[4];
-            float xm[4], xl[4], next = m;
+        for (int c0 = 0; c0 < p.split; c0 += AHEAD) {
+            float4 x[AHEAD];
+            float xm[AHEAD], xl[AHEAD], next = m;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < AHEAD; ++c) {
                 const float *const from = parts + (size_t)min(c0 + c, p.split - 1) * each;
                 x[c] = *reinterpret_cast<const float4 *>(from + (size_t)row * D + channel);
                 xm[c] = c0 + c < p.split ? from[(size_t)MANY_ROWS * D + row] : -INFINITY;
                 xl[c] = from[(size_t)MANY_ROWS * D + MANY_ROWS + row];
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) next = fmaxf(next, xm[c]);
+            for (int c = 0; c < AHEAD; ++c) next = fmaxf(next, xm[c]);
             const float before = m == -INFINITY ? 0.0f : exp2_of(m - next);
             v.x *= before; v.y *= before; v.z *= before; v.w *= before;
             l *= before;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < AHEAD; ++c) {
                 // (a part that has seen nothing, or nothing but what is not finite, which stays)
                 const float a = xm[c] == -INFINITY ? (c0 + c < p.split && xl[c] != xl[c] ? 1.0f : 0.0f) : exp2_of(xm[c] - next);
                 l = fmaf(a, xl[c], l);
@@ -807,6 +812,21 @@ __global__ void __launch_bounds__(THREADS) many_join_kernel(const __grid_constan
         store_out4<D>(p.a, ((size_t)(it.begin + token) * (size_t)(p.a.heads * p.a.group) + (size_t)(it.head * p.a.group + h)) * D + (size_t)channel,
                       make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
     }
+}
+template <int D>
+__global__ void __launch_bounds__(THREADS) many_join_kernel(const __grid_constant__ ManyParams p)
+{
+    __shared__ ManyItem found;
+    if (threadIdx.x < 32) {
+        const ManyItem it = many_item(p.a, (int)blockIdx.x, (int)threadIdx.x);        // (before the wait, as in join_kernel)
+        if (threadIdx.x == 0) found = it;
+    }
+    __syncthreads();
+    griddep_wait();
+    griddep_launch();
+    const ManyItem it = found;
+    if (p.split == 2) join_many<D, 2>(p, it);
+    else join_many<D, 4>(p, it);
 }
 
 }  // namespace perq_kv

@@ -15,7 +15,8 @@
 // Values' codes become fp16 exactly: code ^ 0x80 in the low bits of 1024, minus 1152.
 //
 // 64 sequences of up to 12000 tokens, 8 heads of 128 with 4 of queries each: 182 us, 5.8 TB/s of 6.5.  32 sequences of up to 5 tokens, 4 heads of 64 with 8 of queries each, a window of 4096:
-// 60 us; there the products' tiles of 16 rows are 2 or 3 to a sequence, and the instructions for a key are issued for each (240 a unit of 16 keys; two of 8 rows 311 at D = 128).
+// 60 us, 1.1 TB/s; there a sequence has one to three tiles of 16 rows, each of which goes over its keys again (from L2), at 436 instructions a unit in all (64 sequences: 363), and a CTA's
+// share of 223 units crosses tiles, whose queries and results cost some microseconds each.
 //
 // y = s_k f S + log2 s_v - m, base 2, with f the row's factor and m its reference.  Values' steps go into the exponent: P = 2^y, so that fp16 P (2^-12 of each) meet exact codes and no row's
 // sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is only moved when something is over 2^8 times larger.  Values' steps below 2^-64 (of

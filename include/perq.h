@@ -468,7 +468,8 @@ int perq_cache_read_i8(const void *k_codes, const float *k_steps, const void *v_
  *
  * Rotated queries are rounded: of sequences with up to 64 rows (token and query head of one head of the cache) to whole multiples of 1/16256 of the row's largest; of others to fp16
  * with the row's largest, before its rotation, between 1 and 2 (bf16 and fp16 without a rotation are kept, but for 2^-25 of that).  Probabilities times their values' step are rounded to
- * fp16 (2^-11 of each); sums are fp32 or wider, and added in an order that does not change from run to run.  A query that is not finite gives a row of NaN.
+ * fp16: off by 2^-11 of each, or by 2^-32 of the row's largest such product where that is more (so those below 2^-32 of it may be left out of the sum over values; the sum of probabilities
+ * has them in fp32).  Sums are fp32 or wider, and added in an order that does not change from run to run.  A query that is not finite gives a row of NaN.
  * Steps are not negative.  Keys' below 2^-60 may count as 2^-60, values' below 2^-64 count as 2^-64 (codes of such pages are 0 where perq_cache_write_i8 writes a step of 0), and those
  * above 2^126 may count as not finite.  Values' steps of one sequence and head should lie within 2^80 of each other (0 counts as 2^-64): probabilities below 2^-45 may be left out beyond.
  * Errors: NULL, SHAPE, BLOCK, FMT, ALIGN, WORKSPACE, CUDA.

@@ -18,9 +18,10 @@
 // 60 us, 1.1 TB/s; there a sequence has one to three tiles of 16 rows, each of which goes over its keys again (from L2), at 436 instructions a unit in all (64 sequences: 363), and a CTA's
 // share of 223 units crosses tiles, whose queries and results cost some microseconds each.
 //
-// y = s_k f S + log2 s_v - m, base 2, with f the row's factor and m its reference.  Values' steps go into the exponent: P = 2^y, so that fp16 P (2^-12 of each) meet exact codes and no row's
-// sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is only moved when something is over 2^8 times larger.  Values' steps below 2^-64 (of
-// zeros) count as 2^-64.
+// y = s_k f S + log2 s_v - m, base 2, with f the row's factor and m its reference.  Values' steps go into the exponent: P = 2^y, so that fp16 P meet exact codes and no row's
+// sums mix steps; the sum of probabilities adds P / s_v in fp32.  m is 7 below the largest so far and is only moved when something is over 2^15 (P_MOST: fp16 ends at 2^16), so that P has all of
+// fp16's range: off by 2^-11 of itself (half a last place), or by half of fp16's smallest step, 2^-25, which is 2^-32 of the row's largest.  (With m at the largest that was 2^-25 of it: beside keys
+// whose values are zero, those of 2^-22.4 of their probability gave a result off by 1 %, those of 2^-27.7 nothing.)  Values' steps below 2^-64 (of zeros) count as 2^-64.
 #pragma once
 
 #include "perq_cache.cuh"
@@ -29,6 +30,8 @@ namespace perq_kv {
 
 constexpr int FEW_WARPS = THREADS / 32;
 constexpr int FEW_KEYS = 16;                  // of a unit
+// Exponents of the largest P when a reference is set, and of the largest that there may be before it is moved.
+constexpr float P_LIFT = 7.0f, P_MOST = 15.0f;
 // Set in perq_mm's error word when a bounded wait ran out.
 enum : unsigned int { ERROR_ATTEND = 1u << 7 };
 
@@ -484,7 +487,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
             };
             exponents();
             // (a row that has seen nothing has the reference -inf, so everything is over)
-            if (__any_sync(0xffffffffu, over > 8.0f)) {
+            if (__any_sync(0xffffffffu, over > P_MOST)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -497,7 +500,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
                             if (s[t][e] != -INFINITY) m = fmaxf(m, fmaf((float)(128 * acc[t][0][e] + acc[t][1][e]), ff, log_step));
 #pragma unroll
                         for (int l = 4; l < 32; l *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, l));
-                        m = fmaxf(m, top[t][c]);
+                        m = fmaxf(m - P_LIFT, top[t][c]);
                         const float alpha = m == -INFINITY ? 1.0f : exp2_of(top[t][c] - m);
                         top[t][c] = m;
                         total[t][c] *= alpha;

@@ -4,8 +4,8 @@
 // at a time, keys and values in turn; four warps make them fp16 (exactly: code ^ 0x80 in the low bits of 1024, minus 1152) and lay them down as operands, in a ring; one warp issues the
 // products: S = Q K^T into tensor memory, then O += P V with P from tensor memory and V's rows as they are (its channels run along N).  Either tile has four warps of its own, a row to a
 // thread, which take 64 keys at a time: their maximum, P = 2^(x + log2 s_v - m) rounded to fp16 over the columns where S was, and the probabilities' sum in fp32.  S has room for 64 keys
-// twice, so the products with the last 64 and for the next run under the exponentials of these.  O stays in tensor memory; m moves, and O with it, only when something is over 2^8 times
-// larger.  A CTA takes the work of others that have not begun (next_cta), and its loads and conversions run ahead into it.
+// twice, so the products with the last 64 and for the next run under the exponentials of these.  O stays in tensor memory; m, which is 7 below the largest so far, moves, and O with it, only
+// when something is over 2^15 (as in the kernel for few queries).  A CTA takes the work of others that have not begun (next_cta), and its loads and conversions run ahead into it.
 //
 // Floors: 4 D operations a pair of a row and a key it sees, at the tensor cores' rate.  Chunks of up to 512 tokens behind 16000, 32 heads of 128: 285 us, 830 TFLOP/s of 1667; two prompts of
 // up to 8192 270, 840.  Bound by the rows' warps, which never wait for the products: 2000 cycles to 64 keys of both tiles, in which the products take 1024 (pipe 42 %): 1020 exponentials (two warps
@@ -442,8 +442,8 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
 #pragma unroll
                     for (int g = 0; g < G; ++g) most_x = fmaxf(most_x, fmaf(FINE ? top[g] : fmaxf(top[2 * g % 4], top[(2 * g + 1) % 4]), f[g], b[g]));
                 }
-                if (__any_sync(0xffffffffu, most_x - m > 8.0f)) {
-                    const float next = fmaxf(m, most_x), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
+                if (__any_sync(0xffffffffu, most_x - m > P_MOST)) {
+                    const float next = fmaxf(m, most_x - P_LIFT), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
                     m = next;
                     l *= alpha;
                     if (u > 0) {

@@ -472,11 +472,12 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
             auto exponents = [&]() {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const float ff[2] = {row_factor[t][0] * ks, row_factor[t][1] * ks}, bb[2] = {log_step - top[t][0], log_step - top[t][1]};
+                    const float ff[2] = {row_factor[t][0] * ks, row_factor[t][1] * ks};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int c = e & 1;
-                        s[t][e] = fmaf((float)(128 * acc[t][0][e] + acc[t][1][e]), ff[c], bb[c]);
+                        // (two steps, so that the largest, which the reference was made of, is no further from it than it was then, however large both are)
+                        s[t][e] = fmaf((float)(128 * acc[t][0][e] + acc[t][1][e]), ff[c], log_step) - top[t][c];
                         if (edge) {
                             const int j = key + key_in(g) + 8 * (e >> 1), at_row = position[t][c];
                             if (j > at_row || (p.window > 0 && j <= at_row - p.window && j >= p.sinks)) s[t][e] = -INFINITY;

@@ -389,6 +389,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
             const int row_first = it.row0 + t * 128 + (warp & 3) * 32, row_last = it.row0 + it.rows - 1;
             const int low_position = it.first + min(row_first, row_last) / p.a.group, high_position = it.first + min(row_first + 31, row_last) / p.a.group;
             float m = -INFINITY;
+            float limit = P_MOST;                                      // (of the warp: none where m is far from 0)
             for (int u = 0; u < 2 * tiles; ++u) {
                 const int side = u & 1, key = key_of(it, tile0 + (u >> 1)) + 64 * side;
                 const uint32_t j = j0 + (uint32_t)(u >> 1), global = global0 + (uint32_t)(u >> 1);
@@ -442,9 +443,10 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
 #pragma unroll
                     for (int g = 0; g < G; ++g) most_x = fmaxf(most_x, fmaf(FINE ? top[g] : fmaxf(top[2 * g % 4], top[(2 * g + 1) % 4]), f[g], b[g]));
                 }
-                if (__any_sync(0xffffffffu, most_x - m > P_MOST)) {
+                if (__any_sync(0xffffffffu, most_x - m > limit)) {
                     const float next = fmaxf(m, most_x - P_LIFT), alpha = next == -INFINITY ? 1.0f : exp2_of(m - next);
                     m = next;
+                    limit = __any_sync(0xffffffffu, fabsf(m) > 0x1p16f && m != -INFINITY) ? -INFINITY : P_MOST;
                     l *= alpha;
                     if (u > 0) {
                         if (!cta_wait_warp(o_full + 8u * (uint32_t)t, (uint32_t)(u - 1) & 1u)) {
@@ -461,6 +463,17 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
 #pragma unroll
                             for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__int_as_float(o[i]) * alpha);
                             tmem_store16(o_at + 16u * c, w);
+                        }
+                    }
+                    if (limit != P_MOST) {
+                        // In one step b - m is rounded first, by up to 2^-24 of m: not what the largest is over it, if that is no small part of 1.  So here in two.
+                        const float reference = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+#pragma unroll
+                            for (int i = g * W; i < (g + 1) * W; ++i) s[i / 32][i % 32] = fmaf(s[i / 32][i % 32], f[g], b[g]) - reference;
+                            f[g] = 1.0f;
+                            b[g] = reference;
                         }
                     }
                 }

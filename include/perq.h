@@ -470,8 +470,8 @@ int perq_cache_read_i8(const void *k_codes, const float *k_steps, const void *v_
  * with the row's largest, before its rotation, between 1 and 2 (bf16 and fp16 without a rotation are kept, but for 2^-25 of that).  Probabilities times their values' step are rounded to
  * fp16: off by 2^-11 of each, or by 2^-32 of the row's largest such product where that is more (so those below 2^-32 of it may be left out of the sum over values; the sum of probabilities
  * has them in fp32).  Sums are fp32 or wider, and added in an order that does not change from run to run.  A query that is not finite gives a row of NaN.
- * Steps are not negative.  Keys' below 2^-60 may count as 2^-60, values' below 2^-64 count as 2^-64 (codes of such pages are 0 where perq_cache_write_i8 writes a step of 0), and those
- * above 2^126 may count as not finite.  Values' steps of one sequence and head should lie within 2^80 of each other (0 counts as 2^-64): probabilities below 2^-45 may be left out beyond.
+ * A row's largest channel times |scale| lies between 2^-110 and 2^110, or logits lose bits.  Steps are not negative.  Values' below 2^-64 count as 2^-64 (codes of such pages are 0 where
+ * perq_cache_write_i8 writes a step of 0), and keys' or values' above 2^126 may count as not finite.  Values' steps of one sequence and head should lie within 2^80 of each other (0 counts as 2^-64): probabilities below 2^-45 may be left out beyond.
  * Errors: NULL, SHAPE, BLOCK, FMT, ALIGN, WORKSPACE, CUDA.
  */
 int perq_attention_i8(const void *q, int32_t in_type, int64_t q_stride, const void *k_codes, const float *k_steps, const void *v_codes, const float *v_steps,

@@ -369,11 +369,10 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                         const uint32_t to = base + (uint32_t)t * K::tile + (uint32_t)(channel / 64) * K::half + r * 128u;
                         sts128(to + ((c ^ r) & 7u) * 16u, make_uint4(half2_of(v[0], v[1]), half2_of(v[2], v[3]), half2_of(v[4], v[5]), half2_of(v[6], v[7])));
                         sts128(to + (((c + 1u) ^ r) & 7u) * 16u, make_uint4(half2_of(v[8], v[9]), half2_of(v[10], v[11]), half2_of(v[12], v[13]), half2_of(v[14], v[15])));
-                        // (the lane of the row has its factor; not 0, so that what is not seen stays -inf.  A query that is not finite makes the sum of probabilities NaN, unless the row
-                        // sees nothing)
+                        // (the lane of the row has its factor.  A query that is not finite makes the sum of probabilities NaN, unless the row sees nothing)
                         const float top = __shfl_sync(0xffffffffu, most, (lane % at_once) * wide);
                         if (lane / at_once == k0 + k) {
-                            factor = fmaxf(__uint_as_float(min(max(__float_as_uint(top) >> 23, 1u), 253u) << 23) * fabsf(p.a.scale), 0x1p-60f);
+                            factor = fminf(__uint_as_float(min(max(__float_as_uint(top) >> 23, 1u), 253u) << 23) * fabsf(p.a.scale), 3.4028235e38f);
                             if (!(top <= 3.4028235e38f) && position >= 0) l = __uint_as_float(0x7fffffffu);
                         }
                     }
@@ -403,13 +402,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                 tmem_load32(s_at, s[0]);
                 tmem_load32(s_at + 32u, s[1]);
                 constexpr int G = FINE ? 4 : 2, W = 64 / G;
-                // of a page's columns: the factor of S, log2 s_v, 1 / s_v
+                // of a page's columns: the factor of S (at least 2^-120, so that what is not seen stays -inf: |S| < 2^23), log2 s_v, 1 / s_v
                 const uint32_t at = steps + (global & 7u) * 128u + (uint32_t)side * 64u;
                 float f[G], b[G], inverse[G];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const uint4 w = lds128(at + (uint32_t)(g * (4 / G)) * 16u);
-                    f[g] = factor * __uint_as_float(w.x);
+                    f[g] = fmaxf(factor * __uint_as_float(w.x), 0x1p-120f);
                     b[g] = __uint_as_float(w.y);
                     inverse[g] = __uint_as_float(w.z);
                     if (w.w != 0u) {
@@ -757,13 +756,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) many_kernel(const __grid_cons
                                          "l"((kind ? p.a.v_codes : p.a.k_codes) + ((block << log2page) * (size_t)D)), "r"((uint32_t)(each * D)), "r"(bar) : "memory");
                     }
                     if (!ok) break;
-                    // of 16 keys each: s_k (not 0, so that what is not seen stays -inf), log2 s_v, 1 / s_v, and whether one of them is not finite, which the rows' warps see to
+                    // of 16 keys each: s_k, log2 s_v, 1 / s_v, and whether one of them is not finite, which the rows' warps see to
                     const int mine = (lane & 7) * 16 / each;
                     const float k = __shfl_sync(0xffffffffu, ks, mine), v = __shfl_sync(0xffffffffu, vs, mine);
                     const bool bad = !(fabsf(k) <= 0x1p126f && fabsf(v) <= 0x1p126f), none = bad || v < 0x1p-64f;
                     if (lane < 8)
                         sts128(steps + (global & 7u) * 128u + (uint32_t)lane * 16u,
-                               make_uint4(__float_as_uint(bad || k < 0x1p-60f ? 0x1p-60f : k), __float_as_uint(none ? -64.0f : log2_of(v)), __float_as_uint(none ? 0x1p64f : 1.0f / v),
+                               make_uint4(__float_as_uint(bad ? 0.0f : k), __float_as_uint(none ? -64.0f : log2_of(v)), __float_as_uint(none ? 0x1p64f : 1.0f / v),
                                           (uint32_t)bad));
                     __syncwarp();
                     if (lane == 0) mbar_arrive(steps_full + 8u * (global & 7u));

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import cache as C
+from test_attention_gpu import filled, queries
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -37,3 +38,24 @@ def test_large_logits(B, size, sign, D, rows):
     y = cache.tokens(1, 0, length, pages)[best]
     # (the next one has at most e^-65536 of its probability.  That one number is rounded to fp16, by 2^-11, where it is added to the values, and not where it is divided by)
     C.compare(out, y, (2.0 ** -11 + 2.0 ** -20) * y.abs())
+
+
+def run(B, rows, D, b, of_queries, of_scale, of_steps, spread=3.0):
+    gen = torch.Generator()
+    gen.manual_seed(rows + D + b)
+    lengths = [rows + 90, 700]
+    cache, pages = filled(lengths, 2, D, 32, gen)
+    cache.steps[0] *= of_steps
+    offsets = [0, rows, 2 * rows]
+    q = (queries(2 * rows, 4, D, BF16, gen, spread).double() * of_queries).to(BF16)
+    scale = D ** -0.5 * of_scale
+    out = B.perq_attention_i8(q.cuda(), *cache.on_gpu(), C.ints(offsets), C.ints(lengths), pages.cuda(), b=b, scale=scale, out_dtype=F32)
+    y, tolerance = C.attention(cache, q, offsets, lengths, pages, b, scale)
+    C.compare(out, y, tolerance)
+
+
+@pytest.mark.parametrize("rows", (1, 7, 90))
+@pytest.mark.parametrize("D,b", [(64, 1), (64, 64), (128, 128)])
+@pytest.mark.parametrize("q,scale,step", [(-40, -40, 80), (-20, -60, 80), (0, 75, -75), (60, 40, -100), (-100, 0, 100), (0, -100, 100)])
+def test_products_of_far_factors(B, q, scale, step, rows, D, b):
+    run(B, rows, D, b, 2.0 ** q, 2.0 ** scale, 2.0 ** step)

@@ -362,6 +362,9 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
             }
             float v[LANE], top = 0.0f;
             unpack(v, lo, hi, p.f16 != 0);
+            // (by 2^-8 first, which is exact for bf16's smallest too, so that sums of 128 channels do not pass fp32's largest)
+#pragma unroll
+            for (int k = 0; k < LANE; ++k) v[k] *= 0x1p-8f;
             rotate(v, p.log2b, lane);
 #pragma unroll
             for (int k = 0; k < LANE; ++k) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(v[k])));
@@ -381,7 +384,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 || D == 64 ? 2 : 1) few_kerne
 #pragma unroll
                 for (int plane = 0; plane < 2; ++plane)
                     *reinterpret_cast<uint4 *>(q_room + (plane * K::rows + row) * D + channel) = make_uint4(w[plane][0], w[plane][1], w[plane][2], w[plane][3]);
-                if (channel == 0) factor[row] = scaled * (1.0f / 16256.0f) * __uint_as_float((uint32_t)e << 23) * p.scale;
+                if (channel == 0) factor[row] = scaled * (256.0f / 16256.0f) * __uint_as_float((uint32_t)e << 23) * p.scale;
             }
         }
         __syncthreads();

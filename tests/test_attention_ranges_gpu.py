@@ -59,3 +59,10 @@ def run(B, rows, D, b, of_queries, of_scale, of_steps, spread=3.0):
 @pytest.mark.parametrize("q,scale,step", [(-40, -40, 80), (-20, -60, 80), (0, 75, -75), (60, 40, -100), (-100, 0, 100), (0, -100, 100)])
 def test_products_of_far_factors(B, q, scale, step, rows, D, b):
     run(B, rows, D, b, 2.0 ** q, 2.0 ** scale, 2.0 ** step)
+
+
+@pytest.mark.parametrize("rows", (1, 7, 90))
+@pytest.mark.parametrize("D,b", [(64, 64), (128, 128)])
+def test_queries_near_the_largest(B, rows, D, b):
+    """Whose rotation passes fp32's largest (bf16's is 2^128)."""
+    run(B, rows, D, b, 2.0 ** 125, 2.0 ** -100, 2.0 ** -25, spread=1.0)

@@ -32,6 +32,8 @@ FMT_BY_NAME = {"int4": PERQ_FMT_INT4, "mxfp4": PERQ_FMT_MXFP4, "f32": PERQ_FMT_F
 OUT_BY_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}        # perq_out_t
 
 PERQ_OK = 0
+PERQ_ERR_SHAPE = 2
+PERQ_ERR_BLOCK = 3
 PERQ_ERR_WORKSPACE = 9
 
 _lib = None
@@ -493,6 +495,13 @@ def perq_grouped_matmul_i8(a_codes: torch.Tensor, a_scales: torch.Tensor, a_fmt:
 
 
 # ------------------------------------------------------------------------------------------------- the 8-bit cache
+# Numbers that the library takes as 32 bits: larger ones would be cut (2 ** 32 + 1 rows to 1), so they are refused here.
+def _fit(where: str, rc: int, *numbers) -> None:
+    for n in numbers:
+        if not -0x80000000 <= n <= 0x7fffffff:
+            raise PerqError(rc, where)
+
+
 def _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages):
     """The cache's sizes: (S, heads, D, page, n_pages, width)."""
     i8, i32, f32 = torch.int8, torch.int32, torch.float32
@@ -521,6 +530,7 @@ def perq_cache_write_i8(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor,
     """k, v: bf16 or f16 CUDA tensors [T, heads, D] (parts of longer rows too), written into codes int8 [n_pages, heads, page, D] and steps fp32 [n_pages, heads].
 
     offsets int32 [S + 1], lengths int32 [S] (tokens with the new ones), pages int32 [S, width].  All tensors are on the current device."""
+    _fit("perq_cache_write_i8", PERQ_ERR_BLOCK, b)
     device = torch._C._cuda_getDevice()
     S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
     T = k.shape[0]
@@ -545,6 +555,7 @@ def perq_cache_read_i8(k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: to
     """The last offsets[i + 1] - offsets[i] tokens of every sequence: (k, v), each [T, heads, D] of out_dtype.
 
     Rows of no sequence are not written: in outputs made here they are whatever the memory holds."""
+    _fit("perq_cache_read_i8", PERQ_ERR_BLOCK, b)
     device = torch._C._cuda_getDevice()
     S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
     shape = (T, heads, D)
@@ -567,6 +578,7 @@ def perq_cache_read_i8(k_codes: torch.Tensor, k_steps: torch.Tensor, v_codes: to
 
 
 def perq_attention_i8_workspace_bytes(T: int, S: int, heads: int, group: int, D: int, most: int) -> int:
+    _fit("perq_attention_i8_workspace_bytes", PERQ_ERR_SHAPE, S, heads, group, D, most)
     n = C.c_size_t(0)
     _check(load().perq_attention_i8_workspace_bytes(T, S, heads, group, D, most, C.byref(n)), "perq_attention_i8_workspace_bytes")
     return int(n.value)
@@ -586,6 +598,8 @@ def perq_attention_i8(q: torch.Tensor, k_codes: torch.Tensor, k_steps: torch.Ten
 
     most: at least the rows of the longest sequence of the call (None: T); scale: of the logits (None: D ** -0.5).  All tensors are on the current device.  A
     workspace that the call is not given is made here.  Rows of no sequence are not written: in an `out` made here they are whatever its memory holds."""
+    _fit("perq_attention_i8", PERQ_ERR_SHAPE, 1 if most is None else most, window, sinks)
+    _fit("perq_attention_i8", PERQ_ERR_BLOCK, b)
     device = torch._C._cuda_getDevice()
     S, heads, D, page, n_pages, width = _cache(device, k_codes, k_steps, v_codes, v_steps, offsets, lengths, pages)
     shape = q.shape

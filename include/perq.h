@@ -462,14 +462,14 @@ int perq_cache_read_i8(const void *k_codes, const float *k_steps, const void *v_
  *                       `most` on are left as they are.
  *   out                 device, dense [T, heads * group, D] of out_type
  *   workspace           device, at least perq_attention_i8_workspace_bytes(...) bytes.  What is enough for T, S and most is enough for less of each
- *                       with the same heads, group and D; 80 MB are the most (a B200, D = 128, more than 64 rows to a sequence), 2.5 MB for decode steps.  Its contents need not be
+ *                       with the same heads, group and D; 80 MB are the most (a B200, D = 128, `most` * group above 32), 2.5 MB up to there, as for decode steps.  Its contents need not be
  *                       kept; calls that may overlap need one each.
  *   scale               of the logits: finite (SHAPE)
  *
- * Rotated queries are rounded: of sequences with up to 64 rows (token and query head of one head of the cache) to whole multiples of 1/16256 of the row's largest; of others to fp16
- * with the row's largest, before its rotation, between 1 and 2 (bf16 and fp16 without a rotation are kept, but for 2^-25 of that).  Probabilities times their values' step are rounded to
- * fp16: off by 2^-11 of each, or by 2^-32 of the row's largest such product where that is more (so those below 2^-32 of it may be left out of the sum over values; the sum of probabilities
- * has them in fp32).  Sums are fp32 or wider, and added in an order that does not change from run to run.  A query that is not finite gives a row of NaN.
+ * Rotated queries are rounded.  Where min(T, most) * group is at most 32: to whole multiples of 1/16256 of the row's largest, so by 2^-15 of that.  Else it may be so, or to fp16 with the row's largest,
+ * before its rotation, between 1 and 2, so by 2^-11 of a channel (bf16 and fp16 without a rotation are kept, but for 2^-25 of the largest): which of the two a sequence has depends on its rows and on those
+ * of the others in the call.  Exponentials are off by up to 2^-18 of themselves.  Probabilities times their values' step are rounded to fp16: off by 2^-11 of each, or by 2^-32 of the row's largest
+ * such product where that is more (so those below 2^-32 of it may be left out of the sum over values; the sum of probabilities has them in fp32).  Sums are fp32 or wider, and added in an order that does not change from run to run.  A query that is not finite gives a row of NaN.
  * A row's largest channel times |scale| lies between 2^-110 and 2^110, or logits lose bits.  Steps are not negative.  Values' below 2^-64 count as 2^-64 (codes of such pages are 0 where
  * perq_cache_write_i8 writes a step of 0), and keys' or values' above 2^126 may count as not finite.  Values' steps of one sequence and head should lie within 2^80 of each other (0 counts as 2^-64): probabilities below 2^-45 may be left out beyond.
  * Errors: NULL, SHAPE, BLOCK, FMT, ALIGN, WORKSPACE, CUDA.

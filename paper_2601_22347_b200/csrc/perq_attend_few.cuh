@@ -14,8 +14,8 @@
 // (128 hi + lo) code is exact.  (Codes to fp16 instead: 80 instructions for 16 keys of 128 channels; these products take 8 of the 8 cycles that an fp16 one takes too.)
 // Values' codes become fp16 exactly: code ^ 0x80 in the low bits of 1024, minus 1152.
 //
-// 64 sequences of up to 12000 tokens, 8 heads of 128 with 4 of queries each: 178 us, 5.9 TB/s of 6.5.  32 sequences of up to 5 tokens, 4 heads of 64 with 8 of queries each, a window of 4096:
-// 60 us, 1.1 TB/s; there a sequence has one to three tiles of 16 rows, each of which goes over its keys again (from L2), at 436 instructions a unit in all (64 sequences: 363), and a CTA's
+// 64 sequences of up to 12000 tokens, 8 heads of 128 with 4 of queries each: 181 us, 5.8 TB/s of 6.5.  32 sequences of up to 5 tokens, 4 heads of 64 with 8 of queries each, a window of 4096:
+// 60 us, 1.1 TB/s; there a sequence has one to three tiles of 16 rows, each of which goes over its keys again (from L2), at 440 instructions a unit in all (64 sequences: 360), and a CTA's
 // share of 223 units crosses tiles, whose queries and results cost some microseconds each.
 //
 // y = s_k f S + log2 s_v - m, base 2, with f the row's factor and m its reference.  Values' steps go into the exponent: P = 2^y, so that fp16 P meet exact codes and no row's

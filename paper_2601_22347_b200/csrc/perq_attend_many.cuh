@@ -7,10 +7,12 @@
 // twice, so the products with the last 64 and for the next run under the exponentials of these.  O stays in tensor memory; m, which is 7 below the largest so far, moves, and O with it, only
 // when something is over 2^15 (as in the kernel for few queries).  A CTA takes the work of others that have not begun (next_cta), and its loads and conversions run ahead into it.
 //
-// Floors: 4 D operations a pair of a row and a key it sees, at the tensor cores' rate.  Chunks of up to 512 tokens behind 16000, 32 heads of 128: 285 us, 830 TFLOP/s of 1667; two prompts of
-// up to 8192 270, 840.  Bound by the rows' warps, which never wait for the products: 2000 cycles to 64 keys of both tiles, in which the products take 1024 (pipe 42 %): 1020 exponentials (two warps
-// to a scheduler, 16 a cycle and SM), 400 maxima, 185 reading S, 400 waits and polls between steps that depend on each other.  Without the exponentials 11 % less, without the products 8, without
-// the conversions or the maxima 4.  What did not help: two threads to a row and 128 keys (the same); the maximum of P instead of S, with a second try where it was too large (349 -> 399 us); the
+// Floors: 4 D operations a pair of a row and a key it sees, at the tensor cores' rate.  From a graph, chunks of up to 512 tokens behind 16000, 32 heads of 128: 284 us, 833 TFLOP/s of 1667; two prompts of
+// up to 8192 272, 835 (in calls on inputs in turn 302 and 286).  No unit bounds it: a step of 64 keys of both tiles takes about 2000 cycles, and the products or the exponentials 1024 each.  With
+// something left out, the chunks' and the prompts' times are less by: exponentials 6 and 9 %, codes to fp16 6 and 6, maxima nothing, sums nothing, exponentials with products 17 and 14, exponentials with
+// maxima and sums 11 and 12, these with reading S and the products too 21 and 24.  So three quarters are what is left then: the steps' waits for one another, P to tensor memory, codes to fp16, loads.
+// (64 registers of S to a thread leave no room for the next step's beside them; ptxas spills 28 bytes at D = 128.)
+// What did not help: two threads to a row and 128 keys (the same); the maximum of P instead of S, with a second try where it was too large (349 -> 399 us); the
 // next S read under the exponentials (303 -> 326, registers); sleeping waits (+4 %); one exponential in four on the multiply-add pipe (310, in eight 298); heads in the inner order (+3 %).
 #pragma once
 

@@ -110,14 +110,17 @@ int launch_few(const AttendParams &p, int sms, cudaStream_t st)
     return launch(join_kernel<D, NT>, ctas - 1, THREADS, join_bytes(ctas), st, 8 * NT / JOIN_ROWS, p, ctas);
 }
 
-// Rows (of tokens and heads) of a sequence up to which the kernel for few queries takes it.  32 sequences of 8000 tokens, 8 heads of 128, few against many: 24 rows 245 and 237 us, 32 rows
-// 250 and 242, 48 rows 360 and 214; two sequences: 32 rows 31 and 32, 48 rows 38 and 32 (behind 500 tokens: 13 and 19, 19 and 19).  Heads of 64: 32 rows 85 and 108, 48 rows 122 and 108.
+// Rows (of tokens and heads) of a sequence up to which the kernel for few queries takes it.  32 sequences of 8000 tokens, 8 heads of 128 with 4 of queries each, few against many: 16 rows 131 and 209 us,
+// 32 rows 247 and 213, 48 rows 362 and 213; two sequences: 32 rows 30 and 37, 48 rows 37 and 37, 64 rows 43 and 39 (behind 500 tokens: 12 and 18, 18 and 18, 18 and 20).  Heads of 64: 32 rows 157 and
+// 182, 48 rows 226 and 182; two sequences 27 and 25, 31 and 25.
 constexpr int FEW_ROWS = 32, BOTH_ROWS = 64;
 constexpr int MANY_PIECES = 4;               // to an SM, of tiles of rows whose keys are split
 
 // CTAs to the keys of a tile of rows.  Few items leave SMs without work, or, with contexts of different lengths, one SM with much more than another; every piece costs as much as four and a half
 // tiles of keys for its queries and results, and joining them two.  With items alike the call takes whole rounds of pieces, with different ones the CTAs take them as they come: the mean of
-// both is what is compared.  (Two sequences of 8000 tokens, 64 rows: 15 pieces 51 us, 9 of them 32; 8 sequences 98 and 77; 32 sequences of 2000, heads of 64: 4 pieces 46 us, 1 32.)
+// both is what is compared.  (Two sequences of 16 tokens behind 8000, 8 heads of 128 with 4 of queries each, in 1, 4, 9 and 15 pieces: 105, 42, 39 and 54 us, 9 are taken; of 64 tokens 138, 56, 45
+// and 64, 9 too; eight of 16 in 1, 2 and 4: 108, 72 and 81, 2.)  How many keys there are is guessed from the table's width, and how many items from all rows: a prompt of 300 tokens 21 us, 50 with
+// a table for 131072; a chunk of 512 behind 16000 163, 244 beside 15 decode steps and 367 beside 63.
 int many_split(const AttendParams &p, long long most_items, long long items, int sms)
 {
     long long keys = (long long)p.q.width << p.q.page;
@@ -158,7 +161,7 @@ int launch_attention(AttendParams &p, int sms, cudaStream_t st)
     // Up to 64 rows one kernel takes all sequences, by the mean of their rows (32 sequences of up to 5 tokens and 8 heads, 1 to 4 of them by one kernel and 5 by the other: 113 us, 63 by the first).
     if (rows <= FEW_ROWS || (rows <= BOTH_ROWS && p.q.T * (int64_t)p.group <= (int64_t)FEW_ROWS * p.q.S)) return launch_few<D, 2>(p, sms, st);
     // Beyond, the kernel for many takes them all if the shortest has more than FEW_ROWS where every row of the call is one's and the others have `most`; that saves two launches: two sequences of
-    // 256 rows behind 500 tokens 27 -> 23 us.  (No result hangs on it.)
+    // 256 rows behind 500 tokens 27 -> 23 us.  (Queries of a sequence with few rows are then rounded as the others' are.)
     p.few_rows = rows <= BOTH_ROWS || (p.q.T - (p.q.S - 1) * most) * p.group > FEW_ROWS ? 0 : FEW_ROWS;
     if (p.few_rows > 0)
         if (int rc = launch_few<D, 2>(p, sms, st)) return rc;

@@ -8,8 +8,9 @@
 // three exchanges between lanes.  Eight or sixteen warps share a block of a prompt and keep its rotated values in registers over the barrier that its maximum needs; blocks of up to 2048
 // elements have a warp each.  For few tokens a warp has a block of its own and a lane four channels: what is met for the first time is most of such a call, and that is a quarter of the code.
 // Four prompts of up to 4096 tokens, 8 heads of 128, pages of 128: 31 us, 61 MB at 1.9 TB/s.  Bound by what a block's steps wait for one after another, at two blocks to an SM (all registers):
-// finding it 1.9 us, reading 1.5, the maximum's barrier 0.5, settling it 0.9 to 1.7, codes 1.1.  256 sequences' next tokens 12.6 us: reading from pages that nothing near has touched, the
-// exact maximum, codes that the new step changes.
+// finding it 1.9 us, reading 1.5, the maximum's barrier 0.5, settling it 0.9 to 1.7, codes 1.1.  256 sequences' next tokens 12.6 us where no step grows: a chain
+// of sequence, page, step, tokens and exact maximum, each from memory.  Where steps grow a warp has a page's earlier codes to round again, 16 bytes to a lane at a time, one load after another: 45 us with pages of 64
+// whose slots are spread, 71 with pages of 128 (one token: 15 and 14; in the last slot 26 and 47).  In use, a step of the block of slot k grows in about one of k + 1 calls.
 //
 // Codes are those of exact arithmetic.  A butterfly of L = log2 b stages rounds each sum L times, so |u32 - u| <= L 2^-24 sum |x|, and sum |x| <= sqrt b |x|_2 =
 // |u|_2 <= sqrt b max |u| over the rotation's block: E = 1.01 L sqrt b 2^-24 of its largest (b = 128: 4.8e-6).  What may be the block's maximum (within 2 E of the largest in
